@@ -9,8 +9,8 @@
 //   du = delta sum_n g_n B_n + D dy,  dA_n = sum g_n a_n h_n(before) delta,
 //   ddelta = u sum_n g_n B_n + sum_n g_n a_n h_n(before) A_n.
 //
-// Four states are one lane's, Q = 1, 2, 4, 8 or 16 neighbouring lanes are a
-// channel's (N <= 4 Q; missing states have A = B = C = 0), so sums over a
+// S = 2 or 4 states are one lane's, Q = 1, 2, 4, 8 or 16 neighbouring lanes are
+// a channel's (N <= S Q; missing states have A = B = C = 0), so sums over a
 // channel's states are Q-lane sums and sums over channels are strided ones.
 // A token past its sequence's end is a step with delta = u = dy = B = C = 0:
 // the state stays, every product is 0.
@@ -20,63 +20,71 @@ using namespace rcops;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 16;           // tokens between two kept states
+constexpr int kChannels = 64;       // of a workgroup
+constexpr int kFwdTile = 32;        // tokens staged together, forward
+constexpr int kSumThreads = 256;
+
+// Tokens between two kept states, and of a backward tile: the states of a
+// tile and their decays stay in registers, 64 of each a lane.
+constexpr int keep_of(int S) { return 64 / S; }
 
 __device__ __forceinline__ int seq_end(const int32_t* lengths, int64_t b, int32_t length) {
   if (!lengths) return length;
   return min(max(lengths[b], 0), length);
 }
 
-// Sum over the Q lanes of a channel, in each of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRor4 = 0x124,
+              kRor8 = 0x128;
+
+// Sum over the Q lanes of a channel, in each of them (a mirror is as good as
+// an exchange once the lanes below are equal).
 template <int Q>
 __device__ __forceinline__ float state_sum(float x) {
-#pragma unroll
-  for (int m = 1; m < Q; m *= 2) x += __shfl_xor(x, m);
-  return x;
-}
-// Sum over the channels of a wave, lanes of equal q apart.
-template <int Q>
-__device__ __forceinline__ float channel_sum(float x) {
-#pragma unroll
-  for (int m = Q; m < 64; m *= 2) x += __shfl_xor(x, m);
+  if (Q > 1) x = dpp_add<kXor1>(x);
+  if (Q > 2) x = dpp_add<kXor2>(x);
+  if (Q > 4) x = dpp_add<kHalfMirror>(x);
+  if (Q > 8) x = dpp_add<kMirror>(x);
   return x;
 }
 
-struct ScanPlan {
-  int Q;
-  int64_t group_width;      // channels of a group
-  int64_t blocks;           // workgroups of a group's channels
-  int64_t tiles;
-};
+// Sum over the lanes of a row of 16 that hold the same states of different channels.
+template <int Q>
+__device__ __forceinline__ float row_channel_sum(float x) {
+  if (Q <= 1) x = dpp_add<kXor1>(x);
+  if (Q <= 2) x = dpp_add<kXor2>(x);
+  if (Q <= 4) x = dpp_add<kRor4>(x);
+  if (Q <= 8) x = dpp_add<kRor8>(x);
+  return x;
+}
+// Sums of x and y over pairs of rows: even rows hold x's, odd ones y's.
+__device__ __forceinline__ float row_pair_sum(float x, float y) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x),
+                                                  __builtin_bit_cast(unsigned, y), false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+// Sums of x and y over pairs of halves: the low half holds x's, the high one y's.
+__device__ __forceinline__ float half_pair_sum(float x, float y) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x),
+                                                  __builtin_bit_cast(unsigned, y), false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
 
 struct ScanParams {
   rc_scan_args a;
-  int32_t group_width, blocks, tiles, parts;
-  float* part_bc;           // backward: [parts][batch][length][groups][2][4 Q]
-  float* part_a;            // [batch][width][4 Q]
-  float* part_d;            // [batch][width][2]: D, dt_bias
-};
-
-// A workgroup's sequence, group and channel; a wave's slot among those that
-// share B and C.
-template <int Q>
-struct Place {
-  int64_t b, g, d;
-  int q, part;
-  bool on;
-  __device__ Place(const ScanParams& p) {
-    int64_t i = blockIdx.x;
-    const int64_t blk = i % p.blocks;
-    i /= p.blocks;
-    g = i % p.a.groups;
-    b = i / p.a.groups;
-    q = threadIdx.x % Q;
-    const int64_t ch = blk * (kThreads / Q) + threadIdx.x / Q;
-    on = ch < p.group_width;
-    d = g * p.group_width + (on ? ch : 0);
-    part = (int)(blk * (kThreads / 64) + threadIdx.x / 64);
-  }
+  int32_t group_width, blocks;      // channels of a group, workgroups for them
+  int32_t chunks, chunk;            // pieces of the length, tokens of one (a multiple of the tile)
+  int32_t keeps;                    // kept states of a sequence
+  float* ends;                      // [batch][chunks][width][N]: a chunk's own end state (forward)
+                                    // or gradient before it (backward), from nothing
+  float* steps;                     // [batch][chunks][width]: sum of delta over the chunk
+  float* part_bc;                   // backward: [blocks][batch][length][groups][2][N]
+  float* part_a;                    // [batch][chunks][width][N]
+  float* part_d;                    // [batch][chunks][width][2]: D, dt_bias
 };
 
 template <class T>
@@ -88,159 +96,475 @@ __device__ __forceinline__ T* row_out(const rc_view& v, int64_t b, int64_t t) {
   return static_cast<T*>(v.data) + b * v.batch + t * v.time;
 }
 
-// The four states 4 q .. 4 q + 3 of B or C at one token.
-template <class T>
-__device__ __forceinline__ void load_states(const T* p, int q, int n, float (&x)[4]) {
-  load_vec<4>(p + 4 * q, max(0, min(4, n - 4 * q)), x);
-}
-
-// delta of a token and its slope ddelta / ddt.
 __device__ __forceinline__ float delta_of(float raw, bool soft) {
   return soft ? softplus(raw) : raw;
 }
 
-template <class T, int Q>
-__global__ __launch_bounds__(kThreads) void k_scan_forward(ScanParams p) {
-  const rc_scan_args& a = p.a;
-  const Place<Q> w(p);
-  if (!w.on) return;
-  const int end = seq_end(a.lengths, w.b, a.length);
-  const int ns = max(0, min(4, a.states - 4 * w.q));
-  const int64_t at = (w.b * a.width + w.d) * a.states + 4 * w.q;
-  float A[4], h[4];
-  load_vec<4>(a.A + w.d * a.states + 4 * w.q, ns, A);
+// What a workgroup works on.  Workgroup i runs on XCD i % 8: neighbours in
+// (batch, group, chunk, block) go to one XCD, whose L2 then holds the B and C that they share.
+template <int Q, int S>
+struct Place {
+  static constexpr int N = Q * S;
+  int64_t b, g;
+  int blk, piece;                   // block of channels, chunk
+  int q, ch;                        // the lane's states and channel (in the block)
+  int64_t d;                        // its channel, clamped to the group
+  bool on;
+  __device__ Place(const ScanParams& p) {
+    const uint32_t per = gridDim.x / 8, rem = gridDim.x % 8, xcd = blockIdx.x % 8;
+    int64_t i = (int64_t)xcd * per + min(xcd, rem) + blockIdx.x / 8;
+    blk = (int)(i % p.blocks);
+    i /= p.blocks;
+    piece = (int)(i % p.chunks);
+    i /= p.chunks;
+    g = i % p.a.groups;
+    b = i / p.a.groups;
+    q = threadIdx.x % Q;
+    ch = threadIdx.x / Q;
+    on = blk * kChannels + ch < p.group_width;
+    d = g * p.group_width + min(blk * kChannels + ch, p.group_width - 1);
+  }
+  // The lane's S values of an array [.][width][states] (0 for missing states).
+  __device__ void load(const float* x, int64_t before, const ScanParams& p, float (&v)[S]) const {
+    const float* at = x + (before * p.a.width + d) * p.a.states;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < S; i++) v[i] = q * S + i < p.a.states ? at[q * S + i] : 0.f;
+  }
+  __device__ void store(float* x, int64_t before, const ScanParams& p, const float (&v)[S]) const {
+    float* at = x + (before * p.a.width + d) * p.a.states;
+#pragma unroll
+    for (int i = 0; i < S; i++)
+      if (on && q * S + i < p.a.states) at[q * S + i] = v[i];
+  }
+  // The same of a padded array [.][width][N].
+  __device__ float* padded(float* x, int64_t before, const ScanParams& p) const {
+    return x + (before * p.a.width + d) * N + q * S;
+  }
+};
+
+// A thread's share of a tile: NV vectors of VEC channels of one column.
+template <class T, int Q, int VEC, int TILE>
+struct Tile {
+  static constexpr int threads = kChannels * Q;
+  static constexpr int columns = kChannels / VEC;
+  static constexpr int rows = threads / columns > TILE ? TILE : threads / columns;
+  static constexpr int NV = TILE / rows;
+  typedef T Raw __attribute__((ext_vector_type(VEC)));
+  int64_t d;                        // first channel of the column, clamped
+  int c, r;                         // its place in the block, first row
+  bool on;                          // has work in a tile, channel exists
+  __device__ Tile(const ScanParams& p, int64_t g, int blk) {
+    c = threadIdx.x % columns * VEC;
+    r = threadIdx.x / columns;
+    on = r < rows && blk * kChannels + c < p.group_width;
+    d = g * p.group_width + min(blk * kChannels + c, p.group_width - VEC);
+  }
+  // Loads are unconditional (rows clamped to the sequence): what is past an end is
+  // dropped where it is used.
+  __device__ void load(const rc_view& v, int64_t b, int t0, int length, Raw (&x)[NV]) const {
+#pragma unroll
+    for (int k = 0; k < NV; k++)
+      __builtin_memcpy(&x[k], row<T>(v, b, min(t0 + k * rows + r, length - 1)) + d, sizeof(Raw));
+  }
+  __device__ void vector(const float* w, float (&x)[VEC]) const {
+#pragma unroll
+    for (int i = 0; i < VEC; i++) x[i] = w ? w[d + i] : 0.f;
+  }
+};
+
+// A tile of B or C to LDS in 32 bits: [TILE][N], zeros past the end and for missing states.
+template <class T, int N, int TILE, int THREADS>
+struct StateTile {
+  static constexpr int NE = (TILE * N + THREADS - 1) / THREADS;
+  T x[NE];
+  __device__ void load(const rc_view& v, int64_t group, int64_t b, int t0, const rc_scan_args& a) {
+#pragma unroll
+    for (int k = 0; k < NE; k++) {
+      const int e = k * THREADS + threadIdx.x;
+      x[k] = row<T>(v, b, min(t0 + e / N, a.length - 1))[group + min(e % N, a.states - 1)];
+    }
+  }
+  __device__ void put(float* lds, int t0, int end, int states) const {
+#pragma unroll
+    for (int k = 0; k < NE; k++) {
+      const int e = k * THREADS + threadIdx.x;
+      const bool ok = t0 + e / N < end && e % N < states;
+      if (e < TILE * N) lds[e] = ok ? (float)x[k] : 0.f;
+    }
+  }
+};
+
+template <int S>
+__device__ __forceinline__ void read_states(const float* lds, float (&x)[S]) {
+  typedef float FV __attribute__((ext_vector_type(S)));
+  const FV v = *reinterpret_cast<const FV*>(lds);
+#pragma unroll
+  for (int i = 0; i < S; i++) x[i] = v[i];
+}
+template <int S>
+__device__ __forceinline__ void write_states(float* at, const float (&x)[S]) {
+  typedef float FV __attribute__((ext_vector_type(S)));
+  FV v;
+#pragma unroll
+  for (int i = 0; i < S; i++) v[i] = x[i];
+  *reinterpret_cast<FV*>(at) = v;
+}
+
+// The state that enters chunk `piece`, from the chunks before it (or, REVERSE, the
+// gradient of the state that leaves it, from the chunks after it).
+template <int Q, int S, bool REVERSE>
+__device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
+                                      const float (&A)[S], float (&h)[S]) {
+  const int first = REVERSE ? p.chunks - 1 : 0, step = REVERSE ? -1 : 1;
+  for (int k = first; k != w.piece; k += step) {
+    float own[S];
+    read_states<S>(w.padded(p.ends, w.b * p.chunks + k, p), own);
+    const float sum = p.steps[(w.b * p.chunks + k) * p.a.width + w.d];
+#pragma unroll
+    for (int i = 0; i < S; i++) h[i] = fmaf(fast_exp2(sum * A[i]), h[i], own[i]);
+  }
+}
+
+// Forward.  A tile of tokens is staged to LDS in 32 bits (delta and delta u of
+// 64 channels, B, C), each element converted once by one thread; then the
+// lanes walk over it.  ENDS: only the end state of the chunk from nothing, and its sum of delta.
+template <class T, int Q, int S, int VEC, bool ENDS>
+__global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
+  constexpr int TILE = kFwdTile, N = Q * S, KEEP = keep_of(S);
+  __shared__ float2 lds_d[TILE * kChannels];
+  __shared__ float lds_b[TILE * N], lds_c[ENDS ? 1 : TILE * N], lds_y[ENDS ? 1 : TILE * kChannels];
+  const rc_scan_args& a = p.a;
+  const Place<Q, S> w(p);
+  const Tile<T, Q, VEC, TILE> tile(p, w.g, w.blk);
+  using TileT = Tile<T, Q, VEC, TILE>;
+  const int end = seq_end(a.lengths, w.b, a.length);
+  const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
+  float A[S], h[S], total = 0.f;
+  w.load(a.A, 0, p, A);
+#pragma unroll
+  for (int i = 0; i < S; i++) {
     A[i] *= kLog2e;
     h[i] = 0.f;
   }
-  if (a.state_in) load_vec<4>(a.state_in + at, ns, h);
-  const float D = a.D ? a.D[w.d] : 0.f, bias = a.dt_bias ? a.dt_bias[w.d] : 0.f;
-  for (int t = 0; t < a.length; t++) {
-    if (a.kept && t % kTile == 0)
-      store_vec<4>(a.kept + ((w.b * p.tiles + t / kTile) * a.width + w.d) * (4 * Q) + 4 * w.q, 4,
-                   h);
-    float y = 0.f;
-    if (t < end) {
-      float B[4], C[4];
-      load_states(row<T>(a.B, w.b, t) + w.g * a.B_group, w.q, a.states, B);
-      load_states(row<T>(a.C, w.b, t) + w.g * a.C_group, w.q, a.states, C);
-      const float u = (float)row<T>(a.u, w.b, t)[w.d];
-      const float delta = delta_of((float)row<T>(a.dt, w.b, t)[w.d] + bias, a.softplus);
+  if (!ENDS) {
+    if (a.state_in) w.load(a.state_in, w.b, p, h);
+    if (p.chunks > 1) enter<Q, S, false>(p, w, A, h);
+  }
+  float D[VEC], bias[VEC];
+  tile.vector(a.D, D);
+  tile.vector(a.dt_bias, bias);
+  typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV];
+  StateTile<T, N, TILE, kChannels * Q> B, C;
+  const auto fetch = [&](int t0) {
+    tile.load(a.u, w.b, t0, a.length, u);
+    tile.load(a.dt, w.b, t0, a.length, dt);
+    if (!ENDS && a.z.data) tile.load(a.z, w.b, t0, a.length, z);
+    B.load(a.B, w.g * a.B_group, w.b, t0, a);
+    if (!ENDS) C.load(a.C, w.g * a.C_group, w.b, t0, a);
+  };
+  if (t_first < min(t_last, end)) fetch(t_first);
+  for (int t0 = t_first; t0 < t_last; t0 += TILE) {
+    if (t0 >= end) {                                   // nothing but zeros from here on
+      if (!ENDS && tile.on) {
+        const float zero[VEC] = {};
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        h[i] = fmaf(fast_exp2(delta * A[i]), h[i], delta * u * B[i]);
-        y = fmaf(h[i], C[i], y);
+        for (int k = 0; k < TileT::NV; k++) {
+          const int t = t0 + k * TileT::rows + tile.r;
+          if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, zero);
+        }
       }
-      y = fmaf(D, u, state_sum<Q>(y));
-      if (a.z.data) {
-        const float z = (float)row<T>(a.z, w.b, t)[w.d];
-        y *= z * sigmoid(z);
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < TileT::NV; k++) {
+      const int r = k * TileT::rows + tile.r;
+      const bool ok = tile.on && t0 + r < end;
+      if (r < TILE && tile.r < TileT::rows) {
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+          const float delta = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
+          lds_d[r * kChannels + tile.c + i] = {delta, ok ? delta * (float)u[k][i] : 0.f};
+        }
       }
     }
-    if (w.q == 0) row_out<T>(a.y, w.b, t)[w.d] = (T)y;
+    B.put(lds_b, t0, end, a.states);
+    if (!ENDS) C.put(lds_c, t0, end, a.states);
+    __syncthreads();
+    typename TileT::Raw u0[TileT::NV], z0[TileT::NV];  // of this tile, for its outputs
+#pragma unroll
+    for (int k = 0; k < TileT::NV; k++) {
+      u0[k] = u[k];
+      z0[k] = z[k];
+    }
+    fetch(min(t0 + TILE, t_last - 1));
+#pragma unroll 8
+    for (int j = 0; j < TILE; j++) {
+      if (!ENDS && a.kept && j % KEEP == 0 && w.on && t0 + j < a.length)
+        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + j) / KEEP, p), h);
+      const float2 d = lds_d[j * kChannels + w.ch];
+      float b[S], c[S], y = 0.f;
+      read_states<S>(lds_b + j * N + w.q * S, b);
+      if (!ENDS) read_states<S>(lds_c + j * N + w.q * S, c);
+#pragma unroll
+      for (int i = 0; i < S; i++) {
+        h[i] = fmaf(fast_exp2(d.x * A[i]), h[i], d.y * b[i]);
+        if (!ENDS) y = fmaf(h[i], c[i], y);
+      }
+      if (ENDS)
+        total += d.x;
+      else
+        lds_y[j * kChannels + w.ch] = state_sum<Q>(y); // the same from each of the Q lanes
+    }
+    __syncthreads();
+    if (!ENDS && tile.on) {
+#pragma unroll
+      for (int k = 0; k < TileT::NV; k++) {
+        const int r = k * TileT::rows + tile.r, t = t0 + r;
+        float y[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+          y[i] = fmaf(D[i], (float)u0[k][i], lds_y[r * kChannels + tile.c + i]);
+          if (a.z.data) {
+            const float zi = (float)z0[k][i];
+            y[i] *= zi * sigmoid(zi);
+          }
+          if (t >= end) y[i] = 0.f;
+        }
+        if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, y);
+      }
+    }
   }
-  if (a.state_out) store_vec<4>(a.state_out + at, ns, h);
+  if (ENDS) {
+    if (w.on) {
+      write_states<S>(w.padded(p.ends, w.b * p.chunks + w.piece, p), h);
+      if (w.q == 0) p.steps[(w.b * p.chunks + w.piece) * a.width + w.d] = total;
+    }
+  } else if (a.state_out && w.piece == p.chunks - 1) {
+    w.store(a.state_out, w.b, p, h);
+  }
 }
 
-template <class T, int Q>
-__global__ __launch_bounds__(kThreads) void k_scan_backward(ScanParams p) {
+// Backward.  Tiles from the last to the first: staged as forward (with dy =
+// dout z sigmoid(z)), then the lanes compute the tile's states again from the
+// kept one, with the decays, into registers, and walk back over them.  The
+// sums over a channel's states take the staged inputs' places in LDS (a
+// channel is read and written by one wave), where the staging threads pick
+// them up for du, ddt and dz.  ENDS: only the gradient of the state before the chunk,
+// from nothing after it, and its sum of delta.
+template <class T, int Q, int S, int VEC, bool ENDS>
+__global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
+  constexpr int TILE = keep_of(S), N = Q * S, THREADS = kChannels * Q, WAVES = Q;
+  __shared__ float2 lds_d[TILE * kChannels];
+  __shared__ float lds_dy[TILE * kChannels], lds_c[TILE * N], lds_b[ENDS ? 1 : TILE * N];
+  __shared__ float lds_bc[ENDS ? 1 : WAVES * TILE * 2 * N];
   const rc_scan_args& a = p.a;
-  const Place<Q> w(p);
+  const Place<Q, S> w(p);
+  const Tile<T, Q, VEC, TILE> tile(p, w.g, w.blk);
+  using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
-  const int ns = w.on ? max(0, min(4, a.states - 4 * w.q)) : 0;
-  const int64_t at = (w.b * a.width + w.d) * a.states + 4 * w.q;
-  float A[4], g[4], dA[4];          // g: gradient of the state before the later token
-  load_vec<4>(a.A + w.d * a.states + 4 * w.q, ns, A);
+  const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  float A[S], g[S], dA[S], total = 0.f;                // g: of the state before the later token
+  w.load(a.A, 0, p, A);
 #pragma unroll
-  for (int i = 0; i < 4; i++) g[i] = dA[i] = 0.f;
-  if (a.dstate_out) load_vec<4>(a.dstate_out + at, ns, g);
-  const float D = a.D ? a.D[w.d] : 0.f, bias = a.dt_bias ? a.dt_bias[w.d] : 0.f;
-  float dD = 0.f, dbias = 0.f;
-  for (int tile = p.tiles - 1; tile >= 0; tile--) {
-    const int t0 = tile * kTile;
-    float h0[4], h[kTile][4];
-    load_vec<4>(a.kept + ((w.b * p.tiles + tile) * a.width + w.d) * (4 * Q) + 4 * w.q, 4, h0);
+  for (int i = 0; i < S; i++) {
+    A[i] *= kLog2e;
+    g[i] = dA[i] = 0.f;
+  }
+  if (!ENDS) {
+    if (a.dstate_out) w.load(a.dstate_out, w.b, p, g);
+    if (p.chunks > 1) enter<Q, S, true>(p, w, A, g);
+  }
+  float D[VEC], bias[VEC], dD[VEC], dbias[VEC];
+  tile.vector(a.D, D);
+  tile.vector(a.dt_bias, bias);
 #pragma unroll
-    for (int j = 0; j < kTile; j++) {
-      const int t = t0 + j;
-      float B[4] = {0.f, 0.f, 0.f, 0.f}, u = 0.f, delta = 0.f;
-      if (t < end) {
-        load_states(row<T>(a.B, w.b, t) + w.g * a.B_group, w.q, a.states, B);
-        u = (float)row<T>(a.u, w.b, t)[w.d];
-        delta = delta_of((float)row<T>(a.dt, w.b, t)[w.d] + bias, a.softplus);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        h[j][i] = fmaf(fast_exp2(delta * A[i] * kLog2e), j ? h[j ? j - 1 : 0][i] : h0[i],
-                       delta * u * B[i]);
+  for (int i = 0; i < VEC; i++) dD[i] = dbias[i] = 0.f;
+  typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV], dout[TileT::NV];
+  StateTile<T, N, TILE, THREADS> B, C;
+  float h0[S];
+  const auto fetch = [&](int t0) {
+    if (!ENDS) tile.load(a.u, w.b, t0, a.length, u);
+    tile.load(a.dt, w.b, t0, a.length, dt);
+    if (a.z.data) tile.load(a.z, w.b, t0, a.length, z);
+    tile.load(a.dy, w.b, t0, a.length, dout);
+    C.load(a.C, w.g * a.C_group, w.b, t0, a);
+    if (!ENDS) {
+      B.load(a.B, w.g * a.B_group, w.b, t0, a);
+      read_states<S>(w.padded(a.kept, w.b * p.keeps + t0 / TILE, p), h0);
     }
+  };
+  // tiles past the end: zeros
+  const int live = t_first + (int)cdiv(max(0, min(t_last, end) - t_first), TILE) * TILE;
+  if (!ENDS) {
+    const float zero[VEC] = {};
+    for (int t = live + threadIdx.x / TileT::columns; t < t_last; t += THREADS / TileT::columns)
+      if (w.blk * kChannels + tile.c < p.group_width) {
+        store_vec<VEC>(row_out<T>(a.du, w.b, t) + tile.d, VEC, zero);
+        store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, zero);
+        if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, zero);
+      }
+    const int64_t cell = ((w.blk * (int64_t)a.batch + w.b) * a.length) * a.groups + w.g;
+    for (int e = threadIdx.x; e < max(0, t_last - live) * 2 * N; e += THREADS)
+      p.part_bc[(cell + (int64_t)(live + e / (2 * N)) * a.groups) * (2 * N) + e % (2 * N)] = 0.f;
+  }
+  if (live > t_first) fetch(live - TILE);
+  for (int t0 = live - TILE; t0 >= t_first; t0 -= TILE) {
 #pragma unroll
-    for (int j = kTile - 1; j >= 0; j--) {
-      const int t = t0 + j;
-      if (t >= a.length) continue;
-      float B[4] = {0.f, 0.f, 0.f, 0.f}, C[4] = {0.f, 0.f, 0.f, 0.f};
-      float u = 0.f, raw = 0.f, delta = 0.f, z = 0.f, dout = 0.f;
-      const bool live = t < end && w.on;
-      if (live) {
-        load_states(row<T>(a.B, w.b, t) + w.g * a.B_group, w.q, a.states, B);
-        load_states(row<T>(a.C, w.b, t) + w.g * a.C_group, w.q, a.states, C);
-        u = (float)row<T>(a.u, w.b, t)[w.d];
-        raw = (float)row<T>(a.dt, w.b, t)[w.d] + bias;
-        delta = delta_of(raw, a.softplus);
-        dout = (float)row<T>(a.dy, w.b, t)[w.d];
-        if (a.z.data) z = (float)row<T>(a.z, w.b, t)[w.d];
-      }
-      const float s = sigmoid(z), dy = a.z.data ? dout * (z * s) : dout;
-      float y = 0.f, through = 0.f, dd = 0.f, dB[4], dC[4];
+    for (int k = 0; k < TileT::NV; k++) {
+      const int r = k * TileT::rows + tile.r;
+      const bool ok = tile.on && t0 + r < end;
+      if (r < TILE && tile.r < TileT::rows) {
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const float before = j ? h[j ? j - 1 : 0][i] : h0[i];
-        y = fmaf(h[j][i], C[i], y);
-        const float gi = fmaf(C[i], dy, g[i]);
-        dC[i] = dy * h[j][i];
-        dB[i] = gi * (delta * u);
-        through = fmaf(gi, B[i], through);
-        g[i] = fast_exp2(delta * A[i] * kLog2e) * gi;
-        const float via = g[i] * before;
-        dA[i] = fmaf(via, delta, dA[i]);
-        dd = fmaf(via, A[i], dd);
+        for (int i = 0; i < VEC; i++) {
+          const float delta = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
+          const float zi = (float)z[k][i], act = a.z.data ? zi * sigmoid(zi) : 1.f;
+          const int at = r * kChannels + tile.c + i;
+          lds_d[at] = {delta, !ENDS && ok ? delta * (float)u[k][i] : 0.f};
+          lds_dy[at] = ok ? (float)dout[k][i] * act : 0.f;
+        }
       }
-      y = fmaf(D, u, state_sum<Q>(y));
-      through = state_sum<Q>(through);
-      dd = fmaf(u, through, state_sum<Q>(dd));
-      const float draw = live ? (a.softplus ? dd * sigmoid(raw) : dd) : 0.f;
-      dD = fmaf(dy, u, dD);
-      dbias += draw;
-      if (w.on && w.q == 0) {
-        row_out<T>(a.du, w.b, t)[w.d] = (T)fmaf(delta, through, D * dy);
-        row_out<T>(a.ddt, w.b, t)[w.d] = (T)draw;
-        if (a.z.data)
-          row_out<T>(a.dz, w.b, t)[w.d] = (T)(dout * y * (s * (1.f + z * (1.f - s))));
-      }
-      float* out = p.part_bc +
-                   (((w.part * (int64_t)a.batch + w.b) * a.length + t) * a.groups + w.g) * (8 * Q);
+    }
+    C.put(lds_c, t0, end, a.states);
+    if (!ENDS) B.put(lds_b, t0, end, a.states);
+    float h[ENDS ? 1 : TILE + 1][S], decay[ENDS ? 1 : TILE][S];
+    if (!ENDS) {
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        dB[i] = channel_sum<Q>(dB[i]);
-        dC[i] = channel_sum<Q>(dC[i]);
+      for (int i = 0; i < S; i++) h[0][i] = h0[i];
+    }
+    __syncthreads();
+    typename TileT::Raw u0[TileT::NV], dt0[TileT::NV], z0[TileT::NV], dout0[TileT::NV];
+#pragma unroll
+    for (int k = 0; k < TileT::NV; k++) {
+      u0[k] = u[k];
+      dt0[k] = dt[k];
+      z0[k] = z[k];
+      dout0[k] = dout[k];
+    }
+    fetch(max(t0 - TILE, t_first));
+    if (ENDS) {
+#pragma unroll 8
+      for (int j = TILE - 1; j >= 0; j--) {
+        const float delta = lds_d[j * kChannels + w.ch].x, dy = lds_dy[j * kChannels + w.ch];
+        float c[S];
+        read_states<S>(lds_c + j * N + w.q * S, c);
+#pragma unroll
+        for (int i = 0; i < S; i++) g[i] = fast_exp2(delta * A[i]) * fmaf(c[i], dy, g[i]);
+        total += delta;
       }
-      if (threadIdx.x % 64 < Q) {
-        store_vec<4>(out + 4 * w.q, 4, dB);
-        store_vec<4>(out + 4 * Q + 4 * w.q, 4, dC);
+    } else {
+#pragma unroll
+      for (int j = 0; j < TILE; j++) {
+        const float2 d = lds_d[j * kChannels + w.ch];
+        float b[S];
+        read_states<S>(lds_b + j * N + w.q * S, b);
+#pragma unroll
+        for (int i = 0; i < S; i++) {
+          decay[j][i] = fast_exp2(d.x * A[i]);
+          h[j + 1][i] = fmaf(decay[j][i], h[j][i], d.y * b[i]);
+        }
       }
+#pragma unroll
+      for (int j = TILE - 1; j >= 0; j--) {
+        const int at = j * kChannels + w.ch;
+        const float2 d = lds_d[at];
+        const float dy = lds_dy[at];
+        float b[S], c[S], v[2 * S], y = 0.f, through = 0.f, dd = 0.f;
+        read_states<S>(lds_b + j * N + w.q * S, b);
+        read_states<S>(lds_c + j * N + w.q * S, c);
+#pragma unroll
+        for (int i = 0; i < S; i++) {
+          y = fmaf(h[j + 1][i], c[i], y);
+          const float gi = fmaf(c[i], dy, g[i]);
+          v[i] = gi * d.y;
+          v[S + i] = dy * h[j + 1][i];
+          through = fmaf(gi, b[i], through);
+          g[i] = decay[j][i] * gi;
+          const float via = g[i] * h[j][i];
+          dA[i] = fmaf(via, d.x, dA[i]);
+          dd = fmaf(via, A[i], dd);
+        }
+        lds_d[at] = {state_sum<Q>(through), state_sum<Q>(dd)};
+        lds_dy[at] = state_sum<Q>(y);
+#pragma unroll
+        for (int i = 0; i < 2 * S; i++) v[i] = row_channel_sum<Q>(v[i]);
+        // rows hold values (row & 1) + 2 (row >> 1) + 4 m of v
+#pragma unroll
+        for (int m = 0; m < 2 * S / 4; m++) {
+          const float x = half_pair_sum(row_pair_sum(v[4 * m], v[4 * m + 1]),
+                                        row_pair_sum(v[4 * m + 2], v[4 * m + 3]));
+          const int e = 4 * m + lane / 16;             // of dB[S], dC[S]
+          lds_bc[(wave * TILE + j) * 2 * N + e / S * N + w.q * S + e % S] = x;
+        }
+      }
+    }
+    __syncthreads();
+    if (!ENDS) {
+      const int64_t cell = ((w.blk * (int64_t)a.batch + w.b) * a.length + t0) * a.groups + w.g;
+      for (int e = threadIdx.x; e < TILE * 2 * N; e += THREADS) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < WAVES; k++) s += lds_bc[k * TILE * 2 * N + e];
+        if (t0 + e / (2 * N) < t_last)
+          p.part_bc[(cell + (int64_t)(e / (2 * N)) * a.groups) * (2 * N) + e % (2 * N)] = s;
+      }
+#pragma unroll
+      for (int k = 0; k < TileT::NV; k++) {
+        const int r = k * TileT::rows + tile.r, t = t0 + r;
+        if (!tile.on || t >= t_last) continue;
+        const bool ok = t < end;
+        float du[VEC], ddt[VEC], dz[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+          const float2 sums = lds_d[r * kChannels + tile.c + i];
+          const float ui = (float)u0[k][i], zi = (float)z0[k][i], o = (float)dout0[k][i];
+          const float raw = (float)dt0[k][i] + bias[i], s = sigmoid(zi);
+          const float dy = a.z.data ? o * (zi * s) : o;
+          const float y = fmaf(D[i], ui, lds_dy[r * kChannels + tile.c + i]);
+          const float dd = fmaf(ui, sums.x, sums.y * kLn2);
+          du[i] = ok ? fmaf(delta_of(raw, a.softplus), sums.x, D[i] * dy) : 0.f;
+          ddt[i] = ok ? (a.softplus ? dd * sigmoid(raw) : dd) : 0.f;
+          dz[i] = ok ? o * y * (s * (1.f + zi * (1.f - s))) : 0.f;
+          dD[i] += ok ? dy * ui : 0.f;
+          dbias[i] += ddt[i];
+        }
+        store_vec<VEC>(row_out<T>(a.du, w.b, t) + tile.d, VEC, du);
+        store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, ddt);
+        if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, dz);
+      }
+      __syncthreads();                                 // the next tile takes the same LDS
     }
   }
-  if (!w.on) return;
-  if (a.dstate_in) store_vec<4>(a.dstate_in + at, ns, g);
-  store_vec<4>(p.part_a + (w.b * a.width + w.d) * (4 * Q) + 4 * w.q, 4, dA);
-  if (w.q == 0) {
-    p.part_d[(w.b * a.width + w.d) * 2] = dD;
-    p.part_d[(w.b * a.width + w.d) * 2 + 1] = dbias;
+  const int64_t before = w.b * p.chunks + w.piece;
+  if (ENDS) {
+    if (w.on) {
+      write_states<S>(w.padded(p.ends, before, p), g);
+      if (w.q == 0) p.steps[before * a.width + w.d] = total;
+    }
+    return;
+  }
+  if (w.on) write_states<S>(w.padded(p.part_a, before, p), dA);
+  if (a.dstate_in && w.piece == 0) w.store(a.dstate_in, w.b, p, g);
+  // D and dt_bias: the threads of a column, then one sum for each channel
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(lds_d);       // [rows][channels] of (dD, dbias)
+  if (tile.r < TileT::rows) {
+#pragma unroll
+    for (int i = 0; i < VEC; i++) {
+      sums[(tile.r * kChannels + tile.c + i) * 2] = dD[i];
+      sums[(tile.r * kChannels + tile.c + i) * 2 + 1] = dbias[i];
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < 2 * kChannels; e += THREADS) {
+    if (w.blk * kChannels + e / 2 >= p.group_width) continue;
+    float s = 0.f;
+    for (int r = 0; r < TileT::rows; r++) s += sums[r * 2 * kChannels + e];
+    p.part_d[(before * a.width + w.g * p.group_width + w.blk * kChannels + e / 2) * 2 + e % 2] = s;
   }
 }
 
-// dB and dC from the waves' parts: one thread per (batch, token, group, state).
+// dB and dC from the blocks' parts: one thread per (batch, token, group, state).
 template <class T>
 __global__ __launch_bounds__(256) void k_scan_sum_bc(const float* in, int64_t parts, int64_t cells,
                                                      int32_t padded, int32_t states, T* dB, T* dC) {
@@ -253,7 +577,7 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(const float* in, int64_t pa
   (k < padded ? dB : dC)[cell * states + n] = (T)s;
 }
 
-// dA, dD and ddt_bias from the sequences' parts.
+// dA, dD and ddt_bias from the parts of sequences and chunks.
 __global__ __launch_bounds__(256) void k_scan_sum_a(const float* pa, const float* pd,
                                                     int64_t parts, int32_t width, int32_t padded,
                                                     int32_t states, float* dA, float* dD,
@@ -274,10 +598,12 @@ __global__ __launch_bounds__(256) void k_scan_sum_a(const float* pa, const float
   }
 }
 
+constexpr int kStepThreads = 256;
+
 template <class T, int Q>
-__global__ __launch_bounds__(kThreads) void k_scan_step(rc_scan_step_args a, int32_t blocks) {
+__global__ __launch_bounds__(kStepThreads) void k_scan_step(rc_scan_step_args a, int32_t blocks) {
   const int64_t b = blockIdx.x / blocks;
-  const int64_t d = (int64_t)(blockIdx.x % blocks) * (kThreads / Q) + threadIdx.x / Q;
+  const int64_t d = (int64_t)(blockIdx.x % blocks) * (kStepThreads / Q) + threadIdx.x / Q;
   const int q = threadIdx.x % Q;
   if (d >= a.width) return;
   const int64_t slot = a.slots ? a.slots[b] : b;
@@ -307,9 +633,9 @@ __global__ __launch_bounds__(kThreads) void k_scan_step(rc_scan_step_args a, int
   if (q == 0) row_out<T>(a.y, b, 0)[d] = (T)y;
 }
 
-int lanes_of(int32_t states) {
+int lanes_of(int32_t states, int S) {
   int q = 1;
-  while (4 * q < states) q *= 2;
+  while (S * q < states) q *= 2;
   return q;
 }
 
@@ -333,22 +659,54 @@ bool scan_sizes_ok(const rc_scan_args* a) {
   return a && scan_sizes_ok(a->dtype, a->batch, a->length, a->width, a->states, a->groups);
 }
 
+// How a scan is cut up.  Each wave of a SIMD issues an instruction every six
+// cycles at best, two together one every three: at least two waves a SIMD
+// are wanted.  Two states a lane give twice as many waves as four (and pay with
+// more lanes to sum over); beyond that the length is cut into chunks, which costs a
+// pass over all but one of them for their end states.
+struct ScanPlan {
+  int S, Q, VEC;
+  int64_t group_width, blocks;
+  int64_t chunks, chunk, keeps;
+};
 ScanPlan scan_plan(const rc_scan_args& a) {
   ScanPlan p;
-  p.Q = lanes_of(a.states);
   p.group_width = a.width / a.groups;
-  p.blocks = cdiv(p.group_width, kThreads / p.Q);
-  p.tiles = cdiv(a.length, kTile);
+  p.blocks = cdiv(p.group_width, kChannels);
+  const int64_t rows = (int64_t)a.batch * a.groups * p.blocks;
+  const int64_t want = 8 * (int64_t)rcdp::num_cus();             // waves
+  p.S = a.states > 32 || rows * lanes_of(a.states, 4) >= want ? 4 : 2;
+  p.Q = lanes_of(a.states, p.S);
+  p.VEC = p.group_width % 4 ? 1 : 4;
+  p.chunks = 1;
+  const int64_t most = cdiv(a.length, 64) < 32 ? cdiv(a.length, 64) : 32;
+  if (rows > 0 && rows * p.Q < want) p.chunks = cdiv(want, rows * p.Q);
+  if (p.chunks > most) p.chunks = most;
+  if (p.chunks < 1) p.chunks = 1;
+  p.chunk = cdiv(cdiv(a.length, p.chunks), kFwdTile) * kFwdTile;
+  if (p.chunk < kFwdTile) p.chunk = kFwdTile;
+  p.chunks = a.length > 0 ? cdiv(a.length, p.chunk) : 1;
+  p.keeps = cdiv(a.length, keep_of(p.S));
   return p;
 }
 
 struct ScanScratch {
-  uint64_t bc, a, d;
+  uint64_t ends, steps, bc, a, d;
+  uint64_t total() const { return ends + steps + bc + a + d; }
 };
-ScanScratch scan_scratch(const rc_scan_args& a, const ScanPlan& p) {
-  const uint64_t rows = (uint64_t)a.batch * a.width;
-  return {(uint64_t)p.blocks * (kThreads / 64) * a.batch * a.length * a.groups * 8 * p.Q * 4,
-          rows * 4 * p.Q * 4, rows * 2 * 4};
+ScanScratch scan_scratch(const rc_scan_args& a, const ScanPlan& p, bool backward) {
+  const uint64_t rows = (uint64_t)a.batch * p.chunks * a.width, N = p.Q * p.S;
+  ScanScratch s = {};
+  if (p.chunks > 1) {
+    s.ends = rows * N * 4;
+    s.steps = (rows * 4 + 255) & ~255ull;
+  }
+  if (backward) {
+    s.bc = (uint64_t)p.blocks * a.batch * a.length * a.groups * 2 * N * 4;
+    s.a = rows * N * 4;
+    s.d = rows * 2 * 4;
+  }
+  return s;
 }
 
 int scan_check(const rc_scan_args* a, bool backward) {
@@ -368,19 +726,40 @@ int scan_check(const rc_scan_args* a, bool backward) {
     return RC_E_ARG;
   const ScanPlan p = scan_plan(*a);
   const int64_t cells = (int64_t)a->batch * a->length * a->groups;
-  if (p.blocks * a->groups * a->batch >= kMaxBlocks || cdiv(cells * 8 * p.Q, 256) >= kMaxBlocks)
+  if (p.blocks * a->groups * a->batch * p.chunks >= kMaxBlocks ||
+      cdiv(cells * 2 * p.Q * p.S, kSumThreads) >= kMaxBlocks)
     return RC_E_OVERFLOW;
   return RC_OK;
 }
 
-ScanParams scan_params(const rc_scan_args& a, const ScanPlan& p) {
+ScanParams scan_params(const rc_scan_args& a, const ScanPlan& p, const ScanScratch& s) {
   ScanParams q = {};
   q.a = a;
   q.group_width = (int32_t)p.group_width;
   q.blocks = (int32_t)p.blocks;
-  q.tiles = (int32_t)p.tiles;
-  q.parts = (int32_t)p.blocks * (kThreads / 64);
+  q.chunks = (int32_t)p.chunks;
+  q.chunk = (int32_t)p.chunk;
+  q.keeps = (int32_t)p.keeps;
+  char* ws = static_cast<char*>(a.workspace);
+  q.ends = reinterpret_cast<float*>(ws);
+  q.steps = reinterpret_cast<float*>(ws + s.ends);
+  q.part_bc = reinterpret_cast<float*>(ws + s.ends + s.steps);
+  q.part_a = reinterpret_cast<float*>(ws + s.ends + s.steps + s.bc);
+  q.part_d = reinterpret_cast<float*>(ws + s.ends + s.steps + s.bc + s.a);
   return q;
+}
+
+// Calls f(Q, S, VEC) with the plan's constants.
+template <class F>
+int by_plan(const ScanPlan& p, F&& f) {
+  using std::integral_constant;
+  const auto with = [&](auto S) {
+    return by_lanes(p.Q, [&](auto Q) {
+      if (p.VEC == 1) return f(Q, S, integral_constant<int, 1>{});
+      return f(Q, S, integral_constant<int, 4>{});
+    });
+  };
+  return p.S == 2 ? with(integral_constant<int, 2>{}) : with(integral_constant<int, 4>{});
 }
 
 }  // namespace
@@ -388,20 +767,19 @@ ScanParams scan_params(const rc_scan_args& a, const ScanPlan& p) {
 extern "C" int rc_scan_kept_bytes(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
   const ScanPlan p = scan_plan(*a);
-  *bytes_host = (uint64_t)a->batch * p.tiles * a->width * 4 * p.Q * 4;
+  *bytes_host = (uint64_t)a->batch * p.keeps * a->width * p.Q * p.S * 4;
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = 0;
+  *bytes_host = scan_scratch(*a, scan_plan(*a), false).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_backward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  const ScanScratch s = scan_scratch(*a, scan_plan(*a));
-  *bytes_host = s.bc + s.a + s.d;
+  *bytes_host = scan_scratch(*a, scan_plan(*a), true).total();
   return RC_OK;
 }
 
@@ -409,12 +787,21 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, false)) return st;
   const rc_scan_args& a = *args;
   const ScanPlan p = scan_plan(a);
-  const int64_t blocks = p.blocks * a.groups * a.batch;
+  const ScanScratch need = scan_scratch(a, p, false);
+  if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
+  const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
   if (blocks == 0) return RC_OK;
+  const ScanParams q = scan_params(a, p, need);
+  const hipStream_t s = (hipStream_t)stream;
   return by_dtype(a.dtype, [&](auto t) {
-    return by_lanes(p.Q, [&](auto q) {
-      k_scan_forward<decltype(t), q()><<<dim3((uint32_t)blocks), kThreads, 0,
-                                         (hipStream_t)stream>>>(scan_params(a, p));
+    return by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
+      using T = decltype(t);
+      const dim3 grid((uint32_t)blocks), threads(kChannels * Q());
+      if (p.chunks > 1) {
+        k_scan_forward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
+        if (const int st = launched("k_scan_forward ends")) return st;
+      }
+      k_scan_forward<T, Q(), S(), VEC(), false><<<grid, threads, 0, s>>>(q);
       return launched("k_scan_forward");
     });
   });
@@ -424,37 +811,37 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, true)) return st;
   const rc_scan_args& a = *args;
   const ScanPlan p = scan_plan(a);
-  const ScanScratch need = scan_scratch(a, p);
-  const uint64_t total = need.bc + need.a + need.d;
-  if (total > 0 && (!a.workspace || a.workspace_bytes < total)) return RC_E_SCRATCH;
+  const ScanScratch need = scan_scratch(a, p, true);
+  if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   if (a.width == 0) return RC_OK;
-  ScanParams q = scan_params(a, p);
-  char* ws = static_cast<char*>(a.workspace);
-  q.part_bc = reinterpret_cast<float*>(ws);
-  q.part_a = reinterpret_cast<float*>(ws + need.bc);
-  q.part_d = reinterpret_cast<float*>(ws + need.bc + need.a);
+  const ScanParams q = scan_params(a, p, need);
   const hipStream_t s = (hipStream_t)stream;
-  const int64_t blocks = p.blocks * a.groups * a.batch;
+  const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
   const int64_t cells = (int64_t)a.batch * a.length * a.groups;
+  const int N = p.Q * p.S;
   return by_dtype(a.dtype, [&](auto t) -> int {
     using T = decltype(t);
     if (blocks > 0) {
-      const int st = by_lanes(p.Q, [&](auto lanes) {
-        k_scan_backward<T, lanes()><<<dim3((uint32_t)blocks), kThreads, 0, s>>>(q);
+      const int st = by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
+        const dim3 grid((uint32_t)blocks), threads(kChannels * Q());
+        if (p.chunks > 1) {
+          k_scan_backward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
+          if (const int e = launched("k_scan_backward ends")) return e;
+        }
+        k_scan_backward<T, Q(), S(), VEC(), false><<<grid, threads, 0, s>>>(q);
         return launched("k_scan_backward");
       });
       if (st) return st;
     }
     if (cells > 0) {
-      k_scan_sum_bc<T><<<dim3((uint32_t)cdiv(cells * 8 * p.Q, 256)), 256, 0, s>>>(
-          q.part_bc, q.parts, cells, 4 * p.Q, a.states, static_cast<T*>(a.dB),
-          static_cast<T*>(a.dC));
+      k_scan_sum_bc<T><<<dim3((uint32_t)cdiv(cells * 2 * N, kSumThreads)), kSumThreads, 0, s>>>(
+          q.part_bc, p.blocks, cells, N, a.states, static_cast<T*>(a.dB), static_cast<T*>(a.dC));
       if (const int st = launched("k_scan_sum_bc")) return st;
     }
-    const int64_t cols = (int64_t)a.width * 4 * p.Q;
+    const int64_t cols = (int64_t)a.width * N;
     k_scan_sum_a<<<dim3((uint32_t)(cdiv(cols, kSumCols) + cdiv(2 * (int64_t)a.width, kSumCols))),
-                   256, 0, s>>>(q.part_a, q.part_d, a.batch, a.width, 4 * p.Q, a.states, a.dA,
-                                a.dD, a.ddt_bias);
+                   kSumThreads, 0, s>>>(q.part_a, q.part_d, a.batch * p.chunks, a.width, N,
+                                        a.states, a.dA, a.dD, a.ddt_bias);
     return launched("k_scan_sum_a");
   });
 }
@@ -468,12 +855,12 @@ extern "C" int rc_scan_step(const rc_scan_step_args* args, void* stream) {
   if (a.batch == 0 || a.width == 0) return RC_OK;
   if (!a.u.data || !a.dt.data || !a.B.data || !a.C.data || !a.y.data || !a.A || !a.state)
     return RC_E_ARG;
-  const int Q = lanes_of(a.states);
-  const int64_t blocks = cdiv(a.width, kThreads / Q);
+  const int Q = lanes_of(a.states, 4);
+  const int64_t blocks = cdiv(a.width, kStepThreads / Q);
   if (blocks * a.batch >= kMaxBlocks) return RC_E_OVERFLOW;
   return by_dtype(a.dtype, [&](auto t) {
     return by_lanes(Q, [&](auto q) {
-      k_scan_step<decltype(t), q()><<<dim3((uint32_t)(blocks * a.batch)), kThreads, 0,
+      k_scan_step<decltype(t), q()><<<dim3((uint32_t)(blocks * a.batch)), kStepThreads, 0,
                                       (hipStream_t)stream>>>(a, (int32_t)blocks);
       return launched("k_scan_step");
     });
