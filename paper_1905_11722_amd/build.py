@@ -1,10 +1,11 @@
-"""Compile the HIP libraries for gfx950 with hipcc.
+"""Compile the HIP libraries for gfx950 with hipcc, and the PyTorch binding.
 
 All HIP sources under ``csrc/`` are compiled into one shared library,
 ``librcdp.so``, next to this file: the solver behind include/rc.h.  The
 microbenchmarks of the chip's peaks under ``peak/`` (measurement only, not
 part of the solver) go into ``libpeak.so``.  Packed-FP32 instruction
-selection is disabled.
+selection is disabled.  The operators' PyTorch binding under ``bind/`` is
+host code: g++ compiles it against the installed PyTorch into ``_ops.so``.
 """
 
 import glob
@@ -15,6 +16,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "librcdp.so")
+OPS_LIB = os.path.join(HERE, "_ops.so")
 PEAK_LIB = os.path.join(HERE, "libpeak.so")
 ARCH = os.environ.get("RCDP_OFFLOAD_ARCH", "gfx950")
 
@@ -57,8 +59,35 @@ def _compile(lib, srcs, verbose):
     os.replace(tmp, lib)
 
 
+def bind_command(out):
+    """One g++ line that builds the PyTorch binding (links librcdp.so)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    include = [os.path.join(ROOT, "include"), *cpp_extension.include_paths(),
+               os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+             "-DUSE_ROCM=1", "-DTORCH_EXTENSION_NAME=_ops",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+            + [x for d in include for x in ("-isystem", d)]
+            + [os.path.join(HERE, "bind", "ops_bind.cpp"), "-L", HERE, "-lrcdp", "-L", lib, "-lc10",
+               "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-o", out])
+
+
+def build_binding(verbose=False):
+    cmd = bind_command(OPS_LIB + ".tmp")
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(OPS_LIB + ".tmp", OPS_LIB)
+
+
 def build(verbose=False):
     _compile(LIB, sources(), verbose)
+    build_binding(verbose)
     _compile(PEAK_LIB, sorted(glob.glob(os.path.join(HERE, "peak", "*.hip"))), verbose)
     return LIB
 

@@ -12,12 +12,13 @@ import pytest
 import torch
 
 from paper_1905_11722_amd import ops, rcdp
+from tests import ops_abi as abi
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "rc_ops.h")
-STRUCTS = {"rc_conv_args": ops._ConvArgs, "rc_conv_step_args": ops._ConvStepArgs,
-           "rc_scan_args": ops._ScanArgs, "rc_scan_step_args": ops._ScanStepArgs,
-           "rc_norm_args": ops._NormArgs}
+STRUCTS = {"rc_conv_args": abi.ConvArgs, "rc_conv_step_args": abi.ConvStepArgs,
+           "rc_scan_args": abi.ScanArgs, "rc_scan_step_args": abi.ScanStepArgs,
+           "rc_norm_args": abi.NormArgs}
 
 
 def test_every_declared_symbol_is_exported():
@@ -53,24 +54,24 @@ X = 0x1000          # stands for a device pointer; no call below gets as far as 
 
 
 def view(data=X):
-    return ops._View(data, 64, 8)
+    return abi.View(data, 64, 8)
 
 
 def conv(**kw):
-    a = ops._ConvArgs(dtype=1, activation=1, batch=2, length=8, width=8, taps=4, x=view(), y=view(),
+    a = abi.ConvArgs(dtype=1, activation=1, batch=2, length=8, width=8, taps=4, x=view(), y=view(),
                       weight=X, dy=view(), dx=view())
     return set_all(a, kw)
 
 
 def scan(**kw):
-    a = ops._ScanArgs(dtype=1, batch=2, length=8, width=8, states=16, groups=2, u=view(), dt=view(),
+    a = abi.ScanArgs(dtype=1, batch=2, length=8, width=8, states=16, groups=2, u=view(), dt=view(),
                       B=view(), C=view(), y=view(), A=X, kept=X, dy=view(), du=view(), ddt=view(),
                       dB=X, dC=X, dA=X)
     return set_all(a, kw)
 
 
 def norm(**kw):
-    a = ops._NormArgs(dtype=1, gate_activation=1, rows=4, width=8, eps=1e-5, block=view(),
+    a = abi.NormArgs(dtype=1, gate_activation=1, rows=4, width=8, eps=1e-5, block=view(),
                       residual=view(), out=view(), normed=view(), pre_weight=X, stats=X,
                       dblock=view(), dresidual=view())
     return set_all(a, kw)
@@ -82,7 +83,7 @@ def set_all(a, kw):
     return a
 
 
-NONE = ops._View()
+NONE = abi.View()
 BAD = [
     ("rc_conv_forward", conv, dict(dtype=3)), ("rc_conv_forward", conv, dict(dtype=-1)),
     ("rc_conv_forward", conv, dict(param_dtype=2)), ("rc_conv_forward", conv, dict(activation=2)),
@@ -110,11 +111,11 @@ BAD = [
 
 @pytest.mark.parametrize("call,make,change", BAD, ids=lambda v: v if isinstance(v, str) else None)
 def test_bad_arguments(call, make, change):
-    assert getattr(ops._library(), call)(make(**change), None) == rcdp.E_ARG
+    assert getattr(abi.library(), call)(make(**change), None) == rcdp.E_ARG
 
 
 def test_null_and_scratch():
-    lib = ops._library()
+    lib = abi.library()
     n = ctypes.c_uint64()
     for call in ("conv_forward", "conv_backward", "conv_step", "scan_forward", "scan_backward",
                  "scan_step", "norm_forward", "norm_backward"):
@@ -138,13 +139,13 @@ def test_null_and_scratch():
 
 
 def test_step_arguments():
-    lib = ops._library()
-    a = ops._ConvStepArgs(dtype=0, activation=1, batch=3, width=8, taps=4, num_slots=2, x=view(),
+    lib = abi.library()
+    a = abi.ConvStepArgs(dtype=0, activation=1, batch=3, width=8, taps=4, num_slots=2, x=view(),
                           y=view(), state=view(), weight=X)
     assert lib.rc_conv_step(a, None) == rcdp.E_ARG                 # fewer slots than rows
     a.slots, a.weight = X, None
     assert lib.rc_conv_step(a, None) == rcdp.E_ARG
-    b = ops._ScanStepArgs(dtype=0, batch=3, width=8, states=4, groups=1, num_slots=2, u=view(),
+    b = abi.ScanStepArgs(dtype=0, batch=3, width=8, states=4, groups=1, num_slots=2, u=view(),
                           dt=view(), B=view(), C=view(), y=view(), A=X, state=X)
     assert lib.rc_scan_step(b, None) == rcdp.E_ARG
     b.slots, b.state = X, None
@@ -152,7 +153,7 @@ def test_step_arguments():
 
 
 def test_empty_calls_do_nothing():
-    lib = ops._library()
+    lib = abi.library()
     assert lib.rc_conv_forward(conv(batch=0), None) == 0
     assert lib.rc_conv_forward(conv(width=0), None) == 0
     assert lib.rc_scan_forward(scan(batch=0), None) == 0
