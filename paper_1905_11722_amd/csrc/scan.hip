@@ -9,8 +9,8 @@
 //   du = delta sum_n g_n B_n + D dy,  dA_n = sum g_n a_n h_n(before) delta,
 //   ddelta = u sum_n g_n B_n + sum_n g_n a_n h_n(before) A_n.
 //
-// S = 2 or 4 states are one lane's, Q = 1, 2, 4, 8 or 16 neighbouring lanes are
-// a channel's (N <= S Q; missing states have A = B = C = 0), so sums over a
+// S = 1, 2 or 4 states are one lane's, Q = 4, 8 or 16 neighbouring lanes are a
+// channel's (N <= S Q; missing states have A = B = C = 0), so sums over a
 // channel's states are Q-lane sums and sums over channels are strided ones.
 // A token past its sequence's end is a step with delta = u = dy = B = C = 0:
 // the state stays, every product is 0.
@@ -20,13 +20,13 @@ using namespace rcops;
 
 namespace {
 
-constexpr int kChannels = 64;       // of a workgroup
 constexpr int kFwdTile = 32;        // tokens staged together, forward
 constexpr int kSumThreads = 256;
 
-// Tokens between two kept states, and of a backward tile: the states of a
-// tile and their decays stay in registers, 64 of each a lane.
-constexpr int keep_of(int S) { return 64 / S; }
+// Channels of a workgroup, and tokens between two kept states: a backward
+// tile's states and decays stay in registers, at most 64 of each a lane.
+constexpr int channels_of(int Q) { return Q > 8 ? 32 : 64; }
+constexpr int keep_of(int S) { return S > 2 ? 16 : 32; }
 
 __device__ __forceinline__ int seq_end(const int32_t* lengths, int64_t b, int32_t length) {
   if (!lengths) return length;
@@ -34,44 +34,98 @@ __device__ __forceinline__ int seq_end(const int32_t* lengths, int64_t b, int32_
 }
 
 template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
-                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL,
+                                                               0xf, 0xf, true));
 }
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRor4 = 0x124,
-              kRor8 = 0x128;
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 
-// Sum over the Q lanes of a channel, in each of them (a mirror is as good as
-// an exchange once the lanes below are equal).
-template <int Q>
-__device__ __forceinline__ float state_sum(float x) {
-  if (Q > 1) x = dpp_add<kXor1>(x);
-  if (Q > 2) x = dpp_add<kXor2>(x);
-  if (Q > 4) x = dpp_add<kHalfMirror>(x);
-  if (Q > 8) x = dpp_add<kMirror>(x);
-  return x;
+// x of lane J of the quad, in each of its lanes.
+template <int J>
+__device__ __forceinline__ float quad_lane(float x) {
+  return dpp<J * 0x55>(x);
 }
 
-// Sum over the lanes of a row of 16 that hold the same states of different channels.
+// Sums over the Q lanes of a channel of four values at once: lane q gets that
+// of v[q & 3].  (Mirrors first: the quads then hold the whole sums.)
 template <int Q>
-__device__ __forceinline__ float row_channel_sum(float x) {
-  if (Q <= 1) x = dpp_add<kXor1>(x);
-  if (Q <= 2) x = dpp_add<kXor2>(x);
-  if (Q <= 4) x = dpp_add<kRor4>(x);
-  if (Q <= 8) x = dpp_add<kRor8>(x);
-  return x;
+__device__ __forceinline__ float state_sums(float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    if (Q > 4) v[j] += dpp<kHalfMirror>(v[j]);
+    if (Q > 8) v[j] += dpp<kMirror>(v[j]);
+  }
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+  const float a = (odd ? v[1] : v[0]) + dpp<kXor1>(odd ? v[0] : v[1]);
+  const float b = (odd ? v[3] : v[2]) + dpp<kXor1>(odd ? v[2] : v[3]);
+  return (high ? b : a) + dpp<kXor2>(high ? a : b);
 }
-// Sums of x and y over pairs of rows: even rows hold x's, odd ones y's.
-__device__ __forceinline__ float row_pair_sum(float x, float y) {
+
+// One step of a sum over the lanes of a row of 16 that hold the same states
+// of different channels, for pairs of values at once: half of the lanes go on
+// with v[2 i], half with v[2 i + 1].  BANKS = 8: lanes 8 apart, lane bit 3
+// chooses; 4: lanes 4 apart, bit 2 chooses.  The bank masks write each
+// half in place of a select; two wait states before a DPP read and after the
+// block cover what the compiler does not see inside.
+template <int BANKS, int M>
+__device__ __forceinline__ void bank_sums(const float* v, float* r) {
+#pragma unroll
+  for (int i = 0; i < M; i += 2) {
+    if (BANKS == 8)
+      asm("s_nop 1\n\t"
+          "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+          "v_add_f32_dpp %1, %4, %4 row_ror:8 row_mask:0xf bank_mask:0x3\n\t"
+          "v_add_f32_dpp %0, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+          "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+          "s_nop 1"
+          : "=&v"(r[i]), "=&v"(r[i + 1])
+          : "v"(v[2 * i]), "v"(v[2 * i + 1]), "v"(v[2 * i + 2]), "v"(v[2 * i + 3]));
+    else
+      asm("s_nop 1\n\t"
+          "v_add_f32_dpp %0, %2, %2 row_ror:12 row_mask:0xf bank_mask:0x5\n\t"
+          "v_add_f32_dpp %1, %4, %4 row_ror:12 row_mask:0xf bank_mask:0x5\n\t"
+          "v_add_f32_dpp %0, %3, %3 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+          "v_add_f32_dpp %1, %5, %5 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+          "s_nop 1"
+          : "=&v"(r[i]), "=&v"(r[i + 1])
+          : "v"(v[2 * i]), "v"(v[2 * i + 1]), "v"(v[2 * i + 2]), "v"(v[2 * i + 3]));
+  }
+}
+// The same over rows: even rows go on with x, odd ones with y; and over halves.
+__device__ __forceinline__ float row_sums(float x, float y) {
   const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x),
                                                   __builtin_bit_cast(unsigned, y), false, false);
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
-// Sums of x and y over pairs of halves: the low half holds x's, the high one y's.
-__device__ __forceinline__ float half_pair_sum(float x, float y) {
+__device__ __forceinline__ float half_sums(float x, float y) {
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x),
                                                   __builtin_bit_cast(unsigned, y), false, false);
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+// Sums over the 64 / Q channels of a wave of 64 / Q values at once; the lane
+// gets that of v[channel_value<Q>(lane)].
+template <int Q>
+__device__ __forceinline__ float channel_sums(const float* v) {
+  if (Q == 4) {
+    float a[8], b[4];
+    bank_sums<8, 8>(v, a);
+    bank_sums<4, 4>(a, b);
+    return half_sums(row_sums(b[0], b[1]), row_sums(b[2], b[3]));
+  } else if (Q == 8) {
+    float a[4];
+    bank_sums<8, 4>(v, a);
+    return half_sums(row_sums(a[0], a[1]), row_sums(a[2], a[3]));
+  } else {
+    return half_sums(row_sums(v[0], v[1]), row_sums(v[2], v[3]));
+  }
+}
+template <int Q>
+__device__ __forceinline__ int channel_value(int lane) {
+  const int rows = lane >> 4;                          // row bits 0 and 1
+  if (Q == 4) return (lane >> 3 & 1) | (lane >> 2 & 1) << 1 | rows << 2;
+  if (Q == 8) return (lane >> 3 & 1) | rows << 1;
+  return rows;
 }
 
 struct ScanParams {
@@ -104,7 +158,7 @@ __device__ __forceinline__ float delta_of(float raw, bool soft) {
 // (batch, group, chunk, block) go to one XCD, whose L2 then holds the B and C that they share.
 template <int Q, int S>
 struct Place {
-  static constexpr int N = Q * S;
+  static constexpr int N = Q * S, CW = channels_of(Q);
   int64_t b, g;
   int blk, piece;                   // block of channels, chunk
   int q, ch;                        // the lane's states and channel (in the block)
@@ -112,17 +166,17 @@ struct Place {
   bool on;
   __device__ Place(const ScanParams& p) {
     const uint32_t per = gridDim.x / 8, rem = gridDim.x % 8, xcd = blockIdx.x % 8;
-    int64_t i = (int64_t)xcd * per + min(xcd, rem) + blockIdx.x / 8;
-    blk = (int)(i % p.blocks);
-    i /= p.blocks;
-    piece = (int)(i % p.chunks);
-    i /= p.chunks;
-    g = i % p.a.groups;
-    b = i / p.a.groups;
+    uint32_t i = xcd * per + min(xcd, rem) + blockIdx.x / 8;
+    blk = (int)(i % (uint32_t)p.blocks);
+    i /= (uint32_t)p.blocks;
+    piece = (int)(i % (uint32_t)p.chunks);
+    i /= (uint32_t)p.chunks;
+    g = i % (uint32_t)p.a.groups;
+    b = i / (uint32_t)p.a.groups;
     q = threadIdx.x % Q;
     ch = threadIdx.x / Q;
-    on = blk * kChannels + ch < p.group_width;
-    d = g * p.group_width + min(blk * kChannels + ch, p.group_width - 1);
+    on = blk * CW + ch < p.group_width;
+    d = g * p.group_width + min(blk * CW + ch, p.group_width - 1);
   }
   // The lane's S values of an array [.][width][states] (0 for missing states).
   __device__ void load(const float* x, int64_t before, const ScanParams& p, float (&v)[S]) const {
@@ -145,8 +199,9 @@ struct Place {
 // A thread's share of a tile: NV vectors of VEC channels of one column.
 template <class T, int Q, int VEC, int TILE>
 struct Tile {
-  static constexpr int threads = kChannels * Q;
-  static constexpr int columns = kChannels / VEC;
+  static constexpr int CW = channels_of(Q);
+  static constexpr int threads = CW * Q;
+  static constexpr int columns = CW / VEC;
   static constexpr int rows = threads / columns > TILE ? TILE : threads / columns;
   static constexpr int NV = TILE / rows;
   typedef T Raw __attribute__((ext_vector_type(VEC)));
@@ -156,8 +211,8 @@ struct Tile {
   __device__ Tile(const ScanParams& p, int64_t g, int blk) {
     c = threadIdx.x % columns * VEC;
     r = threadIdx.x / columns;
-    on = r < rows && blk * kChannels + c < p.group_width;
-    d = g * p.group_width + min(blk * kChannels + c, p.group_width - VEC);
+    on = r < rows && blk * CW + c < p.group_width;
+    d = g * p.group_width + min(blk * CW + c, p.group_width - VEC);
   }
   // Loads are unconditional (rows clamped to the sequence): what is past an end is
   // dropped where it is used.
@@ -226,13 +281,17 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 }
 
 // Forward.  A tile of tokens is staged to LDS in 32 bits (delta and delta u of
-// 64 channels, B, C), each element converted once by one thread; then the
-// lanes walk over it.  ENDS: only the end state of the chunk from nothing, and its sum of delta.
+// each channel, B, C), each element converted once by one thread; then the
+// lanes walk over it, four tokens at a time: each lane of a quad reads one
+// token's delta and delta u of its channel and the quad shares them, and each
+// ends with one token's y, which takes their place.  Rows of LDS are padded so that the four
+// rows that a quad reads lie in different banks.
+// ENDS: only the end state of the chunk from nothing, and its sum of delta.
 template <class T, int Q, int S, int VEC, bool ENDS>
-__global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
-  constexpr int TILE = kFwdTile, N = Q * S, KEEP = keep_of(S);
-  __shared__ float2 lds_d[TILE * kChannels];
-  __shared__ float lds_b[TILE * N], lds_c[ENDS ? 1 : TILE * N], lds_y[ENDS ? 1 : TILE * kChannels];
+__global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams p) {
+  constexpr int TILE = kFwdTile, N = Q * S, KEEP = keep_of(S), CW = channels_of(Q), ROW = CW + 8;
+  __shared__ float2 lds_d[TILE * ROW];
+  __shared__ __align__(16) float lds_b[TILE * N], lds_c[ENDS ? 4 : TILE * N];
   const rc_scan_args& a = p.a;
   const Place<Q, S> w(p);
   const Tile<T, Q, VEC, TILE> tile(p, w.g, w.blk);
@@ -254,7 +313,7 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
   tile.vector(a.D, D);
   tile.vector(a.dt_bias, bias);
   typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV];
-  StateTile<T, N, TILE, kChannels * Q> B, C;
+  StateTile<T, N, TILE, CW * Q> B, C;
   const auto fetch = [&](int t0) {
     tile.load(a.u, w.b, t0, a.length, u);
     tile.load(a.dt, w.b, t0, a.length, dt);
@@ -279,11 +338,11 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
       const bool ok = tile.on && t0 + r < end;
-      if (r < TILE && tile.r < TileT::rows) {
+      if (tile.r < TileT::rows) {
 #pragma unroll
         for (int i = 0; i < VEC; i++) {
           const float delta = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
-          lds_d[r * kChannels + tile.c + i] = {delta, ok ? delta * (float)u[k][i] : 0.f};
+          lds_d[r * ROW + tile.c + i] = {delta, ok ? delta * (float)u[k][i] : 0.f};
         }
       }
     }
@@ -297,44 +356,59 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
       z0[k] = z[k];
     }
     fetch(min(t0 + TILE, t_last - 1));
-#pragma unroll 8
-    for (int j = 0; j < TILE; j++) {
-      if (!ENDS && a.kept && j % KEEP == 0 && w.on && t0 + j < a.length)
-        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + j) / KEEP, p), h);
-      const float2 d = lds_d[j * kChannels + w.ch];
-      float b[S], c[S], y = 0.f;
-      read_states<S>(lds_b + j * N + w.q * S, b);
-      if (!ENDS) read_states<S>(lds_c + j * N + w.q * S, c);
+#pragma unroll 2
+    for (int i4 = 0; i4 < TILE / 4; i4++) {
+      if (!ENDS && a.kept && i4 % (KEEP / 4) == 0 && w.on && t0 + 4 * i4 < a.length)
+        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + 4 * i4) / KEEP, p), h);
+      const int at = (4 * i4 + (w.q & 3)) * ROW + w.ch;
+      const float2 d = lds_d[at];
+      float y[4];
+      const auto token = [&](auto J) {
+        const float delta = quad_lane<J()>(d.x), du = quad_lane<J()>(d.y);
+        float b[S], c[S];
+        read_states<S>(lds_b + (4 * i4 + J()) * N + w.q * S, b);
+        if (!ENDS) read_states<S>(lds_c + (4 * i4 + J()) * N + w.q * S, c);
+        y[J()] = 0.f;
 #pragma unroll
-      for (int i = 0; i < S; i++) {
-        h[i] = fmaf(fast_exp2(d.x * A[i]), h[i], d.y * b[i]);
-        if (!ENDS) y = fmaf(h[i], c[i], y);
-      }
+        for (int i = 0; i < S; i++) {
+          h[i] = fmaf(fast_exp2(delta * A[i]), h[i], du * b[i]);
+          if (!ENDS) y[J()] = fmaf(h[i], c[i], y[J()]);
+        }
+      };
+      token(std::integral_constant<int, 0>{});
+      token(std::integral_constant<int, 1>{});
+      token(std::integral_constant<int, 2>{});
+      token(std::integral_constant<int, 3>{});
       if (ENDS)
-        total += d.x;
+        total += d.x;                                  // of the lane's token of four
       else
-        lds_y[j * kChannels + w.ch] = state_sum<Q>(y); // the same from each of the Q lanes
+        lds_d[at].x = state_sums<Q>(y);
     }
     __syncthreads();
-    if (!ENDS && tile.on) {
+    if (!ENDS) {
+      if (tile.on) {
 #pragma unroll
-      for (int k = 0; k < TileT::NV; k++) {
-        const int r = k * TileT::rows + tile.r, t = t0 + r;
-        float y[VEC];
+        for (int k = 0; k < TileT::NV; k++) {
+          const int r = k * TileT::rows + tile.r, t = t0 + r;
+          float y[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; i++) {
-          y[i] = fmaf(D[i], (float)u0[k][i], lds_y[r * kChannels + tile.c + i]);
-          if (a.z.data) {
-            const float zi = (float)z0[k][i];
-            y[i] *= zi * sigmoid(zi);
+          for (int i = 0; i < VEC; i++) {
+            y[i] = fmaf(D[i], (float)u0[k][i], lds_d[r * ROW + tile.c + i].x);
+            if (a.z.data) {
+              const float zi = (float)z0[k][i];
+              y[i] *= zi * sigmoid(zi);
+            }
+            if (t >= end) y[i] = 0.f;
           }
-          if (t >= end) y[i] = 0.f;
+          if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, y);
         }
-        if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, y);
       }
+      // a thread stages the elements whose outputs it has just read
     }
   }
   if (ENDS) {
+    total += dpp<kXor1>(total);
+    total += dpp<kXor2>(total);
     if (w.on) {
       write_states<S>(w.padded(p.ends, w.b * p.chunks + w.piece, p), h);
       if (w.q == 0) p.steps[(w.b * p.chunks + w.piece) * a.width + w.d] = total;
@@ -352,10 +426,13 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_forward(ScanParams p) {
 // them up for du, ddt and dz.  ENDS: only the gradient of the state before the chunk,
 // from nothing after it, and its sum of delta.
 template <class T, int Q, int S, int VEC, bool ENDS>
-__global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
-  constexpr int TILE = keep_of(S), N = Q * S, THREADS = kChannels * Q, WAVES = Q;
-  __shared__ float2 lds_d[TILE * kChannels];
-  __shared__ float lds_dy[TILE * kChannels], lds_c[TILE * N], lds_b[ENDS ? 1 : TILE * N];
+__global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanParams p) {
+  constexpr int TILE = keep_of(S), N = Q * S, CW = channels_of(Q), ROW = CW + 4;
+  constexpr int THREADS = CW * Q, WAVES = THREADS / 64;
+  constexpr int VALUES = 64 / Q;                       // of a sum over a wave's channels
+  constexpr int STEPS = VALUES > 2 * S ? VALUES / (2 * S) : 1;   // tokens of one such sum
+  __shared__ float4 lds_d[TILE * ROW];                 // delta, delta u, dy
+  __shared__ __align__(16) float lds_c[TILE * N], lds_b[ENDS ? 4 : TILE * N];
   __shared__ float lds_bc[ENDS ? 1 : WAVES * TILE * 2 * N];
   const rc_scan_args& a = p.a;
   const Place<Q, S> w(p);
@@ -363,7 +440,7 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
   using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
   const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wave = threadIdx.x / 64, mine = channel_value<Q>(threadIdx.x % 64);
   float A[S], g[S], dA[S], total = 0.f;                // g: of the state before the later token
   w.load(a.A, 0, p, A);
 #pragma unroll
@@ -399,7 +476,7 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
   if (!ENDS) {
     const float zero[VEC] = {};
     for (int t = live + threadIdx.x / TileT::columns; t < t_last; t += THREADS / TileT::columns)
-      if (w.blk * kChannels + tile.c < p.group_width) {
+      if (w.blk * CW + tile.c < p.group_width) {
         store_vec<VEC>(row_out<T>(a.du, w.b, t) + tile.d, VEC, zero);
         store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, zero);
         if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, zero);
@@ -410,19 +487,18 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
   }
   if (live > t_first) fetch(live - TILE);
   for (int t0 = live - TILE; t0 >= t_first; t0 -= TILE) {
+    float step[TileT::NV][VEC];                        // delta of the thread's elements
 #pragma unroll
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
       const bool ok = tile.on && t0 + r < end;
-      if (r < TILE && tile.r < TileT::rows) {
 #pragma unroll
-        for (int i = 0; i < VEC; i++) {
-          const float delta = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
-          const float zi = (float)z[k][i], act = a.z.data ? zi * sigmoid(zi) : 1.f;
-          const int at = r * kChannels + tile.c + i;
-          lds_d[at] = {delta, !ENDS && ok ? delta * (float)u[k][i] : 0.f};
-          lds_dy[at] = ok ? (float)dout[k][i] * act : 0.f;
-        }
+      for (int i = 0; i < VEC; i++) {
+        step[k][i] = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
+        const float zi = (float)z[k][i], act = a.z.data ? zi * sigmoid(zi) : 1.f;
+        if (tile.r < TileT::rows)
+          lds_d[r * ROW + tile.c + i] = {step[k][i], !ENDS && ok ? step[k][i] * (float)u[k][i] : 0.f,
+                                         ok ? (float)dout[k][i] * act : 0.f, 0.f};
       }
     }
     C.put(lds_c, t0, end, a.states);
@@ -443,59 +519,82 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
     }
     fetch(max(t0 - TILE, t_first));
     if (ENDS) {
-#pragma unroll 8
-      for (int j = TILE - 1; j >= 0; j--) {
-        const float delta = lds_d[j * kChannels + w.ch].x, dy = lds_dy[j * kChannels + w.ch];
-        float c[S];
-        read_states<S>(lds_c + j * N + w.q * S, c);
+#pragma unroll 2
+      for (int i4 = TILE / 4 - 1; i4 >= 0; i4--) {
+        const float4 d = lds_d[(4 * i4 + (w.q & 3)) * ROW + w.ch];
+        const auto token = [&](auto J) {
+          const float delta = quad_lane<J()>(d.x), dy = quad_lane<J()>(d.z);
+          float c[S];
+          read_states<S>(lds_c + (4 * i4 + J()) * N + w.q * S, c);
 #pragma unroll
-        for (int i = 0; i < S; i++) g[i] = fast_exp2(delta * A[i]) * fmaf(c[i], dy, g[i]);
-        total += delta;
+          for (int i = 0; i < S; i++) g[i] = fast_exp2(delta * A[i]) * fmaf(c[i], dy, g[i]);
+        };
+        token(std::integral_constant<int, 3>{});
+        token(std::integral_constant<int, 2>{});
+        token(std::integral_constant<int, 1>{});
+        token(std::integral_constant<int, 0>{});
+        total += d.x;
       }
     } else {
+      float4 d[TILE / 4];
 #pragma unroll
-      for (int j = 0; j < TILE; j++) {
-        const float2 d = lds_d[j * kChannels + w.ch];
-        float b[S];
-        read_states<S>(lds_b + j * N + w.q * S, b);
+      for (int i4 = 0; i4 < TILE / 4; i4++) {
+        d[i4] = lds_d[(4 * i4 + (w.q & 3)) * ROW + w.ch];
+        const auto token = [&](auto J) {
+          const int j = 4 * i4 + J();
+          const float delta = quad_lane<J()>(d[i4].x), du = quad_lane<J()>(d[i4].y);
+          float b[S];
+          read_states<S>(lds_b + j * N + w.q * S, b);
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-          decay[j][i] = fast_exp2(d.x * A[i]);
-          h[j + 1][i] = fmaf(decay[j][i], h[j][i], d.y * b[i]);
-        }
+          for (int i = 0; i < S; i++) {
+            decay[j][i] = fast_exp2(delta * A[i]);
+            h[j + 1][i] = fmaf(decay[j][i], h[j][i], du * b[i]);
+          }
+        };
+        token(std::integral_constant<int, 0>{});
+        token(std::integral_constant<int, 1>{});
+        token(std::integral_constant<int, 2>{});
+        token(std::integral_constant<int, 3>{});
       }
+      float v[STEPS * 2 * S];                          // dB, dC of STEPS tokens
 #pragma unroll
-      for (int j = TILE - 1; j >= 0; j--) {
-        const int at = j * kChannels + w.ch;
-        const float2 d = lds_d[at];
-        const float dy = lds_dy[at];
-        float b[S], c[S], v[2 * S], y = 0.f, through = 0.f, dd = 0.f;
-        read_states<S>(lds_b + j * N + w.q * S, b);
-        read_states<S>(lds_c + j * N + w.q * S, c);
+      for (int i4 = TILE / 4 - 1; i4 >= 0; i4--) {
+        float y[4], through[4], dd[4];
+        const auto token = [&](auto J) {
+          const int j = 4 * i4 + J();
+          const float delta = quad_lane<J()>(d[i4].x), du = quad_lane<J()>(d[i4].y);
+          const float dy = quad_lane<J()>(d[i4].z);
+          float b[S], c[S], *bc = v + j % STEPS * 2 * S;
+          read_states<S>(lds_b + j * N + w.q * S, b);
+          read_states<S>(lds_c + j * N + w.q * S, c);
+          y[J()] = through[J()] = dd[J()] = 0.f;
 #pragma unroll
-        for (int i = 0; i < S; i++) {
-          y = fmaf(h[j + 1][i], c[i], y);
-          const float gi = fmaf(c[i], dy, g[i]);
-          v[i] = gi * d.y;
-          v[S + i] = dy * h[j + 1][i];
-          through = fmaf(gi, b[i], through);
-          g[i] = decay[j][i] * gi;
-          const float via = g[i] * h[j][i];
-          dA[i] = fmaf(via, d.x, dA[i]);
-          dd = fmaf(via, A[i], dd);
-        }
-        lds_d[at] = {state_sum<Q>(through), state_sum<Q>(dd)};
-        lds_dy[at] = state_sum<Q>(y);
+          for (int i = 0; i < S; i++) {
+            y[J()] = fmaf(h[j + 1][i], c[i], y[J()]);
+            const float gi = fmaf(c[i], dy, g[i]);
+            bc[i] = gi * du;
+            bc[S + i] = dy * h[j + 1][i];
+            through[J()] = fmaf(gi, b[i], through[J()]);
+            g[i] = decay[j][i] * gi;
+            const float via = g[i] * h[j][i];
+            dA[i] = fmaf(via, delta, dA[i]);
+            dd[J()] = fmaf(via, A[i], dd[J()]);
+          }
+          if (j % STEPS == 0) {
 #pragma unroll
-        for (int i = 0; i < 2 * S; i++) v[i] = row_channel_sum<Q>(v[i]);
-        // rows hold values (row & 1) + 2 (row >> 1) + 4 m of v
-#pragma unroll
-        for (int m = 0; m < 2 * S / 4; m++) {
-          const float x = half_pair_sum(row_pair_sum(v[4 * m], v[4 * m + 1]),
-                                        row_pair_sum(v[4 * m + 2], v[4 * m + 3]));
-          const int e = 4 * m + lane / 16;             // of dB[S], dC[S]
-          lds_bc[(wave * TILE + j) * 2 * N + e / S * N + w.q * S + e % S] = x;
-        }
+            for (int m = 0; m < STEPS * 2 * S; m += VALUES) {
+              const int e = m + mine;                  // value of token j + e / 2S
+              lds_bc[(wave * TILE + j + e / (2 * S)) * 2 * N + e / S % 2 * N + w.q * S + e % S] =
+                  channel_sums<Q>(v + m);
+            }
+          }
+        };
+        token(std::integral_constant<int, 3>{});
+        token(std::integral_constant<int, 2>{});
+        token(std::integral_constant<int, 1>{});
+        token(std::integral_constant<int, 0>{});
+        lds_d[(4 * i4 + (w.q & 3)) * ROW + w.ch] = {state_sums<Q>(through), state_sums<Q>(dd),
+                                                    state_sums<Q>(y), 0.f};
       }
     }
     __syncthreads();
@@ -516,14 +615,12 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
         float du[VEC], ddt[VEC], dz[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; i++) {
-          const float2 sums = lds_d[r * kChannels + tile.c + i];
+          const float4 sums = lds_d[r * ROW + tile.c + i];
           const float ui = (float)u0[k][i], zi = (float)z0[k][i], o = (float)dout0[k][i];
-          const float raw = (float)dt0[k][i] + bias[i], s = sigmoid(zi);
-          const float dy = a.z.data ? o * (zi * s) : o;
-          const float y = fmaf(D[i], ui, lds_dy[r * kChannels + tile.c + i]);
-          const float dd = fmaf(ui, sums.x, sums.y * kLn2);
-          du[i] = ok ? fmaf(delta_of(raw, a.softplus), sums.x, D[i] * dy) : 0.f;
-          ddt[i] = ok ? (a.softplus ? dd * sigmoid(raw) : dd) : 0.f;
+          const float s = sigmoid(zi), dy = a.z.data ? o * (zi * s) : o;
+          const float y = fmaf(D[i], ui, sums.z), dd = fmaf(ui, sums.x, sums.y * kLn2);
+          du[i] = ok ? fmaf(step[k][i], sums.x, D[i] * dy) : 0.f;
+          ddt[i] = ok ? (a.softplus ? dd * sigmoid((float)dt0[k][i] + bias[i]) : dd) : 0.f;
           dz[i] = ok ? o * y * (s * (1.f + zi * (1.f - s))) : 0.f;
           dD[i] += ok ? dy * ui : 0.f;
           dbias[i] += ddt[i];
@@ -532,11 +629,13 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
         store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, ddt);
         if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, dz);
       }
-      __syncthreads();                                 // the next tile takes the same LDS
     }
+    __syncthreads();                                   // the next tile takes the same LDS
   }
   const int64_t before = w.b * p.chunks + w.piece;
   if (ENDS) {
+    total += dpp<kXor1>(total);
+    total += dpp<kXor2>(total);
     if (w.on) {
       write_states<S>(w.padded(p.ends, before, p), g);
       if (w.q == 0) p.steps[before * a.width + w.d] = total;
@@ -546,21 +645,20 @@ __global__ __launch_bounds__(kChannels* Q) void k_scan_backward(ScanParams p) {
   if (w.on) write_states<S>(w.padded(p.part_a, before, p), dA);
   if (a.dstate_in && w.piece == 0) w.store(a.dstate_in, w.b, p, g);
   // D and dt_bias: the threads of a column, then one sum for each channel
-  __syncthreads();
   float* sums = reinterpret_cast<float*>(lds_d);       // [rows][channels] of (dD, dbias)
   if (tile.r < TileT::rows) {
 #pragma unroll
     for (int i = 0; i < VEC; i++) {
-      sums[(tile.r * kChannels + tile.c + i) * 2] = dD[i];
-      sums[(tile.r * kChannels + tile.c + i) * 2 + 1] = dbias[i];
+      sums[(tile.r * CW + tile.c + i) * 2] = dD[i];
+      sums[(tile.r * CW + tile.c + i) * 2 + 1] = dbias[i];
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < 2 * kChannels; e += THREADS) {
-    if (w.blk * kChannels + e / 2 >= p.group_width) continue;
+  for (int e = threadIdx.x; e < 2 * CW; e += THREADS) {
+    if (w.blk * CW + e / 2 >= p.group_width) continue;
     float s = 0.f;
-    for (int r = 0; r < TileT::rows; r++) s += sums[r * 2 * kChannels + e];
-    p.part_d[(before * a.width + w.g * p.group_width + w.blk * kChannels + e / 2) * 2 + e % 2] = s;
+    for (int r = 0; r < TileT::rows; r++) s += sums[r * 2 * CW + e];
+    p.part_d[(before * a.width + w.g * p.group_width + w.blk * CW + e / 2) * 2 + e % 2] = s;
   }
 }
 
@@ -600,6 +698,27 @@ __global__ __launch_bounds__(256) void k_scan_sum_a(const float* pa, const float
 
 constexpr int kStepThreads = 256;
 
+// Sum over the Q lanes of a channel, in each of them.
+template <int Q>
+__device__ __forceinline__ float state_sum(float x) {
+  if (Q > 1) x += dpp<kXor1>(x);
+  if (Q > 2) x += dpp<kXor2>(x);
+  if (Q > 4) x += dpp<kHalfMirror>(x);
+  if (Q > 8) x += dpp<kMirror>(x);
+  return x;
+}
+
+template <class F>
+int by_lanes(int q, F&& f) {
+  switch (q) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+    case 8: return f(std::integral_constant<int, 8>{});
+    default: return f(std::integral_constant<int, 16>{});
+  }
+}
+
 template <class T, int Q>
 __global__ __launch_bounds__(kStepThreads) void k_scan_step(rc_scan_step_args a, int32_t blocks) {
   const int64_t b = blockIdx.x / blocks;
@@ -633,23 +752,6 @@ __global__ __launch_bounds__(kStepThreads) void k_scan_step(rc_scan_step_args a,
   if (q == 0) row_out<T>(a.y, b, 0)[d] = (T)y;
 }
 
-int lanes_of(int32_t states, int S) {
-  int q = 1;
-  while (S * q < states) q *= 2;
-  return q;
-}
-
-template <class F>
-int by_lanes(int q, F&& f) {
-  switch (q) {
-    case 1: return f(std::integral_constant<int, 1>{});
-    case 2: return f(std::integral_constant<int, 2>{});
-    case 4: return f(std::integral_constant<int, 4>{});
-    case 8: return f(std::integral_constant<int, 8>{});
-    default: return f(std::integral_constant<int, 16>{});
-  }
-}
-
 bool scan_sizes_ok(int32_t dtype, int32_t batch, int32_t length, int32_t width, int32_t states,
                    int32_t groups) {
   return dtype_ok(dtype) && batch >= 0 && length >= 0 && width >= 0 && states >= 1 &&
@@ -659,28 +761,27 @@ bool scan_sizes_ok(const rc_scan_args* a) {
   return a && scan_sizes_ok(a->dtype, a->batch, a->length, a->width, a->states, a->groups);
 }
 
-// How a scan is cut up.  Each wave of a SIMD issues an instruction every six
-// cycles at best, two together one every three: at least two waves a SIMD
-// are wanted.  Two states a lane give twice as many waves as four (and pay with
-// more lanes to sum over); beyond that the length is cut into chunks, which costs a
-// pass over all but one of them for their end states.
+// How a scan is cut up.  A channel takes a quad of lanes (more above 16
+// states).  Each wave of a SIMD issues an instruction every six cycles at
+// best, two together one every three, so at least `want` waves are wanted on the chip:
+// where batch and channels give fewer, the length is cut into chunks, which
+// costs a pass over them for their end states.
 struct ScanPlan {
   int S, Q, VEC;
   int64_t group_width, blocks;
   int64_t chunks, chunk, keeps;
 };
-ScanPlan scan_plan(const rc_scan_args& a) {
+ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   ScanPlan p;
   p.group_width = a.width / a.groups;
-  p.blocks = cdiv(p.group_width, kChannels);
-  const int64_t rows = (int64_t)a.batch * a.groups * p.blocks;
-  const int64_t want = 8 * (int64_t)rcdp::num_cus();             // waves
-  p.S = a.states > 32 || rows * lanes_of(a.states, 4) >= want ? 4 : 2;
-  p.Q = lanes_of(a.states, p.S);
+  p.S = a.states > 8 ? 4 : a.states > 4 ? 2 : 1;
+  p.Q = a.states > 32 ? 16 : a.states > 16 ? 8 : 4;
   p.VEC = p.group_width % 4 ? 1 : 4;
-  p.chunks = 1;
+  p.blocks = cdiv(p.group_width, channels_of(p.Q));
+  const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
+  const int64_t want = (backward ? 8 : 16) * (int64_t)rcdp::num_cus();
   const int64_t most = cdiv(a.length, 64) < 32 ? cdiv(a.length, 64) : 32;
-  if (rows > 0 && rows * p.Q < want) p.chunks = cdiv(want, rows * p.Q);
+  p.chunks = waves > 0 && waves < want ? cdiv(want, waves) : 1;
   if (p.chunks > most) p.chunks = most;
   if (p.chunks < 1) p.chunks = 1;
   p.chunk = cdiv(cdiv(a.length, p.chunks), kFwdTile) * kFwdTile;
@@ -724,7 +825,7 @@ int scan_check(const rc_scan_args* a, bool backward) {
   if (backward && a->width > 0 &&
       (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias)))
     return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a);
+  const ScanPlan p = scan_plan(*a, backward);
   const int64_t cells = (int64_t)a->batch * a->length * a->groups;
   if (p.blocks * a->groups * a->batch * p.chunks >= kMaxBlocks ||
       cdiv(cells * 2 * p.Q * p.S, kSumThreads) >= kMaxBlocks)
@@ -753,40 +854,42 @@ ScanParams scan_params(const rc_scan_args& a, const ScanPlan& p, const ScanScrat
 template <class F>
 int by_plan(const ScanPlan& p, F&& f) {
   using std::integral_constant;
-  const auto with = [&](auto S) {
-    return by_lanes(p.Q, [&](auto Q) {
-      if (p.VEC == 1) return f(Q, S, integral_constant<int, 1>{});
-      return f(Q, S, integral_constant<int, 4>{});
-    });
+  const auto with = [&](auto Q, auto S) {
+    if (p.VEC == 1) return f(Q, S, integral_constant<int, 1>{});
+    return f(Q, S, integral_constant<int, 4>{});
   };
-  return p.S == 2 ? with(integral_constant<int, 2>{}) : with(integral_constant<int, 4>{});
+  if (p.Q == 16) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  if (p.Q == 8) return with(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  if (p.S == 4) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  if (p.S == 2) return with(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  return with(integral_constant<int, 4>{}, integral_constant<int, 1>{});
 }
 
 }  // namespace
 
 extern "C" int rc_scan_kept_bytes(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a);
+  const ScanPlan p = scan_plan(*a, false);
   *bytes_host = (uint64_t)a->batch * p.keeps * a->width * p.Q * p.S * 4;
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a), false).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a, false), false).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_backward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a), true).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a, true), true).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, false)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a);
+  const ScanPlan p = scan_plan(a, false);
   const ScanScratch need = scan_scratch(a, p, false);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
@@ -796,7 +899,7 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   return by_dtype(a.dtype, [&](auto t) {
     return by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
       using T = decltype(t);
-      const dim3 grid((uint32_t)blocks), threads(kChannels * Q());
+      const dim3 grid((uint32_t)blocks), threads(channels_of(Q()) * Q());
       if (p.chunks > 1) {
         k_scan_forward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
         if (const int st = launched("k_scan_forward ends")) return st;
@@ -810,7 +913,7 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
 extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, true)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a);
+  const ScanPlan p = scan_plan(a, true);
   const ScanScratch need = scan_scratch(a, p, true);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   if (a.width == 0) return RC_OK;
@@ -823,7 +926,7 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
     using T = decltype(t);
     if (blocks > 0) {
       const int st = by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
-        const dim3 grid((uint32_t)blocks), threads(kChannels * Q());
+        const dim3 grid((uint32_t)blocks), threads(channels_of(Q()) * Q());
         if (p.chunks > 1) {
           k_scan_backward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
           if (const int e = launched("k_scan_backward ends")) return e;
@@ -855,7 +958,7 @@ extern "C" int rc_scan_step(const rc_scan_step_args* args, void* stream) {
   if (a.batch == 0 || a.width == 0) return RC_OK;
   if (!a.u.data || !a.dt.data || !a.B.data || !a.C.data || !a.y.data || !a.A || !a.state)
     return RC_E_ARG;
-  const int Q = lanes_of(a.states, 4);
+  const int Q = a.states > 32 ? 16 : a.states > 16 ? 8 : a.states > 8 ? 4 : a.states > 4 ? 2 : 1;
   const int64_t blocks = cdiv(a.width, kStepThreads / Q);
   if (blocks * a.batch >= kMaxBlocks) return RC_E_OVERFLOW;
   return by_dtype(a.dtype, [&](auto t) {
