@@ -23,10 +23,11 @@ namespace {
 constexpr int kFwdTile = 32;        // tokens staged together, forward
 constexpr int kSumThreads = 256;
 
-// Channels of a workgroup, and tokens between two kept states: a backward
-// tile's states and decays stay in registers, at most 64 of each a lane.
+constexpr int kKeep = 16;           // tokens between two kept states, a backward tile:
+                                    // its states stay in registers
+
+// Channels of a workgroup.
 constexpr int channels_of(int Q) { return Q > 8 ? 32 : 64; }
-constexpr int keep_of(int S) { return S > 2 ? 16 : 32; }
 
 __device__ __forceinline__ int seq_end(const int32_t* lengths, int64_t b, int32_t length) {
   if (!lengths) return length;
@@ -289,7 +290,7 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 // ENDS: only the end state of the chunk from nothing, and its sum of delta.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams p) {
-  constexpr int TILE = kFwdTile, N = Q * S, KEEP = keep_of(S), CW = channels_of(Q), ROW = CW + 8;
+  constexpr int TILE = kFwdTile, N = Q * S, CW = channels_of(Q), ROW = CW + 8;
   __shared__ float2 lds_d[TILE * ROW];
   __shared__ __align__(16) float lds_b[TILE * N], lds_c[ENDS ? 4 : TILE * N];
   const rc_scan_args& a = p.a;
@@ -358,8 +359,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     fetch(min(t0 + TILE, t_last - 1));
 #pragma unroll 2
     for (int i4 = 0; i4 < TILE / 4; i4++) {
-      if (!ENDS && a.kept && i4 % (KEEP / 4) == 0 && w.on && t0 + 4 * i4 < a.length)
-        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + 4 * i4) / KEEP, p), h);
+      if (!ENDS && a.kept && i4 % (kKeep / 4) == 0 && w.on && t0 + 4 * i4 < a.length)
+        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + 4 * i4) / kKeep, p), h);
       const int at = (4 * i4 + (w.q & 3)) * ROW + w.ch;
       const float2 d = lds_d[at];
       float y[4];
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
 // from nothing after it, and its sum of delta.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanParams p) {
-  constexpr int TILE = keep_of(S), N = Q * S, CW = channels_of(Q), ROW = CW + 4;
+  constexpr int TILE = kKeep, N = Q * S, CW = channels_of(Q), ROW = CW + 4;
   constexpr int THREADS = CW * Q, WAVES = THREADS / 64;
   constexpr int VALUES = 64 / Q;                       // of a sum over a wave's channels
   constexpr int STEPS = VALUES > 2 * S ? VALUES / (2 * S) : 1;   // tokens of one such sum
@@ -503,7 +504,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     }
     C.put(lds_c, t0, end, a.states);
     if (!ENDS) B.put(lds_b, t0, end, a.states);
-    float h[ENDS ? 1 : TILE + 1][S], decay[ENDS ? 1 : TILE][S];
+    float h[ENDS ? 1 : TILE + 1][S];
     if (!ENDS) {
 #pragma unroll
       for (int i = 0; i < S; i++) h[0][i] = h0[i];
@@ -547,8 +548,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
           read_states<S>(lds_b + j * N + w.q * S, b);
 #pragma unroll
           for (int i = 0; i < S; i++) {
-            decay[j][i] = fast_exp2(delta * A[i]);
-            h[j + 1][i] = fmaf(decay[j][i], h[j][i], du * b[i]);
+            h[j + 1][i] = fmaf(fast_exp2(delta * A[i]), h[j][i], du * b[i]);
           }
         };
         token(std::integral_constant<int, 0>{});
@@ -562,8 +562,9 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
         float y[4], through[4], dd[4];
         const auto token = [&](auto J) {
           const int j = 4 * i4 + J();
-          const float delta = quad_lane<J()>(d[i4].x), du = quad_lane<J()>(d[i4].y);
-          const float dy = quad_lane<J()>(d[i4].z);
+          float delta = quad_lane<J()>(d[i4].x);
+          asm("" : "+v"(delta));                       // decays again, not kept: registers
+          const float du = quad_lane<J()>(d[i4].y), dy = quad_lane<J()>(d[i4].z);
           float b[S], c[S], *bc = v + j % STEPS * 2 * S;
           read_states<S>(lds_b + j * N + w.q * S, b);
           read_states<S>(lds_c + j * N + w.q * S, c);
@@ -575,7 +576,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
             bc[i] = gi * du;
             bc[S + i] = dy * h[j + 1][i];
             through[J()] = fmaf(gi, b[i], through[J()]);
-            g[i] = decay[j][i] * gi;
+            g[i] = fast_exp2(delta * A[i]) * gi;
             const float via = g[i] * h[j][i];
             dA[i] = fmaf(via, delta, dA[i]);
             dd[J()] = fmaf(via, A[i], dd[J()]);
@@ -762,16 +763,19 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 }
 
 // How a scan is cut up.  A channel takes a quad of lanes (more above 16
-// states).  Each wave of a SIMD issues an instruction every six cycles at
-// best, two together one every three, so at least `want` waves are wanted on the chip:
-// where batch and channels give fewer, the length is cut into chunks, which
-// costs a pass over them for their end states.
+// states).  The kernels are bound by instruction issue, which needs two to four
+// waves on every SIMD: where batch and channels give fewer, the length is cut into
+// chunks, which costs a pass over them for their end states.  Forward and
+// backward, us, bfloat16, 16 states: batch 8, 2048 tokens, 2048 channels (one
+// wave a SIMD): 1 chunk 257 + 692, 4 chunks 257 + 628; batch 1, 16384 tokens: 2
+// chunks 418 + 1107, 16 chunks 265 + 641; batch 16, 4096 channels (16 waves a compute
+// unit): 1 chunk 595 + 1935, 2 chunks 937 + 2355.
 struct ScanPlan {
   int S, Q, VEC;
   int64_t group_width, blocks;
   int64_t chunks, chunk, keeps;
 };
-ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
+ScanPlan scan_plan(const rc_scan_args& a) {
   ScanPlan p;
   p.group_width = a.width / a.groups;
   p.S = a.states > 8 ? 4 : a.states > 4 ? 2 : 1;
@@ -779,7 +783,7 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.VEC = p.group_width % 4 ? 1 : 4;
   p.blocks = cdiv(p.group_width, channels_of(p.Q));
   const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
-  const int64_t want = (backward ? 8 : 16) * (int64_t)rcdp::num_cus();
+  const int64_t want = 16 * (int64_t)rcdp::num_cus();
   const int64_t most = cdiv(a.length, 64) < 32 ? cdiv(a.length, 64) : 32;
   p.chunks = waves > 0 && waves < want ? cdiv(want, waves) : 1;
   if (p.chunks > most) p.chunks = most;
@@ -787,7 +791,7 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.chunk = cdiv(cdiv(a.length, p.chunks), kFwdTile) * kFwdTile;
   if (p.chunk < kFwdTile) p.chunk = kFwdTile;
   p.chunks = a.length > 0 ? cdiv(a.length, p.chunk) : 1;
-  p.keeps = cdiv(a.length, keep_of(p.S));
+  p.keeps = cdiv(a.length, kKeep);
   return p;
 }
 
@@ -825,7 +829,7 @@ int scan_check(const rc_scan_args* a, bool backward) {
   if (backward && a->width > 0 &&
       (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias)))
     return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a, backward);
+  const ScanPlan p = scan_plan(*a);
   const int64_t cells = (int64_t)a->batch * a->length * a->groups;
   if (p.blocks * a->groups * a->batch * p.chunks >= kMaxBlocks ||
       cdiv(cells * 2 * p.Q * p.S, kSumThreads) >= kMaxBlocks)
@@ -869,27 +873,27 @@ int by_plan(const ScanPlan& p, F&& f) {
 
 extern "C" int rc_scan_kept_bytes(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a, false);
+  const ScanPlan p = scan_plan(*a);
   *bytes_host = (uint64_t)a->batch * p.keeps * a->width * p.Q * p.S * 4;
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a, false), false).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a), false).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_backward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a, true), true).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a), true).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, false)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a, false);
+  const ScanPlan p = scan_plan(a);
   const ScanScratch need = scan_scratch(a, p, false);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
@@ -913,7 +917,7 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
 extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, true)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a, true);
+  const ScanPlan p = scan_plan(a);
   const ScanScratch need = scan_scratch(a, p, true);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   if (a.width == 0) return RC_OK;
