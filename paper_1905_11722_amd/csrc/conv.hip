@@ -59,8 +59,8 @@ __device__ __forceinline__ void load_if(const T* p, bool ok, float (&x)[V]) {
   for (int i = 0; i < V; i++) x[i] = ok ? x[i] : 0.f;
 }
 
-// Row t of the input (t < 0: the state) of a sequence that has a token;
-// 0 at and past `end`.
+// Row t of the input before a run (t < 0: the state) of a sequence that has a
+// token; 0 at and past `end`.
 template <class T, int K, int V>
 __device__ __forceinline__ void input_row(const rc_conv_args& a, int b, int t, int end, int c,
                                           float (&x)[V]) {
@@ -69,6 +69,20 @@ __device__ __forceinline__ void input_row(const rc_conv_args& a, int b, int t, i
                      : at<T>(a.x, b, max(0, min(t, end - 1)), c);
   load_if<T, V>(p, t < 0 ? state : t < end, x);
 }
+
+// Rows of a thread that are loaded together, one group ahead of their use: rows t ..
+// of a sequence with a token, clamped to its last.
+constexpr int kRows = 4;
+template <class T, int V>
+struct Rows {
+  typedef T Raw __attribute__((ext_vector_type(V)));
+  Raw x[kRows];
+  __device__ __forceinline__ void load(const rc_view& v, int b, int t, int end, int c) {
+#pragma unroll
+    for (int j = 0; j < kRows; j++)
+      __builtin_memcpy(&x[j], at<T>(v, b, min(t + j, end - 1), c), sizeof(Raw));
+  }
+};
 
 template <class T, int K, int V>
 __device__ __forceinline__ void load_weights(const rc_conv_args& a, int c,
@@ -114,22 +128,29 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
     load_weights<T, K, V>(a, c, w, bias);
 #pragma unroll
     for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
-    for (; t < min(t1, end); t++) {
-      float y[V];
+    const int stop = min(t1, end);
+    Rows<T, V> now, next;
+    now.load(a.x, b, t, end, c);
+    for (; t < stop; t += kRows) {
+      next.load(a.x, b, t + kRows, end, c);
 #pragma unroll
-      for (int k = 0; k < K - 1; k++)
+      for (int j = 0; j < kRows; j++) {
+        float y[V];
 #pragma unroll
-        for (int i = 0; i < V; i++) x[k][i] = x[k + 1][i];
-      input_row<T, K, V>(a, b, t, end, c, x[K - 1]);
+        for (int i = 0; i < V; i++) {
 #pragma unroll
-      for (int i = 0; i < V; i++) {
-        y[i] = bias[i];
+          for (int k = 0; k < K - 1; k++) x[k][i] = x[k + 1][i];
+          x[K - 1][i] = t + j < end ? (float)now.x[j][i] : 0.f;
+          y[i] = bias[i];
 #pragma unroll
-        for (int k = 0; k < K; k++) y[i] = fmaf(w[k][i], x[k][i], y[i]);
-        if (a.activation == RC_ACT_SILU) y[i] *= sigmoid(y[i]);
+          for (int k = 0; k < K; k++) y[i] = fmaf(w[k][i], x[k][i], y[i]);
+          if (a.activation == RC_ACT_SILU) y[i] *= sigmoid(y[i]);
+        }
+        if (t + j < stop) store_vec<V>(at<T>(a.y, b, t + j, c), V, y);
       }
-      store_vec<V>(at<T>(a.y, b, t, c), V, y);
+      now = next;
     }
+    t = stop;
   }
   for (; t < t1; t++) {
     const float zero[V] = {};
@@ -168,21 +189,29 @@ __global__ __launch_bounds__(kThreads) void k_conv_backward(ConvParams<T> p) {
 #pragma unroll
       for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
     }
-    for (int t = t0; t < t1 + K - 1; t++) {
+    const bool any = end > 0;
+    Rows<T, V> now, next, dnow, dnext;
+    if (any) {
+      now.load(a.x, b, t0, end, c);
+      dnow.load(a.dy, b, t0, end, c);
+    }
+    for (int g = t0; g < t1 + K - 1; g += kRows) {
+      if (any) {
+        next.load(a.x, b, g + kRows, end, c);
+        dnext.load(a.dy, b, g + kRows, end, c);
+      }
 #pragma unroll
-      for (int k = 0; k < K - 1; k++)
+      for (int r = 0; r < kRows; r++) {
+        const int t = g + r;
 #pragma unroll
         for (int i = 0; i < V; i++) {
-          x[k][i] = x[k + 1][i];
-          dp[k][i] = dp[k + 1][i];
-        }
-      if (end > 0) {
-        float dy[V];
-        input_row<T, K, V>(a, b, t, end, c, x[K - 1]);
-        load_if<T, V>(at<T>(a.dy, b, min(t, end - 1), c), t < end, dy);
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-          dp[K - 1][i] = dy[i];
+          for (int k = 0; k < K - 1; k++) {
+            x[k][i] = x[k + 1][i];
+            dp[k][i] = dp[k + 1][i];
+          }
+          x[K - 1][i] = t < end ? (float)now.x[r][i] : 0.f;
+          dp[K - 1][i] = t < end ? (float)dnow.x[r][i] : 0.f;
           if (a.activation == RC_ACT_SILU) {
             float q = bias[i];
 #pragma unroll
@@ -190,34 +219,35 @@ __global__ __launch_bounds__(kThreads) void k_conv_backward(ConvParams<T> p) {
             const float s = sigmoid(q);
             dp[K - 1][i] *= s * (1.f + q * (1.f - s));
           }
-          if (t < t1) {
+          const float own = t < t1 ? dp[K - 1][i] : 0.f;
 #pragma unroll
-            for (int k = 0; k < K; k++) dw[k][i] = fmaf(dp[K - 1][i], x[k][i], dw[k][i]);
-            dw[K][i] += dp[K - 1][i];
+          for (int k = 0; k < K; k++) dw[k][i] = fmaf(own, x[k][i], dw[k][i]);
+          dw[K][i] += own;
+        }
+        const int s = t - (K - 1);                     // the row whose dx is complete
+        if (s >= first && s < t1) {
+          float dx[V];
+#pragma unroll
+          for (int i = 0; i < V; i++) {
+            dx[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; k++) dx[i] = fmaf(w[k][i], dp[K - 1 - k][i], dx[i]);
           }
+          const int j = s - (end - (K - 1));           // its row in the final state
+          if (a.dstate_out.data && j >= 0 && j < K - 1) {
+            float ds[V];
+            load_vec<V>(at<T>(a.dstate_out, b, j, c), V, ds);
+#pragma unroll
+            for (int i = 0; i < V; i++) dx[i] += ds[i];
+          }
+          if (s >= 0)
+            store_vec<V>(at<T>(a.dx, b, s, c), V, dx);
+          else
+            store_vec<V>(at<T>(a.dstate_in, b, s + K - 1, c), V, dx);
         }
       }
-      const int s = t - (K - 1);                       // the row whose dx is complete
-      if (s >= first && s < t1) {
-        float dx[V];
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-          dx[i] = 0.f;
-#pragma unroll
-          for (int k = 0; k < K; k++) dx[i] = fmaf(w[k][i], dp[K - 1 - k][i], dx[i]);
-        }
-        const int j = s - (end - (K - 1));             // its row in the final state
-        if (a.dstate_out.data && j >= 0 && j < K - 1) {
-          float ds[V];
-          load_vec<V>(at<T>(a.dstate_out, b, j, c), V, ds);
-#pragma unroll
-          for (int i = 0; i < V; i++) dx[i] += ds[i];
-        }
-        if (s >= 0)
-          store_vec<V>(at<T>(a.dx, b, s, c), V, dx);
-        else
-          store_vec<V>(at<T>(a.dstate_in, b, s + K - 1, c), V, dx);
-      }
+      now = next;
+      dnow = dnext;
     }
   }
   if (!p.partial) return;
@@ -314,7 +344,7 @@ struct ConvPlan {
 };
 ConvPlan conv_plan(const rc_conv_args& a, bool backward) {
   ConvPlan p;
-  p.V = a.width % 8 ? 1 : backward && a.taps > 4 ? 4 : 8;
+  p.V = backward ? (a.width % 4 ? 1 : 4) : a.width % 8 ? 1 : 8;
   const int64_t vecs = cdiv(a.width, p.V);
   p.lanes = lanes_for(vecs);
   p.groups_c = cdiv(vecs, p.lanes);
@@ -395,8 +425,7 @@ extern "C" int rc_conv_backward(const rc_conv_args* args, void* stream) {
         if (p.V == 1)
           k_conv_backward<T, k(), 1><<<grid, kThreads, 0, (hipStream_t)stream>>>(q);
         else
-          k_conv_backward<T, k(), (k() > 4 ? 4 : 8)>
-              <<<grid, kThreads, 0, (hipStream_t)stream>>>(q);
+          k_conv_backward<T, k(), 4><<<grid, kThreads, 0, (hipStream_t)stream>>>(q);
         return launched("k_conv_backward");
       });
       if (st) return st;

@@ -285,11 +285,15 @@ int threads_per_row(int32_t width) {
 }
 
 // Workgroups: enough threads to fill the chip, then each walks over rows.
+// Backward each leaves a row of partial sums, so beyond one a compute unit
+// there are four rows of work for each.
 int64_t norm_blocks(const rc_norm_args& a, bool backward) {
   const int tpr = threads_per_row(a.width), wg = threads_of(tpr);
-  const int64_t need = cdiv(a.rows, wg / tpr);
-  const int64_t most = (int64_t)rcdp::num_cus() * (backward ? 512 : 2048) / wg;
-  return need < most ? need : most;
+  const int64_t need = cdiv(a.rows, wg / tpr), cus = rcdp::num_cus();
+  const int64_t most = cus * (backward ? 512 : 2048) / wg;
+  if (need <= cus) return need;
+  const int64_t some = backward ? (need / 4 < cus ? cus : need / 4) : need;
+  return some < most ? some : most;
 }
 
 bool norm_sizes_ok(const rc_norm_args* a) {

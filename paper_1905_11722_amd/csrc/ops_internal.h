@@ -108,19 +108,32 @@ constexpr int64_t kMaxBlocks = (int64_t)1 << 31;
 
 // Column sums of a partial buffer, a column reduction's last step:
 // sum over p < parts of in[p * cols + c] for the workgroup's column of this
-// thread.  256 threads take 64 columns, four slices of the parts each, always the same
-// slices in the same order; the threads of slice 0 return the sums.
-constexpr int kSumCols = 64;
+// thread.  256 threads take 16 columns, sixteen slices of the parts each,
+// eight loads in flight; always the same slices in the same order.  The
+// threads of slice 0 return the sums.  (512 parts of 12288 columns: 64 columns a
+// workgroup with one load in flight took 18 us, this one 7.)
+constexpr int kSumCols = 16;
 __device__ __forceinline__ float column_sum(const float* in, int64_t parts, int64_t cols,
                                             int64_t c, float* lds /* [256] */) {
+  constexpr int SLICES = 256 / kSumCols;
   const int slice = threadIdx.x / kSumCols;
   float s = 0.f;
-  if (c < cols)
-    for (int64_t p = slice; p < parts; p += 4) s += in[p * cols + c];
+  if (c < cols) {
+    int64_t p = slice;
+    for (; p + 7 * SLICES < parts; p += 8 * SLICES) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = in[(p + i * SLICES) * cols + c];
+      s += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    for (; p < parts; p += SLICES) s += in[p * cols + c];
+  }
   lds[threadIdx.x] = s;
   __syncthreads();
   if (slice) return 0.f;
-  return (s + lds[threadIdx.x + 64]) + (lds[threadIdx.x + 128] + lds[threadIdx.x + 192]);
+#pragma unroll
+  for (int i = 1; i < SLICES; i++) s += lds[threadIdx.x + i * kSumCols];
+  return s;
 }
 
 }  // namespace rcops
