@@ -77,8 +77,7 @@ __device__ __forceinline__ float softplus(float x) {
   const float s = 1.f + w;
   const float r = s - 1.f;
   const float l = r == 0.f ? w : kLn2 * __builtin_amdgcn_logf(s) * (w * fast_rcp(r));
-  const float y = __builtin_fmaxf(x, 0.f) + l;
-  return x != x ? x : y;
+  return __builtin_fmaxf(x, 0.f) + l;                  // a NaN comes through w
 }
 
 __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

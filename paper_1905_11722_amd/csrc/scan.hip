@@ -152,7 +152,8 @@ __device__ __forceinline__ T* row_out(const rc_view& v, int64_t b, int64_t t) {
 }
 
 __device__ __forceinline__ float delta_of(float raw, bool soft) {
-  return soft ? softplus(raw) : raw;
+  const float s = softplus(raw);    // chosen, not branched to: elements overlap
+  return soft ? s : raw;
 }
 
 // What a workgroup works on.  Workgroup i runs on XCD i % 8: neighbours in
@@ -208,19 +209,29 @@ struct Tile {
   typedef T Raw __attribute__((ext_vector_type(VEC)));
   int64_t d;                        // first channel of the column, clamped
   int c, r;                         // its place in the block, first row
-  bool on;                          // has work in a tile, channel exists
+  bool lead;                        // has a row of its own in a tile
+  bool on;                          // and its channel exists
   __device__ Tile(const ScanParams& p, int64_t g, int blk) {
     c = threadIdx.x % columns * VEC;
-    r = threadIdx.x / columns;
-    on = r < rows && blk * CW + c < p.group_width;
+    lead = threadIdx.x / columns < rows;
+    r = min((int)threadIdx.x / columns, rows - 1);
+    on = lead && blk * CW + c < p.group_width;
     d = g * p.group_width + min(blk * CW + c, p.group_width - VEC);
   }
-  // Loads are unconditional (rows clamped to the sequence): what is past an end is
-  // dropped where it is used.
-  __device__ void load(const rc_view& v, int64_t b, int t0, int length, Raw (&x)[NV]) const {
+  // The thread's place in row `t` + its first row.
+  __device__ T* start(const rc_view& v, int64_t b, int t) const {
+    return static_cast<T*>(v.data) + b * v.batch + (int64_t)(t + r) * v.time + d;
+  }
+  // The tile of tokens t0 .. from the thread's place p in it.  Loads are
+  // unconditional, rows past the sequence clamped to its last: what is past an
+  // end is dropped where it is used.
+  __device__ void load(const T* p, int64_t time, int t0, int length, Raw (&x)[NV]) const {
 #pragma unroll
-    for (int k = 0; k < NV; k++)
-      __builtin_memcpy(&x[k], row<T>(v, b, min(t0 + k * rows + r, length - 1)) + d, sizeof(Raw));
+    for (int k = 0; k < NV; k++) {
+      int64_t at = (int64_t)(k * rows) * time;
+      if (t0 + TILE > length) at -= max(0, t0 + k * rows + r - (length - 1)) * time;
+      __builtin_memcpy(&x[k], p + at, sizeof(Raw));
+    }
   }
   __device__ void vector(const float* w, float (&x)[VEC]) const {
 #pragma unroll
@@ -231,21 +242,30 @@ struct Tile {
 // A tile of B or C to LDS in 32 bits: [TILE][N], zeros past the end and for missing states.
 template <class T, int N, int TILE, int THREADS>
 struct StateTile {
-  static constexpr int NE = (TILE * N + THREADS - 1) / THREADS;
+  static constexpr int ROWS = THREADS / N;
+  static constexpr int NE = TILE > ROWS ? TILE / ROWS : 1;
+  const T* p;                       // the thread's place in the tile to load next
   T x[NE];
-  __device__ void load(const rc_view& v, int64_t group, int64_t b, int t0, const rc_scan_args& a) {
+  __device__ void start(const rc_view& v, int64_t group, int64_t b, int t, int states) {
+    p = static_cast<const T*>(v.data) + b * v.batch + (int64_t)(t + threadIdx.x / N) * v.time +
+        group + min((int)threadIdx.x % N, states - 1);
+  }
+  __device__ void load(int64_t time, int t0, int length) {
 #pragma unroll
     for (int k = 0; k < NE; k++) {
-      const int e = k * THREADS + threadIdx.x;
-      x[k] = row<T>(v, b, min(t0 + e / N, a.length - 1))[group + min(e % N, a.states - 1)];
+      int64_t at = (int64_t)(k * ROWS) * time;
+      if (t0 + (TILE > ROWS ? TILE : ROWS) > length)
+        at -= max(0, t0 + k * ROWS + (int)(threadIdx.x / N) - (length - 1)) * time;
+      x[k] = p[at];
     }
   }
   __device__ void put(float* lds, int t0, int end, int states) const {
 #pragma unroll
     for (int k = 0; k < NE; k++) {
-      const int e = k * THREADS + threadIdx.x;
-      const bool ok = t0 + e / N < end && e % N < states;
-      if (e < TILE * N) lds[e] = ok ? (float)x[k] : 0.f;
+      const int r = k * ROWS + threadIdx.x / N;
+      const float v = (float)x[k];
+      if (TILE >= ROWS || r < TILE)
+        lds[r * N + threadIdx.x % N] = t0 + r < end && (int)threadIdx.x % N < states ? v : 0.f;
     }
   }
 };
@@ -299,6 +319,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
   using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
   const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
+  if (ENDS && w.piece == p.chunks - 1) return;         // nothing follows it
   float A[S], h[S], total = 0.f;
   w.load(a.A, 0, p, A);
 #pragma unroll
@@ -313,25 +334,36 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
   float D[VEC], bias[VEC];
   tile.vector(a.D, D);
   tile.vector(a.dt_bias, bias);
-  typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV];
+  typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV] = {};
   StateTile<T, N, TILE, CW * Q> B, C;
-  const auto fetch = [&](int t0) {
-    tile.load(a.u, w.b, t0, a.length, u);
-    tile.load(a.dt, w.b, t0, a.length, dt);
-    if (!ENDS && a.z.data) tile.load(a.z, w.b, t0, a.length, z);
-    B.load(a.B, w.g * a.B_group, w.b, t0, a);
-    if (!ENDS) C.load(a.C, w.g * a.C_group, w.b, t0, a);
+  const T *at_u = tile.start(a.u, w.b, t_first), *at_dt = tile.start(a.dt, w.b, t_first);
+  const T* at_z = tile.start(a.z, w.b, t_first);
+  T* at_y = tile.start(a.y, w.b, t_first);
+  B.start(a.B, w.g * a.B_group, w.b, t_first, a.states);
+  C.start(a.C, w.g * a.C_group, w.b, t_first, a.states);
+  const bool gated = a.z.data;
+  const auto fetch = [&](int t0) {                     // and on to the next tile
+    tile.load(at_u, a.u.time, t0, a.length, u);
+    tile.load(at_dt, a.dt.time, t0, a.length, dt);
+    at_u += TILE * a.u.time;
+    at_dt += TILE * a.dt.time;
+    B.load(a.B.time, t0, a.length);
+    B.p += TILE * a.B.time;
+    if (ENDS) return;
+    if (gated) tile.load(at_z, a.z.time, t0, a.length, z);
+    at_z += TILE * a.z.time;
+    C.load(a.C.time, t0, a.length);
+    C.p += TILE * a.C.time;
   };
   if (t_first < min(t_last, end)) fetch(t_first);
-  for (int t0 = t_first; t0 < t_last; t0 += TILE) {
+  for (int t0 = t_first; t0 < t_last; t0 += TILE, at_y += TILE * a.y.time) {
     if (t0 >= end) {                                   // nothing but zeros from here on
       if (!ENDS && tile.on) {
         const float zero[VEC] = {};
 #pragma unroll
-        for (int k = 0; k < TileT::NV; k++) {
-          const int t = t0 + k * TileT::rows + tile.r;
-          if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, zero);
-        }
+        for (int k = 0; k < TileT::NV; k++)
+          if (t0 + k * TileT::rows + tile.r < t_last)
+            store_vec<VEC>(at_y + k * TileT::rows * a.y.time, VEC, zero);
       }
       continue;
     }
@@ -339,12 +371,12 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
       const bool ok = tile.on && t0 + r < end;
-      if (tile.r < TileT::rows) {
 #pragma unroll
-        for (int i = 0; i < VEC; i++) {
-          const float delta = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
-          lds_d[r * ROW + tile.c + i] = {delta, ok ? delta * (float)u[k][i] : 0.f};
-        }
+      for (int i = 0; i < VEC; i++) {
+        const float delta = delta_of((float)dt[k][i] + bias[i], a.softplus);
+        const float du = delta * (float)u[k][i];
+        if (tile.lead)
+          lds_d[r * ROW + tile.c + i] = {ok ? delta : 0.f, ok ? du : 0.f};
       }
     }
     B.put(lds_b, t0, end, a.states);
@@ -356,7 +388,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
       u0[k] = u[k];
       z0[k] = z[k];
     }
-    fetch(min(t0 + TILE, t_last - 1));
+    fetch(t0 + TILE);
 #pragma unroll 2
     for (int i4 = 0; i4 < TILE / 4; i4++) {
       if (!ENDS && a.kept && i4 % (kKeep / 4) == 0 && w.on && t0 + 4 * i4 < a.length)
@@ -386,26 +418,22 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
         lds_d[at].x = state_sums<Q>(y);
     }
     __syncthreads();
-    if (!ENDS) {
-      if (tile.on) {
+    if (!ENDS && tile.on) {
 #pragma unroll
-        for (int k = 0; k < TileT::NV; k++) {
-          const int r = k * TileT::rows + tile.r, t = t0 + r;
-          float y[VEC];
+      for (int k = 0; k < TileT::NV; k++) {
+        const int r = k * TileT::rows + tile.r, t = t0 + r;
+        float y[VEC];
 #pragma unroll
-          for (int i = 0; i < VEC; i++) {
-            y[i] = fmaf(D[i], (float)u0[k][i], lds_d[r * ROW + tile.c + i].x);
-            if (a.z.data) {
-              const float zi = (float)z0[k][i];
-              y[i] *= zi * sigmoid(zi);
-            }
-            if (t >= end) y[i] = 0.f;
-          }
-          if (t < t_last) store_vec<VEC>(row_out<T>(a.y, w.b, t) + tile.d, VEC, y);
+        for (int i = 0; i < VEC; i++) {
+          const float zi = (float)z0[k][i], act = zi * sigmoid(zi);
+          y[i] = fmaf(D[i], (float)u0[k][i], lds_d[r * ROW + tile.c + i].x);
+          y[i] *= gated ? act : 1.f;
+          y[i] = t < end ? y[i] : 0.f;
         }
+        if (t < t_last) store_vec<VEC>(at_y + k * TileT::rows * a.y.time, VEC, y);
       }
-      // a thread stages the elements whose outputs it has just read
     }
+    // a thread stages the elements whose outputs it has just read
   }
   if (ENDS) {
     total += dpp<kXor1>(total);
@@ -441,6 +469,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
   const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
+  if (ENDS && w.piece == 0) return;                    // nothing precedes it
   const int wave = threadIdx.x / 64, mine = channel_value<Q>(threadIdx.x % 64);
   float A[S], g[S], dA[S], total = 0.f;                // g: of the state before the later token
   w.load(a.A, 0, p, A);
@@ -458,20 +487,10 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   tile.vector(a.dt_bias, bias);
 #pragma unroll
   for (int i = 0; i < VEC; i++) dD[i] = dbias[i] = 0.f;
-  typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV], dout[TileT::NV];
+  typename TileT::Raw u[TileT::NV] = {}, dt[TileT::NV], z[TileT::NV] = {}, dout[TileT::NV];
   StateTile<T, N, TILE, THREADS> B, C;
   float h0[S];
-  const auto fetch = [&](int t0) {
-    if (!ENDS) tile.load(a.u, w.b, t0, a.length, u);
-    tile.load(a.dt, w.b, t0, a.length, dt);
-    if (a.z.data) tile.load(a.z, w.b, t0, a.length, z);
-    tile.load(a.dy, w.b, t0, a.length, dout);
-    C.load(a.C, w.g * a.C_group, w.b, t0, a);
-    if (!ENDS) {
-      B.load(a.B, w.g * a.B_group, w.b, t0, a);
-      read_states<S>(w.padded(a.kept, w.b * p.keeps + t0 / TILE, p), h0);
-    }
-  };
+  const bool gated = a.z.data;
   // tiles past the end: zeros
   const int live = t_first + (int)cdiv(max(0, min(t_last, end) - t_first), TILE) * TILE;
   if (!ENDS) {
@@ -486,7 +505,34 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     for (int e = threadIdx.x; e < max(0, t_last - live) * 2 * N; e += THREADS)
       p.part_bc[(cell + (int64_t)(live + e / (2 * N)) * a.groups) * (2 * N) + e % (2 * N)] = 0.f;
   }
-  if (live > t_first) fetch(live - TILE);
+  // from the last live tile back; the first one is fetched twice
+  const int t_top = max(live - TILE, t_first);
+  const T *at_u = tile.start(a.u, w.b, t_top), *at_dt = tile.start(a.dt, w.b, t_top);
+  const T *at_z = tile.start(a.z, w.b, t_top), *at_dy = tile.start(a.dy, w.b, t_top);
+  T *at_du = tile.start(a.du, w.b, t_top), *at_ddt = tile.start(a.ddt, w.b, t_top);
+  T* at_dz = tile.start(a.dz, w.b, t_top);
+  const float* at_kept = w.padded(a.kept, w.b * p.keeps + t_top / TILE, p);
+  B.start(a.B, w.g * a.B_group, w.b, t_top, a.states);
+  C.start(a.C, w.g * a.C_group, w.b, t_top, a.states);
+  const auto fetch = [&](int t0) {                     // and back to the tile before
+    const int64_t back = t0 > t_first ? TILE : 0;
+    tile.load(at_dt, a.dt.time, t0, a.length, dt);
+    at_dt -= back * a.dt.time;
+    if (gated) tile.load(at_z, a.z.time, t0, a.length, z);
+    at_z -= back * a.z.time;
+    tile.load(at_dy, a.dy.time, t0, a.length, dout);
+    at_dy -= back * a.dy.time;
+    C.load(a.C.time, t0, a.length);
+    C.p -= back * a.C.time;
+    if (ENDS) return;
+    tile.load(at_u, a.u.time, t0, a.length, u);
+    at_u -= back * a.u.time;
+    B.load(a.B.time, t0, a.length);
+    B.p -= back * a.B.time;
+    read_states<S>(at_kept, h0);
+    at_kept -= back / TILE * a.width * N;
+  };
+  if (live > t_first) fetch(t_top);
   for (int t0 = live - TILE; t0 >= t_first; t0 -= TILE) {
     float step[TileT::NV][VEC];                        // delta of the thread's elements
 #pragma unroll
@@ -495,11 +541,12 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
       const bool ok = tile.on && t0 + r < end;
 #pragma unroll
       for (int i = 0; i < VEC; i++) {
-        step[k][i] = ok ? delta_of((float)dt[k][i] + bias[i], a.softplus) : 0.f;
-        const float zi = (float)z[k][i], act = a.z.data ? zi * sigmoid(zi) : 1.f;
-        if (tile.r < TileT::rows)
-          lds_d[r * ROW + tile.c + i] = {step[k][i], !ENDS && ok ? step[k][i] * (float)u[k][i] : 0.f,
-                                         ok ? (float)dout[k][i] * act : 0.f, 0.f};
+        const float delta = delta_of((float)dt[k][i] + bias[i], a.softplus);
+        const float zi = (float)z[k][i], act = zi * sigmoid(zi), o = (float)dout[k][i];
+        const float du = delta * (float)u[k][i], dy = o * (gated ? act : 1.f);
+        step[k][i] = ok ? delta : 0.f;
+        if (tile.lead)
+          lds_d[r * ROW + tile.c + i] = {step[k][i], ok ? du : 0.f, ok ? dy : 0.f, 0.f};
       }
     }
     C.put(lds_c, t0, end, a.states);
@@ -611,25 +658,33 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
 #pragma unroll
       for (int k = 0; k < TileT::NV; k++) {
         const int r = k * TileT::rows + tile.r, t = t0 + r;
-        if (!tile.on || t >= t_last) continue;
         const bool ok = t < end;
         float du[VEC], ddt[VEC], dz[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; i++) {
           const float4 sums = lds_d[r * ROW + tile.c + i];
           const float ui = (float)u0[k][i], zi = (float)z0[k][i], o = (float)dout0[k][i];
-          const float s = sigmoid(zi), dy = a.z.data ? o * (zi * s) : o;
+          const float s = sigmoid(zi), dy = o * (gated ? zi * s : 1.f);
+          const float slope = sigmoid((float)dt0[k][i] + bias[i]);
           const float y = fmaf(D[i], ui, sums.z), dd = fmaf(ui, sums.x, sums.y * kLn2);
-          du[i] = ok ? fmaf(step[k][i], sums.x, D[i] * dy) : 0.f;
-          ddt[i] = ok ? (a.softplus ? dd * sigmoid((float)dt0[k][i] + bias[i]) : dd) : 0.f;
-          dz[i] = ok ? o * y * (s * (1.f + zi * (1.f - s))) : 0.f;
-          dD[i] += ok ? dy * ui : 0.f;
+          const float own = dy * ui, raw = dd * (a.softplus ? slope : 1.f);
+          const float through = fmaf(step[k][i], sums.x, D[i] * dy);
+          const float gate = o * y * (s * (1.f + zi * (1.f - s)));
+          du[i] = ok ? through : 0.f;
+          ddt[i] = ok ? raw : 0.f;
+          dz[i] = ok ? gate : 0.f;
+          dD[i] += ok ? own : 0.f;
           dbias[i] += ddt[i];
         }
-        store_vec<VEC>(row_out<T>(a.du, w.b, t) + tile.d, VEC, du);
-        store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, ddt);
-        if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, dz);
+        if (tile.on && t < t_last) {
+          store_vec<VEC>(at_du + k * TileT::rows * a.du.time, VEC, du);
+          store_vec<VEC>(at_ddt + k * TileT::rows * a.ddt.time, VEC, ddt);
+          if (gated) store_vec<VEC>(at_dz + k * TileT::rows * a.dz.time, VEC, dz);
+        }
       }
+      at_du -= TILE * a.du.time;
+      at_ddt -= TILE * a.ddt.time;
+      at_dz -= TILE * a.dz.time;
     }
     __syncthreads();                                   // the next tile takes the same LDS
   }
@@ -647,7 +702,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   if (a.dstate_in && w.piece == 0) w.store(a.dstate_in, w.b, p, g);
   // D and dt_bias: the threads of a column, then one sum for each channel
   float* sums = reinterpret_cast<float*>(lds_d);       // [rows][channels] of (dD, dbias)
-  if (tile.r < TileT::rows) {
+  if (tile.lead) {
 #pragma unroll
     for (int i = 0; i < VEC; i++) {
       sums[(tile.r * CW + tile.c + i) * 2] = dD[i];
