@@ -718,37 +718,47 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   }
 }
 
-// dB and dC from the blocks' parts: one thread per (batch, token, group, state).
+// The sums over workgroups, in one launch: the first `cell_blocks` workgroups
+// take dB and dC (one thread for each (batch, token, group, state), eight
+// blocks' parts in flight), the next dA, the last dD and ddt_bias (columns of the
+// parts of sequences and chunks).
 template <class T>
-__global__ __launch_bounds__(256) void k_scan_sum_bc(const float* in, int64_t parts, int64_t cells,
-                                                     int32_t padded, int32_t states, T* dB, T* dC) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t cell = id / (2 * padded);
-  const int k = (int)(id % (2 * padded)), n = k % padded;
-  if (cell >= cells || n >= states) return;
-  float s = 0.f;
-  for (int64_t j = 0; j < parts; j++) s += in[(j * cells + cell) * (2 * padded) + k];
-  (k < padded ? dB : dC)[cell * states + n] = (T)s;
-}
-
-// dA, dD and ddt_bias from the parts of sequences and chunks.
-__global__ __launch_bounds__(256) void k_scan_sum_a(const float* pa, const float* pd,
-                                                    int64_t parts, int32_t width, int32_t padded,
-                                                    int32_t states, float* dA, float* dD,
-                                                    float* dbias) {
-  __shared__ float lds[256];
-  const int64_t ca = (int64_t)width * padded, cd = (int64_t)width * 2;
-  const int64_t na = cdiv(ca, kSumCols);
-  if (blockIdx.x < na) {
-    const int64_t c = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
-    const float s = column_sum(pa, parts, ca, c, lds);
-    if (threadIdx.x < kSumCols && c < ca && c % padded < states)
-      dA[c / padded * states + c % padded] = s;
+__global__ __launch_bounds__(kSumThreads) void k_scan_sums(ScanParams p, int64_t cells, int32_t N,
+                                                           int64_t cell_blocks,
+                                                           int64_t a_blocks) {
+  __shared__ float lds[kSumThreads];
+  const int32_t states = p.a.states;
+  const int64_t blk = blockIdx.x;
+  if (blk < cell_blocks) {
+    const int64_t id = blk * kSumThreads + threadIdx.x;
+    const int64_t cell = id / (2 * N), stride = cells * 2 * N;
+    const int k = (int)(id % (2 * N)), n = k % N;
+    if (cell >= cells || n >= states) return;
+    const float* in = p.part_bc + cell * (2 * N) + k;
+    float s = 0.f;
+    int j = 0;
+    for (; j + 8 <= p.blocks; j += 8) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = in[(j + i) * stride];
+      s += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    for (; j < p.blocks; j++) s += in[j * stride];
+    static_cast<T*>(k < N ? p.a.dB : p.a.dC)[cell * states + n] = (T)s;
+    return;
+  }
+  const bool decay = blk < cell_blocks + a_blocks;
+  const int64_t cols = (int64_t)p.a.width * (decay ? N : 2);
+  const int64_t c = (blk - cell_blocks - (decay ? 0 : a_blocks)) * kSumCols +
+                    threadIdx.x % kSumCols;
+  const float s = column_sum(decay ? p.part_a : p.part_d, (int64_t)p.a.batch * p.chunks, cols, c,
+                             lds);
+  if (threadIdx.x >= kSumCols || c >= cols) return;
+  if (decay) {
+    if (c % N < states) p.a.dA[c / N * states + c % N] = s;
   } else {
-    const int64_t c = (int64_t)(blockIdx.x - na) * kSumCols + threadIdx.x % kSumCols;
-    const float s = column_sum(pd, parts, cd, c, lds);
-    float* out = c % 2 ? dbias : dD;
-    if (threadIdx.x < kSumCols && c < cd && out) out[c / 2] = s;
+    float* out = c % 2 ? p.a.ddt_bias : p.a.dD;
+    if (out) out[c / 2] = s;
   }
 }
 
@@ -818,19 +828,19 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 }
 
 // How a scan is cut up.  A channel takes a quad of lanes (more above 16
-// states).  The kernels are bound by instruction issue, which needs two to four
-// waves on every SIMD: where batch and channels give fewer, the length is cut into
-// chunks, which costs a pass over them for their end states.  Forward and
-// backward, us, bfloat16, 16 states: batch 8, 2048 tokens, 2048 channels (one
-// wave a SIMD): 1 chunk 257 + 692, 4 chunks 257 + 628; batch 1, 16384 tokens: 2
-// chunks 418 + 1107, 16 chunks 265 + 641; batch 16, 4096 channels (16 waves a compute
-// unit): 1 chunk 595 + 1935, 2 chunks 937 + 2355.
+// states).  The kernels are bound by instruction issue, which wants waves on
+// every SIMD: where batch and channels give too few, the length is cut into
+// chunks, which costs a pass over all but one of them for their end states.
+// us for bfloat16 and 16 states by waves a compute unit without and with
+// chunks, to 16 waves: 2048 tokens and channels, batch 4 (2 waves) forward 190 /
+// 132, batch 8 (4 waves) forward 231 / 230, backward 654 / 573, batch 12 (6
+// waves) forward 327 / 379, backward 944 / 870.
 struct ScanPlan {
   int S, Q, VEC;
   int64_t group_width, blocks;
   int64_t chunks, chunk, keeps;
 };
-ScanPlan scan_plan(const rc_scan_args& a) {
+ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   ScanPlan p;
   p.group_width = a.width / a.groups;
   p.S = a.states > 8 ? 4 : a.states > 4 ? 2 : 1;
@@ -838,9 +848,9 @@ ScanPlan scan_plan(const rc_scan_args& a) {
   p.VEC = p.group_width % 4 ? 1 : 4;
   p.blocks = cdiv(p.group_width, channels_of(p.Q));
   const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
-  const int64_t want = 16 * (int64_t)rcdp::num_cus();
+  const int64_t cus = rcdp::num_cus(), enough = (backward ? 8 : 4) * cus;
   const int64_t most = cdiv(a.length, 64) < 32 ? cdiv(a.length, 64) : 32;
-  p.chunks = waves > 0 && waves < want ? cdiv(want, waves) : 1;
+  p.chunks = waves > 0 && waves < enough ? cdiv(16 * cus, waves) : 1;
   if (p.chunks > most) p.chunks = most;
   if (p.chunks < 1) p.chunks = 1;
   p.chunk = cdiv(cdiv(a.length, p.chunks), kFwdTile) * kFwdTile;
@@ -884,10 +894,12 @@ int scan_check(const rc_scan_args* a, bool backward) {
   if (backward && a->width > 0 &&
       (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias)))
     return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a);
+  const ScanPlan p = scan_plan(*a, backward);
   const int64_t cells = (int64_t)a->batch * a->length * a->groups;
   if (p.blocks * a->groups * a->batch * p.chunks >= kMaxBlocks ||
-      cdiv(cells * 2 * p.Q * p.S, kSumThreads) >= kMaxBlocks)
+      cdiv(cells * 2 * p.Q * p.S, kSumThreads) + cdiv((int64_t)a->width * p.Q * p.S, kSumCols) +
+              cdiv((int64_t)a->width * 2, kSumCols) >=
+          kMaxBlocks)
     return RC_E_OVERFLOW;
   return RC_OK;
 }
@@ -928,27 +940,27 @@ int by_plan(const ScanPlan& p, F&& f) {
 
 extern "C" int rc_scan_kept_bytes(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  const ScanPlan p = scan_plan(*a);
+  const ScanPlan p = scan_plan(*a, false);
   *bytes_host = (uint64_t)a->batch * p.keeps * a->width * p.Q * p.S * 4;
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a), false).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a, false), false).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_backward_workspace(const rc_scan_args* a, uint64_t* bytes_host) {
   if (!bytes_host || !scan_sizes_ok(a)) return RC_E_ARG;
-  *bytes_host = scan_scratch(*a, scan_plan(*a), true).total();
+  *bytes_host = scan_scratch(*a, scan_plan(*a, true), true).total();
   return RC_OK;
 }
 
 extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, false)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a);
+  const ScanPlan p = scan_plan(a, false);
   const ScanScratch need = scan_scratch(a, p, false);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
@@ -972,7 +984,7 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
 extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   if (const int st = scan_check(args, true)) return st;
   const rc_scan_args& a = *args;
-  const ScanPlan p = scan_plan(a);
+  const ScanPlan p = scan_plan(a, true);
   const ScanScratch need = scan_scratch(a, p, true);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
   if (a.width == 0) return RC_OK;
@@ -995,16 +1007,12 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
       });
       if (st) return st;
     }
-    if (cells > 0) {
-      k_scan_sum_bc<T><<<dim3((uint32_t)cdiv(cells * 2 * N, kSumThreads)), kSumThreads, 0, s>>>(
-          q.part_bc, p.blocks, cells, N, a.states, static_cast<T*>(a.dB), static_cast<T*>(a.dC));
-      if (const int st = launched("k_scan_sum_bc")) return st;
-    }
-    const int64_t cols = (int64_t)a.width * N;
-    k_scan_sum_a<<<dim3((uint32_t)(cdiv(cols, kSumCols) + cdiv(2 * (int64_t)a.width, kSumCols))),
-                   kSumThreads, 0, s>>>(q.part_a, q.part_d, a.batch * p.chunks, a.width, N,
-                                        a.states, a.dA, a.dD, a.ddt_bias);
-    return launched("k_scan_sum_a");
+    const int64_t cell_blocks = cdiv(cells * 2 * N, kSumThreads);
+    const int64_t a_blocks = cdiv((int64_t)a.width * N, kSumCols);
+    const int64_t d_blocks = cdiv((int64_t)a.width * 2, kSumCols);
+    k_scan_sums<T><<<dim3((uint32_t)(cell_blocks + a_blocks + d_blocks)), kSumThreads, 0, s>>>(
+        q, cells, N, cell_blocks, a_blocks);
+    return launched("k_scan_sums");
   });
 }
 
