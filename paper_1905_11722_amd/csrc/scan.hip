@@ -291,13 +291,24 @@ __device__ __forceinline__ void write_states(float* at, const float (&x)[S]) {
 template <int Q, int S, bool REVERSE>
 __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
                                       const float (&A)[S], float (&h)[S]) {
+  constexpr int AHEAD = 8;          // chunks whose loads are in flight together
+  const int count = REVERSE ? p.chunks - 1 - w.piece : w.piece;
   const int first = REVERSE ? p.chunks - 1 : 0, step = REVERSE ? -1 : 1;
-  for (int k = first; k != w.piece; k += step) {
-    float own[S];
-    read_states<S>(w.padded(p.ends, w.b * p.chunks + k, p), own);
-    const float sum = p.steps[(w.b * p.chunks + k) * p.a.width + w.d];
+  for (int k0 = 0; k0 < count; k0 += AHEAD) {
+    float own[AHEAD][S], sum[AHEAD];
 #pragma unroll
-    for (int i = 0; i < S; i++) h[i] = fmaf(fast_exp2(sum * A[i]), h[i], own[i]);
+    for (int k = 0; k < AHEAD; k++) {
+      const int64_t at = w.b * p.chunks + first + step * min(k0 + k, count - 1);
+      read_states<S>(w.padded(p.ends, at, p), own[k]);
+      sum[k] = p.steps[at * p.a.width + w.d];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++)
+#pragma unroll
+      for (int i = 0; i < S; i++) {
+        const float next = fmaf(fast_exp2(sum[k] * A[i]), h[i], own[k][i]);
+        h[i] = k0 + k < count ? next : h[i];
+      }
   }
 }
 
@@ -834,7 +845,10 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 // us for bfloat16 and 16 states by waves a compute unit without and with
 // chunks, to 16 waves: 2048 tokens and channels, batch 4 (2 waves) forward 190 /
 // 132, batch 8 (4 waves) forward 231 / 230, backward 654 / 573, batch 12 (6
-// waves) forward 327 / 379, backward 944 / 870.
+// waves) forward 327 / 379, backward 944 / 870.  Chunks have 64 tokens at least
+// (32: 2048 tokens of 1024 channels forward 40 for 37) and number 128 at most,
+// whose joining is a loop (16384 tokens of 64 channels forward and backward, 32
+// chunks 324, 128 chunks 117).
 struct ScanPlan {
   int S, Q, VEC;
   int64_t group_width, blocks;
@@ -849,7 +863,7 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.blocks = cdiv(p.group_width, channels_of(p.Q));
   const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
   const int64_t cus = rcdp::num_cus(), enough = (backward ? 8 : 4) * cus;
-  const int64_t most = cdiv(a.length, 64) < 32 ? cdiv(a.length, 64) : 32;
+  const int64_t most = cdiv(a.length, 64) < 128 ? cdiv(a.length, 64) : 128;
   p.chunks = waves > 0 && waves < enough ? cdiv(16 * cus, waves) : 1;
   if (p.chunks > most) p.chunks = most;
   if (p.chunks < 1) p.chunks = 1;
