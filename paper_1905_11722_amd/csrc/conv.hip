@@ -87,14 +87,22 @@ struct Rows {
 template <class T, int K, int V>
 __device__ __forceinline__ void load_weights(const rc_conv_args& a, int c,
                                              float (&w)[K][V], float (&bias)[V]) {
-  const bool f32 = a.param_dtype == RC_F32;
+  // the weights of V channels lie together: wide loads
+  const auto read = [&](auto type) {
+    using P = decltype(type);
+    const P *pw = static_cast<const P*>(a.weight) + (int64_t)c * K;
+    const P* pb = static_cast<const P*>(a.bias) + c;
 #pragma unroll
-  for (int i = 0; i < V; i++) {
+    for (int i = 0; i < V; i++) {
 #pragma unroll
-    for (int k = 0; k < K; k++)
-      w[k][i] = load_param<T>(a.weight, (int64_t)(c + i) * K + k, f32);
-    bias[i] = a.bias ? load_param<T>(a.bias, c + i, f32) : 0.f;
-  }
+      for (int k = 0; k < K; k++) w[k][i] = (float)pw[i * K + k];
+      bias[i] = a.bias ? (float)pb[i] : 0.f;
+    }
+  };
+  if (a.param_dtype == RC_F32)
+    read(float{});
+  else
+    read(T{});
 }
 
 template <class T, int K, int V>
@@ -176,6 +184,10 @@ __global__ __launch_bounds__(kThreads) void k_conv_backward(ConvParams<T> p) {
     const int c = (int)c64;
     const int b = (int)(cell / p.runs), t0 = (int)(cell % p.runs) * p.run;
     const int t1 = min(t0 + p.run, a.length), end = seq_end(a.lengths, b, a.length);
+    if (t0 > 0 && t0 >= end) {                         // past the end: zeros, no gradients
+      const float zero[V] = {};
+      for (int t = t0; t < t1; t++) store_vec<V>(at<T>(a.dx, b, t, c), V, zero);
+    } else {
     // row t finishes dx of row t - (K - 1); the first run also writes the
     // state's rows -(K - 1) .. -1
     const int first = t0 == 0 && a.dstate_in.data ? -(K - 1) : t0;
@@ -248,6 +260,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_backward(ConvParams<T> p) {
       }
       now = next;
       dnow = dnext;
+    }
     }
   }
   if (!p.partial) return;
