@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
 }
 
 template <class T, int K, int V>
-__global__ __launch_bounds__(kThreads) void k_conv_backward(ConvParams<T> p) {
+__global__ __launch_bounds__(kThreads, K <= 4 && sizeof(T) == 2 ? 4 : 2) void k_conv_backward(ConvParams<T> p) {
   __shared__ float lds[kThreads * V];
   const rc_conv_args& a = p.a;
   const int lane = threadIdx.x % p.lanes, slot = threadIdx.x / p.lanes;
