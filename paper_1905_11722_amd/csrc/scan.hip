@@ -209,11 +209,13 @@ struct Tile {
   typedef T Raw __attribute__((ext_vector_type(VEC)));
   int64_t d;                        // first channel of the column, clamped
   int c, r;                         // its place in the block, first row
-  bool lead;                        // has a row of its own in a tile
+  // Every thread has a row of its own in a tile (else: `lead`).
+  static constexpr bool all = threads / columns <= TILE;
+  bool lead;
   bool on;                          // and its channel exists
   __device__ Tile(const ScanParams& p, int64_t g, int blk) {
     c = threadIdx.x % columns * VEC;
-    lead = threadIdx.x / columns < rows;
+    lead = all || threadIdx.x / columns < rows;
     r = min((int)threadIdx.x / columns, rows - 1);
     on = lead && blk * CW + c < p.group_width;
     d = g * p.group_width + min(blk * CW + c, p.group_width - VEC);
@@ -382,12 +384,16 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
       const bool ok = tile.on && t0 + r < end;
+      float2 d[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; i++) {
         const float delta = delta_of((float)dt[k][i] + bias[i], a.softplus);
         const float du = delta * (float)u[k][i];
-        if (tile.lead)
-          lds_d[r * ROW + tile.c + i] = {ok ? delta : 0.f, ok ? du : 0.f};
+        d[i] = {ok ? delta : 0.f, ok ? du : 0.f};
+      }
+      if (TileT::all || tile.lead) {
+#pragma unroll
+        for (int i = 0; i < VEC; i++) lds_d[r * ROW + tile.c + i] = d[i];
       }
     }
     B.put(lds_b, t0, end, a.states);
@@ -550,14 +556,18 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
       const bool ok = tile.on && t0 + r < end;
+      float4 d[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; i++) {
         const float delta = delta_of((float)dt[k][i] + bias[i], a.softplus);
         const float zi = (float)z[k][i], act = zi * sigmoid(zi), o = (float)dout[k][i];
         const float du = delta * (float)u[k][i], dy = o * (gated ? act : 1.f);
         step[k][i] = ok ? delta : 0.f;
-        if (tile.lead)
-          lds_d[r * ROW + tile.c + i] = {step[k][i], ok ? du : 0.f, ok ? dy : 0.f, 0.f};
+        d[i] = {step[k][i], ok ? du : 0.f, ok ? dy : 0.f, 0.f};
+      }
+      if (TileT::all || tile.lead) {
+#pragma unroll
+        for (int i = 0; i < VEC; i++) lds_d[r * ROW + tile.c + i] = d[i];
       }
     }
     C.put(lds_c, t0, end, a.states);
