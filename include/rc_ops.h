@@ -21,6 +21,7 @@
  *    enqueued then, except after RC_E_DEVICE.  Nothing crosses the ABI as an
  *    exception.
  *  - Sizes may be zero.  A call whose outputs are empty does nothing.
+ *    length and width are at most 2^30.
  *  - Channels are contiguous; batch and time strides are in elements and
  *    free, with any alignment that the type has.  Outputs must not overlap
  *    inputs or each other.

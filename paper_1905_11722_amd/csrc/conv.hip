@@ -347,7 +347,7 @@ bool conv_sizes_ok(int32_t dtype, int32_t param, int32_t act, int32_t batch, int
                    int32_t width, int32_t taps) {
   return dtype_ok(dtype) && param_ok(param, dtype) &&
          (act == RC_ACT_NONE || act == RC_ACT_SILU) && batch >= 0 && length >= 0 && width >= 0 &&
-         taps >= 1 && taps <= 8;
+         length <= kMaxExtent && width <= kMaxExtent && taps >= 1 && taps <= 8;
 }
 
 // The launch shape: lanes along the channels, rows of a thread, workgroups.

@@ -104,6 +104,8 @@ inline int by_dtype(int32_t d, F&& f) {
 }
 
 constexpr int64_t kMaxBlocks = (int64_t)1 << 31;
+// Tokens and channels: indexes a few tiles past the last stay in 32 bits.
+constexpr int32_t kMaxExtent = 1 << 30;
 
 // Column sums of a partial buffer, a column reduction's last step:
 // sum over p < parts of in[p * cols + c] for the workgroup's column of this

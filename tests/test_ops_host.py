@@ -92,6 +92,8 @@ BAD = [
     ("rc_conv_forward", conv, dict(length=-1)), ("rc_conv_forward", conv, dict(weight=None)),
     ("rc_conv_forward", conv, dict(x=NONE)), ("rc_conv_forward", conv, dict(y=NONE)),
     ("rc_conv_backward", conv, dict(dy=NONE)), ("rc_conv_backward", conv, dict(dx=NONE)),
+    ("rc_conv_forward", conv, dict(length=2 ** 30 + 1)), ("rc_conv_forward", conv, dict(width=2 ** 30 + 8)),
+    ("rc_scan_forward", scan, dict(length=2 ** 30 + 1)), ("rc_scan_forward", scan, dict(width=2 ** 30 + 8)),
     ("rc_scan_forward", scan, dict(states=0)), ("rc_scan_forward", scan, dict(states=65)),
     ("rc_scan_forward", scan, dict(groups=3)), ("rc_scan_forward", scan, dict(groups=0)),
     ("rc_scan_forward", scan, dict(A=None)), ("rc_scan_forward", scan, dict(B=NONE)),
