@@ -9,8 +9,11 @@
 //
 // A few operations for each value moved: bound by memory.  A row stays in the
 // registers of its threads from the loads to the stores, so every tensor is
-// read or written once; a row needs two sums over its threads.  Workgroups
-// walk over rows with the weights (and backward the weights' gradients) in registers.
+// read or written once; a row needs two sums over its threads, one after the
+// other.  Workgroups walk over rows with the weights' gradients (and up to
+// 8192 channels the weights) in registers.  (Backward with four sums in one step,
+// the second mean being linear in the first, cancels where the gradient is
+// small: not kept.)
 #include "ops_internal.h"
 
 using namespace rcops;
@@ -28,22 +31,49 @@ struct NormParams {
 // Threads of a workgroup with TPR threads a row.
 constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
-// Sum over the TPR threads of a row.  lds has 16 floats of its own for each
-// of the two sums of a row: a row's second barrier is between its first
-// sum's reads and the next row's writes.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float x, float* lds) {
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// Sum over 32 or 64 lanes, in each of them (a mirror is as good as an
+// exchange once the lanes below are equal).
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float x) {
+  x = dpp_add<0xB1>(x);                                // lanes 1 apart
+  x = dpp_add<0x4E>(x);                                // 2 apart
+  x = dpp_add<0x141>(x);                               // half rows mirrored
+  x = dpp_add<0x140>(x);                               // rows mirrored
+  const unsigned a = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  if (LANES == 32) return x;
+  const unsigned b = __builtin_bit_cast(unsigned, x);
+  const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
+}
+
+// Sums over the TPR threads of a row of M values.  lds has 16 M floats of its
+// own for each of two calls in a row: the barrier of one call is between the
+// reads of the one before and the writes of the one after.
+template <int TPR, int M>
+__device__ __forceinline__ void row_sums(float (&x)[M], float* lds) {
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-  if (TPR == 64) return x;
+  for (int m = 0; m < M; m++) x[m] = lane_sum<TPR == 32 ? 32 : 64>(x[m]);
+  if (TPR <= 64) return;
   constexpr int W = TPR / 64;
-  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
+  if (threadIdx.x % 64 == 0) {
+#pragma unroll
+    for (int m = 0; m < M; m++) lds[threadIdx.x / 64 * M + m] = x[m];
+  }
   __syncthreads();
   const int first = threadIdx.x / TPR * W;
-  float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < W; i++) s += lds[first + i];
-  return s;
+  for (int m = 0; m < M; m++) {
+    x[m] = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; i++) x[m] += lds[(first + i) * M + m];
+  }
 }
 
 // act(x) and its slope.
@@ -91,7 +121,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
   for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < a.rows; r0 += (int64_t)gridDim.x * RPW) {
     const int64_t row = r0 + group;
     const bool on = row < a.rows;
-    float out[NV][V], v[NV][V], ss = 0.f;
+    float out[NV][V], v[NV][V], ss[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const int n = on ? a.width - c[k] : 0;
@@ -105,12 +135,15 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
           for (int i = 0; i < V; i++) v[k][i] *= gate_of(g[i], a.gate_activation, slope);
         }
 #pragma unroll
-        for (int i = 0; i < V; i++) ss = fmaf(v[k][i], v[k][i], ss);
+        for (int i = 0; i < V; i++) ss[0] = fmaf(v[k][i], v[k][i], ss[0]);
       }
     }
     float rv = 1.f, ro = 0.f;
     if (a.block.data) {
-      if (a.post_weight) rv = __builtin_amdgcn_rsqf(fmaf(row_sum<TPR>(ss, lds[0]), inv, a.eps));
+      if (a.post_weight) {
+        row_sums<TPR>(ss, lds[0]);
+        rv = __builtin_amdgcn_rsqf(fmaf(ss[0], inv, a.eps));
+      }
 #pragma unroll
       for (int k = 0; k < NV; k++) {
 #pragma unroll
@@ -120,12 +153,13 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
       }
     }
     if (a.pre_weight) {
-      ss = 0.f;
+      ss[0] = 0.f;
 #pragma unroll
       for (int k = 0; k < NV; k++)
 #pragma unroll
-        for (int i = 0; i < V; i++) ss = fmaf(out[k][i], out[k][i], ss);
-      ro = __builtin_amdgcn_rsqf(fmaf(row_sum<TPR>(ss, lds[1]), inv, a.eps));
+        for (int i = 0; i < V; i++) ss[0] = fmaf(out[k][i], out[k][i], ss[0]);
+      row_sums<TPR>(ss, lds[1]);
+      ro = __builtin_amdgcn_rsqf(fmaf(ss[0], inv, a.eps));
 #pragma unroll
       for (int k = 0; k < NV; k++) {
 #pragma unroll
@@ -142,9 +176,12 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
   }
 }
 
+// Backward.  (Above 8192 channels a row and its sums spill: 16384 channels run at a
+// sixth of the rate of 4096.)
 template <class T, class R, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p) {
   constexpr int RPW = threads_of(TPR) / TPR;
+  constexpr bool HOLD = NV == 1;                       // the weights stay in registers
   __shared__ float lds[2][16];
   __shared__ float cols[RPW > 1 ? threads_of(TPR) * V : 1];
   const rc_norm_args& a = p.a;
@@ -154,10 +191,19 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
   int c[NV];
 #pragma unroll
   for (int k = 0; k < NV; k++) c[k] = min((k * TPR + lane) * V, a.width);
-  float wpost[NV][V], wpre[NV][V], scale[NV][V], dw[3][NV][V];
-  load_weight<T>(a.post_weight, f32, c, a.width, 1.f, wpost);
-  load_weight<T>(a.pre_weight, f32, c, a.width, 0.f, wpre);
-  load_weight<T>(a.scale, f32, c, a.width, 1.f, scale);
+  float held[3][V], dw[3][NV][V];
+  const auto weight = [&](const void* w, int k, float absent, float (&x)[V]) {
+    const int at[1] = {c[k]};
+    float y[1][V];
+    load_weight<T>(w, f32, at, a.width, absent, y);
+#pragma unroll
+    for (int i = 0; i < V; i++) x[i] = y[0][i];
+  };
+  if (HOLD) {
+    weight(a.post_weight, 0, 1.f, held[0]);
+    weight(a.scale, 0, 1.f, held[1]);
+    weight(a.pre_weight, 0, 0.f, held[2]);
+  }
 #pragma unroll
   for (int j = 0; j < 3; j++)
 #pragma unroll
@@ -168,7 +214,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     const int64_t row = r0 + group;
     const bool on = row < a.rows;
     const float rv = on ? a.stats[row * 2] : 0.f, ro = on ? a.stats[row * 2 + 1] : 0.f;
-    float dr[NV][V], dn[NV][V], vn[NV][V], act[NV][V], dact[NV][V], unit[NV][V], dot = 0.f;
+    float dr[NV][V], dn[NV][V], vn[NV][V], act[NV][V], dact[NV][V], unit[NV][V], dot[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; k++) {
       const int n = on ? a.width - c[k] : 0;
@@ -177,45 +223,63 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
       load_vec<V>(row_at<T>(a.dnormed, row) + c[k], a.dnormed.data ? n : 0, dn[k]);
       load_vec<V>(row_at<T>(a.block, row) + c[k], a.block.data ? n : 0, vn[k]);
       if (a.gate.data) load_vec<V>(row_at<T>(a.gate, row) + c[k], n, act[k]);
+      float wpost[V], scale[V], wpre[V];
+      if (!HOLD) {
+        weight(a.post_weight, k, 1.f, wpost);
+        weight(a.scale, k, 1.f, scale);
+        weight(a.pre_weight, k, 0.f, wpre);
+      }
 #pragma unroll
       for (int i = 0; i < V; i++) {
         if (a.gate.data) {
           float slope;
           act[k][i] = gate_of(act[k][i], a.gate_activation, slope);
-          dact[k][i] = vn[k][i] * slope;            // u act'
+          dact[k][i] = vn[k][i] * slope;               // u act'
           vn[k][i] *= act[k][i];
         }
         vn[k][i] *= rv;
-        unit[k][i] = fmaf(scale[k][i], vn[k][i] * wpost[k][i], unit[k][i]) * ro;
+        const float part = vn[k][i] * (HOLD ? held[0][i] : wpost[i]);
+        unit[k][i] = fmaf(HOLD ? held[1][i] : scale[i], part, unit[k][i]) * ro;
         dw[0][k][i] = fmaf(dn[k][i], unit[k][i], dw[0][k][i]);
-        dn[k][i] *= wpre[k][i];
-        dot = fmaf(dn[k][i], unit[k][i], dot);
+        dn[k][i] *= HOLD ? held[2][i] : wpre[i];
+        dot[0] = fmaf(dn[k][i], unit[k][i], dot[0]);
       }
     }
     if (a.pre_weight) {
-      const float m = row_sum<TPR>(dot, lds[0]) * inv;
+      row_sums<TPR>(dot, lds[0]);
+      const float m = dot[0] * inv;
 #pragma unroll
       for (int k = 0; k < NV; k++)
 #pragma unroll
         for (int i = 0; i < V; i++)
           dr[k][i] = fmaf(ro, dn[k][i] - unit[k][i] * m, dr[k][i]);
     }
-    dot = 0.f;
+    dot[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; k++) {
-      if (on && a.dresidual.data)
+      if (on)
         store_vec<V>(row_at<R>(a.dresidual, row) + c[k], a.width - c[k], dr[k]);
+      float wpost[V], scale[V];
+      if (!HOLD) {
+        weight(a.post_weight, k, 1.f, wpost);
+        weight(a.scale, k, 1.f, scale);
+      }
 #pragma unroll
       for (int i = 0; i < V; i++) {
-        dw[1][k][i] = fmaf(dr[k][i], vn[k][i] * wpost[k][i], dw[1][k][i]);
-        dr[k][i] *= scale[k][i];                    // dp
+        const float post = HOLD ? held[0][i] : wpost[i];
+        dw[1][k][i] = fmaf(dr[k][i], vn[k][i] * post, dw[1][k][i]);
+        dr[k][i] *= HOLD ? held[1][i] : scale[i];      // dp
         dw[2][k][i] = fmaf(dr[k][i], vn[k][i], dw[2][k][i]);
-        dr[k][i] *= wpost[k][i];
-        dot = fmaf(dr[k][i], vn[k][i], dot);
+        dr[k][i] *= post;
+        dot[0] = fmaf(dr[k][i], vn[k][i], dot[0]);
       }
     }
     if (a.block.data) {
-      const float m = a.post_weight ? row_sum<TPR>(dot, lds[1]) * inv : 0.f;
+      float m = 0.f;
+      if (a.post_weight) {
+        row_sums<TPR>(dot, lds[1]);
+        m = dot[0] * inv;
+      }
 #pragma unroll
       for (int k = 0; k < NV; k++) {
 #pragma unroll
@@ -231,6 +295,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
         if (on) store_vec<V>(row_at<T>(a.dblock, row) + c[k], a.width - c[k], dr[k]);
       }
     }
+    // one sum a row: its buffer is read before the next row writes it
     if (TPR > 64 && !(a.pre_weight && a.block.data && a.post_weight)) __syncthreads();
   }
   if (!p.partial) return;
@@ -269,28 +334,33 @@ __global__ __launch_bounds__(256) void k_norm_weight_sum(const float* in, int64_
 }
 
 // Threads of a row and loads of a thread: enough threads for one load each up to
-// 4096 channels, for two each above.
-template <class F>
+// 8192 channels (backward, where two loads' registers still fit, 4096), for two
+// each above.
+template <bool BACKWARD, class F>
 int by_width(int32_t width, F&& f) {
   using std::integral_constant;
+  if (width <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
   if (width <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   if (width <= 1024) return f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
   if (width <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   if (width <= 4096) return f(integral_constant<int, 512>{}, integral_constant<int, 1>{});
-  if (width <= 8192) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+  if (width <= 8192)
+    return f(integral_constant<int, BACKWARD ? 512 : 1024>{},
+             integral_constant<int, BACKWARD ? 2 : 1>{});
   return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
-int threads_per_row(int32_t width) {
-  return by_width(width, [](auto tpr, auto) { return int(tpr()); });
+int threads_per_row(int32_t width, bool backward) {
+  const auto threads = [](auto tpr, auto) { return int(tpr()); };
+  return backward ? by_width<true>(width, threads) : by_width<false>(width, threads);
 }
 
 // Workgroups: enough threads to fill the chip, then each walks over rows.
 // Backward each leaves a row of partial sums, so beyond one a compute unit
 // there are four rows of work for each.
 int64_t norm_blocks(const rc_norm_args& a, bool backward) {
-  const int tpr = threads_per_row(a.width), wg = threads_of(tpr);
+  const int tpr = threads_per_row(a.width, backward), wg = threads_of(tpr);
   const int64_t need = cdiv(a.rows, wg / tpr), cus = rcdp::num_cus();
-  const int64_t most = cus * (backward ? 512 : 2048) / wg;
+  const int64_t most = cus * (backward ? (wg < 512 ? 512 / wg : 1) : 2048 / wg);
   if (need <= cus) return need;
   const int64_t some = backward ? (need / 4 < cus ? cus : need / 4) : need;
   return some < most ? some : most;
@@ -334,7 +404,7 @@ extern "C" int rc_norm_forward(const rc_norm_args* args, void* stream) {
   const rc_norm_args& a = *args;
   if (a.rows == 0 || a.width == 0) return RC_OK;
   return by_dtypes(a, [&](auto t, auto r) {
-    return by_width(a.width, [&](auto tpr, auto nv) {
+    return by_width<false>(a.width, [&](auto tpr, auto nv) {
       k_norm_forward<decltype(t), decltype(r), tpr(), nv()>
           <<<dim3((uint32_t)norm_blocks(a, false)), threads_of(tpr()), 0, (hipStream_t)stream>>>(
               {a, nullptr});
@@ -362,7 +432,7 @@ extern "C" int rc_norm_backward(const rc_norm_args* args, void* stream) {
   return by_dtypes(a, [&](auto t, auto r) -> int {
     using T = decltype(t);
     if (blocks > 0) {
-      const int st = by_width(a.width, [&](auto tpr, auto nv) {
+      const int st = by_width<true>(a.width, [&](auto tpr, auto nv) {
         k_norm_backward<T, decltype(r), tpr(), nv()>
             <<<dim3((uint32_t)blocks), threads_of(tpr()), 0, (hipStream_t)stream>>>({a, partial});
         return launched("k_norm_backward");
