@@ -177,7 +177,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
 }
 
 // Backward.  (Above 8192 channels a row and its sums spill: 16384 channels run at a
-// sixth of the rate of 4096.)
+// fifth of the rate of 4096.)
 template <class T, class R, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p) {
   constexpr int RPW = threads_of(TPR) / TPR;

@@ -87,7 +87,8 @@ inline int dtype_size(int32_t d) { return d == RC_F32 ? 4 : 2; }
 inline bool dtype_ok(int32_t d) { return d >= RC_F32 && d <= RC_F16; }
 inline bool param_ok(int32_t p, int32_t d) { return p == RC_F32 || p == d; }
 
-// The launch's own error, if any, as a status.
+// The launch's own error, if any, as a status (by_dtype, before the first launch of a
+// call, drops what another library's calls left).
 inline int launched(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return RC_OK;
@@ -98,6 +99,7 @@ inline int launched(const char* what) {
 // Calls f(T{}) with the element type of a (checked) dtype.
 template <class F>
 inline int by_dtype(int32_t d, F&& f) {
+  (void)hipGetLastError();
   if (d == RC_F32) return f(float{});
   if (d == RC_BF16) return f(bf16{});
   return f(f16{});

@@ -519,8 +519,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
         if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, zero);
       }
     const int64_t cell = ((w.blk * (int64_t)a.batch + w.b) * a.length) * a.groups + w.g;
-    for (int e = threadIdx.x; e < max(0, t_last - live) * 2 * N; e += THREADS)
-      p.part_bc[(cell + (int64_t)(live + e / (2 * N)) * a.groups) * (2 * N) + e % (2 * N)] = 0.f;
+    for (int t = live + threadIdx.x / (2 * N); t < t_last; t += THREADS / (2 * N))
+      p.part_bc[(cell + (int64_t)t * a.groups) * (2 * N) + threadIdx.x % (2 * N)] = 0.f;
   }
   // from the last live tile back; the first one is fetched twice
   const int t_top = max(live - TILE, t_first);

@@ -99,6 +99,8 @@ CONV = [  # dtype, batch, length, width, taps, state, bias, activation, lengths,
     ("f32", 1, 33, 16, 6, True, True, "silu", None, "f32"),
     ("f16", 2, 31, 20, 7, True, False, "silu", (31, 5), "f32"),
     ("bf16", 2, 2100, 16, 4, False, True, "silu", (2100, 1999), "f32"),
+    ("f32", 3, 300, 36, 4, True, True, "silu", (300, 33, 100), "f32"),
+    ("f16", 2, 260, 12, 8, True, True, "silu", (260, 7), "f16"),
 ]
 
 
@@ -172,6 +174,41 @@ def test_conv_empty():
         assert dx.shape == x.shape and not dw.any()
 
 
+def test_conv_state_of_short_sequences():
+    """Sequences shorter than the state, down to none: the state moves on by
+    their tokens, and its gradient goes back through it."""
+    x = Inputs(9, torch.float32)
+    x.add("x", 4, 2, 8)
+    x.add("weight", 8, 5)
+    x.add("state", 4, 4, 8)
+    x.grads()
+    n = torch.tensor([0, 1, 2, 2], dtype=torch.int32, device=DEV)
+    outs = ops.causal_conv(x.gpu["x"], x.gpu["weight"], state=x.gpu["state"], lengths=n, return_state=True)
+    wants = ref.causal_conv(x.cpu["x"], x.cpu["weight"], None, x.cpu["state"], [0, 1, 2, 2])
+    for o, w in zip(outs, wants):
+        check(o, w, "output")
+    compare_grads(x, outs, wants)
+    empty = torch.zeros(4, 0, 8, device=DEV)
+    s = x.gpu["state"]
+    _, out = ops.causal_conv(empty, x.gpu["weight"], state=s, return_state=True)
+    assert torch.equal(out, s)
+    g, = torch.autograd.grad(out, s, torch.ones_like(out))
+    assert torch.equal(g, torch.ones_like(g))
+
+
+def test_lengths_outside_the_batch():
+    """Lengths are clamped to [0, length]."""
+    x = torch.randn(3, 20, 16, device=DEV)
+    w, A = torch.randn(16, 4, device=DEV), -torch.rand(16, 4, device=DEV)
+    bc = torch.randn(3, 20, 4, device=DEV)
+    odd = torch.tensor([-5, 1000, 20], dtype=torch.int32, device=DEV)
+    fair = torch.tensor([0, 20, 20], dtype=torch.int32, device=DEV)
+    for f in (lambda n: ops.causal_conv(x, w, lengths=n, return_state=True),
+              lambda n: ops.selective_scan(x, x, A, bc, bc, softplus=True, lengths=n, return_state=True)):
+        for a, b in zip(f(odd), f(fair)):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype,batch,width,taps", [
     ("f32", 3, 10, 4), ("bf16", 5, 257, 4), ("f16", 1, 1, 2), ("bf16", 2, 64, 8), ("f32", 2, 6, 1)])
 def test_conv_step(dtype, batch, width, taps):
@@ -215,6 +252,15 @@ SCAN = [  # dtype, batch, length, width, states, groups, parts, lengths
     ("f32", 1, 300, 5, 16, 1, "Dzbs", None),
     ("f32", 2, 600, 66, 16, 1, "Dzbs", (600, 333)),
     ("bf16", 1, 1030, 130, 4, 2, "Dzbs", None),
+    # several chunks of the length, sequences that end inside, at and before one; every
+    # number of states that changes the lanes; enough channels for one chunk
+    ("f32", 3, 900, 68, 16, 1, "Dzbs", (900, 448, 130)),
+    ("f16", 2, 500, 36, 40, 1, "Dzb", (500, 64)),
+    ("bf16", 2, 400, 40, 24, 2, "Dzbs", (399, 0)),
+    ("f32", 1, 260, 12, 2, 3, "zbs", (257,)),
+    ("f32", 1, 210, 130, 7, 1, "Dzbs", None),
+    ("bf16", 64, 33, 1024, 4, 1, "Dzb", None),
+    ("bf16", 130, 20, 64, 64, 1, "Dz", None),
 ]
 
 
@@ -410,6 +456,11 @@ NORM = [  # dtype, residual, rows, width, parts, gate activation, param
     ("f32", "f32", 4, 300, "b", "silu", "f32"),
     ("bf16", "f32", 3001, 40, "bgpsn", "silu", "f32"),
     ("f16", "f16", 1400, 1030, "bpsn", "silu", "f32"),
+    ("bf16", "f32", 40, 200, "bgpsn", "sigmoid", "f32"),
+    ("bf16", "bf16", 300, 256, "bgpsn", "silu", "bf16"),
+    ("bf16", "f32", 5, 5000, "bgpsn", "silu", "f32"),
+    ("f32", "f32", 300, 8192, "bgpsn", "silu", "f32"),
+    ("bf16", "f32", 3, 12345, "bgpsn", "silu", "f32"),
 ]
 
 
