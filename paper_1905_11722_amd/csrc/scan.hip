@@ -156,6 +156,14 @@ __device__ __forceinline__ float delta_of(float raw, bool soft) {
   return soft ? s : raw;
 }
 
+// First channel (of the group) of a block: blocks of equal sizes but for one
+// channel, or for four where four divide the group, so that no block has less than a
+// load.
+__device__ __forceinline__ int block_start(const ScanParams& p, int blk) {
+  const int unit = p.group_width % 4 ? 1 : 4;
+  return (int)((int64_t)blk * (p.group_width / unit) / p.blocks) * unit;
+}
+
 // What a workgroup works on.  Workgroup i runs on XCD i % 8: neighbours in
 // (batch, group, chunk, block) go to one XCD, whose L2 then holds the B and C that they share.
 template <int Q, int S>
@@ -163,6 +171,7 @@ struct Place {
   static constexpr int N = Q * S, CW = channels_of(Q);
   int64_t b, g;
   int blk, piece;                   // block of channels, chunk
+  int base, have;                   // the block's first channel (of the group) and channels
   int q, ch;                        // the lane's states and channel (in the block)
   int64_t d;                        // its channel, clamped to the group
   bool on;
@@ -177,8 +186,10 @@ struct Place {
     b = i / (uint32_t)p.a.groups;
     q = threadIdx.x % Q;
     ch = threadIdx.x / Q;
-    on = blk * CW + ch < p.group_width;
-    d = g * p.group_width + min(blk * CW + ch, p.group_width - 1);
+    base = block_start(p, blk);
+    have = block_start(p, blk + 1) - base;
+    on = ch < have;
+    d = g * p.group_width + base + min(ch, have - 1);
   }
   // The lane's S values of an array [.][width][states] (0 for missing states).
   __device__ void load(const float* x, int64_t before, const ScanParams& p, float (&v)[S]) const {
@@ -198,7 +209,11 @@ struct Place {
   }
 };
 
-// A thread's share of a tile: NV vectors of VEC channels of one column.
+// A thread's share of a tile: NV vectors of VEC channels of one column.  Where VEC
+// does not divide the block's channels, the last column moves back by the
+// difference: its first elements are its neighbour's too, whose thread is a
+// lane of the same wave, reads and writes the same values in the same order,
+// and sums them once (see `put`).
 template <class T, int Q, int VEC, int TILE>
 struct Tile {
   static constexpr int CW = channels_of(Q);
@@ -209,16 +224,30 @@ struct Tile {
   typedef T Raw __attribute__((ext_vector_type(VEC)));
   int64_t d;                        // first channel of the column, clamped
   int c, r;                         // its place in the block, first row
+  int over;                         // elements past the block's last channel, to be zeros
   // Every thread has a row of its own in a tile (else: `lead`).
   static constexpr bool all = threads / columns <= TILE;
   bool lead;
   bool on;                          // and its channel exists
-  __device__ Tile(const ScanParams& p, int64_t g, int blk) {
+  template <class P>
+  __device__ Tile(const ScanParams& p, const P& place) {
+    const int have = place.have;
     c = threadIdx.x % columns * VEC;
     lead = all || threadIdx.x / columns < rows;
     r = min((int)threadIdx.x / columns, rows - 1);
-    on = lead && blk * CW + c < p.group_width;
-    d = g * p.group_width + min(blk * CW + c, p.group_width - VEC);
+    on = lead && c < have;
+    over = on ? max(0, c + VEC - have) : 0;
+    c -= over;
+    d = place.g * p.group_width + place.base + min(c, have - VEC);
+  }
+  // Row r of the column to LDS.
+  template <class E, int ROW>
+  __device__ void put(E* lds, int row, const E (&x)[VEC]) const {
+    if (!all && !lead) return;
+#pragma unroll
+    for (int i = 0; i < VEC; i++) lds[row * ROW + c + i] = x[i];
+    if (VEC > 1)
+      for (int i = 0; i < over; i++) lds[row * ROW + c + VEC + i] = E{};
   }
   // The thread's place in row `t` + its first row.
   __device__ T* start(const rc_view& v, int64_t b, int t) const {
@@ -328,7 +357,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
   __shared__ __align__(16) float lds_b[TILE * N], lds_c[ENDS ? 4 : TILE * N];
   const rc_scan_args& a = p.a;
   const Place<Q, S> w(p);
-  const Tile<T, Q, VEC, TILE> tile(p, w.g, w.blk);
+  const Tile<T, Q, VEC, TILE> tile(p, w);
   using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
   const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
@@ -391,10 +420,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
         const float du = delta * (float)u[k][i];
         d[i] = {ok ? delta : 0.f, ok ? du : 0.f};
       }
-      if (TileT::all || tile.lead) {
-#pragma unroll
-        for (int i = 0; i < VEC; i++) lds_d[r * ROW + tile.c + i] = d[i];
-      }
+      tile.template put<float2, ROW>(lds_d, r, d);
     }
     B.put(lds_b, t0, end, a.states);
     if (!ENDS) C.put(lds_c, t0, end, a.states);
@@ -450,7 +476,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
         if (t < t_last) store_vec<VEC>(at_y + k * TileT::rows * a.y.time, VEC, y);
       }
     }
-    // a thread stages the elements whose outputs it has just read
+    // a wave stages the elements whose outputs it has just read
   }
   if (ENDS) {
     total += dpp<kXor1>(total);
@@ -482,7 +508,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   __shared__ float lds_bc[ENDS ? 1 : WAVES * TILE * 2 * N];
   const rc_scan_args& a = p.a;
   const Place<Q, S> w(p);
-  const Tile<T, Q, VEC, TILE> tile(p, w.g, w.blk);
+  const Tile<T, Q, VEC, TILE> tile(p, w);
   using TileT = Tile<T, Q, VEC, TILE>;
   const int end = seq_end(a.lengths, w.b, a.length);
   const int t_first = w.piece * p.chunk, t_last = min(t_first + p.chunk, a.length);
@@ -513,7 +539,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   if (!ENDS) {
     const float zero[VEC] = {};
     for (int t = live + threadIdx.x / TileT::columns; t < t_last; t += THREADS / TileT::columns)
-      if (w.blk * CW + tile.c < p.group_width) {
+      if (tile.on || tile.c < w.have) {
         store_vec<VEC>(row_out<T>(a.du, w.b, t) + tile.d, VEC, zero);
         store_vec<VEC>(row_out<T>(a.ddt, w.b, t) + tile.d, VEC, zero);
         if (a.z.data) store_vec<VEC>(row_out<T>(a.dz, w.b, t) + tile.d, VEC, zero);
@@ -565,10 +591,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
         step[k][i] = ok ? delta : 0.f;
         d[i] = {step[k][i], ok ? du : 0.f, ok ? dy : 0.f, 0.f};
       }
-      if (TileT::all || tile.lead) {
-#pragma unroll
-        for (int i = 0; i < VEC; i++) lds_d[r * ROW + tile.c + i] = d[i];
-      }
+      tile.template put<float4, ROW>(lds_d, r, d);
     }
     C.put(lds_c, t0, end, a.states);
     if (!ENDS) B.put(lds_b, t0, end, a.states);
@@ -732,10 +755,10 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   }
   __syncthreads();
   for (int e = threadIdx.x; e < 2 * CW; e += THREADS) {
-    if (w.blk * CW + e / 2 >= p.group_width) continue;
+    if (e / 2 >= w.have) continue;
     float s = 0.f;
     for (int r = 0; r < TileT::rows; r++) s += sums[r * 2 * CW + e];
-    p.part_d[(before * a.width + w.g * p.group_width + w.blk * CW + e / 2) * 2 + e % 2] = s;
+    p.part_d[(before * a.width + w.g * p.group_width + w.base + e / 2) * 2 + e % 2] = s;
   }
 }
 
@@ -885,7 +908,7 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.group_width = a.width / a.groups;
   p.S = a.states > 8 ? 4 : a.states > 4 ? 2 : 1;
   p.Q = a.states > 32 ? 16 : a.states > 16 ? 8 : 4;
-  p.VEC = p.group_width % 4 ? 1 : 4;
+  p.VEC = p.group_width < 4 ? 1 : 4;                   // channels of a load
   p.blocks = cdiv(p.group_width, channels_of(p.Q));
   const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
   const int64_t cus = rcdp::num_cus(), enough = (backward ? 8 : 4) * cus;

@@ -261,6 +261,13 @@ SCAN = [  # dtype, batch, length, width, states, groups, parts, lengths
     ("f32", 1, 210, 130, 7, 1, "Dzbs", None),
     ("bf16", 64, 33, 1024, 4, 1, "Dzb", None),
     ("bf16", 130, 20, 64, 64, 1, "Dz", None),
+    # a last load of channels that moves back by one to three, each number of lanes
+    ("f32", 2, 120, 71, 16, 1, "Dzbs", (120, 41)),
+    ("bf16", 2, 75, 133, 10, 1, "Dzbs", (75, 0)),
+    ("f16", 1, 50, 90, 16, 2, "Dzbs", None),
+    ("f32", 2, 40, 78, 24, 1, "Dzbs", (40, 5)),
+    ("bf16", 1, 70, 37, 40, 1, "Dzbs", (69,)),
+    ("f32", 1, 40, 7, 3, 1, "Dzbs", None),
 ]
 
 
