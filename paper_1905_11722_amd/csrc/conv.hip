@@ -4,9 +4,12 @@
 //
 // Each value is used K times and each output needs ~2K + 6 operations for 4
 // bytes moved (16-bit types), so the bound is memory.  A thread owns V
-// neighbouring channels (one wide load per row; V = 1 where 8 does not
-// divide the width) and a run of rows, and keeps the last K - 1 rows in
-// registers: x is read once plus K - 1 rows per run.
+// neighbouring channels (one wide load per row) and a run of rows, and keeps
+// the last K - 1 rows in registers: x is read once plus K - 1 rows per run.
+// Where V does not divide the width, the last thread of a row moves back to
+// the last V channels; it and its neighbour store the same values where they
+// overlap.  (Odd widths with V = 1 instead: 8 x 2047 x 2049 in bfloat16
+// forward 46, backward 87 us; this way 35 and 66.)
 //
 // Backward: dp_t = dy_t act'(p_t) (p_t again from x), dx_t = sum_k w_k
 // dp_{t+K-1-k}, dw_k = sum_t dp_t x_{t-(K-1)+k}, dbias = sum_t dp_t.  The same walk,
@@ -105,6 +108,10 @@ __device__ __forceinline__ void load_weights(const rc_conv_args& a, int c,
     read(T{});
 }
 
+// Forward: V = 8, kRows rows of loads in flight ahead of their use, no LDS.
+// At 2 x 4096 x 4096, K = 4 in bfloat16 (134 MB): 29.5 us, 4.6 TB/s, a large copy's rate;
+// 8 taps at 8 x 2048 x 2048 44 us (3.0 TB/s), 4 taps 37: the multiply-adds
+// show.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
   const rc_conv_args& a = p.a;
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
   const int64_t cell = gt * (kThreads / p.lanes) + slot;          // (batch, run)
   const int64_t c64 = (gc * p.lanes + lane) * V;
   if (c64 >= a.width || cell >= (int64_t)a.batch * p.runs) return;
-  const int c = (int)c64;
+  const int c = min((int)c64, a.width - V);
   const int b = (int)(cell / p.runs), t0 = (int)(cell % p.runs) * p.run;
   const int t1 = min(t0 + p.run, a.length), end = seq_end(a.lengths, b, a.length);
   if (t0 == 0 && a.state_out.data) {
@@ -166,8 +173,16 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
   }
 }
 
+// Backward: V = 4, since a thread holds K rows of x, of dp and the weights'
+// gradients of its channels.  Four waves a SIMD where that leaves registers enough
+// (16-bit types up to 4 taps): 8 x 2047 x 2048 in bfloat16 (201 MB) 58 us by the compiler's
+// choice, 52 so, 3.8 TB/s; above it spills, and two are asked for.
+template <class T>
+constexpr int conv_waves(int taps) {
+  return taps <= 4 && sizeof(T) == 2 ? 4 : 2;
+}
 template <class T, int K, int V>
-__global__ __launch_bounds__(kThreads, K <= 4 && sizeof(T) == 2 ? 4 : 2) void k_conv_backward(ConvParams<T> p) {
+__global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(ConvParams<T> p) {
   __shared__ float lds[kThreads * V];
   const rc_conv_args& a = p.a;
   const int lane = threadIdx.x % p.lanes, slot = threadIdx.x / p.lanes;
@@ -175,92 +190,95 @@ __global__ __launch_bounds__(kThreads, K <= 4 && sizeof(T) == 2 ? 4 : 2) void k_
   const int64_t gc = blockIdx.x % p.groups_c, gt = blockIdx.x / p.groups_c;
   const int64_t cell = gt * slots + slot;
   const int64_t c64 = (gc * p.lanes + lane) * V;
+  // channels that the load moves back by
+  const int over = (int)(c64 < a.width ? max((int64_t)0, c64 + V - a.width) : 0);
   float dw[K + 1][V];                                  // the last one: bias
 #pragma unroll
   for (int k = 0; k <= K; k++)
 #pragma unroll
     for (int i = 0; i < V; i++) dw[k][i] = 0.f;
   if (c64 < a.width && cell < (int64_t)a.batch * p.runs) {
-    const int c = (int)c64;
+    const int c = min((int)c64, a.width - V);
     const int b = (int)(cell / p.runs), t0 = (int)(cell % p.runs) * p.run;
     const int t1 = min(t0 + p.run, a.length), end = seq_end(a.lengths, b, a.length);
     if (t0 > 0 && t0 >= end) {                         // past the end: zeros, no gradients
       const float zero[V] = {};
       for (int t = t0; t < t1; t++) store_vec<V>(at<T>(a.dx, b, t, c), V, zero);
     } else {
-    // row t finishes dx of row t - (K - 1); the first run also writes the
-    // state's rows -(K - 1) .. -1
-    const int first = t0 == 0 && a.dstate_in.data ? -(K - 1) : t0;
-    float w[K][V], bias[V], x[K][V], dp[K][V];         // dp[j]: of row t - (K - 1) + j
-    load_weights<T, K, V>(a, c, w, bias);
+      // row t finishes dx of row t - (K - 1); the first run also writes the
+      // state's rows -(K - 1) .. -1
+      const int first = t0 == 0 && a.dstate_in.data ? -(K - 1) : t0;
+      float w[K][V], bias[V], x[K][V], dp[K][V];       // dp[j]: of row t - (K - 1) + j
+      load_weights<T, K, V>(a, c, w, bias);
 #pragma unroll
-    for (int k = 0; k < K; k++)
+      for (int k = 0; k < K; k++)
 #pragma unroll
-      for (int i = 0; i < V; i++) dp[k][i] = x[k][i] = 0.f;
-    if (end > 0) {
+        for (int i = 0; i < V; i++) dp[k][i] = x[k][i] = 0.f;
+      if (end > 0) {
 #pragma unroll
-      for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
-    }
-    const bool any = end > 0;
-    Rows<T, V> now, next, dnow, dnext;
-    if (any) {
-      now.load(a.x, b, t0, end, c);
-      dnow.load(a.dy, b, t0, end, c);
-    }
-    for (int g = t0; g < t1 + K - 1; g += kRows) {
-      if (any) {
-        next.load(a.x, b, g + kRows, end, c);
-        dnext.load(a.dy, b, g + kRows, end, c);
+        for (int k = 0; k < K - 1; k++)
+          input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
       }
-#pragma unroll
-      for (int r = 0; r < kRows; r++) {
-        const int t = g + r;
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-#pragma unroll
-          for (int k = 0; k < K - 1; k++) {
-            x[k][i] = x[k + 1][i];
-            dp[k][i] = dp[k + 1][i];
-          }
-          x[K - 1][i] = t < end ? (float)now.x[r][i] : 0.f;
-          dp[K - 1][i] = t < end ? (float)dnow.x[r][i] : 0.f;
-          if (a.activation == RC_ACT_SILU) {
-            float q = bias[i];
-#pragma unroll
-            for (int k = 0; k < K; k++) q = fmaf(w[k][i], x[k][i], q);
-            const float s = sigmoid(q);
-            dp[K - 1][i] *= s * (1.f + q * (1.f - s));
-          }
-          const float own = t < t1 ? dp[K - 1][i] : 0.f;
-#pragma unroll
-          for (int k = 0; k < K; k++) dw[k][i] = fmaf(own, x[k][i], dw[k][i]);
-          dw[K][i] += own;
+      const bool any = end > 0;
+      Rows<T, V> now, next, dnow, dnext;
+      if (any) {
+        now.load(a.x, b, t0, end, c);
+        dnow.load(a.dy, b, t0, end, c);
+      }
+      for (int g = t0; g < t1 + K - 1; g += kRows) {
+        if (any) {
+          next.load(a.x, b, g + kRows, end, c);
+          dnext.load(a.dy, b, g + kRows, end, c);
         }
-        const int s = t - (K - 1);                     // the row whose dx is complete
-        if (s >= first && s < t1) {
-          float dx[V];
+#pragma unroll
+        for (int r = 0; r < kRows; r++) {
+          const int t = g + r;
 #pragma unroll
           for (int i = 0; i < V; i++) {
-            dx[i] = 0.f;
 #pragma unroll
-            for (int k = 0; k < K; k++) dx[i] = fmaf(w[k][i], dp[K - 1 - k][i], dx[i]);
-          }
-          const int j = s - (end - (K - 1));           // its row in the final state
-          if (a.dstate_out.data && j >= 0 && j < K - 1) {
-            float ds[V];
-            load_vec<V>(at<T>(a.dstate_out, b, j, c), V, ds);
+            for (int k = 0; k < K - 1; k++) {
+              x[k][i] = x[k + 1][i];
+              dp[k][i] = dp[k + 1][i];
+            }
+            x[K - 1][i] = t < end ? (float)now.x[r][i] : 0.f;
+            dp[K - 1][i] = t < end ? (float)dnow.x[r][i] : 0.f;
+            if (a.activation == RC_ACT_SILU) {
+              float q = bias[i];
 #pragma unroll
-            for (int i = 0; i < V; i++) dx[i] += ds[i];
+              for (int k = 0; k < K; k++) q = fmaf(w[k][i], x[k][i], q);
+              const float s = sigmoid(q);
+              dp[K - 1][i] *= s * (1.f + q * (1.f - s));
+            }
+            const float own = t < t1 ? dp[K - 1][i] : 0.f;
+#pragma unroll
+            for (int k = 0; k < K; k++) dw[k][i] = fmaf(own, x[k][i], dw[k][i]);
+            dw[K][i] += own;
           }
-          if (s >= 0)
-            store_vec<V>(at<T>(a.dx, b, s, c), V, dx);
-          else
-            store_vec<V>(at<T>(a.dstate_in, b, s + K - 1, c), V, dx);
+          const int s = t - (K - 1);                     // the row whose dx is complete
+          if (s >= first && s < t1) {
+            float dx[V];
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+              dx[i] = 0.f;
+#pragma unroll
+              for (int k = 0; k < K; k++) dx[i] = fmaf(w[k][i], dp[K - 1 - k][i], dx[i]);
+            }
+            const int j = s - (end - (K - 1));           // its row in the final state
+            if (a.dstate_out.data && j >= 0 && j < K - 1) {
+              float ds[V];
+              load_vec<V>(at<T>(a.dstate_out, b, j, c), V, ds);
+#pragma unroll
+              for (int i = 0; i < V; i++) dx[i] += ds[i];
+            }
+            if (s >= 0)
+              store_vec<V>(at<T>(a.dx, b, s, c), V, dx);
+            else
+              store_vec<V>(at<T>(a.dstate_in, b, s + K - 1, c), V, dx);
+          }
         }
+        now = next;
+        dnow = dnext;
       }
-      now = next;
-      dnow = dnext;
-    }
     }
   }
   if (!p.partial) return;
@@ -268,7 +286,8 @@ __global__ __launch_bounds__(kThreads, K <= 4 && sizeof(T) == 2 ? 4 : 2) void k_
   for (int k = 0; k <= K; k++) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; i++) lds[threadIdx.x * V + i] = dw[k][i];
+    for (int i = 0; i < V; i++)                        // a moved load's own channels only
+      if (i >= over) lds[threadIdx.x * V + i - over] = dw[k][i];
     __syncthreads();
     for (int o = threadIdx.x; o < p.lanes * V; o += kThreads) {
       const int64_t ch = gc * p.lanes * V + o;
@@ -296,6 +315,9 @@ __global__ __launch_bounds__(256) void k_conv_weight_sum(const float* in, int64_
   }
 }
 
+// One token: y from the slot's K - 1 rows and x, the rows move up by one.  V = 2 channels
+// a thread, or 1: many small threads, since a row of channels is all the work
+// there is.  Bound by the launch: 48 rows of 2048 channels (1 MB) 5 us a call.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kThreads) void k_conv_step(rc_conv_step_args a, int32_t vecs) {
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -351,19 +373,22 @@ bool conv_sizes_ok(int32_t dtype, int32_t param, int32_t act, int32_t batch, int
 }
 
 // The launch shape: lanes along the channels, rows of a thread, workgroups.
+// Long runs read fewer rows twice and leave fewer partial sums, short ones fill the
+// chip: 32 rows, halved while that gives fewer than four workgroups a compute unit.
 struct ConvPlan {
   int V, lanes, run;
   int64_t runs, groups_c, groups_t;
 };
 ConvPlan conv_plan(const rc_conv_args& a, bool backward) {
   ConvPlan p;
-  p.V = backward ? (a.width % 4 ? 1 : 4) : a.width % 8 ? 1 : 8;
+  p.V = backward ? (a.width < 4 ? 1 : 4) : a.width < 8 ? 1 : 8;
   const int64_t vecs = cdiv(a.width, p.V);
   p.lanes = lanes_for(vecs);
   p.groups_c = cdiv(vecs, p.lanes);
   const int slots = kThreads / p.lanes;
+  const int64_t cus4 = 4 * (int64_t)rcdp::num_cus();
   p.run = 32;
-  while (p.run > 4 && p.groups_c * cdiv((int64_t)a.batch * cdiv(a.length, p.run), slots) < 1024)
+  while (p.run > 4 && p.groups_c * cdiv((int64_t)a.batch * cdiv(a.length, p.run), slots) < cus4)
     p.run /= 2;
   p.runs = a.length > 0 ? cdiv(a.length, p.run) : 1;
   p.groups_t = cdiv((int64_t)a.batch * p.runs, slots);

@@ -114,7 +114,7 @@ constexpr int32_t kMaxExtent = 1 << 30;
 // thread.  256 threads take 16 columns, sixteen slices of the parts each,
 // eight loads in flight; always the same slices in the same order.  The
 // threads of slice 0 return the sums.  (512 parts of 12288 columns: 64 columns a
-// workgroup with one load in flight took 18 us, this one 7.)
+// workgroup with one load in flight took 18 us, this way 6.)
 constexpr int kSumCols = 16;
 __device__ __forceinline__ float column_sum(const float* in, int64_t parts, int64_t cols,
                                             int64_t c, float* lds /* [256] */) {

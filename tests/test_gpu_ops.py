@@ -101,6 +101,13 @@ CONV = [  # dtype, batch, length, width, taps, state, bias, activation, lengths,
     ("bf16", 2, 2100, 16, 4, False, True, "silu", (2100, 1999), "f32"),
     ("f32", 3, 300, 36, 4, True, True, "silu", (300, 33, 100), "f32"),
     ("f16", 2, 260, 12, 8, True, True, "silu", (260, 7), "f16"),
+    # the last load of a row moves back by one to seven channels
+    ("bf16", 2, 35, 1031, 4, True, True, "silu", (35, 17), "f32"),
+    ("f32", 2, 66, 521, 4, True, True, "silu", (66, 1), "f32"),
+    ("f16", 1, 50, 9, 3, True, True, "silu", None, "f16"),
+    ("bf16", 2, 40, 15, 4, True, True, None, None, "bf16"),
+    ("bf16", 1, 40, 6, 2, True, True, "silu", None, "f32"),
+    ("f32", 1, 12, 3, 4, True, True, "silu", (11,), "f32"),
 ]
 
 
