@@ -889,15 +889,18 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 
 // How a scan is cut up.  A channel takes a quad of lanes (more above 16
 // states).  The kernels are bound by instruction issue, which wants waves on
-// every SIMD: where batch and channels give too few, the length is cut into
-// chunks, which costs a pass over all but one of them for their end states.
-// us for bfloat16 and 16 states by waves a compute unit without and with
-// chunks, to 16 waves: 2048 tokens and channels, batch 4 (2 waves) forward 190 /
-// 132, batch 8 (4 waves) forward 231 / 230, backward 654 / 573, batch 12 (6
-// waves) forward 327 / 379, backward 944 / 870.  Chunks have 64 tokens at least
-// (32: 2048 tokens of 1024 channels forward 40 for 37) and number 128 at most,
-// whose joining is a loop (16384 tokens of 64 channels forward and backward, 32
-// chunks 324, 128 chunks 117).
+// every SIMD, and evenly: where batch and channels give few, or just more than a
+// whole number for each, the length is cut into chunks, which costs a pass
+// over all but one of them for their end states.  bfloat16, 16 states, 2048 tokens and
+// channels (a batch of 8 is one wave a SIMD), whole or best cut, us:
+//   batch     2        4        6        8       10       12       16       20
+//   forward  229/75   225/131  226/185  228/233  335/289  335/340  338/409  458/520
+//   backward 655/175  658/317  664/460  672/590  957/729  964/865  977/1110 1482/1390
+// With v waves a SIMD on average and k on the fullest, a whole pass costs 95 + 130 k
+// forward, a cut one 1.7 times 130 v; backward 490 k (one wave: 665) and 1.18 times 490 v.
+bool scan_cut(double v, double k, bool backward) {
+  return backward ? k == 1. || 1.18 * v < k : 1.7 * v < .5 + k;
+}
 struct ScanPlan {
   int S, Q, VEC;
   int64_t group_width, blocks;
@@ -910,11 +913,27 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.Q = a.states > 32 ? 16 : a.states > 16 ? 8 : 4;
   p.VEC = p.group_width < 4 ? 1 : 4;                   // channels of a load
   p.blocks = cdiv(p.group_width, channels_of(p.Q));
-  const int64_t waves = (int64_t)a.batch * a.groups * p.blocks * channels_of(p.Q) * p.Q / 64;
-  const int64_t cus = rcdp::num_cus(), enough = (backward ? 8 : 4) * cus;
+  // Chunks: sixteen waves a compute unit at least, up to twice as many where
+  // that spreads them more evenly (batch 12 above: 3 chunks 4.5 workgroups a compute unit, 959 us;
+  // 4 chunks 6 workgroups, 865).  They have 64 tokens at least (32: 2048 tokens of 1024
+  // channels forward 40 for 37) and number 128 at most, whose joining is a
+  // loop (16384 tokens of 64 channels forward and backward, 32 chunks 324, 128 chunks 117).
+  const int64_t groups = (int64_t)a.batch * a.groups * p.blocks, cus = rcdp::num_cus();
+  const int64_t group_waves = channels_of(p.Q) * p.Q / 64;
   const int64_t most = cdiv(a.length, 64) < 128 ? cdiv(a.length, 64) : 128;
-  p.chunks = waves > 0 && waves < enough ? cdiv(16 * cus, waves) : 1;
-  if (p.chunks > most) p.chunks = most;
+  p.chunks = 1;
+  if (groups > 0 && scan_cut((double)(groups * group_waves) / (4 * cus),
+                             (double)(cdiv(groups, cus) * group_waves / 4), backward)) {
+    const int64_t least = cdiv(16 * cus, groups * group_waves);
+    double best = 0.;
+    for (int64_t n = least; n <= 2 * least && n <= most; n++) {
+      const double even = (double)(groups * n) / cdiv(groups * n, cus);
+      if (even <= best) continue;
+      best = even;
+      p.chunks = n;
+    }
+    if (least > most) p.chunks = most;
+  }
   if (p.chunks < 1) p.chunks = 1;
   p.chunk = cdiv(cdiv(a.length, p.chunks), kFwdTile) * kFwdTile;
   if (p.chunk < kFwdTile) p.chunk = kFwdTile;
