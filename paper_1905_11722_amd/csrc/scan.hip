@@ -495,7 +495,9 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
 // kept one, with the decays, into registers, and walk back over them.  The
 // sums over a channel's states take the staged inputs' places in LDS (a
 // channel is read and written by one wave), where the staging threads pick
-// them up for du, ddt and dz.  ENDS: only the gradient of the state before the chunk,
+// them up for du, ddt and dz.  With four states a lane the decays are computed again on the
+// way back, since keeping them spills; with fewer they stay (8 x 1024 x 2048 with
+// 8 states 232 -> 221 us).  ENDS: only the gradient of the state before the chunk,
 // from nothing after it, and its sum of delta.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanParams p) {
@@ -654,7 +656,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
         const auto token = [&](auto J) {
           const int j = 4 * i4 + J();
           float delta = quad_lane<J()>(d[i4].x);
-          asm("" : "+v"(delta));                       // decays again, not kept: registers
+          if (S == 4) asm("" : "+v"(delta));           // decays again, not kept: registers
           const float du = quad_lane<J()>(d[i4].y), dy = quad_lane<J()>(d[i4].z);
           float b[S], c[S], *bc = v + j % STEPS * 2 * S;
           read_states<S>(lds_b + j * N + w.q * S, b);
