@@ -11,7 +11,7 @@
 // registers of its threads from the loads to the stores, so every tensor is
 // read or written once; a row needs two sums over its threads, one after the
 // other.  Workgroups walk over rows with the weights' gradients (and up to
-// 8192 channels the weights) in registers.  (Backward with four sums in one step,
+// 6144 channels the weights) in registers.  (Backward with four sums in one step,
 // the second mean being linear in the first, cancels where the gradient is
 // small: not kept.)
 #include "ops_internal.h"
@@ -20,7 +20,7 @@ using namespace rcops;
 
 namespace {
 
-constexpr int V = 8;                        // channels of a load
+constexpr int kVec = 8;                     // channels of a load
 constexpr int kMaxWidth = 16384;
 
 struct NormParams {
@@ -83,19 +83,36 @@ __device__ __forceinline__ float gate_of(float x, int32_t act, float& slope) {
   return act == RC_ACT_SILU ? x * s : s;
 }
 
-template <class T, int NV>
-__device__ __forceinline__ void load_weight(const void* w, bool f32, const int (&c)[NV], int width,
-                                            float absent, float (&x)[NV][V]) {
+// A thread's channels of a row: NV loads of V.  Where V does not divide the width, the
+// last load moves back to the last V channels: its first `over` elements are
+// its neighbour's too, are left out of the sums, and are stored twice with the same
+// value.  A load that begins past the width has nothing of its own.
+template <int TPR, int NV, int V>
+struct Columns {
+  int c[NV], over[NV];
+  __device__ Columns(int lane, int width) {
 #pragma unroll
-  for (int k = 0; k < NV; k++)
-    if (!w) {
-#pragma unroll
-      for (int i = 0; i < V; i++) x[k][i] = absent;
-    } else if (f32) {
-      load_vec<V>(static_cast<const float*>(w) + c[k], width - c[k], x[k]);
-    } else {
-      load_vec<V>(static_cast<const T*>(w) + c[k], width - c[k], x[k]);
+    for (int k = 0; k < NV; k++) {
+      const int at = (k * TPR + lane) * V;
+      c[k] = min(at, width - V);
+      over[k] = at - c[k];
     }
+  }
+  __device__ bool any(int k) const { return over[k] < V; }
+  __device__ float own(int k, int i, float x) const { return i >= over[k] ? x : 0.f; }
+};
+
+template <class T, int V>
+__device__ __forceinline__ void load_weight(const void* w, bool f32, int c, float absent,
+                                            float (&x)[V]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < V; i++) x[i] = absent;
+  } else if (f32) {
+    load_vec<V>(static_cast<const float*>(w) + c, V, x);
+  } else {
+    load_vec<V>(static_cast<const T*>(w) + c, V, x);
+  }
 }
 
 template <class T>
@@ -103,7 +120,10 @@ __device__ __forceinline__ T* row_at(const rc_view& v, int64_t row) {
   return static_cast<T*>(v.data) + row * v.batch;
 }
 
-template <class T, class R, int TPR, int NV>
+// Forward: several workgroups a compute unit, so that others' loads run while one sums.
+// 16384 rows of 4096 channels with a gate, residual in 32 bits (940 MB): 172 us, 5.5 TB/s; in 16
+// bits (671 MB) 125 us, 5.4 TB/s: a large copy's rate and more.
+template <class T, class R, int TPR, int NV, int V>
 __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) {
   __shared__ float lds[2][16];
   const rc_norm_args& a = p.a;
@@ -111,31 +131,31 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const bool f32 = a.param_dtype == RC_F32;
   const float inv = 1.f / (float)a.width;
-  int c[NV];
-#pragma unroll
-  for (int k = 0; k < NV; k++) c[k] = min((k * TPR + lane) * V, a.width);
+  const Columns<TPR, NV, V> at(lane, a.width);
   float wpost[NV][V], wpre[NV][V], scale[NV][V];
-  load_weight<T>(a.post_weight, f32, c, a.width, 1.f, wpost);
-  load_weight<T>(a.pre_weight, f32, c, a.width, 0.f, wpre);
-  load_weight<T>(a.scale, f32, c, a.width, 1.f, scale);
+#pragma unroll
+  for (int k = 0; k < NV; k++) {
+    load_weight<T>(a.post_weight, f32, at.c[k], 1.f, wpost[k]);
+    load_weight<T>(a.pre_weight, f32, at.c[k], 0.f, wpre[k]);
+    load_weight<T>(a.scale, f32, at.c[k], 1.f, scale[k]);
+  }
   for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < a.rows; r0 += (int64_t)gridDim.x * RPW) {
-    const int64_t row = r0 + group;
-    const bool on = row < a.rows;
+    const int64_t row = min(r0 + group, a.rows - 1);
+    const bool on = RPW == 1 || r0 + group < a.rows;
     float out[NV][V], v[NV][V], ss[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; k++) {
-      const int n = on ? a.width - c[k] : 0;
-      load_vec<V>(row_at<R>(a.residual, row) + c[k], n, out[k]);
+      load_vec<V>(row_at<R>(a.residual, row) + at.c[k], V, out[k]);
       if (a.block.data) {
-        load_vec<V>(row_at<T>(a.block, row) + c[k], n, v[k]);
+        load_vec<V>(row_at<T>(a.block, row) + at.c[k], V, v[k]);
         if (a.gate.data) {
           float g[V], slope;
-          load_vec<V>(row_at<T>(a.gate, row) + c[k], n, g);
+          load_vec<V>(row_at<T>(a.gate, row) + at.c[k], V, g);
 #pragma unroll
           for (int i = 0; i < V; i++) v[k][i] *= gate_of(g[i], a.gate_activation, slope);
         }
 #pragma unroll
-        for (int i = 0; i < V; i++) ss[0] = fmaf(v[k][i], v[k][i], ss[0]);
+        for (int i = 0; i < V; i++) ss[0] += at.own(k, i, v[k][i] * v[k][i]);
       }
     }
     float rv = 1.f, ro = 0.f;
@@ -149,7 +169,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
 #pragma unroll
         for (int i = 0; i < V; i++)
           out[k][i] = fmaf(scale[k][i], v[k][i] * rv * wpost[k][i], out[k][i]);
-        if (on) store_vec<V>(row_at<R>(a.out, row) + c[k], a.width - c[k], out[k]);
+        if (on && at.any(k)) store_vec<V>(row_at<R>(a.out, row) + at.c[k], V, out[k]);
       }
     }
     if (a.pre_weight) {
@@ -157,14 +177,14 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
 #pragma unroll
       for (int k = 0; k < NV; k++)
 #pragma unroll
-        for (int i = 0; i < V; i++) ss[0] = fmaf(out[k][i], out[k][i], ss[0]);
+        for (int i = 0; i < V; i++) ss[0] += at.own(k, i, out[k][i] * out[k][i]);
       row_sums<TPR>(ss, lds[1]);
       ro = __builtin_amdgcn_rsqf(fmaf(ss[0], inv, a.eps));
 #pragma unroll
       for (int k = 0; k < NV; k++) {
 #pragma unroll
         for (int i = 0; i < V; i++) out[k][i] *= ro * wpre[k][i];
-        if (on) store_vec<V>(row_at<T>(a.normed, row) + c[k], a.width - c[k], out[k]);
+        if (on && at.any(k)) store_vec<V>(row_at<T>(a.normed, row) + at.c[k], V, out[k]);
       }
     }
     if (a.stats && on && lane == 0) {
@@ -176,33 +196,29 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
   }
 }
 
-// Backward.  (Above 8192 channels a row and its sums spill: 16384 channels run at a
-// fifth of the rate of 4096.)
-template <class T, class R, int TPR, int NV>
+// Backward: the row's values and the weights' gradients leave registers for two waves a
+// SIMD, too few to hide the loads behind others' work, so up to 4096 channels the next row's loads
+// are in flight during this row's sums.  16384 rows of 4096 channels with a gate,
+// residual in 32 bits (1.48 GB): 310 us without, 277 with, 5.3 TB/s; in 16 bits (1.07 GB)
+// 322 and 203 us, 5.3 TB/s.  Above: 5000 channels 4.7 TB/s, 8192 4.2; above 8192 a
+// row and its sums spill, 16384 channels run at 1.05 TB/s.
+template <class T, class R, int TPR, int NV, int V>
 __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p) {
   constexpr int RPW = threads_of(TPR) / TPR;
   constexpr bool HOLD = NV == 1;                       // the weights stay in registers
+  constexpr bool AHEAD = NV == 1 && TPR <= 512;        // and the next row's loads
   __shared__ float lds[2][16];
   __shared__ float cols[RPW > 1 ? threads_of(TPR) * V : 1];
   const rc_norm_args& a = p.a;
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const bool f32 = a.param_dtype == RC_F32;
   const float inv = 1.f / (float)a.width;
-  int c[NV];
-#pragma unroll
-  for (int k = 0; k < NV; k++) c[k] = min((k * TPR + lane) * V, a.width);
+  const Columns<TPR, NV, V> at(lane, a.width);
   float held[3][V], dw[3][NV][V];
-  const auto weight = [&](const void* w, int k, float absent, float (&x)[V]) {
-    const int at[1] = {c[k]};
-    float y[1][V];
-    load_weight<T>(w, f32, at, a.width, absent, y);
-#pragma unroll
-    for (int i = 0; i < V; i++) x[i] = y[0][i];
-  };
   if (HOLD) {
-    weight(a.post_weight, 0, 1.f, held[0]);
-    weight(a.scale, 0, 1.f, held[1]);
-    weight(a.pre_weight, 0, 0.f, held[2]);
+    load_weight<T>(a.post_weight, f32, at.c[0], 1.f, held[0]);
+    load_weight<T>(a.scale, f32, at.c[0], 1.f, held[1]);
+    load_weight<T>(a.pre_weight, f32, at.c[0], 0.f, held[2]);
   }
 #pragma unroll
   for (int j = 0; j < 3; j++)
@@ -210,24 +226,58 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     for (int k = 0; k < NV; k++)
 #pragma unroll
       for (int i = 0; i < V; i++) dw[j][k][i] = 0.f;
+  typedef T TV __attribute__((ext_vector_type(V)));
+  typedef R RV __attribute__((ext_vector_type(V)));
+  // Loads for the next row are unconditional (elements loaded in a branch and handed on by a
+  // loop: the compiler of ROCm 7.2 drops some): what is absent reads the residual's memory.
+  RV in_r, in_dout;
+  TV in_dn, in_v, in_g;
+  float in_stats[2];
+  const auto present = [&](const rc_view& v) { return v.data ? v : a.residual; };
+  const rc_view from_dout = present(a.dout), from_dn = present(a.dnormed);
+  const rc_view from_v = present(a.block), from_g = present(a.gate);
+  const auto next = [&](int64_t r0) {                  // rows past the last: the last
+    const int64_t row = min(r0 + group, a.rows - 1);
+    const int c = at.c[0];
+    in_stats[0] = a.stats[row * 2];
+    in_stats[1] = a.stats[row * 2 + 1];
+    __builtin_memcpy(&in_r, row_at<R>(a.residual, row) + c, sizeof(RV));
+    __builtin_memcpy(&in_dout, row_at<R>(from_dout, row) + c, sizeof(RV));
+    __builtin_memcpy(&in_dn, row_at<T>(from_dn, row) + c, sizeof(TV));
+    __builtin_memcpy(&in_v, row_at<T>(from_v, row) + c, sizeof(TV));
+    __builtin_memcpy(&in_g, row_at<T>(from_g, row) + c, sizeof(TV));
+  };
+  if (AHEAD) next((int64_t)blockIdx.x * RPW);
   for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < a.rows; r0 += (int64_t)gridDim.x * RPW) {
-    const int64_t row = r0 + group;
-    const bool on = row < a.rows;
-    const float rv = on ? a.stats[row * 2] : 0.f, ro = on ? a.stats[row * 2 + 1] : 0.f;
+    const int64_t row = min(r0 + group, a.rows - 1);
+    const bool on = RPW == 1 || r0 + group < a.rows;
+    const float rv = AHEAD ? in_stats[0] : a.stats[row * 2];
+    const float ro = AHEAD ? in_stats[1] : a.stats[row * 2 + 1];
     float dr[NV][V], dn[NV][V], vn[NV][V], act[NV][V], dact[NV][V], unit[NV][V], dot[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; k++) {
-      const int n = on ? a.width - c[k] : 0;
-      load_vec<V>(row_at<R>(a.residual, row) + c[k], n, unit[k]);
-      load_vec<V>(row_at<R>(a.dout, row) + c[k], a.dout.data ? n : 0, dr[k]);
-      load_vec<V>(row_at<T>(a.dnormed, row) + c[k], a.dnormed.data ? n : 0, dn[k]);
-      load_vec<V>(row_at<T>(a.block, row) + c[k], a.block.data ? n : 0, vn[k]);
-      if (a.gate.data) load_vec<V>(row_at<T>(a.gate, row) + c[k], n, act[k]);
+      if (AHEAD) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          unit[k][i] = (float)in_r[i];
+          dr[k][i] = on && a.dout.data ? (float)in_dout[i] : 0.f;
+          dn[k][i] = on && a.dnormed.data ? (float)in_dn[i] : 0.f;
+          vn[k][i] = a.block.data ? (float)in_v[i] : 0.f;
+          if (a.gate.data) act[k][i] = (float)in_g[i];
+        }
+      } else {
+        const int c = at.c[k];
+        load_vec<V>(row_at<R>(a.residual, row) + c, V, unit[k]);
+        load_vec<V>(row_at<R>(a.dout, row) + c, a.dout.data ? V : 0, dr[k]);
+        load_vec<V>(row_at<T>(a.dnormed, row) + c, a.dnormed.data ? V : 0, dn[k]);
+        load_vec<V>(row_at<T>(a.block, row) + c, a.block.data ? V : 0, vn[k]);
+        if (a.gate.data) load_vec<V>(row_at<T>(a.gate, row) + c, V, act[k]);
+      }
       float wpost[V], scale[V], wpre[V];
       if (!HOLD) {
-        weight(a.post_weight, k, 1.f, wpost);
-        weight(a.scale, k, 1.f, scale);
-        weight(a.pre_weight, k, 0.f, wpre);
+        load_weight<T>(a.post_weight, f32, at.c[k], 1.f, wpost);
+        load_weight<T>(a.scale, f32, at.c[k], 1.f, scale);
+        load_weight<T>(a.pre_weight, f32, at.c[k], 0.f, wpre);
       }
 #pragma unroll
       for (int i = 0; i < V; i++) {
@@ -240,11 +290,12 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
         vn[k][i] *= rv;
         const float part = vn[k][i] * (HOLD ? held[0][i] : wpost[i]);
         unit[k][i] = fmaf(HOLD ? held[1][i] : scale[i], part, unit[k][i]) * ro;
-        dw[0][k][i] = fmaf(dn[k][i], unit[k][i], dw[0][k][i]);
+        dw[0][k][i] += on ? dn[k][i] * unit[k][i] : 0.f;
         dn[k][i] *= HOLD ? held[2][i] : wpre[i];
-        dot[0] = fmaf(dn[k][i], unit[k][i], dot[0]);
+        dot[0] += at.own(k, i, dn[k][i] * unit[k][i]);
       }
     }
+    if (AHEAD) next(r0 + (int64_t)gridDim.x * RPW);
     if (a.pre_weight) {
       row_sums<TPR>(dot, lds[0]);
       const float m = dot[0] * inv;
@@ -257,21 +308,20 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     dot[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; k++) {
-      if (on)
-        store_vec<V>(row_at<R>(a.dresidual, row) + c[k], a.width - c[k], dr[k]);
+      if (on && at.any(k)) store_vec<V>(row_at<R>(a.dresidual, row) + at.c[k], V, dr[k]);
       float wpost[V], scale[V];
       if (!HOLD) {
-        weight(a.post_weight, k, 1.f, wpost);
-        weight(a.scale, k, 1.f, scale);
+        load_weight<T>(a.post_weight, f32, at.c[k], 1.f, wpost);
+        load_weight<T>(a.scale, f32, at.c[k], 1.f, scale);
       }
 #pragma unroll
       for (int i = 0; i < V; i++) {
         const float post = HOLD ? held[0][i] : wpost[i];
-        dw[1][k][i] = fmaf(dr[k][i], vn[k][i] * post, dw[1][k][i]);
+        dw[1][k][i] += on ? dr[k][i] * (vn[k][i] * post) : 0.f;
         dr[k][i] *= HOLD ? held[1][i] : scale[i];      // dp
-        dw[2][k][i] = fmaf(dr[k][i], vn[k][i], dw[2][k][i]);
+        dw[2][k][i] += on ? dr[k][i] * vn[k][i] : 0.f;
         dr[k][i] *= post;
-        dot[0] = fmaf(dr[k][i], vn[k][i], dot[0]);
+        dot[0] += at.own(k, i, dr[k][i] * vn[k][i]);
       }
     }
     if (a.block.data) {
@@ -282,6 +332,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
       }
 #pragma unroll
       for (int k = 0; k < NV; k++) {
+        const bool store = on && at.any(k);
 #pragma unroll
         for (int i = 0; i < V; i++) dr[k][i] = rv * (dr[k][i] - vn[k][i] * m);
         if (a.gate.data) {
@@ -290,9 +341,9 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
             dact[k][i] *= dr[k][i];
             dr[k][i] *= act[k][i];
           }
-          if (on) store_vec<V>(row_at<T>(a.dgate, row) + c[k], a.width - c[k], dact[k]);
+          if (store) store_vec<V>(row_at<T>(a.dgate, row) + at.c[k], V, dact[k]);
         }
-        if (on) store_vec<V>(row_at<T>(a.dblock, row) + c[k], a.width - c[k], dr[k]);
+        if (store) store_vec<V>(row_at<T>(a.dblock, row) + at.c[k], V, dr[k]);
       }
     }
     // one sum a row: its buffer is read before the next row writes it
@@ -305,7 +356,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     if (RPW > 1) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < V; i++) cols[threadIdx.x * V + i] = dw[j][0][i];
+      for (int i = 0; i < V; i++)
+        if (i >= at.over[0]) cols[threadIdx.x * V + i - at.over[0]] = dw[j][0][i];
       __syncthreads();
       for (int o = threadIdx.x; o < TPR * V && o < a.width; o += threads_of(TPR)) {
         float s = 0.f;
@@ -315,7 +367,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < NV; k++) store_vec<V>(out + c[k], a.width - c[k], dw[j][k]);
+      for (int k = 0; k < NV; k++)
+        if (at.any(k)) store_vec<V>(out + at.c[k], V, dw[j][k]);
     }
   }
 }
@@ -333,34 +386,42 @@ __global__ __launch_bounds__(256) void k_norm_weight_sum(const float* in, int64_
   if (out) store_param<T>(out, c % width, f32, s);
 }
 
-// Threads of a row and loads of a thread: enough threads for one load each up to
-// 8192 channels (backward, where two loads' registers still fit, 4096), for two
+// Threads of a row, loads of a thread and their width: enough threads for one
+// load each, up to 8192 channels forward and, by the registers, 6144 backward (5000
+// channels backward: 512 threads and two loads 313 us, 768 and one 193), for two
 // each above.
 template <bool BACKWARD, class F>
 int by_width(int32_t width, F&& f) {
   using std::integral_constant;
-  if (width <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-  if (width <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (width <= 1024) return f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
-  if (width <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  if (width <= 4096) return f(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+  const auto with = [&](auto tpr, auto nv) { return f(tpr, nv, integral_constant<int, kVec>{}); };
+  if (width < kVec)
+    return f(integral_constant<int, 32>{}, integral_constant<int, 1>{},
+             integral_constant<int, 1>{});
+  if (width <= 256) return with(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  if (width <= 512) return with(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (width <= 1024) return with(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+  if (width <= 2048) return with(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (width <= 4096) return with(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+  if (width <= 6144) return with(integral_constant<int, 768>{}, integral_constant<int, 1>{});
   if (width <= 8192)
-    return f(integral_constant<int, BACKWARD ? 512 : 1024>{},
-             integral_constant<int, BACKWARD ? 2 : 1>{});
-  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    return with(integral_constant<int, BACKWARD ? 512 : 1024>{},
+                integral_constant<int, BACKWARD ? 2 : 1>{});
+  return with(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 int threads_per_row(int32_t width, bool backward) {
-  const auto threads = [](auto tpr, auto) { return int(tpr()); };
+  const auto threads = [](auto tpr, auto, auto) { return int(tpr()); };
   return backward ? by_width<true>(width, threads) : by_width<false>(width, threads);
 }
 
-// Workgroups: enough threads to fill the chip, then each walks over rows.
-// Backward each leaves a row of partial sums, so beyond one a compute unit
-// there are four rows of work for each.
+// Workgroups: as many as the chip holds at once (forward six waves a SIMD, backward two,
+// by their registers), then each walks over rows.  One more than fits waits for a
+// whole walk: 32768 rows of 1024 channels, eight waves asked for 103 us, six 86.
+// Backward each leaves a row of partial sums, so beyond one a compute unit there are four
+// rows of work for each.
 int64_t norm_blocks(const rc_norm_args& a, bool backward) {
   const int tpr = threads_per_row(a.width, backward), wg = threads_of(tpr);
   const int64_t need = cdiv(a.rows, wg / tpr), cus = rcdp::num_cus();
-  const int64_t most = cus * (backward ? (wg < 512 ? 512 / wg : 1) : 2048 / wg);
+  const int64_t most = cus * (backward ? (wg < 512 ? 512 / wg : 1) : 1536 / wg);
   if (need <= cus) return need;
   const int64_t some = backward ? (need / 4 < cus ? cus : need / 4) : need;
   return some < most ? some : most;
@@ -404,8 +465,8 @@ extern "C" int rc_norm_forward(const rc_norm_args* args, void* stream) {
   const rc_norm_args& a = *args;
   if (a.rows == 0 || a.width == 0) return RC_OK;
   return by_dtypes(a, [&](auto t, auto r) {
-    return by_width<false>(a.width, [&](auto tpr, auto nv) {
-      k_norm_forward<decltype(t), decltype(r), tpr(), nv()>
+    return by_width<false>(a.width, [&](auto tpr, auto nv, auto v) {
+      k_norm_forward<decltype(t), decltype(r), tpr(), nv(), v()>
           <<<dim3((uint32_t)norm_blocks(a, false)), threads_of(tpr()), 0, (hipStream_t)stream>>>(
               {a, nullptr});
       return launched("k_norm_forward");
@@ -432,8 +493,8 @@ extern "C" int rc_norm_backward(const rc_norm_args* args, void* stream) {
   return by_dtypes(a, [&](auto t, auto r) -> int {
     using T = decltype(t);
     if (blocks > 0) {
-      const int st = by_width<true>(a.width, [&](auto tpr, auto nv) {
-        k_norm_backward<T, decltype(r), tpr(), nv()>
+      const int st = by_width<true>(a.width, [&](auto tpr, auto nv, auto v) {
+        k_norm_backward<T, decltype(r), tpr(), nv(), v()>
             <<<dim3((uint32_t)blocks), threads_of(tpr()), 0, (hipStream_t)stream>>>({a, partial});
         return launched("k_norm_backward");
       });

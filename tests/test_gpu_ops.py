@@ -475,6 +475,14 @@ NORM = [  # dtype, residual, rows, width, parts, gate activation, param
     ("bf16", "f32", 5, 5000, "bgpsn", "silu", "f32"),
     ("f32", "f32", 300, 8192, "bgpsn", "silu", "f32"),
     ("bf16", "f32", 3, 12345, "bgpsn", "silu", "f32"),
+    # several rows a workgroup, the last load of a row moved back
+    ("f32", "f32", 700, 1003, "bpsn", "silu", "f32"),
+    ("bf16", "f32", 600, 4095, "bgpsn", "silu", "f32"),
+    ("f16", "f16", 520, 5001, "bgps", "silu", "f16"),
+    ("f32", "f32", 5000, 3, "bgpsn", "sigmoid", "f32"),
+    ("bf16", "bf16", 800, 1000, "n", "silu", "f32"),
+    ("f16", "f32", 550, 7001, "bgpsn", "silu", "f32"),
+    ("f32", "f32", 9000, 9, "bg", "silu", "f32"),
 ]
 
 
