@@ -347,9 +347,12 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 // each channel, B, C), each element converted once by one thread; then the
 // lanes walk over it, four tokens at a time: each lane of a quad reads one
 // token's delta and delta u of its channel and the quad shares them, and each
-// ends with one token's y, which takes their place.  Rows of LDS are padded so that the four
-// rows that a quad reads lie in different banks.
+// ends with one token's y, which takes their place.  Rows of LDS are padded so
+// that the four rows that a quad reads lie in different banks.
 // ENDS: only the end state of the chunk from nothing, and its sum of delta.
+// Bound by VALU issue (87% busy): 33 instructions for a step of a wave over a token,
+// 20 of them the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 580 us, 3.7e12 state
+// steps/s; one prompt of 16384 x 2048 261 us.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams p) {
   constexpr int TILE = kFwdTile, N = Q * S, CW = channels_of(Q), ROW = CW + 8;
@@ -499,6 +502,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
 // way back, since keeping them spills; with fewer they stay (8 x 1024 x 2048 with
 // 8 states 232 -> 221 us).  ENDS: only the gradient of the state before the chunk,
 // from nothing after it, and its sum of delta.
+// Bound by VALU issue (86% busy): 104 instructions for a step of a wave, 60 of them
+// the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 1.8 ms, 1.2e12 state steps/s.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanParams p) {
   constexpr int TILE = kKeep, N = Q * S, CW = channels_of(Q), ROW = CW + 4;
@@ -767,7 +772,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
 // The sums over workgroups, in one launch: the first `cell_blocks` workgroups
 // take dB and dC (one thread for each (batch, token, group, state), eight
 // blocks' parts in flight), the next dA, the last dD and ddt_bias (columns of the
-// parts of sequences and chunks).
+// parts of sequences and chunks).  Memory bound and short: 8 x 2048 x 2048 reads 71 MB in
+// 15 us.
 template <class T>
 __global__ __launch_bounds__(kSumThreads) void k_scan_sums(ScanParams p, int64_t cells, int32_t N,
                                                            int64_t cell_blocks,
