@@ -200,14 +200,19 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_forward(NormParams p) 
 // SIMD, too few to hide the loads behind others' work, so up to 4096 channels the next row's loads
 // are in flight during this row's sums.  16384 rows of 4096 channels with a gate,
 // residual in 32 bits (1.48 GB): 310 us without, 277 with, 5.3 TB/s; in 16 bits (1.07 GB)
-// 322 and 203 us, 5.3 TB/s.  Above: 5000 channels 4.7 TB/s, 8192 4.2; above 8192 a
-// row and its sums spill, 16384 channels run at 1.05 TB/s.
+// 322 and 203 us, 5.3 TB/s.  Above: 5000 channels 4.7 TB/s, 8192 4.2.  Above
+// 8192, where 128 registers a thread hold neither the row nor the sums, two of
+// the three weights' sums are in LDS and the gate is read and evaluated again;
+// the rest still spills.  4096 rows of 16384 channels: 1.42 ms with all in
+// registers or spilled, 0.63 ms (2.3 TB/s) so.
 template <class T, class R, int TPR, int NV, int V>
 __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p) {
   constexpr int RPW = threads_of(TPR) / TPR;
   constexpr bool HOLD = NV == 1;                       // the weights stay in registers
   constexpr bool AHEAD = NV == 1 && TPR <= 512;        // and the next row's loads
+  constexpr bool TIGHT = TPR * NV * V > 8192;          // registers for a part only
   __shared__ float lds[2][16];
+  __shared__ float4 sums[TIGHT ? 2 * NV * V / 4 : 1][TIGHT ? TPR : 1];   // dscale, dpost_weight
   __shared__ float cols[RPW > 1 ? threads_of(TPR) * V : 1];
   const rc_norm_args& a = p.a;
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
@@ -226,6 +231,19 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     for (int k = 0; k < NV; k++)
 #pragma unroll
       for (int i = 0; i < V; i++) dw[j][k][i] = 0.f;
+  // The thread's own slots of LDS in place of dw[1] and dw[2]: x are added to them.
+  const auto add = [&](int j, int k, const float (&x)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      float4& s = sums[(j * NV + k) * (V / 4) + i / 4][threadIdx.x];
+      const float4 was = s;
+      s = {was.x + x[i], was.y + x[i + 1], was.z + x[i + 2], was.w + x[i + 3]};
+    }
+  };
+  if constexpr (TIGHT) {
+#pragma unroll
+    for (int i = 0; i < 2 * NV * V / 4; i++) sums[i][threadIdx.x] = {0.f, 0.f, 0.f, 0.f};
+  }
   typedef T TV __attribute__((ext_vector_type(V)));
   typedef R RV __attribute__((ext_vector_type(V)));
   // Loads for the next row are unconditional (elements loaded in a branch and handed on by a
@@ -314,14 +332,25 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
         load_weight<T>(a.post_weight, f32, at.c[k], 1.f, wpost);
         load_weight<T>(a.scale, f32, at.c[k], 1.f, scale);
       }
+      float ds[V], dpost[V];
 #pragma unroll
       for (int i = 0; i < V; i++) {
         const float post = HOLD ? held[0][i] : wpost[i];
-        dw[1][k][i] += on ? dr[k][i] * (vn[k][i] * post) : 0.f;
+        ds[i] = on ? dr[k][i] * (vn[k][i] * post) : 0.f;
         dr[k][i] *= HOLD ? held[1][i] : scale[i];      // dp
-        dw[2][k][i] += on ? dr[k][i] * vn[k][i] : 0.f;
+        dpost[i] = on ? dr[k][i] * vn[k][i] : 0.f;
         dr[k][i] *= post;
         dot[0] += at.own(k, i, dr[k][i] * vn[k][i]);
+      }
+      if constexpr (TIGHT) {
+        add(0, k, ds);
+        add(1, k, dpost);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          dw[1][k][i] += ds[i];
+          dw[2][k][i] += dpost[i];
+        }
       }
     }
     if (a.block.data) {
@@ -336,8 +365,17 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
 #pragma unroll
         for (int i = 0; i < V; i++) dr[k][i] = rv * (dr[k][i] - vn[k][i] * m);
         if (a.gate.data) {
+          if (TIGHT) {
+            load_vec<V>(row_at<T>(a.gate, row) + at.c[k], V, act[k]);
+            load_vec<V>(row_at<T>(a.block, row) + at.c[k], V, dact[k]);
+          }
 #pragma unroll
           for (int i = 0; i < V; i++) {
+            if (TIGHT) {
+              float slope;
+              act[k][i] = gate_of(act[k][i], a.gate_activation, slope);
+              dact[k][i] *= slope;
+            }
             dact[k][i] *= dr[k][i];
             dr[k][i] *= act[k][i];
           }
@@ -350,6 +388,20 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
     if (TPR > 64 && !(a.pre_weight && a.block.data && a.post_weight)) __syncthreads();
   }
   if (!p.partial) return;
+  if constexpr (TIGHT) {
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int k = 0; k < NV; k++)
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+          const float4 s = sums[(j * NV + k) * (V / 4) + i / 4][threadIdx.x];
+          dw[j + 1][k][i] = s.x;
+          dw[j + 1][k][i + 1] = s.y;
+          dw[j + 1][k][i + 2] = s.z;
+          dw[j + 1][k][i + 3] = s.w;
+        }
+  }
 #pragma unroll
   for (int j = 0; j < 3; j++) {
     float* out = p.partial + ((int64_t)blockIdx.x * 3 + j) * a.width;
