@@ -350,8 +350,8 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 // ends with one token's y, which takes their place.  Rows of LDS are padded so
 // that the four rows that a quad reads lie in different banks.
 // ENDS: only the end state of the chunk from nothing, and its sum of delta.
-// Bound by VALU issue (87% busy): 33 instructions for a step of a wave over a token,
-// 20 of them the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 580 us, 3.7e12 state
+// Bound by VALU issue (87% busy): 33 instructions for a step of a wave over a token
+// with 4 states a lane, 20 of them the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 580 us, 3.7e12 state
 // steps/s; one prompt of 16384 x 2048 261 us.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams p) {
@@ -902,12 +902,13 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 // over all but one of them for their end states.  bfloat16, 16 states, 2048 tokens and
 // channels (a batch of 8 is one wave a SIMD), whole or best cut, us:
 //   batch     2        4        6        8       10       12       16       20
-//   forward  229/75   225/131  226/185  228/233  335/289  335/340  338/409  458/520
+//   forward  198/75   199/131  199/185  202/233  335/289  335/340  338/409  458/520
 //   backward 655/175  658/317  664/460  672/590  957/729  964/865  977/1110 1482/1390
-// With v waves a SIMD on average and k on the fullest, a whole pass costs 95 + 130 k
-// forward, a cut one 1.7 times 130 v; backward 490 k (one wave: 665) and 1.18 times 490 v.
+// With v waves a SIMD on average and k on the fullest, a whole pass costs 95 +
+// 130 k forward (one wave: 202, see scan_plan), a cut one 1.7 times 130 v; backward 490
+// k (one wave: 665) and 1.18 times 490 v.
 bool scan_cut(double v, double k, bool backward) {
-  return backward ? k == 1. || 1.18 * v < k : 1.7 * v < .5 + k;
+  return backward ? k == 1. || 1.18 * v < k : 1.7 * v < (k == 1. ? 1.36 : .5 + k);
 }
 struct ScanPlan {
   int S, Q, VEC;
@@ -947,6 +948,13 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   if (p.chunk < kFwdTile) p.chunk = kFwdTile;
   p.chunks = a.length > 0 ? cdiv(a.length, p.chunk) : 1;
   p.keeps = cdiv(a.length, kKeep);
+  // One wave a SIMD, uncut: eight lanes of two states halve what a wave has to issue for
+  // a token (8 x 2048 x 2048 forward 230 us with four lanes, 202 with eight; with more
+  // waves equal, and cut 133 for 137).  The kept states lie alike.
+  if (!backward && p.chunks == 1 && groups <= cus && p.Q == 4 && p.S == 4) {
+    p.Q = 8;
+    p.S = 2;
+  }
   return p;
 }
 
@@ -1012,13 +1020,15 @@ ScanParams scan_params(const rc_scan_args& a, const ScanPlan& p, const ScanScrat
 }
 
 // Calls f(Q, S, VEC) with the plan's constants.
-template <class F>
+template <bool BACKWARD, class F>
 int by_plan(const ScanPlan& p, F&& f) {
   using std::integral_constant;
   const auto with = [&](auto Q, auto S) {
     if (p.VEC == 1) return f(Q, S, integral_constant<int, 1>{});
     return f(Q, S, integral_constant<int, 4>{});
   };
+  if constexpr (!BACKWARD)
+    if (p.Q == 8 && p.S == 2) return with(integral_constant<int, 8>{}, integral_constant<int, 2>{});
   if (p.Q == 16) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
   if (p.Q == 8) return with(integral_constant<int, 8>{}, integral_constant<int, 4>{});
   if (p.S == 4) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
@@ -1058,13 +1068,14 @@ extern "C" int rc_scan_forward(const rc_scan_args* args, void* stream) {
   const ScanParams q = scan_params(a, p, need);
   const hipStream_t s = (hipStream_t)stream;
   return by_dtype(a.dtype, [&](auto t) {
-    return by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
+    return by_plan<false>(p, [&](auto Q, auto S, auto VEC) -> int {
       using T = decltype(t);
       const dim3 grid((uint32_t)blocks), threads(channels_of(Q()) * Q());
-      if (p.chunks > 1) {
-        k_scan_forward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
-        if (const int st = launched("k_scan_forward ends")) return st;
-      }
+      if constexpr (Q() != 8 || S() != 2)              // (that one is never cut)
+        if (p.chunks > 1) {
+          k_scan_forward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);
+          if (const int st = launched("k_scan_forward ends")) return st;
+        }
       k_scan_forward<T, Q(), S(), VEC(), false><<<grid, threads, 0, s>>>(q);
       return launched("k_scan_forward");
     });
@@ -1086,7 +1097,7 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   return by_dtype(a.dtype, [&](auto t) -> int {
     using T = decltype(t);
     if (blocks > 0) {
-      const int st = by_plan(p, [&](auto Q, auto S, auto VEC) -> int {
+      const int st = by_plan<true>(p, [&](auto Q, auto S, auto VEC) -> int {
         const dim3 grid((uint32_t)blocks), threads(channels_of(Q()) * Q());
         if (p.chunks > 1) {
           k_scan_backward<T, Q(), S(), VEC(), true><<<grid, threads, 0, s>>>(q);

@@ -275,6 +275,9 @@ SCAN = [  # dtype, batch, length, width, states, groups, parts, lengths
     ("f32", 2, 40, 78, 24, 1, "Dzbs", (40, 5)),
     ("bf16", 1, 70, 37, 40, 1, "Dzbs", (69,)),
     ("f32", 1, 40, 7, 3, 1, "Dzbs", None),
+    # a workgroup for nearly every compute unit, several tiles
+    ("bf16", 230, 100, 40, 16, 1, "Dzbs", None),
+    ("f32", 120, 70, 70, 9, 1, "z", None),
 ]
 
 
