@@ -128,6 +128,12 @@ bool differentiated(std::initializer_list<const Tensor*> tensors) {
   return false;
 }
 
+// A tensor that a kernel has written through its pointer: what autograd has
+// saved of it is out of date, as after torch's own operators in place.
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Gradients that must not be differentiated again say so if they are.
 variable_list once(variable_list grads) {
   if (!at::GradMode::is_enabled()) return grads;
@@ -269,6 +275,7 @@ Tensor causal_conv_step(const Tensor& state, const Tensor& x_, const Tensor& wei
   a.bias = ptr(bias);
   a.slots = ptr<int32_t>(slots);
   check(rc_conv_step(&a, stream_of(x)), "rc_conv_step");
+  written(state);
   return y;
 }
 
@@ -450,6 +457,7 @@ Tensor selective_scan_step(const Tensor& state, const Tensor& u, const Tensor& d
   a.state_slot = state.stride(0);
   a.slots = ptr<int32_t>(slots);
   check(rc_scan_step(&a, stream_of(u)), "rc_scan_step");
+  written(state);
   return y;
 }
 

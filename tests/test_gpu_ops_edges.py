@@ -1,0 +1,48 @@
+"""The sequence-model operators where a caller leaves their usual ground:
+states that autograd has saved."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_1905_11722_amd import ops  # noqa: E402
+
+DEV = torch.device("cuda", 0)
+
+
+def token(op, pool, slots=None):
+    """One token through a step form on a pool of states; its y."""
+    x = torch.randn(2, 8, device=DEV)
+    if op == "conv":
+        return ops.causal_conv_step(pool, x, torch.randn(8, 4, device=DEV), slots=slots)
+    bc = torch.randn(2, 4, device=DEV)
+    return ops.selective_scan_step(pool, x, x, -torch.rand(8, 4, device=DEV), bc, bc, softplus=True,
+                                   slots=slots)
+
+
+def pool_of(op, slots=2):
+    return torch.randn((slots, 3, 8) if op == "conv" else (slots, 8, 4), device=DEV)
+
+
+@pytest.mark.parametrize("op", ["conv", "scan"])
+def test_a_step_on_a_saved_state_is_seen(op):
+    """A token that overwrites a state that a backward pass still needs makes
+    that pass raise, as torch's own operators in place do."""
+    pool = pool_of(op)
+    version = pool._version
+    x = torch.randn(2, 6, 8, device=DEV, requires_grad=True)
+    if op == "conv":
+        y = ops.causal_conv(x, torch.randn(8, 4, device=DEV), state=pool)
+    else:
+        bc = torch.randn(2, 6, 4, device=DEV)
+        y = ops.selective_scan(x, x, -torch.rand(8, 4, device=DEV), bc, bc, softplus=True, state=pool)
+    token(op, pool)
+    assert pool._version > version
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with torch.inference_mode():
+        token(op, pool_of(op))                       # tensors without versions
