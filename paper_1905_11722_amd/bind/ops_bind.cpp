@@ -128,6 +128,13 @@ bool differentiated(std::initializer_list<const Tensor*> tensors) {
   return false;
 }
 
+// The token forms have no gradients: where one is asked for they raise, rather than
+// cut what they return from its past.
+void not_differentiated(const char* name, std::initializer_list<const Tensor*> tensors) {
+  TORCH_CHECK_VALUE(!differentiated(tensors), name,
+                    " has no gradients: call it under torch.no_grad(), or with detached tensors");
+}
+
 // A tensor that a kernel has written through its pointer: what autograd has
 // saved of it is out of date, as after torch's own operators in place.
 void written(const Tensor& t) {
@@ -260,6 +267,7 @@ Tensor causal_conv_step(const Tensor& state, const Tensor& x_, const Tensor& wei
   expect("state", state, {state.size(0), k - 1, d}, x.scalar_type(), x);
   TORCH_CHECK_VALUE(state.stride(2) == 1 || d <= 1, "state must have contiguous channels");
   const Tensor slots = slots_of(slots_, x, state.size(0));
+  not_differentiated("causal_conv_step", {&state, &x, &weight, &bias});
   const c10::DeviceGuard guard(x.device());
   const Tensor y = at::empty({x.size(0), d}, x.options());
   a.dtype = code(x.scalar_type());
@@ -430,6 +438,8 @@ Tensor selective_scan_step(const Tensor& state, const Tensor& u, const Tensor& d
   TORCH_CHECK_VALUE((state.stride(2) == 1 || n <= 1) && (state.stride(1) == n || d <= 1),
                     "each slot of state must be contiguous");
   const Tensor slots = slots_of(slots_, u, state.size(0));
+  not_differentiated("selective_scan_step",
+                     {&state, &u, &dt, &A, &B, &C, &t.D, &t.z, &t.dt_bias});
   t = {rows(u), rows(dt), dense(A), rows(B), rows(C), dense(t.D), rows(t.z), dense(t.dt_bias),
        Tensor(), Tensor()};
   const c10::DeviceGuard guard(u.device());

@@ -9,7 +9,9 @@ nodes of a network whose recomputation ``rcdp`` plans.
   block's gate and residual scale.
 
 The whole-sequence forms are differentiable (once); the ``*_step`` forms take
-one token of each sequence and update a pool of states in place.  Activations
+one token of each sequence and update a pool of states in place, without
+gradients: they refuse inputs that require one (call them under
+``torch.no_grad()``).  Activations
 are float32, bfloat16 or float16 on one GPU; sums, states and statistics are
 held in 32 bits.  Work is enqueued on PyTorch's current stream of the
 inputs' device, outputs and scratch come from PyTorch's allocator, nothing

@@ -1,5 +1,5 @@
 """The sequence-model operators where a caller leaves their usual ground:
-states that autograd has saved."""
+states that autograd has saved, gradients that there are none of."""
 
 import pytest
 import torch
@@ -46,3 +46,24 @@ def test_a_step_on_a_saved_state_is_seen(op):
         y.sum().backward()
     with torch.inference_mode():
         token(op, pool_of(op))                       # tensors without versions
+
+
+def test_steps_have_no_gradients():
+    """With gradients recorded, a token form refuses any input that requires one."""
+    def leaf(*shape):
+        return torch.rand(shape, device=DEV)
+
+    conv = {"state": leaf(2, 3, 8), "x": leaf(2, 8), "weight": leaf(8, 4), "bias": leaf(8)}
+    scan = {"state": leaf(2, 8, 4), "u": leaf(2, 8), "dt": leaf(2, 8), "A": -leaf(8, 4), "B": leaf(2, 4),
+            "C": leaf(2, 4), "D": leaf(8), "z": leaf(2, 8), "dt_bias": leaf(8)}
+    for f, args in ((ops.causal_conv_step, conv), (ops.selective_scan_step, scan)):
+        for name in args:
+            args[name].requires_grad_()
+            before = args["state"].detach().clone()
+            with pytest.raises(ValueError, match="no gradients"):
+                f(**args)
+            assert torch.equal(args["state"].detach(), before)
+            with torch.no_grad():
+                assert not f(**args).requires_grad
+            args[name].requires_grad_(False)
+        assert not f(**args).requires_grad
