@@ -3,6 +3,7 @@
 // stream, and autograd.  Native, because a single token's kernels take a few
 // microseconds and the same work in Python took several times that.
 // ops.py documents the functions.
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
@@ -121,7 +122,16 @@ void* stream_of(const Tensor& t) {
   return c10::hip::getCurrentHIPStream(t.device().index()).stream();
 }
 
+// Forward mode does not ask requires_grad: a tangent that is not refused would be dropped.
+void no_tangent(const Tensor& t) {
+  if (t.defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+    TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined(),
+                                "the sequence-model operators have no forward-mode derivatives");
+}
+
+// Whether autograd records this call.
 bool differentiated(std::initializer_list<const Tensor*> tensors) {
+  for (const Tensor* t : tensors) no_tangent(*t);
   if (!at::GradMode::is_enabled()) return false;
   for (const Tensor* t : tensors)
     if (t->defined() && t->requires_grad()) return true;
@@ -206,6 +216,7 @@ struct Conv : torch::autograd::Function<Conv> {
     return conv_forward(x, w, b, state, lengths, act, param, want_state);
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
     const auto saved = ctx->get_saved_variables();
     const Tensor &x = saved[0], &w = saved[1], &b = saved[2], &state = saved[3];
     const c10::DeviceGuard guard(x.device());
@@ -354,6 +365,7 @@ struct Scan : torch::autograd::Function<Scan> {
     return out;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
     const auto s = ctx->get_saved_variables();
     const ScanIn t = {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7], s[8], s[9]};
     const c10::DeviceGuard guard(t.u.device());
@@ -546,6 +558,7 @@ struct Norm : torch::autograd::Function<Norm> {
     return out;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
     const auto s = ctx->get_saved_variables();
     const NormIn t = {s[0], s[1], s[2], s[3], s[4], s[5]};
     const c10::DeviceGuard guard(t.residual.device());

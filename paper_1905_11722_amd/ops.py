@@ -8,7 +8,7 @@ nodes of a network whose recomputation ``rcdp`` plans.
 * :func:`norm_residual`: the norms before and after a block, fused with the
   block's gate and residual scale.
 
-The whole-sequence forms are differentiable (once); the ``*_step`` forms take
+The whole-sequence forms are differentiable (once, in reverse mode); the ``*_step`` forms take
 one token of each sequence and update a pool of states in place, without
 gradients: they refuse inputs that require one (call them under
 ``torch.no_grad()``).  Activations

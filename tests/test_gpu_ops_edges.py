@@ -1,8 +1,9 @@
 """The sequence-model operators where a caller leaves their usual ground:
-states that autograd has saved, gradients that there are none of."""
+states that autograd has saved, derivatives that there are none of."""
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +68,36 @@ def test_steps_have_no_gradients():
                 assert not f(**args).requires_grad
             args[name].requires_grad_(False)
         assert not f(**args).requires_grad
+
+
+def test_forward_mode_is_refused():
+    """A tangent of any input raises, with gradients recorded or not, rather than being dropped."""
+    x, w, A = torch.randn(2, 5, 8, device=DEV), torch.randn(8, 4, device=DEV), -torch.rand(8, 4, device=DEV)
+    bc, v = torch.randn(2, 5, 4, device=DEV), torch.rand(8, device=DEV)
+    pool, h = pool_of("conv"), pool_of("scan")
+    calls = [
+        (lambda *a: ops.causal_conv(*a[:3], state=a[3]), [x, w, v, pool]),
+        (lambda *a: ops.selective_scan(*a[:8], state=a[8]), [x, x, A, bc, bc, v, x, v, h]),
+        (lambda *a: ops.norm_residual(*a)[0], [x, x, x, v, v, v]),
+        (ops.causal_conv_step, [pool, x[:, 0], w, v]),
+        (ops.selective_scan_step, [h, x[:, 0], x[:, 0], A, bc[:, 0], bc[:, 0], v, x[:, 0], v]),
+    ]
+    for f, args in calls:
+        for i in range(len(args)):
+            with forward_ad.dual_level():
+                dual = list(args)
+                dual[i] = forward_ad.make_dual(args[i], torch.ones_like(args[i]))
+                with pytest.raises(NotImplementedError, match="forward-mode"):
+                    f(*dual)
+                with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+                    f(*dual)
+        with forward_ad.dual_level():
+            f(*args)
+    for f, args in calls[:3]:
+        y = f(args[0].requires_grad_(), *args[1:])
+        y = y if isinstance(y, torch.Tensor) else y[0]
+        with forward_ad.dual_level():
+            dy = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                torch.autograd.grad(y, args[0], dy)
+        args[0].requires_grad_(False)
