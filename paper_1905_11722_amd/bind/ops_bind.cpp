@@ -106,6 +106,18 @@ Tensor slots_of(const Opt& t, const Tensor& main, int64_t slots) {
   return Tensor();
 }
 
+// Whether some of `rows` rows of `width` elements at i * slot + k * row, i < slots, share memory.
+bool overlap(int64_t slots, int64_t slot, int64_t rows, int64_t row, int64_t width) {
+  if (slots == 0 || rows == 0 || width == 0) return false;
+  if (slots > 1 && slot < width) return true;
+  for (int64_t k = 1; k < rows; k++) {                 // rows k apart: the slots that come closest
+    const int64_t last = slots - 1, i = slot ? std::min(k * row / slot, last) : 0;
+    for (const int64_t j : {i, std::min(i + 1, last)})
+      if (std::abs(k * row - j * slot) < width) return true;
+  }
+  return false;
+}
+
 template <class Args>
 Tensor scratch(int (*size)(const Args*, uint64_t*), Args& args, const Tensor& main,
                const char* name) {
@@ -277,6 +289,8 @@ Tensor causal_conv_step(const Tensor& state, const Tensor& x_, const Tensor& wei
   TORCH_CHECK_VALUE(state.dim() == 3, "state must have 3 dimensions");
   expect("state", state, {state.size(0), k - 1, d}, x.scalar_type(), x);
   TORCH_CHECK_VALUE(state.stride(2) == 1 || d <= 1, "state must have contiguous channels");
+  TORCH_CHECK_VALUE(!overlap(state.size(0), state.stride(0), k - 1, state.stride(1), d),
+                    "states must not share memory");
   const Tensor slots = slots_of(slots_, x, state.size(0));
   not_differentiated("causal_conv_step", {&state, &x, &weight, &bias});
   const c10::DeviceGuard guard(x.device());
@@ -449,6 +463,8 @@ Tensor selective_scan_step(const Tensor& state, const Tensor& u, const Tensor& d
   expect("state", state, {state.size(0), d, n}, at::kFloat, u);
   TORCH_CHECK_VALUE((state.stride(2) == 1 || n <= 1) && (state.stride(1) == n || d <= 1),
                     "each slot of state must be contiguous");
+  TORCH_CHECK_VALUE(!overlap(state.size(0), state.stride(0), 1, 0, d * n),
+                    "states must not share memory");
   const Tensor slots = slots_of(slots_, u, state.size(0));
   not_differentiated("selective_scan_step",
                      {&state, &u, &dt, &A, &B, &C, &t.D, &t.z, &t.dt_bias});

@@ -86,7 +86,8 @@ def causal_conv_step(state, x, weight, bias=None, *, slots=None, activation="sil
     running states; row i uses ``state[slots[i]]`` (slots: int32 (batch,),
     default 0, 1, ...) and shifts its token into it.  A row whose slot is
     outside the pool (-1, say) is padding: its y is 0 and no state changes.
-    The slots of one call must differ.  Returns y: (batch, width).
+    The slots of one call must differ, and those of the pool must not share
+    memory.  Returns y: (batch, width).
     """
     return (_native or load()).causal_conv_step(
         state, x, weight, bias, slots, _activation("activation", activation, _CONV_ACTIVATIONS))

@@ -1,5 +1,6 @@
 """The sequence-model operators where a caller leaves their usual ground:
-states that autograd has saved, derivatives that there are none of."""
+states that autograd has saved, derivatives that there are none of,
+pools that share memory."""
 
 import pytest
 import torch
@@ -101,3 +102,31 @@ def test_forward_mode_is_refused():
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 torch.autograd.grad(y, args[0], dy)
         args[0].requires_grad_(False)
+
+
+def test_pools_that_share_memory():
+    """A pool whose states overlap is refused; strides that only interleave them are not."""
+    flat = torch.randn(4096, device=DEV)
+    conv = [(1, 0, 8), (2, 24, 0), (2, 7, 100), (2, 100, 7), (3, 20, 8), (40, 9, 50), (2, 23, 8), (1, 0, 7)]
+    for slots, slot, row in conv:
+        pool = flat.as_strided((slots, 3, 8), (slot, row, 1))
+        at = [i * slot + k * row + c for i in range(slots) for k in range(3) for c in range(8)]
+        n = torch.zeros(2, dtype=torch.int32, device=DEV) - 1          # no state is touched
+        if len(set(at)) < len(at):
+            with pytest.raises(ValueError, match="share memory"):
+                token("conv", pool, n)
+        else:
+            token("conv", pool, n)
+    for slots, slot in ((2, 0), (3, 31), (3, 32), (1, 0)):
+        pool = flat.as_strided((slots, 8, 4), (slot, 4, 1))
+        if slots > 1 and slot < 32:
+            with pytest.raises(ValueError, match="share memory"):
+                token("scan", pool, n)
+        else:
+            token("scan", pool, n)
+    pool, other = flat.as_strided((4, 3, 8), (8, 32, 1)), flat.clone()   # slots between rows
+    x, w = torch.randn(2, 8, device=DEV), torch.randn(8, 4, device=DEV)
+    n = torch.tensor([3, 1], dtype=torch.int32, device=DEV)
+    dense = pool.contiguous()
+    assert torch.equal(ops.causal_conv_step(pool, x, w, slots=n), ops.causal_conv_step(dense, x, w, slots=n))
+    assert torch.equal(pool, dense) and torch.equal(flat[96:], other[96:])
