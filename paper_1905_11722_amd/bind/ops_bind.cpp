@@ -98,6 +98,7 @@ Tensor lengths_of(const Opt& t, const Tensor& main) {
   return dense(*t);
 }
 Tensor slots_of(const Opt& t, const Tensor& main, int64_t slots) {
+  TORCH_CHECK_VALUE(slots < (int64_t)1 << 31, "state has too many slots: ", slots);
   if (t) {
     expect("slots", *t, {main.size(0)}, at::kInt, main);
     return dense(*t);

@@ -1,6 +1,6 @@
 """The sequence-model operators where a caller leaves their usual ground:
 states that autograd has saved, derivatives that there are none of,
-pools that share memory."""
+pools that share memory or are too large."""
 
 import pytest
 import torch
@@ -130,3 +130,12 @@ def test_pools_that_share_memory():
     dense = pool.contiguous()
     assert torch.equal(ops.causal_conv_step(pool, x, w, slots=n), ops.causal_conv_step(dense, x, w, slots=n))
     assert torch.equal(pool, dense) and torch.equal(flat[96:], other[96:])
+
+
+def test_pools_of_more_slots_than_an_index_reaches():
+    """2^32 + 2 slots without rows (one tap): not taken for 2 of them."""
+    pool = torch.empty(2 ** 32 + 2, 0, 8, device=DEV)
+    x, w = torch.randn(2, 8, device=DEV), torch.randn(8, 1, device=DEV)
+    for n in (torch.tensor([0, 5], dtype=torch.int32, device=DEV), None):
+        with pytest.raises(ValueError, match="too many slots"):
+            ops.causal_conv_step(pool, x, w, slots=n)
