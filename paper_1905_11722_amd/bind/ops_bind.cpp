@@ -58,11 +58,17 @@ void expect(const char* name, const Tensor& t, at::IntArrayRef shape, at::Scalar
                     t.device());
 }
 
-// t with contiguous channels: itself, or a copy.
+// t with contiguous channels and its values in memory (not those of a view that negates them):
+// itself, or a copy.
+Tensor plain(const Tensor& t) { return t.is_neg() ? t.resolve_neg() : t; }
 Tensor rows(const Tensor& t) {
-  return !t.defined() || t.size(-1) <= 1 || t.stride(-1) == 1 ? t : t.contiguous();
+  if (!t.defined()) return t;
+  return plain(t.size(-1) <= 1 || t.stride(-1) == 1 ? t : t.contiguous());
 }
-Tensor dense(const Tensor& t) { return !t.defined() || t.is_contiguous() ? t : t.contiguous(); }
+Tensor dense(const Tensor& t) {
+  if (!t.defined()) return t;
+  return plain(t.is_contiguous() ? t : t.contiguous());
+}
 
 // A (batch, time, channel) or (batch, channel) tensor.
 rc_view view(const Tensor& t) {
@@ -97,7 +103,9 @@ Tensor lengths_of(const Opt& t, const Tensor& main) {
   expect("lengths", *t, {main.size(0)}, at::kInt, main);
   return dense(*t);
 }
-Tensor slots_of(const Opt& t, const Tensor& main, int64_t slots) {
+Tensor slots_of(const Opt& t, const Tensor& main, const Tensor& state) {
+  const int64_t slots = state.size(0);
+  TORCH_CHECK_VALUE(!state.is_neg(), "state must not be a view that negates its memory");
   TORCH_CHECK_VALUE(slots < (int64_t)1 << 31, "state has too many slots: ", slots);
   if (t) {
     expect("slots", *t, {main.size(0)}, at::kInt, main);
@@ -292,7 +300,7 @@ Tensor causal_conv_step(const Tensor& state, const Tensor& x_, const Tensor& wei
   TORCH_CHECK_VALUE(state.stride(2) == 1 || d <= 1, "state must have contiguous channels");
   TORCH_CHECK_VALUE(!overlap(state.size(0), state.stride(0), k - 1, state.stride(1), d),
                     "states must not share memory");
-  const Tensor slots = slots_of(slots_, x, state.size(0));
+  const Tensor slots = slots_of(slots_, x, state);
   not_differentiated("causal_conv_step", {&state, &x, &weight, &bias});
   const c10::DeviceGuard guard(x.device());
   const Tensor y = at::empty({x.size(0), d}, x.options());
@@ -466,7 +474,7 @@ Tensor selective_scan_step(const Tensor& state, const Tensor& u, const Tensor& d
                     "each slot of state must be contiguous");
   TORCH_CHECK_VALUE(!overlap(state.size(0), state.stride(0), 1, 0, d * n),
                     "states must not share memory");
-  const Tensor slots = slots_of(slots_, u, state.size(0));
+  const Tensor slots = slots_of(slots_, u, state);
   not_differentiated("selective_scan_step",
                      {&state, &u, &dt, &A, &B, &C, &t.D, &t.z, &t.dt_bias});
   t = {rows(u), rows(dt), dense(A), rows(B), rows(C), dense(t.D), rows(t.z), dense(t.dt_bias),

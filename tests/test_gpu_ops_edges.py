@@ -1,6 +1,6 @@
 """The sequence-model operators where a caller leaves their usual ground:
 states that autograd has saved, derivatives that there are none of,
-pools that share memory or are too large."""
+pools that share memory or are too large, views that negate."""
 
 import pytest
 import torch
@@ -139,3 +139,33 @@ def test_pools_of_more_slots_than_an_index_reaches():
     for n in (torch.tensor([0, 5], dtype=torch.int32, device=DEV), None):
         with pytest.raises(ValueError, match="too many slots"):
             ops.causal_conv_step(pool, x, w, slots=n)
+
+
+def test_views_that_negate():
+    """Lazily negated views (the imaginary part of a conjugate) are taken at
+    their values; a pool that is one is refused."""
+    neg = torch._neg_view
+    x, w, v = torch.randn(2, 5, 8, device=DEV), torch.randn(8, 4, device=DEV), torch.rand(8, device=DEV)
+    A, bc, h = -torch.rand(8, 4, device=DEV), torch.randn(2, 5, 4, device=DEV), torch.randn(2, 8, 4, device=DEV)
+    pool = torch.randn(2, 3, 8, device=DEV)
+    calls = [
+        (lambda *a: ops.causal_conv(*a[:3], state=a[3]), [x, w, v, pool]),
+        (lambda *a: ops.selective_scan(*a[:8], state=a[8]), [x, x, A, bc, bc, v, x, v, h]),
+        (lambda *a: torch.cat(ops.norm_residual(*a)), [x, x, x, v, v, v]),
+        (lambda *a: ops.causal_conv_step(pool.clone(), *a), [x[:, 0], w, v]),
+        (lambda *a: ops.selective_scan_step(h.clone(), *a), [x[:, 0], x[:, 0], A, bc[:, 0], bc[:, 0], v, x[:, 0], v]),
+    ]
+    for f, args in calls:
+        want = f(*args)
+        for i in range(len(args)):
+            view = neg(args[i].neg())
+            assert view.is_neg()
+            assert torch.equal(f(*args[:i], view, *args[i + 1:]), want)
+    lazy = neg(pool.neg())
+    for op, p in (("conv", lazy), ("scan", neg(h.neg()))):
+        with pytest.raises(ValueError, match="negates"):
+            token(op, p)
+    xs = x.clone().requires_grad_()
+    want, = torch.autograd.grad(ops.causal_conv(xs, w), xs, x)
+    got, = torch.autograd.grad(ops.causal_conv(xs, w), xs, neg(x.neg()))
+    assert torch.equal(got, want)
