@@ -984,11 +984,12 @@ int scan_check(const rc_scan_args* a, bool backward) {
     if (a->length > 0) {
       if (!a->u.data || !a->dt.data || !a->B.data || !a->C.data) return RC_E_ARG;
       if (!backward && !a->y.data) return RC_E_ARG;
-      if (backward && (!a->dy.data || !a->du.data || !a->ddt.data || !a->dB || !a->dC ||
-                       !a->kept || (a->z.data == nullptr) != (a->dz.data == nullptr)))
+      if (backward && (!a->dy.data || !a->du.data || !a->ddt.data || !a->kept ||
+                       (a->z.data == nullptr) != (a->dz.data == nullptr)))
         return RC_E_ARG;
     }
   }
+  if (backward && a->batch > 0 && a->length > 0 && (!a->dB || !a->dC)) return RC_E_ARG;
   if (backward && a->width > 0 &&
       (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias)))
     return RC_E_ARG;
@@ -1088,7 +1089,6 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   const ScanPlan p = scan_plan(a, true);
   const ScanScratch need = scan_scratch(a, p, true);
   if (need.total() > 0 && (!a.workspace || a.workspace_bytes < need.total())) return RC_E_SCRATCH;
-  if (a.width == 0) return RC_OK;
   const ScanParams q = scan_params(a, p, need);
   const hipStream_t s = (hipStream_t)stream;
   const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
@@ -1111,6 +1111,8 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
     const int64_t cell_blocks = cdiv(cells * 2 * N, kSumThreads);
     const int64_t a_blocks = cdiv((int64_t)a.width * N, kSumCols);
     const int64_t d_blocks = cdiv((int64_t)a.width * 2, kSumCols);
+    // (without channels dB and dC are sums of nothing)
+    if (cell_blocks + a_blocks + d_blocks == 0) return RC_OK;
     k_scan_sums<T><<<dim3((uint32_t)(cell_blocks + a_blocks + d_blocks)), kSumThreads, 0, s>>>(
         q, cells, N, cell_blocks, a_blocks);
     return launched("k_scan_sums");

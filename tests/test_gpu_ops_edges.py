@@ -1,6 +1,7 @@
 """The sequence-model operators where a caller leaves their usual ground:
 states that autograd has saved, derivatives that there are none of,
-pools that share memory or are too large, views that negate."""
+pools that share memory or are too large, views that negate,
+no channels."""
 
 import pytest
 import torch
@@ -169,3 +170,27 @@ def test_views_that_negate():
     want, = torch.autograd.grad(ops.causal_conv(xs, w), xs, x)
     got, = torch.autograd.grad(ops.causal_conv(xs, w), xs, neg(x.neg()))
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("groups", [0, 2])
+def test_scan_without_channels(groups):
+    """No channels: nothing depends on B and C, whose gradients are zeros (not what
+    their memory held)."""
+    b, n, s = 3, 40, 5
+    shape = (b, n, groups, s) if groups else (b, n, s)
+    u = torch.zeros(b, n, 0, device=DEV, requires_grad=True)
+    B, C = (torch.randn(shape, device=DEV, requires_grad=True) for _ in range(2))
+    A = torch.zeros(0, s, device=DEV, requires_grad=True)
+    h = torch.zeros(b, 0, s, device=DEV, requires_grad=True)
+    y, out = ops.selective_scan(u, u, A, B, C, softplus=True, state=h, return_state=True)
+    assert y.shape == u.shape and out.shape == h.shape
+    old = [torch.full(shape, float("nan"), device=DEV) for _ in range(8)]
+    del old
+    grads = torch.autograd.grad([y, out], [B, C, u, A, h], [torch.ones_like(y), torch.ones_like(out)])
+    for g, t in zip(grads, (B, C, u, A, h)):
+        assert g.shape == t.shape and not g.any()
+    for shape in ((0, 4, 0), (2, 0, 0)):
+        u = torch.zeros(shape, device=DEV, requires_grad=True)
+        B = torch.zeros(*shape[:2], s, device=DEV, requires_grad=True)
+        g, = torch.autograd.grad(ops.selective_scan(u, u, A, B, B).sum(), B)
+        assert g.shape == B.shape
