@@ -21,7 +21,8 @@
  *    enqueued then, except after RC_E_DEVICE.  Nothing crosses the ABI as an
  *    exception.
  *  - Sizes may be zero.  A call whose outputs are empty does nothing.
- *    length and width are at most 2^30.
+ *    length and width are at most 2^30; sizes that need a launch of 2^32
+ *    threads or more return RC_E_OVERFLOW.
  *  - Channels are contiguous; batch and time strides are in elements and
  *    free, with any alignment that the type has.  Outputs must not overlap
  *    inputs or each other.

@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(Co
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void k_conv_weight_sum(const float* in, int64_t parts,
+__global__ __launch_bounds__(kThreads) void k_conv_weight_sum(const float* in, int64_t parts,
                                                          int32_t width, int32_t taps, void* dw,
                                                          void* db, int32_t f32) {
   __shared__ float lds[256];
@@ -400,6 +400,10 @@ ConvParams<T> conv_params(const rc_conv_args& a, const ConvPlan& p) {
   return {a, p.lanes, p.run, (int32_t)p.runs, (int32_t)p.groups_c, nullptr};
 }
 
+int64_t weight_sum_blocks(const rc_conv_args& a) {
+  return cdiv((int64_t)a.width * (a.taps + 1), kSumCols);
+}
+
 int conv_check(const rc_conv_args* a, bool backward) {
   if (!a || !conv_sizes_ok(a->dtype, a->param_dtype, a->activation, a->batch, a->length, a->width,
                            a->taps))
@@ -410,7 +414,8 @@ int conv_check(const rc_conv_args* a, bool backward) {
   if (some && a->length > 0 && (backward ? !a->dy.data || !a->dx.data : !a->y.data))
     return RC_E_ARG;
   const ConvPlan p = conv_plan(*a, backward);
-  if (p.groups_c * p.groups_t >= kMaxBlocks || (int64_t)a->batch * p.runs >= kMaxBlocks)
+  if (!launchable(p.groups_c * p.groups_t, kThreads)) return RC_E_OVERFLOW;
+  if (backward && (a->dweight || a->dbias) && !launchable(weight_sum_blocks(*a), kThreads))
     return RC_E_OVERFLOW;
   return RC_OK;
 }
@@ -469,7 +474,7 @@ extern "C" int rc_conv_backward(const rc_conv_args* args, void* stream) {
       if (st) return st;
     }
     if (!weights) return RC_OK;
-    k_conv_weight_sum<T><<<dim3((uint32_t)cdiv((int64_t)a.width * (a.taps + 1), kSumCols)), 256, 0,
+    k_conv_weight_sum<T><<<dim3((uint32_t)weight_sum_blocks(a)), kThreads, 0,
                            (hipStream_t)stream>>>(static_cast<const float*>(a.workspace),
                                                   p.groups_t, a.width, a.taps, a.dweight, a.dbias,
                                                   a.param_dtype == RC_F32);
@@ -487,7 +492,7 @@ extern "C" int rc_conv_step(const rc_conv_step_args* args, void* stream) {
   if (!a.x.data || !a.y.data || !a.weight || (a.taps > 1 && !a.state.data)) return RC_E_ARG;
   const int V = a.width % 2 ? 1 : 2;
   const int64_t vecs = a.width / V, blocks = cdiv(vecs * a.batch, kThreads);
-  if (blocks >= kMaxBlocks) return RC_E_OVERFLOW;
+  if (!launchable(blocks, kThreads)) return RC_E_OVERFLOW;
   return by_dtype(a.dtype, [&](auto t) {
     using T = decltype(t);
     return by_taps(a.taps, [&](auto k) {

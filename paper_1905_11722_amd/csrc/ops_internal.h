@@ -105,7 +105,10 @@ inline int by_dtype(int32_t d, F&& f) {
   return f(f16{});
 }
 
-constexpr int64_t kMaxBlocks = (int64_t)1 << 31;
+// Whether a launch holds that many workgroups: its threads are fewer than 2^32.
+inline bool launchable(int64_t blocks, int threads) {
+  return blocks <= (((int64_t)1 << 32) - 1) / threads;
+}
 // Tokens and channels: indexes a few tiles past the last stay in 32 bits.
 constexpr int32_t kMaxExtent = 1 << 30;
 

@@ -977,6 +977,17 @@ ScanScratch scan_scratch(const rc_scan_args& a, const ScanPlan& p, bool backward
   return s;
 }
 
+// Workgroups of k_scan_sums: for dB and dC, for dA, for dD and ddt_bias.
+struct SumBlocks {
+  int64_t cells, a, d;
+  int64_t total() const { return cells + a + d; }
+};
+SumBlocks sum_blocks(const rc_scan_args& a, const ScanPlan& p) {
+  const int N = p.Q * p.S;
+  return {cdiv((int64_t)a.batch * a.length * a.groups * (2 * N), kSumThreads),
+          cdiv((int64_t)a.width * N, kSumCols), cdiv((int64_t)a.width * 2, kSumCols)};
+}
+
 int scan_check(const rc_scan_args* a, bool backward) {
   if (!scan_sizes_ok(a)) return RC_E_ARG;
   if (a->batch > 0 && a->width > 0) {
@@ -994,12 +1005,9 @@ int scan_check(const rc_scan_args* a, bool backward) {
       (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias)))
     return RC_E_ARG;
   const ScanPlan p = scan_plan(*a, backward);
-  const int64_t cells = (int64_t)a->batch * a->length * a->groups;
-  if (p.blocks * a->groups * a->batch * p.chunks >= kMaxBlocks ||
-      cdiv(cells * 2 * p.Q * p.S, kSumThreads) + cdiv((int64_t)a->width * p.Q * p.S, kSumCols) +
-              cdiv((int64_t)a->width * 2, kSumCols) >=
-          kMaxBlocks)
+  if (!launchable(p.blocks * a->groups * a->batch * p.chunks, channels_of(p.Q) * p.Q))
     return RC_E_OVERFLOW;
+  if (backward && !launchable(sum_blocks(*a, p).total(), kSumThreads)) return RC_E_OVERFLOW;
   return RC_OK;
 }
 
@@ -1092,8 +1100,6 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
   const ScanParams q = scan_params(a, p, need);
   const hipStream_t s = (hipStream_t)stream;
   const int64_t blocks = p.blocks * a.groups * a.batch * p.chunks;
-  const int64_t cells = (int64_t)a.batch * a.length * a.groups;
-  const int N = p.Q * p.S;
   return by_dtype(a.dtype, [&](auto t) -> int {
     using T = decltype(t);
     if (blocks > 0) {
@@ -1108,13 +1114,10 @@ extern "C" int rc_scan_backward(const rc_scan_args* args, void* stream) {
       });
       if (st) return st;
     }
-    const int64_t cell_blocks = cdiv(cells * 2 * N, kSumThreads);
-    const int64_t a_blocks = cdiv((int64_t)a.width * N, kSumCols);
-    const int64_t d_blocks = cdiv((int64_t)a.width * 2, kSumCols);
-    // (without channels dB and dC are sums of nothing)
-    if (cell_blocks + a_blocks + d_blocks == 0) return RC_OK;
-    k_scan_sums<T><<<dim3((uint32_t)(cell_blocks + a_blocks + d_blocks)), kSumThreads, 0, s>>>(
-        q, cells, N, cell_blocks, a_blocks);
+    const SumBlocks n = sum_blocks(a, p);
+    if (n.total() == 0) return RC_OK;                  // (without channels: zeros to dB and dC)
+    k_scan_sums<T><<<dim3((uint32_t)n.total()), kSumThreads, 0, s>>>(
+        q, (int64_t)a.batch * a.length * a.groups, p.Q * p.S, n.cells, n.a);
     return launched("k_scan_sums");
   });
 }
@@ -1133,7 +1136,7 @@ extern "C" int rc_scan_step(const rc_scan_step_args* args, void* stream) {
   const int64_t wide = cdiv(a.width, kStepThreads / Q * kStepRows);
   const bool many = wide * a.batch >= 8 * (int64_t)rcdp::num_cus();
   const int64_t blocks = many ? wide : cdiv(a.width, kStepThreads / Q);
-  if (blocks * a.batch >= kMaxBlocks) return RC_E_OVERFLOW;
+  if (!launchable(blocks * a.batch, kStepThreads)) return RC_E_OVERFLOW;
   return by_dtype(a.dtype, [&](auto t) {
     return by_lanes(Q, [&](auto q) {
       using T = decltype(t);
