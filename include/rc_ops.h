@@ -16,7 +16,8 @@
  *    No call synchronises, allocates or copies to the host, so every call can
  *    be captured into a graph.  Scratch is the caller's: the *_workspace
  *    calls give its size for the same arguments (its pointers are not read), and
- *    a smaller one returns RC_E_SCRATCH.
+ *    a smaller one returns RC_E_SCRATCH.  Like every 32-bit array, the scan's
+ *    kept states among them, it is aligned to 4 bytes (else RC_E_ARG).
  *  - A negative return is an error (enum rc_status of rc.h); nothing is
  *    enqueued then, except after RC_E_DEVICE.  Nothing crosses the ABI as an
  *    exception.

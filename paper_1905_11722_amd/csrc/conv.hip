@@ -406,7 +406,8 @@ int64_t weight_sum_blocks(const rc_conv_args& a) {
 
 int conv_check(const rc_conv_args* a, bool backward) {
   if (!a || !conv_sizes_ok(a->dtype, a->param_dtype, a->activation, a->batch, a->length, a->width,
-                           a->taps))
+                           a->taps) ||
+      !float_aligned(a->workspace))
     return RC_E_ARG;
   const bool some = a->batch > 0 && a->width > 0;
   if (some && !a->weight) return RC_E_ARG;

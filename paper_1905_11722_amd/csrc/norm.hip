@@ -487,7 +487,7 @@ bool norm_sizes_ok(const rc_norm_args* a) {
 }
 
 int norm_check(const rc_norm_args* a, bool backward) {
-  if (!norm_sizes_ok(a)) return RC_E_ARG;
+  if (!norm_sizes_ok(a) || !float_aligned(a->workspace)) return RC_E_ARG;
   if (a->rows > 0 && a->width > 0) {
     if (!a->residual.data) return RC_E_ARG;
     if (!a->block.data && (a->gate.data || a->post_weight || a->scale)) return RC_E_ARG;

@@ -85,6 +85,7 @@ __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 
 // ---- host side
 inline int dtype_size(int32_t d) { return d == RC_F32 ? 4 : 2; }
 inline bool dtype_ok(int32_t d) { return d >= RC_F32 && d <= RC_F16; }
+inline bool float_aligned(const void* p) { return (uintptr_t)p % sizeof(float) == 0; }
 inline bool param_ok(int32_t p, int32_t d) { return p == RC_F32 || p == d; }
 
 // The launch's own error, if any, as a status (by_dtype, before the first launch of a

@@ -301,6 +301,8 @@ struct StateTile {
   }
 };
 
+// S states of LDS, where they are aligned to their size.  (kept and the workspace are aligned to a
+// float only: load_vec and store_vec.)
 template <int S>
 __device__ __forceinline__ void read_states(const float* lds, float (&x)[S]) {
   typedef float FV __attribute__((ext_vector_type(S)));
@@ -308,15 +310,6 @@ __device__ __forceinline__ void read_states(const float* lds, float (&x)[S]) {
 #pragma unroll
   for (int i = 0; i < S; i++) x[i] = v[i];
 }
-template <int S>
-__device__ __forceinline__ void write_states(float* at, const float (&x)[S]) {
-  typedef float FV __attribute__((ext_vector_type(S)));
-  FV v;
-#pragma unroll
-  for (int i = 0; i < S; i++) v[i] = x[i];
-  *reinterpret_cast<FV*>(at) = v;
-}
-
 // The state that enters chunk `piece`, from the chunks before it (or, REVERSE, the
 // gradient of the state that leaves it, from the chunks after it).
 template <int Q, int S, bool REVERSE>
@@ -330,7 +323,7 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 #pragma unroll
     for (int k = 0; k < AHEAD; k++) {
       const int64_t at = w.b * p.chunks + first + step * min(k0 + k, count - 1);
-      read_states<S>(w.padded(p.ends, at, p), own[k]);
+      load_vec<S>(w.padded(p.ends, at, p), S, own[k]);
       sum[k] = p.steps[at * p.a.width + w.d];
     }
 #pragma unroll
@@ -438,7 +431,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
 #pragma unroll 2
     for (int i4 = 0; i4 < TILE / 4; i4++) {
       if (!ENDS && a.kept && i4 % (kKeep / 4) == 0 && w.on && t0 + 4 * i4 < a.length)
-        write_states<S>(w.padded(a.kept, w.b * p.keeps + (t0 + 4 * i4) / kKeep, p), h);
+        store_vec<S>(w.padded(a.kept, w.b * p.keeps + (t0 + 4 * i4) / kKeep, p), S, h);
       const int at = (4 * i4 + (w.q & 3)) * ROW + w.ch;
       const float2 d = lds_d[at];
       float y[4];
@@ -485,7 +478,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     total += dpp<kXor1>(total);
     total += dpp<kXor2>(total);
     if (w.on) {
-      write_states<S>(w.padded(p.ends, w.b * p.chunks + w.piece, p), h);
+      store_vec<S>(w.padded(p.ends, w.b * p.chunks + w.piece, p), S, h);
       if (w.q == 0) p.steps[(w.b * p.chunks + w.piece) * a.width + w.d] = total;
     }
   } else if (a.state_out && w.piece == p.chunks - 1) {
@@ -579,7 +572,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     at_u -= back * a.u.time;
     B.load(a.B.time, t0, a.length);
     B.p -= back * a.B.time;
-    read_states<S>(at_kept, h0);
+    load_vec<S>(at_kept, S, h0);
     at_kept -= back / TILE * a.width * N;
   };
   if (live > t_first) fetch(t_top);
@@ -744,12 +737,12 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     total += dpp<kXor1>(total);
     total += dpp<kXor2>(total);
     if (w.on) {
-      write_states<S>(w.padded(p.ends, before, p), g);
+      store_vec<S>(w.padded(p.ends, before, p), S, g);
       if (w.q == 0) p.steps[before * a.width + w.d] = total;
     }
     return;
   }
-  if (w.on) write_states<S>(w.padded(p.part_a, before, p), dA);
+  if (w.on) store_vec<S>(w.padded(p.part_a, before, p), S, dA);
   if (a.dstate_in && w.piece == 0) w.store(a.dstate_in, w.b, p, g);
   // D and dt_bias: the threads of a column, then one sum for each channel
   float* sums = reinterpret_cast<float*>(lds_d);       // [rows][channels] of (dD, dbias)
@@ -989,7 +982,7 @@ SumBlocks sum_blocks(const rc_scan_args& a, const ScanPlan& p) {
 }
 
 int scan_check(const rc_scan_args* a, bool backward) {
-  if (!scan_sizes_ok(a)) return RC_E_ARG;
+  if (!scan_sizes_ok(a) || !float_aligned(a->kept) || !float_aligned(a->workspace)) return RC_E_ARG;
   if (a->batch > 0 && a->width > 0) {
     if (!a->A) return RC_E_ARG;
     if (a->length > 0) {

@@ -1,7 +1,10 @@
 """The sequence-model operators where a caller leaves their usual ground:
 states that autograd has saved, derivatives that there are none of,
 pools that share memory or are too large, views that negate,
-no channels."""
+no channels, scratch that is aligned to
+a float and no more."""
+
+import ctypes
 
 import pytest
 import torch
@@ -13,6 +16,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_1905_11722_amd import ops  # noqa: E402
+from tests import ops_abi as abi  # noqa: E402
 
 DEV = torch.device("cuda", 0)
 
@@ -194,3 +198,46 @@ def test_scan_without_channels(groups):
         B = torch.zeros(*shape[:2], s, device=DEV, requires_grad=True)
         g, = torch.autograd.grad(ops.selective_scan(u, u, A, B, B).sum(), B)
         assert g.shape == B.shape
+
+
+@pytest.mark.parametrize("states,width", [(16, 70), (5, 64), (33, 33)])
+def test_scratch_aligned_to_a_float(states, width):
+    """Kept states and scratch 4, 8 and 12 bytes past an aligned address give the aligned ones' bits."""
+    torch.manual_seed(4)
+    b, n = 2, 300
+    lib = abi.library()
+    u, dt, z, dy = (torch.randn(b, n, width, device=DEV) for _ in range(4))
+    B, C = torch.randn(b, n, states, device=DEV), torch.randn(b, n, states, device=DEV)
+    A = -torch.rand(width, states, device=DEV)
+
+    def view(t):
+        return abi.View(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def floats(count, off):
+        """(its memory, the address of `count` floats `off` floats past an aligned one)"""
+        t = torch.zeros(count + 8, device=DEV)
+        assert t.data_ptr() % 16 == 0
+        return t, t.data_ptr() + 4 * off
+
+    def run(off):
+        out = [torch.full_like(t, 7) for t in (u, u, u, u, B, C, A)]
+        y, du, ddt, dz, dB, dC, dA = out
+        a = abi.ScanArgs(dtype=0, softplus=1, batch=b, length=n, width=width, states=states, groups=1, u=view(u),
+                         dt=view(dt), z=view(z), B=view(B), C=view(C), y=view(y), A=A.data_ptr(), dy=view(dy),
+                         du=view(du), ddt=view(ddt), dz=view(dz), dB=dB.data_ptr(), dC=dC.data_ptr(), dA=dA.data_ptr())
+        size = ctypes.c_uint64()
+        assert lib.rc_scan_kept_bytes(a, size) == 0
+        kept, a.kept = floats(size.value // 4, off)
+        stream = torch.cuda.current_stream().cuda_stream
+        for call in ("forward", "backward"):
+            assert getattr(lib, f"rc_scan_{call}_workspace")(a, size) == 0
+            work, a.workspace = floats(size.value // 4 + 1, off)
+            a.workspace_bytes = size.value
+            assert getattr(lib, "rc_scan_" + call)(a, stream) == 0
+        torch.cuda.synchronize()
+        return out
+
+    want = run(0)
+    for off in (1, 2, 3):
+        for g, w in zip(run(off), want):
+            assert torch.equal(g, w)

@@ -1,11 +1,11 @@
 """Limits of the operators' C ABI that need no GPU: sizes whose outputs are only partly empty, sizes
-beyond a launch's (fewer than 2^32 threads), which are refused before anything is enqueued."""
+beyond a launch's (fewer than 2^32 threads), which are refused before anything is enqueued, alignment."""
 
 import pytest
 
 from paper_1905_11722_amd import rcdp
 from tests import ops_abi as abi
-from tests.test_ops_host import NONE, X, conv, scan, view
+from tests.test_ops_host import NONE, X, conv, norm, scan, view
 
 
 @pytest.mark.parametrize("missing", ["dB", "dC"])
@@ -52,3 +52,12 @@ def test_tokens_beyond_a_launch():
     b = abi.ScanStepArgs(dtype=0, batch=2 ** 24, width=1, states=4, groups=1, num_slots=2 ** 24, u=view(),
                          dt=view(), B=view(), C=view(), y=view(), A=X, state=X)
     assert lib.rc_scan_step(b, None) == rcdp.E_OVERFLOW
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_scratch_and_kept_states_are_aligned_to_a_float(off):
+    lib = abi.library()
+    for call, make, names in (("conv_backward", conv, ["workspace"]), ("scan_forward", scan, ["workspace", "kept"]),
+                              ("scan_backward", scan, ["workspace", "kept"]), ("norm_backward", norm, ["workspace"])):
+        for name in names:
+            assert getattr(lib, "rc_" + call)(make(**{name: X + off}), None) == rcdp.E_ARG
