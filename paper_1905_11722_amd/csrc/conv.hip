@@ -241,14 +241,16 @@ __global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(Co
               dp[k][i] = dp[k + 1][i];
             }
             x[K - 1][i] = t < end ? (float)now.x[r][i] : 0.f;
-            dp[K - 1][i] = t < end ? (float)dnow.x[r][i] : 0.f;
+            float d = (float)dnow.x[r][i];
             if (a.activation == RC_ACT_SILU) {
               float q = bias[i];
 #pragma unroll
               for (int k = 0; k < K; k++) q = fmaf(w[k][i], x[k][i], q);
               const float s = sigmoid(q);
-              dp[K - 1][i] *= s * (1.f + q * (1.f - s));
+              d *= s * (1.f + q * (1.f - s));
             }
+            // chosen last: past the end q may come from tokens that are not finite
+            dp[K - 1][i] = t < end ? d : 0.f;
             const float own = t < t1 ? dp[K - 1][i] : 0.f;
 #pragma unroll
             for (int k = 0; k < K; k++) dw[k][i] = fmaf(own, x[k][i], dw[k][i]);

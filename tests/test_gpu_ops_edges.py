@@ -2,7 +2,7 @@
 states that autograd has saved, derivatives that there are none of,
 pools that share memory or are too large, views that negate,
 no channels, scratch that is aligned to
-a float and no more."""
+a float and no more, values that are not finite just before an end."""
 
 import ctypes
 
@@ -241,3 +241,28 @@ def test_scratch_aligned_to_a_float(states, width):
     for off in (1, 2, 3):
         for g, w in zip(run(off), want):
             assert torch.equal(g, w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("taps", [1, 4, 8])
+def test_conv_gradients_past_an_end(dtype, bad, taps):
+    """A token that is not finite just before an end: the gradients past it are 0 all the same,
+    and the other sequences' are what they were."""
+    torch.manual_seed(2)
+    x = torch.randn(3, 90, 24, device=DEV).to(dtype)
+    w, s = torch.randn(24, taps, device=DEV), torch.randn(3, taps - 1, 24, device=DEV).to(dtype)
+    n = torch.tensor([90, 41, 0], dtype=torch.int32, device=DEV)
+    dy = torch.randn(3, 90, 24, device=DEV).to(dtype)
+
+    def grads():
+        leaf = [x.clone().requires_grad_(), s.clone().requires_grad_()]
+        y, end = ops.causal_conv(leaf[0], w, state=leaf[1], lengths=n, return_state=True)
+        return torch.autograd.grad([y, end], leaf, [dy, torch.ones_like(end)])
+
+    good = grads()
+    x[1, 40], s[2] = bad, bad
+    got = grads()
+    assert torch.equal(got[0][0], good[0][0]) and torch.equal(got[1][0], good[1][0])
+    assert not got[0][1, 41:].any() and not got[0][2].any()
+    assert torch.equal(got[1][2], torch.ones_like(got[1][2]))      # an empty sequence hands it on
