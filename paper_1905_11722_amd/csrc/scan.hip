@@ -696,8 +696,9 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < WAVES; k++) s += lds_bc[k * TILE * 2 * N + e];
-        if (t0 + e / (2 * N) < t_last)
-          p.part_bc[(cell + (int64_t)(e / (2 * N)) * a.groups) * (2 * N) + e % (2 * N)] = s;
+        const int r = e / (2 * N);                     // past the end h may not be finite: chosen
+        if (t0 + r < t_last)
+          p.part_bc[(cell + (int64_t)r * a.groups) * (2 * N) + e % (2 * N)] = t0 + r < end ? s : 0.f;
       }
 #pragma unroll
       for (int k = 0; k < TileT::NV; k++) {

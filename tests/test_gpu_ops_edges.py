@@ -266,3 +266,28 @@ def test_conv_gradients_past_an_end(dtype, bad, taps):
     assert torch.equal(got[0][0], good[0][0]) and torch.equal(got[1][0], good[1][0])
     assert not got[0][1, 41:].any() and not got[0][2].any()
     assert torch.equal(got[1][2], torch.ones_like(got[1][2]))      # an empty sequence hands it on
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("states", [4, 16, 33])
+def test_scan_gradients_past_an_end(dtype, bad, states):
+    torch.manual_seed(3)
+    d = 24
+    u, dt, z, dy = (torch.randn(3, 90, d, device=DEV).to(dtype) for _ in range(4))
+    B, C = (torch.randn(3, 90, states, device=DEV).to(dtype) for _ in range(2))
+    A = -torch.rand(d, states, device=DEV)
+    n = torch.tensor([90, 41, 0], dtype=torch.int32, device=DEV)
+
+    def grads():
+        leaf = [t.clone().requires_grad_() for t in (u, dt, B, C, z)]
+        y = ops.selective_scan(leaf[0], leaf[1], A, leaf[2], leaf[3], z=leaf[4], softplus=True, lengths=n)
+        return y, torch.autograd.grad(y, leaf, dy)
+
+    _, good = grads()
+    u[1, 40] = bad
+    y, got = grads()
+    assert not y[1, 41:].any() and not y[2].any()
+    for name, a, b in zip("u dt B C z".split(), good, got):
+        assert torch.equal(a[0], b[0]), name
+        assert not b[1, 41:].any() and not b[2].any(), name
