@@ -201,9 +201,17 @@ __global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(Co
     const int c = min((int)c64, a.width - V);
     const int b = (int)(cell / p.runs), t0 = (int)(cell % p.runs) * p.run;
     const int t1 = min(t0 + p.run, a.length), end = seq_end(a.lengths, b, a.length);
-    if (t0 > 0 && t0 >= end) {                         // past the end: zeros, no gradients
+    if (t0 >= end) {                                   // past the end: zeros, no gradients
       const float zero[V] = {};
       for (int t = t0; t < t1; t++) store_vec<V>(at<T>(a.dx, b, t, c), V, zero);
+      if (t0 == 0 && a.dstate_in.data) {               // no token: the state's gradient is handed on
+#pragma unroll
+        for (int k = 0; k < K - 1; k++) {
+          float ds[V] = {};
+          if (a.dstate_out.data) load_vec<V>(at<T>(a.dstate_out, b, k, c), V, ds);
+          store_vec<V>(at<T>(a.dstate_in, b, k, c), V, ds);
+        }
+      }
     } else {
       // row t finishes dx of row t - (K - 1); the first run also writes the
       // state's rows -(K - 1) .. -1
@@ -214,22 +222,14 @@ __global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(Co
       for (int k = 0; k < K; k++)
 #pragma unroll
         for (int i = 0; i < V; i++) dp[k][i] = x[k][i] = 0.f;
-      if (end > 0) {
 #pragma unroll
-        for (int k = 0; k < K - 1; k++)
-          input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
-      }
-      const bool any = end > 0;
+      for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
       Rows<T, V> now, next, dnow, dnext;
-      if (any) {
-        now.load(a.x, b, t0, end, c);
-        dnow.load(a.dy, b, t0, end, c);
-      }
+      now.load(a.x, b, t0, end, c);
+      dnow.load(a.dy, b, t0, end, c);
       for (int g = t0; g < t1 + K - 1; g += kRows) {
-        if (any) {
-          next.load(a.x, b, g + kRows, end, c);
-          dnext.load(a.dy, b, g + kRows, end, c);
-        }
+        next.load(a.x, b, g + kRows, end, c);
+        dnext.load(a.dy, b, g + kRows, end, c);
 #pragma unroll
         for (int r = 0; r < kRows; r++) {
           const int t = g + r;

@@ -2,7 +2,8 @@
 states that autograd has saved, derivatives that there are none of,
 pools that share memory or are too large, views that negate,
 no channels, scratch that is aligned to
-a float and no more, values that are not finite just before an end."""
+a float and no more, values that are not finite just before an end,
+the long walks that large inputs take."""
 
 import ctypes
 
@@ -17,8 +18,19 @@ if not torch.cuda.is_available():
 
 from paper_1905_11722_amd import ops  # noqa: E402
 from tests import ops_abi as abi  # noqa: E402
+from tests.test_gpu_ops import F32_NOISE, ROUND  # noqa: E402
 
 DEV = torch.device("cuda", 0)
+
+
+def close(got, want, what):
+    """The bound of tests/test_gpu_ops.py, which says where it comes from, on the GPU."""
+    assert got.shape == want.shape, what
+    w = want.detach()
+    rms = w.square().mean().sqrt()
+    bound = 1.01 * ROUND[got.dtype] * w.abs() + F32_NOISE * torch.maximum(rms, w.abs()) + 2.0 ** -25
+    worst = ((got.detach().double() - w).abs() / bound).max().item()
+    assert worst <= 1, f"{what}: {worst:.2f} times the bound"          # (and no NaN)
 
 
 def token(op, pool, slots=None):
@@ -291,3 +303,44 @@ def test_scan_gradients_past_an_end(dtype, bad, states):
     for name, a, b in zip("u dt B C z".split(), good, got):
         assert torch.equal(a[0], b[0]), name
         assert not b[1, 41:].any() and not b[2].any(), name
+
+
+def conv_definition(x, w, bias, state, n):
+    """y and the final state in 64 bits on the GPU; tokens past the ends are zeros in x."""
+    taps, length = w.shape[1], x.shape[1]
+    seen = torch.cat([state, x], 1)
+    p = bias + sum(w[:, k] * seen[:, k:k + length] for k in range(taps))
+    live = torch.arange(length, device=DEV)[None, :, None] < n[:, None, None]
+    at = (n[:, None] + torch.arange(taps - 1, device=DEV)).long()[:, :, None].expand(-1, -1, x.shape[2])
+    return torch.where(live, p * torch.sigmoid(p), 0.0), torch.gather(seen, 1, at)
+
+
+@pytest.mark.parametrize("dtype,taps", [(torch.float32, k) for k in range(1, 9)]
+                         + [(torch.bfloat16, 4), (torch.bfloat16, 5), (torch.float16, 8)])
+def test_conv_long_walks(dtype, taps):
+    """Enough rows that a thread walks over 16 forward and 32 backward, in groups that are loaded
+    ahead (256 compute units); an odd width, sequences that end inside a walk, one without a token."""
+    rng = torch.Generator(device=DEV).manual_seed(taps)
+    b, length, d = 9, 2047, 2051
+
+    def normal(*shape, t=dtype):
+        return torch.randn(shape, generator=rng, device=DEV).to(t)
+
+    n = torch.tensor([2047, 0, 1, 1023, 2046, 1500, 40, 2047, 7], dtype=torch.int32, device=DEV)
+    dead = torch.arange(length, device=DEV)[None, :, None] >= n[:, None, None]
+    x, dy, state = normal(b, length, d).masked_fill(dead, float("nan")), normal(b, length, d), normal(b, taps - 1, d)
+    w, bias = normal(d, taps, t=torch.float32) * 0.5, normal(d, t=torch.float32) * 0.3
+    dend = normal(b, taps - 1, d)
+    leaf = [t.requires_grad_() for t in (x, w, bias, state)]
+    y, end = ops.causal_conv(x, w, bias, state=state, lengths=n, return_state=True)
+    got = torch.autograd.grad([y, end], leaf, [dy, dend])
+    wide = [t.detach().double().masked_fill(dead, 0.0) if t is x else t.detach().double() for t in leaf]
+    wide = [t.requires_grad_() for t in wide]
+    wy, wend = conv_definition(*wide, n)
+    want = torch.autograd.grad([wy, wend], wide, [dy.double(), dend.double()])
+    close(y, wy, "y")
+    if taps > 1:
+        close(end, wend, "state")
+    for name, g, v in zip(("dx", "dweight", "dbias", "dstate"), got, want):
+        if g.numel():
+            close(g, v, name)
