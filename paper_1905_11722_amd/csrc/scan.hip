@@ -375,11 +375,14 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
   typename TileT::Raw u[TileT::NV], dt[TileT::NV], z[TileT::NV] = {};
   StateTile<T, N, TILE, CW * Q> B, C;
   const T *at_u = tile.start(a.u, w.b, t_first), *at_dt = tile.start(a.dt, w.b, t_first);
-  const T* at_z = tile.start(a.z, w.b, t_first);
+  // Loads are not in branches whose results the loop hands on (the compiler of ROCm 7.2 drops some
+  // of their elements): without a gate dt is read twice.
+  const bool gated = a.z.data;
+  const rc_view from_z = gated ? a.z : a.dt;
+  const T* at_z = tile.start(from_z, w.b, t_first);
   T* at_y = tile.start(a.y, w.b, t_first);
   B.start(a.B, w.g * a.B_group, w.b, t_first, a.states);
   C.start(a.C, w.g * a.C_group, w.b, t_first, a.states);
-  const bool gated = a.z.data;
   const auto fetch = [&](int t0) {                     // and on to the next tile
     tile.load(at_u, a.u.time, t0, a.length, u);
     tile.load(at_dt, a.dt.time, t0, a.length, dt);
@@ -388,8 +391,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     B.load(a.B.time, t0, a.length);
     B.p += TILE * a.B.time;
     if (ENDS) return;
-    if (gated) tile.load(at_z, a.z.time, t0, a.length, z);
-    at_z += TILE * a.z.time;
+    tile.load(at_z, from_z.time, t0, a.length, z);
+    at_z += TILE * from_z.time;
     C.load(a.C.time, t0, a.length);
     C.p += TILE * a.C.time;
   };
@@ -534,6 +537,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   StateTile<T, N, TILE, THREADS> B, C;
   float h0[S];
   const bool gated = a.z.data;
+  const rc_view from_z = gated ? a.z : a.dt;           // as forward
   // tiles past the end: zeros
   const int live = t_first + (int)cdiv(max(0, min(t_last, end) - t_first), TILE) * TILE;
   if (!ENDS) {
@@ -551,7 +555,7 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
   // from the last live tile back; the first one is fetched twice
   const int t_top = max(live - TILE, t_first);
   const T *at_u = tile.start(a.u, w.b, t_top), *at_dt = tile.start(a.dt, w.b, t_top);
-  const T *at_z = tile.start(a.z, w.b, t_top), *at_dy = tile.start(a.dy, w.b, t_top);
+  const T *at_z = tile.start(from_z, w.b, t_top), *at_dy = tile.start(a.dy, w.b, t_top);
   T *at_du = tile.start(a.du, w.b, t_top), *at_ddt = tile.start(a.ddt, w.b, t_top);
   T* at_dz = tile.start(a.dz, w.b, t_top);
   const float* at_kept = w.padded(a.kept, w.b * p.keeps + t_top / TILE, p);
@@ -561,8 +565,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     const int64_t back = t0 > t_first ? TILE : 0;
     tile.load(at_dt, a.dt.time, t0, a.length, dt);
     at_dt -= back * a.dt.time;
-    if (gated) tile.load(at_z, a.z.time, t0, a.length, z);
-    at_z -= back * a.z.time;
+    tile.load(at_z, from_z.time, t0, a.length, z);
+    at_z -= back * from_z.time;
     tile.load(at_dy, a.dy.time, t0, a.length, dout);
     at_dy -= back * a.dy.time;
     C.load(a.C.time, t0, a.length);

@@ -18,7 +18,8 @@ if not torch.cuda.is_available():
 
 from paper_1905_11722_amd import ops  # noqa: E402
 from tests import ops_abi as abi  # noqa: E402
-from tests.test_gpu_ops import F32_NOISE, ROUND  # noqa: E402
+from tests.test_gpu_ops import (F32_NOISE, ROUND, check, compare_grads, run_scan,  # noqa: E402
+                                scan_inputs)
 
 DEV = torch.device("cuda", 0)
 
@@ -344,3 +345,23 @@ def test_conv_long_walks(dtype, taps):
     for name, g, v in zip(("dx", "dweight", "dbias", "dstate"), got, want):
         if g.numel():
             close(g, v, name)
+
+
+@pytest.mark.parametrize("batch,length,width,states,groups", [
+    (3, 300, 20, 16, 1), (3, 90, 70, 4, 1), (2, 150, 6, 8, 2), (2, 130, 36, 24, 1), (2, 100, 21, 40, 1),
+    (260, 40, 40, 16, 1)])
+def test_scan_without_a_gate(batch, length, width, states, groups):
+    """No z, in 32 bits: one chunk and several, sequences that end inside a tile or have no token."""
+    x = scan_inputs("f32", batch, length, width, states, groups, "Dbs")
+    ends = [length, length - 23, 0][:batch] + [length] * (batch - 3)
+    n = torch.tensor(ends, dtype=torch.int32, device=DEV)
+    with torch.no_grad():
+        for name in ("u", "dt", "B", "C"):
+            for i, e in enumerate(ends):
+                x.gpu[name][i, e:] = float("nan")
+                x.cpu[name][i, e:] = 0
+    x.grads()
+    outs, wants = run_scan(x, ends, n)
+    check(outs[0], wants[0], "y")
+    check(outs[1], wants[1], "state")
+    compare_grads(x, outs, wants)
