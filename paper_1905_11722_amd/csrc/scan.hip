@@ -396,18 +396,10 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
     C.load(a.C.time, t0, a.length);
     C.p += TILE * a.C.time;
   };
-  if (t_first < min(t_last, end)) fetch(t_first);
-  for (int t0 = t_first; t0 < t_last; t0 += TILE, at_y += TILE * a.y.time) {
-    if (t0 >= end) {                                   // nothing but zeros from here on
-      if (!ENDS && tile.on) {
-        const float zero[VEC] = {};
-#pragma unroll
-        for (int k = 0; k < TileT::NV; k++)
-          if (t0 + k * TileT::rows + tile.r < t_last)
-            store_vec<VEC>(at_y + k * TileT::rows * a.y.time, VEC, zero);
-      }
-      continue;
-    }
+  const int live = min(t_last, end);                   // tiles from here on are zeros
+  int t0 = t_first;
+  if (t0 < live) fetch(t0);
+  for (; t0 < live; t0 += TILE, at_y += TILE * a.y.time) {
 #pragma unroll
     for (int k = 0; k < TileT::NV; k++) {
       const int r = k * TileT::rows + tile.r;
@@ -476,6 +468,13 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
       }
     }
     // a wave stages the elements whose outputs it has just read
+  }
+  for (; !ENDS && t0 < t_last; t0 += TILE, at_y += TILE * a.y.time) {
+    const float zero[VEC] = {};
+#pragma unroll
+    for (int k = 0; k < TileT::NV; k++)
+      if (tile.on && t0 + k * TileT::rows + tile.r < t_last)
+        store_vec<VEC>(at_y + k * TileT::rows * a.y.time, VEC, zero);
   }
   if (ENDS) {
     total += dpp<kXor1>(total);
@@ -579,8 +578,9 @@ __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanPar
     load_vec<S>(at_kept, S, h0);
     at_kept -= back / TILE * a.width * N;
   };
-  if (live > t_first) fetch(t_top);
-  for (int t0 = live - TILE; t0 >= t_first; t0 -= TILE) {
+  int t0 = live - TILE;
+  if (t0 >= t_first) fetch(t0);
+  for (; t0 >= t_first; t0 -= TILE) {
     float step[TileT::NV][VEC];                        // delta of the thread's elements
 #pragma unroll
     for (int k = 0; k < TileT::NV; k++) {
