@@ -5,7 +5,8 @@
 // Each value is used K times and each output needs ~2K + 6 operations for 4
 // bytes moved (16-bit types), so the bound is memory.  A thread owns V
 // neighbouring channels (one wide load per row) and a run of rows, and keeps
-// the last K - 1 rows in registers: x is read once plus K - 1 rows per run.
+// the last K - 1 rows in registers: x is read once plus K - 1 rows per run
+(backward 2 K - 2, and K - 1 of dy).
 // Where V does not divide the width, the last thread of a row moves back to
 // the last V channels; it and its neighbour store the same values where they
 // overlap.  (Odd widths with V = 1 instead: 8 x 2047 x 2049 in bfloat16
@@ -73,17 +74,17 @@ __device__ __forceinline__ void input_row(const rc_conv_args& a, int b, int t, i
   load_if<T, V>(p, t < 0 ? state : t < end, x);
 }
 
-// Rows of a thread that are loaded together, one group ahead of their use: rows t ..
-// of a sequence with a token, clamped to its last.
+// Rows of a thread that are loaded together, one group ahead of their use: rows t ..,
+// those from `stop` > 0 on row stop - 1 again, so that a walk reads no row past its last.
 constexpr int kRows = 4;
 template <class T, int V>
 struct Rows {
   typedef T Raw __attribute__((ext_vector_type(V)));
   Raw x[kRows];
-  __device__ __forceinline__ void load(const rc_view& v, int b, int t, int end, int c) {
+  __device__ __forceinline__ void load(const rc_view& v, int b, int t, int stop, int c) {
 #pragma unroll
     for (int j = 0; j < kRows; j++)
-      __builtin_memcpy(&x[j], at<T>(v, b, min(t + j, end - 1), c), sizeof(Raw));
+      __builtin_memcpy(&x[j], at<T>(v, b, min(t + j, stop - 1), c), sizeof(Raw));
   }
 };
 
@@ -145,9 +146,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
     for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
     const int stop = min(t1, end);
     Rows<T, V> now, next;
-    now.load(a.x, b, t, end, c);
+    now.load(a.x, b, t, stop, c);
     for (; t < stop; t += kRows) {
-      next.load(a.x, b, t + kRows, end, c);
+      next.load(a.x, b, t + kRows, stop, c);
 #pragma unroll
       for (int j = 0; j < kRows; j++) {
         float y[V];
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
         for (int i = 0; i < V; i++) {
 #pragma unroll
           for (int k = 0; k < K - 1; k++) x[k][i] = x[k + 1][i];
-          x[K - 1][i] = t + j < end ? (float)now.x[j][i] : 0.f;
+          x[K - 1][i] = (float)now.x[j][i];
           y[i] = bias[i];
 #pragma unroll
           for (int k = 0; k < K; k++) y[i] = fmaf(w[k][i], x[k][i], y[i]);
@@ -225,11 +226,12 @@ __global__ __launch_bounds__(kThreads, conv_waves<T>(K)) void k_conv_backward(Co
 #pragma unroll
       for (int k = 0; k < K - 1; k++) input_row<T, K, V>(a, b, t0 - (K - 1) + k, end, c, x[k + 1]);
       Rows<T, V> now, next, dnow, dnext;
-      now.load(a.x, b, t0, end, c);
-      dnow.load(a.dy, b, t0, end, c);
+      const int stop = min(t1 + K - 1, end);
+      now.load(a.x, b, t0, stop, c);
+      dnow.load(a.dy, b, t0, stop, c);
       for (int g = t0; g < t1 + K - 1; g += kRows) {
-        next.load(a.x, b, g + kRows, end, c);
-        dnext.load(a.dy, b, g + kRows, end, c);
+        next.load(a.x, b, g + kRows, stop, c);
+        dnext.load(a.dy, b, g + kRows, stop, c);
 #pragma unroll
         for (int r = 0; r < kRows; r++) {
           const int t = g + r;
