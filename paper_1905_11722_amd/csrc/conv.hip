@@ -6,7 +6,7 @@
 // bytes moved (16-bit types), so the bound is memory.  A thread owns V
 // neighbouring channels (one wide load per row) and a run of rows, and keeps
 // the last K - 1 rows in registers: x is read once plus K - 1 rows per run
-(backward 2 K - 2, and K - 1 of dy).
+// (backward 2 K - 2, and K - 1 of dy).
 // Where V does not divide the width, the last thread of a row moves back to
 // the last V channels; it and its neighbour store the same values where they
 // overlap.  (Odd widths with V = 1 instead: 8 x 2047 x 2049 in bfloat16
