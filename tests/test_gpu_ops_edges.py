@@ -18,6 +18,7 @@ if not torch.cuda.is_available():
 
 from paper_1905_11722_amd import ops  # noqa: E402
 from tests import ops_abi as abi  # noqa: E402
+from tests import ops_reference as ref  # noqa: E402
 from tests.test_gpu_ops import (F32_NOISE, ROUND, check, compare_grads, run_scan,  # noqa: E402
                                 scan_inputs)
 
@@ -365,3 +366,70 @@ def test_scan_without_a_gate(batch, length, width, states, groups):
     check(outs[0], wants[0], "y")
     check(outs[1], wants[1], "state")
     compare_grads(x, outs, wants)
+
+
+@pytest.mark.parametrize("dtype,wide,width,gate", [
+    (torch.bfloat16, True, 9001, True), (torch.float16, False, 9001, False), (torch.float32, True, 16384, True),
+    (torch.bfloat16, False, 12288, True)])
+def test_norm_long_walks(dtype, wide, width, gate):
+    """Above 8192 channels with more rows than twice the compute units, so that each workgroup adds
+    several rows' weight gradients, those in LDS among them, and the first of the rows to the last."""
+    rng = torch.Generator(device=DEV).manual_seed(7)
+    rows, rt = 1100, torch.float32 if wide else dtype
+
+    def normal(*shape, t=dtype, scale=1.0):
+        return (torch.randn(shape, generator=rng, device=DEV) * scale).to(t)
+
+    def weight():
+        return torch.rand(width, generator=rng, device=DEV) + 0.3
+
+    args = [normal(rows, width), normal(rows, width, t=rt, scale=2.0), normal(rows, width) if gate else None,
+            weight(), weight(), weight()]
+    dout, dnormed = normal(rows, width, t=rt), normal(rows, width)
+    args[0][5] = 0
+    leaf = [t.requires_grad_() if t is not None else None for t in args]
+    got = ops.norm_residual(*leaf)
+    grads = torch.autograd.grad(got, [t for t in leaf if t is not None], [dout, dnormed])
+    far = [t.detach().double().requires_grad_() if t is not None else None for t in leaf]
+    want = ref.norm_residual(*far)
+    wants = torch.autograd.grad(want, [t for t in far if t is not None], [dout.double(), dnormed.double()])
+    names = [k for k, t in zip(("block", "residual", "gate", "post", "scale", "pre"), leaf) if t is not None]
+    for k, g, w in zip(("out", "normed"), got, want):
+        close(g, w, k)
+    for k, g, w in zip(names, grads, wants):
+        close(g, w, "d" + k)
+
+
+@pytest.mark.parametrize("dtype,batch,width,states,groups", [
+    (torch.bfloat16, 700, 1090, 16, 1), (torch.float32, 1100, 270, 16, 2), (torch.float16, 1030, 129, 40, 1),
+    (torch.float32, 2100, 700, 3, 1)])
+def test_scan_step_of_many_rows(dtype, batch, width, states, groups):
+    """Two channels a thread (eight workgroups a compute unit and more), the second of them past the
+    width for some; rows that are padding."""
+    rng = torch.Generator(device=DEV).manual_seed(states)
+
+    def normal(*shape, t=dtype, scale=1.0):
+        return (torch.randn(shape, generator=rng, device=DEV) * scale).to(t)
+
+    u, dt, z = normal(batch, width), normal(batch, width, scale=0.5), normal(batch, width)
+    B, C = normal(batch, groups, states), normal(batch, groups, states)
+    A = -torch.rand(width, states, generator=rng, device=DEV) * states - 0.3
+    D, bias = normal(width, t=torch.float32), normal(width, t=torch.float32) - 3
+    pool = normal(batch + 9, width, states, t=torch.float32)
+    slots = torch.randperm(batch + 9, generator=rng, device=DEV)[:batch].to(torch.int32)
+    slots[::50] = -1
+    before = pool.double()
+    y = ops.selective_scan_step(pool, u, dt, A, B, C, D, z, bias, softplus=True, slots=slots)
+    on, at = slots >= 0, slots[slots >= 0].long()
+    group = torch.arange(width, device=DEV) // (width // groups)
+    raw = dt.double()[on] + bias.double()
+    delta = torch.logaddexp(raw, torch.zeros_like(raw))
+    h = (torch.exp(delta[..., None] * A.double()) * before[at]
+         + (delta * u.double()[on])[..., None] * B.double()[on][:, group])
+    want = torch.zeros(batch, width, dtype=torch.float64, device=DEV)
+    want[on] = ((h * C.double()[on][:, group]).sum(-1) + D.double() * u.double()[on]) * ref.silu(z.double()[on])
+    after = before.clone()
+    after[at] = h
+    close(y, want, "y")
+    close(pool, after, "state")
+    assert not y[~on].any()
