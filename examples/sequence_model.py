@@ -6,13 +6,14 @@ scan with a gate, projection back, and the norms after this block and before
 the next one.  Its operators come from ``paper_1905_11722_amd.ops``, its plain
 matrix products from PyTorch.
 
-The training step is planned by ``paper_1905_11722_amd.rcdp``: every
-activation of the step is a node with its forward time (counted, in tenths of
-a microsecond) and its size (in KiB); for a budget the solver returns the
-chain of lower sets of least recomputation overhead, and the step runs its
-canonical strategy (Section 3 of Kusumoto et al.): after each segment only the
-activations on its boundary stay, and in the backward pass each segment is
-computed again from them.  The gradients are those of the plain step.
+The training step is planned by ``paper_1905_11722_amd.rcdp``: every operation
+of the step is a node with its forward time (counted, in tenths of a microsecond) and
+the size of its result (in KiB); for a budget the solver returns the chain
+of lower sets of least recomputation overhead, and the step runs its
+canonical strategy (Section 3 of Kusumoto et al.): forward, the nodes on a segment's boundary
+stay; in the backward pass each segment's other nodes are computed again from them.
+(Those of the last segment need not be, though Eq. 1 counts them.)  The
+gradients are those of the plain step.
 
 Then the model reads a prompt and goes on token by token with the single-token forms,
 from the states that the prompt left.
@@ -32,7 +33,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_1905_11722_amd import ops, rcdp, workloads  # noqa: E402
 
-NODES = ("project", "conv", "steps", "scan", "back", "join")      # of a block, in order
+NODES = ("project", "conv", "steps", "delta", "scan", "back", "join")      # of a block, in order
 
 
 class Model:
@@ -70,19 +71,33 @@ class Model:
     def parameters(self):
         return [t for block in self.p for t in block.values()] + [self.first]
 
+    @property
+    def nodes(self):
+        """Nodes of a step: the first norm, the blocks', the loss."""
+        return self.blocks * len(NODES) + 2
+
+    def place(self, node):
+        """(block, kind) of a node; "start" and "loss" belong to no block."""
+        if node in (0, self.nodes - 1):
+            return None, "loss" if node else "start"
+        block, kind = divmod(node - 1, len(NODES))
+        return block, NODES[kind]
+
+    def owned(self, node):
+        """The parameters that a node takes."""
+        block, kind = self.place(node)
+        names = {"project": ["project"], "conv": ["conv", "conv_bias"], "steps": ["steps"], "delta": ["dt"],
+                 "scan": ["dt_bias", "A", "D"], "back": ["back"], "join": ["post", "scale", "pre"]}
+        return [self.first] if kind == "start" else [self.p[block][k] for k in names.get(kind, [])]
+
     def start(self, x):
         """(residual stream, normed) of the input."""
         return ops.norm_residual(None, x, pre_weight=self.first)
 
-    def split(self, p, steps):
-        """The scan's dt, B and C from the node ``steps``."""
-        dt = steps[..., :self.rank] @ p["dt"]
-        return dt, steps[..., self.rank:self.rank + self.states], steps[..., self.rank + self.states:]
-
     def run(self, block, kind, values, state=None):
-        """The value of a node from its predecessors' (with ``state``, the
+        """The value of a block's node from its predecessors' (with ``state``, the
         states of a prompt or of one token, in the order of `predecessors`)."""
-        p = self.p[block]
+        p, rank, n = self.p[block], self.rank, self.states
         if kind == "project":
             return values[0][1] @ p["project"]
         if kind == "conv":
@@ -92,9 +107,11 @@ class Model:
             return ops.causal_conv_step(state[0], x, p["conv"], p["conv_bias"])
         if kind == "steps":
             return values[0] @ p["steps"]
+        if kind == "delta":
+            return values[0][..., :rank] @ p["dt"]
         if kind == "scan":
-            u, steps, z = values[0], values[1], values[2][..., self.inner:]
-            dt, B, C = self.split(p, steps)
+            u, steps, dt, z = *values[:3], values[3][..., self.inner:]
+            B, C = steps[..., rank:rank + n], steps[..., rank + n:]
             if state is None:
                 return ops.selective_scan(u, dt, p["A"], B, C, p["D"], z, p["dt_bias"], softplus=True)
             return ops.selective_scan_step(state[1], u, dt, p["A"], B, C, p["D"], z, p["dt_bias"],
@@ -105,144 +122,176 @@ class Model:
                                  pre_weight=p["pre"])
 
     def predecessors(self, node):
-        """Nodes whose values the node takes (-1: the model's input)."""
-        block, kind = divmod(node, len(NODES))
-        first = block * len(NODES)
-        return {"project": [first - 1], "conv": [first], "steps": [first + 1],
-                "scan": [first + 1, first + 2, first], "back": [first + 3],
-                "join": [first + 4, first - 1]}[NODES[kind]]
+        """Nodes whose values the node takes."""
+        block, kind = self.place(node)
+        if block is None:
+            return [node - 1] if node else []
+        first = 1 + block * len(NODES)
+        return {"project": [first - 1], "conv": [first], "steps": [first + 1], "delta": [first + 2],
+                "scan": [first + 1, first + 2, first + 3, first], "back": [first + 4],
+                "join": [first + 5, first - 1]}[kind]
 
-    def node(self, node, get, state=None):
-        block, kind = divmod(node, len(NODES))
-        return self.run(block, NODES[kind], [get(v) for v in self.predecessors(node)],
-                        None if state is None else state[block])
+    def node(self, node, get, x=None, dy=None, state=None):
+        """The value of a node of a step on input x with the loss <output, dy>."""
+        block, kind = self.place(node)
+        if kind == "start":
+            return self.start(x)
+        values = [get(v) for v in self.predecessors(node)]
+        if kind == "loss":
+            return (values[0][1] * dy).sum(dtype=torch.float32)
+        return self.run(block, kind, values, None if state is None else state[block])
 
     def graph(self, batch, length):
-        """The step's activations with their times and sizes (workloads.Graph)."""
+        """The step's nodes with their times and sizes (workloads.Graph)."""
         tokens, e = batch * length, torch.finfo(self.dtype).bits // 8
         w, i, n = self.width, self.inner, self.states
         s = self.rank + 2 * n
         # (values of the result, values moved, operations) of a token
-        count = {"project": (2 * i, w + 2 * i, 4 * w * i), "conv": (i, 2 * i, 16 * i),
-                 "steps": (s, i + s, 2 * i * s), "scan": (i, 4 * i + 2 * n, 40 * i * n),
-                 "back": (w, i + w, 2 * i * w), "join": (2 * w, 4 * w, 12 * w)}
-        T, M, names = [], [], []
-        for b in range(self.blocks):
-            for kind in NODES:
-                size, moved, flops = (v * tokens for v in count[kind])
-                rate = 6e14 if kind in ("project", "steps", "back") else 3e13
-                seconds = max(moved * e / 4e12, flops / rate) + 4e-6
-                T.append(max(1, round(seconds * 1e7)))
-                M.append(max(1, size * e // 1024))
-                names.append(f"{kind}{b}")
-        succ = [[] for _ in names]
-        for v in range(len(names)):
+        count = {"start": (w, 2 * w, 4 * w), "project": (2 * i, w + 2 * i, 4 * w * i), "conv": (i, 2 * i, 16 * i),
+                 "steps": (s, i + s, 2 * i * s), "delta": (i, self.rank + i, 2 * self.rank * i),
+                 "scan": (i, 4 * i + 2 * n, 40 * i * n), "back": (w, i + w, 2 * i * w),
+                 "join": (2 * w, 4 * w, 12 * w), "loss": (0, 2 * w, 2 * w)}
+        cost = {}
+        for kind in count:
+            size, moved, flops = (v * tokens for v in count[kind])
+            rate = 6e14 if kind in ("project", "steps", "delta", "back") else 3e13
+            seconds = max(moved * e / 4e12, flops / rate) + 4e-6
+            cost[kind] = max(1, round(seconds * 1e7)), max(1, size * e // 1024)
+        places = [self.place(v) for v in range(self.nodes)]
+        succ = [[] for _ in places]
+        for v in range(self.nodes):
             for u in self.predecessors(v):
-                if u >= 0:
-                    succ[u].append(v)
-        return workloads.Graph(len(names), [sorted(x) for x in succ], T, M, names, list(NODES) * self.blocks)
-
-
-def _leaf(value):
-    """A value cut from its past, with gradients of its own."""
-    if isinstance(value, tuple):
-        return tuple(t.detach().requires_grad_() for t in value)
-    return value.detach().requires_grad_()
+                succ[u].append(v)
+        kinds = [kind for _, kind in places]
+        return workloads.Graph(self.nodes, [sorted(x) for x in succ], [cost[k][0] for k in kinds],
+                               [cost[k][1] for k in kinds],
+                               [k if b is None else f"{k}{b}" for b, k in places], kinds)
 
 
 def _tensors(value):
     return list(value) if isinstance(value, tuple) else [value]
 
 
-def plain_step(model, x, dy):
-    """Loss <output, dy> and the parameters' gradients, everything kept."""
-    values = {-1: model.start(x)}
-    for v in range(model.blocks * len(NODES)):
-        values[v] = model.node(v, values.__getitem__)
-    loss = (values[v][1].float() * dy).sum()
-    return loss.detach(), torch.autograd.grad(loss, model.parameters(), allow_unused=True)
+class _Port(torch.autograd.Function):
+    """A predecessor's value on its way into a node: its gradient goes to
+    ``grads``, and the node's graph holds nothing of the value itself."""
+
+    @staticmethod
+    def forward(ctx, token, value, grads, index):
+        ctx.grads, ctx.index = grads, index
+        return value.view_as(value)
+
+    @staticmethod
+    def backward(ctx, g):
+        old = ctx.grads[ctx.index]
+        ctx.grads[ctx.index] = g if old is None else old + g
+        return None, None, None, None
 
 
-def planned_step(model, x, dy, schedule):
-    """The same through the canonical strategy of a schedule (rcdp.Schedule):
-    forward, the values on a segment's boundary stay; backward, each segment
-    is computed again from them.  (Autograd records a segment as it is computed
-    again, so its own boundary nodes are computed again too.)"""
-    last = int(schedule.seg.max())
-    segments = [[] for _ in range(last + 1)]
-    for v, s in enumerate(schedule.seg):
-        segments[int(s)].append(v)
-    params = model.parameters()
-    total = [None] * len(params)
-    kept = {}
-    with torch.no_grad():
-        kept[-1] = model.start(x)
-        for nodes in segments[:-1]:
-            inside = {}
-            for v in nodes:
-                inside[v] = model.node(v, lambda u: inside[u] if u in inside else kept[u])
-            kept.update({v: inside[v] for v in nodes if schedule.cached[v]})
-            del inside
-    grads, loss = {}, None
-    for k in range(last, -1, -1):
-        nodes, leaves, inside = segments[k], {}, {}
+class Step:
+    """A training step whose nodes run one by one, each with an autograd graph
+    of its own.  What a graph has to keep of its predecessors' values it takes
+    from ``values`` in the backward pass, so that they may be dropped and
+    computed again in between; what else it keeps is the node's."""
+
+    def __init__(self, model, x, dy):
+        self.model, self.x, self.dy = model, x, dy
+        self.values, self.grads, self.params = {}, {}, {}
+        self.runs = [0] * model.nodes
+        self.token = torch.zeros((), device=x.device, requires_grad=True)
+
+    def forward(self, v, record):
+        """Run a node; with ``record`` so that `backward` can follow."""
+        self.runs[v] += 1
+        if not record:
+            with torch.no_grad():
+                self.values[v] = self.model.node(v, self.values.__getitem__, self.x, self.dy)
+            return
+        where = {t.untyped_storage().data_ptr(): (u, i) for u in self.model.predecessors(v)
+                 for i, t in enumerate(_tensors(self.values[u]))}
+
+        def pack(t):
+            at = where.get(t.untyped_storage().data_ptr())
+            if at is None:
+                return t
+            base = _tensors(self.values[at[0]])[at[1]]
+            return at, t.size(), t.stride(), t.storage_offset() - base.storage_offset()
+
+        def unpack(packed):
+            if isinstance(packed, torch.Tensor):
+                return packed
+            (u, i), size, stride, offset = packed
+            base = _tensors(self.values[u])[i].detach()
+            return base.as_strided(size, stride, base.storage_offset() + offset)
 
         def get(u):
-            if u in inside:
-                return inside[u]
-            if u not in leaves:
-                leaves[u] = model.start(x) if u == -1 and k == 0 else _leaf(kept[u])
-            return leaves[u]
+            value = self.values[u]
+            grads = self.grads.setdefault(u, [None] * len(_tensors(value)))
+            ports = tuple(t if t.data_ptr() == self.x.data_ptr() else _Port.apply(self.token, t.detach(), grads, i)
+                          for i, t in enumerate(_tensors(value)))
+            return ports if isinstance(value, tuple) else ports[0]
 
+        with torch.enable_grad(), torch.autograd.graph.saved_tensors_hooks(pack, unpack):
+            self.values[v] = self.model.node(v, get, self.x, self.dy)
+
+    def backward(self, v):
+        """Gradients of a recorded node's predecessors and parameters; its value goes."""
+        outs = [(t, g) for t, g in zip(_tensors(self.values[v]), self.grads.pop(v)) if g is not None]
+        owned = self.model.owned(v)
+        got = torch.autograd.grad([t for t, _ in outs], owned + [self.token], [g for _, g in outs],
+                                  allow_unused=True)
+        self.params.update(zip(map(id, owned), got))
+        del self.values[v]
+
+    def result(self):
+        return [self.params.get(id(p)) for p in self.model.parameters()]
+
+
+def plain_step(model, x, dy):
+    """Loss <output, dy> and the parameters' gradients, everything kept."""
+    values = {}
+    for v in range(model.nodes):
+        values[v] = model.node(v, values.__getitem__, x, dy)
+    return values[v].detach(), torch.autograd.grad(values[v], model.parameters(), allow_unused=True)
+
+
+def planned_step(model, x, dy, schedule, step=None):
+    """The same through the canonical strategy of a schedule (rcdp.Schedule)."""
+    step = step or Step(model, x, dy)
+    segments = [[] for _ in range(int(schedule.seg.max()) + 1)]
+    for v, s in enumerate(schedule.seg):
+        segments[int(s)].append(v)
+    for nodes in segments[:-1]:
         for v in nodes:
-            inside[v] = model.node(v, get)
-        outs, douts = [], []
-        if k == last:
-            loss = (inside[nodes[-1]][1].float() * dy).sum()
-            outs, douts = [loss], [torch.ones_like(loss)]
+            step.forward(v, bool(schedule.cached[v]))
         for v in nodes:
-            for t, g in zip(_tensors(inside[v]), grads.pop(v, ())):
-                if g is not None:
-                    outs.append(t)
-                    douts.append(g)
-        cut = {u: value for u, value in leaves.items() if not (u == -1 and k == 0)}
-        wrt = params + [t for value in cut.values() for t in _tensors(value)]
-        got = torch.autograd.grad(outs, wrt, douts, allow_unused=True)
-        for i, g in enumerate(got[:len(params)]):
-            if g is not None:
-                total[i] = g if total[i] is None else total[i] + g
-        at = len(params)
-        for u, value in cut.items():
-            n = len(_tensors(value))
-            old = grads.get(u, (None,) * n)
-            new = got[at:at + n]
-            grads[u] = tuple(b if a is None else a if b is None else a + b for a, b in zip(old, new))
-            at += n
+            if not schedule.cached[v]:
+                del step.values[v]
+    loss = None
+    for nodes in reversed(segments):
         for v in nodes:
-            kept.pop(v, None)
-        # gradients of the model's own input end in its first norm
-        if k == 0 and -1 in grads:
-            start = model.start(x)
-            pairs = [(t, g) for t, g in zip(start, grads.pop(-1)) if g is not None and t.requires_grad]
-            if pairs:
-                g, = torch.autograd.grad([t for t, _ in pairs], [model.first], [g for _, g in pairs])
-                total[-1] = g if total[-1] is None else total[-1] + g
-        del inside, leaves, cut, outs, douts, got
-    return loss.detach(), total
+            if v not in step.values:
+                step.forward(v, True)
+        if loss is None:
+            loss = step.values[nodes[-1]].detach()
+            step.grads[nodes[-1]] = [torch.ones_like(loss)]
+        for v in reversed(nodes):
+            step.backward(v)
+    return loss, step.result()
 
 
 @torch.no_grad()
 def prompt(model, x):
     """(normed output, the states after the prompt) of a prompt."""
-    values, states = model.start(x), []
+    values, states, n = model.start(x), [], model.states
     for b in range(model.blocks):
         p = model.p[b]
         both = model.run(b, "project", [values])
         u, conv = ops.causal_conv(both[..., :model.inner], p["conv"], p["conv_bias"], return_state=True)
         steps = model.run(b, "steps", [u])
-        dt, B, C = model.split(p, steps)
-        y, scan = ops.selective_scan(u, dt, p["A"], B, C, p["D"], both[..., model.inner:], p["dt_bias"],
-                                     softplus=True, return_state=True)
+        B, C = steps[..., model.rank:model.rank + n], steps[..., model.rank + n:]
+        y, scan = ops.selective_scan(u, model.run(b, "delta", [steps]), p["A"], B, C, p["D"],
+                                     both[..., model.inner:], p["dt_bias"], softplus=True, return_state=True)
         states.append((conv, scan))
         values = model.run(b, "join", [model.run(b, "back", [y]), values])
     return values[1], states
@@ -251,9 +300,9 @@ def prompt(model, x):
 @torch.no_grad()
 def token(model, x, states):
     """The normed output of one token of each sequence; updates the states."""
-    values = {-1: model.start(x)}
-    for v in range(model.blocks * len(NODES)):
-        values[v] = model.node(v, values.__getitem__, states)
+    values = {}
+    for v in range(model.nodes - 1):
+        values[v] = model.node(v, values.__getitem__, x, state=states)
     return values[v][1]
 
 
@@ -268,6 +317,20 @@ def plan(model, batch, length, fraction):
     return graph, budget, solution.reconstruct()
 
 
+def measured(step):
+    """(result, milliseconds, MiB allocated beside what was) of the second of two runs of a step."""
+    step()
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    e0, e1 = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    e0.record()
+    result = step()
+    e1.record()
+    torch.cuda.synchronize()
+    return result, e0.elapsed_time(e1), (torch.cuda.max_memory_allocated() - before) / 2 ** 20
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--blocks", type=int, default=8)
@@ -275,33 +338,30 @@ def main():
     ap.add_argument("--batch", type=int, default=4)
     ap.add_argument("--length", type=int, default=2048)
     ap.add_argument("--fraction", type=float, default=0.0, help="of the way from the smallest budget")
-    ap.add_argument("--tokens", type=int, default=16)
+    ap.add_argument("--tokens", type=int, default=16, help="of the length, one by one after the rest as a prompt")
     a = ap.parse_args()
+    if not 1 <= a.tokens <= a.length:
+        ap.error("--tokens must be at least 1 and at most the length")
     torch.manual_seed(1)
     model = Model(a.blocks, a.width)
     x = torch.randn(a.batch, a.length, a.width, device="cuda").to(model.dtype)
-    dy = torch.randn(a.batch, a.length, a.width, device="cuda")
+    dy = torch.randn_like(x)
     graph, budget, schedule = plan(model, a.batch, a.length, a.fraction)
-    print(f"{graph.n} activations, {sum(graph.M) / 1024:.0f} MiB; budget {budget / 1024:.0f} MiB: "
-          f"{len(schedule.chain)} segments, {int(schedule.cached.sum())} activations kept "
-          f"({schedule.cache_mem / 1024:.0f} MiB), recomputation {schedule.overhead / sum(graph.T):.0%} of forward")
-    results = {}
-    for name, step in (("plain", lambda: plain_step(model, x, dy)),
-                       ("planned", lambda: planned_step(model, x, dy, schedule))):
-        step()
-        torch.cuda.synchronize()
-        torch.cuda.reset_peak_memory_stats()
-        before = torch.cuda.memory_allocated()
-        e0, e1 = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-        e0.record()
-        results[name] = step()
-        e1.record()
-        torch.cuda.synchronize()
-        print(f"{name:8s} step {e0.elapsed_time(e1):8.2f} ms, peak {(torch.cuda.max_memory_allocated() - before) / 2 ** 20:8.0f} MiB")
+    again = sum(graph.T[v] for v in range(graph.n)
+                if not schedule.cached[v] and schedule.seg[v] < schedule.seg.max())
+    print(f"{graph.n} nodes, {sum(graph.M) / 1024:.0f} MiB, {sum(graph.T) / 1e4:.2f} ms forward; budget "
+          f"{budget / 1024:.0f} MiB: {len(schedule.chain)} segments, {int(schedule.cached.sum())} nodes kept "
+          f"({schedule.cache_mem / 1024:.0f} MiB), {again / 1e4:.2f} ms computed again "
+          f"({schedule.overhead / 1e4:.2f} with the last segment)")
+    plain, ms, mib = measured(lambda: plain_step(model, x, dy))
+    print(f"plain    step {ms:8.2f} ms, peak {mib:8.0f} MiB")
+    planned, ms, mib = measured(lambda: planned_step(model, x, dy, schedule))
+    grads = sum(g.nbytes for g in planned[1]) / 2 ** 20
+    print(f"planned  step {ms:8.2f} ms, peak {mib:8.0f} MiB, {grads:.0f} of it the parameters' gradients")
     off = max(((p.float() - q.float()).norm() / p.float().norm()).item()
-              for p, q in zip(results["plain"][1], results["planned"][1]) if p is not None and p.norm() > 0)
+              for p, q in zip(plain[1], planned[1]) if p.norm() > 0)
     print(f"gradients differ by at most {off:.1e} of their size")
-    out, states = prompt(model, x[:, :-a.tokens])
+    out, states = prompt(model, x[:, :a.length - a.tokens])
     for t in range(a.length - a.tokens, a.length):
         out = token(model, x[:, t], states)
     whole, _ = prompt(model, x)
