@@ -7,8 +7,9 @@ the next one.  Its operators come from ``paper_1905_11722_amd.ops``, its plain
 matrix products from PyTorch.
 
 The training step is planned by ``paper_1905_11722_amd.rcdp``: every operation
-of the step is a node with its forward time (counted, in tenths of a microsecond) and
-the size of its result (in KiB); for a budget the solver returns the chain
+of the step is a node with its forward time (measured, in tenths of a microsecond) and
+its size in KiB (measured: its result and what its backward pass keeps beside that, the scan's
+states every few tokens, say).  For a budget the solver returns the chain
 of lower sets of least recomputation overhead, and the step runs its
 canonical strategy (Section 3 of Kusumoto et al.): forward, the nodes on a segment's boundary
 stay; in the backward pass each segment's other nodes are computed again from them.
@@ -25,6 +26,7 @@ from __future__ import annotations
 
 import argparse
 import os
+import statistics
 import sys
 
 import torch
@@ -143,20 +145,7 @@ class Model:
 
     def graph(self, batch, length):
         """The step's nodes with their times and sizes (workloads.Graph)."""
-        tokens, e = batch * length, torch.finfo(self.dtype).bits // 8
-        w, i, n = self.width, self.inner, self.states
-        s = self.rank + 2 * n
-        # (values of the result, values moved, operations) of a token
-        count = {"start": (w, 2 * w, 4 * w), "project": (2 * i, w + 2 * i, 4 * w * i), "conv": (i, 2 * i, 16 * i),
-                 "steps": (s, i + s, 2 * i * s), "delta": (i, self.rank + i, 2 * self.rank * i),
-                 "scan": (i, 4 * i + 2 * n, 40 * i * n), "back": (w, i + w, 2 * i * w),
-                 "join": (2 * w, 4 * w, 12 * w), "loss": (0, 2 * w, 2 * w)}
-        cost = {}
-        for kind in count:
-            size, moved, flops = (v * tokens for v in count[kind])
-            rate = 6e14 if kind in ("project", "steps", "delta", "back") else 3e13
-            seconds = max(moved * e / 4e12, flops / rate) + 4e-6
-            cost[kind] = max(1, round(seconds * 1e7)), max(1, size * e // 1024)
+        cost = measure(self, batch, length)
         places = [self.place(v) for v in range(self.nodes)]
         succ = [[] for _ in places]
         for v in range(self.nodes):
@@ -245,6 +234,57 @@ class Step:
 
     def result(self):
         return [self.params.get(id(p)) for p in self.model.parameters()]
+
+
+@torch.no_grad()
+def measure(model, batch, length, repeats=5):
+    """{kind: (tenths of a microsecond forward, KiB)} of the step's nodes, from
+    running the first block.  The size is that of what a recorded node holds or, if that is more, of
+    its gradient and the scratch of its backward pass."""
+    x = torch.randn(batch, length, model.width, device=model.first.device).to(model.dtype)
+    step, last = Step(model, x, torch.randn_like(x)), model.nodes - 1
+    order = list(range(1 + len(NODES))) + [last]
+    cost = {}
+
+    def pass_over():
+        for v in order:
+            before = torch.cuda.memory_allocated()
+            step.forward(v, True)
+            cost[v] = torch.cuda.memory_allocated() - before
+            if v == len(NODES):                      # the last block's end, for the loss
+                step.values[last - 1] = step.values[v]
+        step.grads[last] = [torch.ones_like(step.values[last])]
+        for v in reversed(order):
+            if v == len(NODES) and last - 1 != v:
+                step.grads[v] = step.grads.pop(last - 1)
+                del step.values[last - 1]
+            if v == 0:
+                step.grads[v][0] = None
+            result = step.values[v]                  # (not freed meanwhile)
+            beside = cost[v] - sum(t.nbytes for t in _tensors(result) if t.data_ptr() != x.data_ptr())
+            torch.cuda.reset_peak_memory_stats()
+            step.backward(v)                         # its own gradient and `beside` are freed
+            freed = torch.cuda.max_memory_allocated() - torch.cuda.memory_allocated()
+            cost[v] = max(cost[v], freed - beside)
+            del result
+
+    pass_over()                                      # (libraries take their workspaces)
+    pass_over()
+    times = {}
+    for v in order:
+        step.forward(v, False)
+        spans = []
+        for _ in range(repeats):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            step.forward(v, False)
+            end.record()
+            end.synchronize()
+            spans.append(start.elapsed_time(end))
+        times[v] = statistics.median(spans)
+        if v == len(NODES):
+            step.values[last - 1] = step.values[v]
+    return {model.place(v)[1]: (max(1, round(times[v] * 1e4)), max(1, -(-cost[v] // 1024))) for v in order}
 
 
 def plain_step(model, x, dy):
