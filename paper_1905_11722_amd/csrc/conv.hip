@@ -10,7 +10,7 @@
 // Where V does not divide the width, the last thread of a row moves back to
 // the last V channels; it and its neighbour store the same values where they
 // overlap.  (Odd widths with V = 1 instead: 8 x 2047 x 2049 in bfloat16
-// forward 46, backward 87 us; this way 35 and 66.)
+// forward 43, backward 71 us, this way 33 and 59; in 32 bits 64 and 112, this way 72 and 94.)
 //
 // Backward: dp_t = dy_t act'(p_t) (p_t again from x), dx_t = sum_k w_k
 // dp_{t+K-1-k}, dw_k = sum_t dp_t x_{t-(K-1)+k}, dbias = sum_t dp_t.  The same walk,
@@ -110,8 +110,8 @@ __device__ __forceinline__ void load_weights(const rc_conv_args& a, int c,
 }
 
 // Forward: V = 8, kRows rows of loads in flight ahead of their use, no LDS.
-// At 2 x 4096 x 4096, K = 4 in bfloat16 (134 MB): 29.5 us, 4.6 TB/s, a large copy's rate;
-// 8 taps at 8 x 2048 x 2048 44 us (3.0 TB/s), 4 taps 37: the multiply-adds
+// At 2 x 4096 x 4096, K = 4 in bfloat16 (134 MB): 27.5 us, 4.9 TB/s, a large copy's rate; in 32 bits
+// (268 MB) 61 us, 4.4 TB/s; 8 taps at 8 x 2048 x 2048 42 us (3.2 TB/s), 4 taps 34: the multiply-adds
 // show.
 template <class T, int K, int V>
 __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
@@ -175,9 +175,10 @@ __global__ __launch_bounds__(kThreads) void k_conv_forward(ConvParams<T> p) {
 }
 
 // Backward: V = 4, since a thread holds K rows of x, of dp and the weights'
-// gradients of its channels.  Four waves a SIMD where that leaves registers enough
-// (16-bit types up to 4 taps): 8 x 2047 x 2048 in bfloat16 (201 MB) 58 us by the compiler's
-// choice, 52 so, 3.8 TB/s; above it spills, and two are asked for.
+// gradients of its channels.  Two waves a SIMD, as many as the registers of 8 taps in 32 bits leave;
+// four for 16-bit types up to 4 taps, which spill a few registers (above, many).  8 x 2047 x 2048,
+// 4 taps: bfloat16 (201 MB) 46 us, 4.4 TB/s, with two waves 49; half of it past the sequences' ends 45 us, with
+// two 37; 2049 channels 59 and 57.  32 bits (402 MB) 83 us, 4.8 TB/s.  8 taps 72 and 93 us.
 template <class T>
 constexpr int conv_waves(int taps) {
   return taps <= 4 && sizeof(T) == 2 ? 4 : 2;
