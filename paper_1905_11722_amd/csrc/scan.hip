@@ -343,9 +343,9 @@ __device__ __forceinline__ void enter(const ScanParams& p, const Place<Q, S>& w,
 // ends with one token's y, which takes their place.  Rows of LDS are padded so
 // that the four rows that a quad reads lie in different banks.
 // ENDS: only the end state of the chunk from nothing, and its sum of delta.
-// Bound by VALU issue (87% busy): 33 instructions for a step of a wave over a token
-// with 4 states a lane, 20 of them the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 580 us, 3.7e12 state
-// steps/s; one prompt of 16384 x 2048 261 us.
+// Bound by VALU issue (89% busy): 33 instructions for a step of a wave over a token
+// with 4 states a lane, 20 of them the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 605 us, 3.5e12 state
+// steps/s, in 32 bits 615; one prompt of 16384 x 2048 264 us.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams p) {
   constexpr int TILE = kFwdTile, N = Q * S, CW = channels_of(Q), ROW = CW + 8;
@@ -497,8 +497,8 @@ __global__ __launch_bounds__(channels_of(Q) * Q) void k_scan_forward(ScanParams 
 // way back, since keeping them spills; with fewer they stay (8 x 1024 x 2048 with
 // 8 states 232 -> 221 us).  ENDS: only the gradient of the state before the chunk,
 // from nothing after it, and its sum of delta.
-// Bound by VALU issue (86% busy): 104 instructions for a step of a wave, 60 of them
-// the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 1.8 ms, 1.2e12 state steps/s.
+// Bound by VALU issue (87% busy): 105 instructions for a step of a wave, 60 of them
+// the recurrence's.  16 x 2048 x 4096, 16 states in bfloat16: 1.86 ms, 1.15e12 state steps/s, in 32 bits 1.83.
 template <class T, int Q, int S, int VEC, bool ENDS>
 __global__ __launch_bounds__(channels_of(Q) * Q, 2) void k_scan_backward(ScanParams p) {
   constexpr int TILE = kKeep, N = Q * S, CW = channels_of(Q), ROW = CW + 4;
@@ -904,7 +904,9 @@ bool scan_sizes_ok(const rc_scan_args* a) {
 //   backward 655/175  658/317  664/460  672/590  957/729  964/865  977/1110 1482/1390
 // With v waves a SIMD on average and k on the fullest, a whole pass costs 95 +
 // 130 k forward (one wave: 202, see scan_plan), a cut one 1.7 times 130 v; backward 490
-// k (one wave: 665) and 1.18 times 490 v.
+// k (one wave: 665) and 1.18 times 490 v.  The factors are this table's; what they choose was then timed
+// in bfloat16 and float32 with 4, 16, 32 and 64 states, batches 1 to 16: the faster of the two or
+// within 6% of it but for 4 states forward at one wave a SIMD (bfloat16, whole 147, cut 128).
 bool scan_cut(double v, double k, bool backward) {
   return backward ? k == 1. || 1.18 * v < k : 1.7 * v < (k == 1. ? 1.36 : .5 + k);
 }
@@ -947,8 +949,9 @@ ScanPlan scan_plan(const rc_scan_args& a, bool backward) {
   p.chunks = a.length > 0 ? cdiv(a.length, p.chunk) : 1;
   p.keeps = cdiv(a.length, kKeep);
   // One wave a SIMD, uncut: eight lanes of two states halve what a wave has to issue for
-  // a token (8 x 2048 x 2048 forward 230 us with four lanes, 202 with eight; with more
-  // waves equal, and cut 133 for 137).  The kept states lie alike.
+  // a token (8 x 2048 x 2048 forward 236 us with four lanes, 199 with eight, where the kept states
+  // are written 232 and 210; lengths of 1 to 64 tokens, which are never cut, 7.0 to 11.0 and 6.5 to 10.2;
+  // with more waves equal, and cut 133 for 137).  The kept states lie alike.
   if (!backward && p.chunks == 1 && groups <= cus && p.Q == 4 && p.S == 4) {
     p.Q = 8;
     p.S = 2;
