@@ -428,14 +428,15 @@ __global__ __launch_bounds__(threads_of(TPR)) void k_norm_backward(NormParams p)
 template <class T>
 __global__ __launch_bounds__(256) void k_norm_weight_sum(const float* in, int64_t parts,
                                                          int32_t width, void* dpre, void* dscale,
-                                                         void* dpost, int32_t f32) {
+                                                         void* dpost, int32_t f32,
+                                                         int32_t second) {
   __shared__ float lds[256];
   const int64_t cols = 3 * (int64_t)width;
   const int64_t c = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
   const float s = column_sum(in, parts, cols, c, lds);
   if (threadIdx.x >= kSumCols || c >= cols) return;
   void* out = c < width ? dpre : c < 2 * (int64_t)width ? dscale : dpost;
-  if (out) store_param<T>(out, c % width, f32, s);
+  if (out) store_param<T>(out, c % width, f32, second || c >= width ? s : 0.f);
 }
 
 // Threads of a row, loads of a thread and their width: enough threads for one
@@ -534,8 +535,12 @@ extern "C" int rc_norm_backward_workspace(const rc_norm_args* a, uint64_t* bytes
 
 extern "C" int rc_norm_backward(const rc_norm_args* args, void* stream) {
   if (const int st = norm_check(args, true)) return st;
-  const rc_norm_args& a = *args;
+  rc_norm_args a = *args;
   if (a.width == 0) return RC_OK;
+  // Without a gradient the second norm is left out, and its weight's gradient is 0: 0 times what is
+  // not finite is no 0.
+  const bool second = a.dnormed.data;
+  if (!second) a.pre_weight = nullptr;
   const bool weights = a.dpost_weight || a.dscale || a.dpre_weight;
   uint64_t need = 0;
   rc_norm_backward_workspace(args, &need);
@@ -556,7 +561,7 @@ extern "C" int rc_norm_backward(const rc_norm_args* args, void* stream) {
     k_norm_weight_sum<T><<<dim3((uint32_t)cdiv(3 * (int64_t)a.width, kSumCols)), 256, 0,
                            (hipStream_t)stream>>>(partial, blocks, a.width, a.dpre_weight,
                                                   a.dscale, a.dpost_weight,
-                                                  a.param_dtype == RC_F32);
+                                                  a.param_dtype == RC_F32, second);
     return launched("k_norm_weight_sum");
   });
 }

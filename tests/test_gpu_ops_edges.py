@@ -433,3 +433,26 @@ def test_scan_step_of_many_rows(dtype, batch, width, states, groups):
     close(y, want, "y")
     close(pool, after, "state")
     assert not y[~on].any()
+
+
+@pytest.mark.parametrize("rows,width", [(6, 90), (5, 700), (4, 4096), (3, 5000), (3, 7001), (3, 9001)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_norm_gradients_without_the_second_norm(rows, width, bad):
+    """Only the first output is used: the second norm has no part in the gradients, not
+    even in a row whose residual is not finite."""
+    rng = torch.Generator(device=DEV).manual_seed(5)
+    args = [torch.randn(rows, width, generator=rng, device=DEV) for _ in range(3)]
+    args += [torch.rand(width, generator=rng, device=DEV) + 0.3 for _ in range(3)]
+    dout = torch.randn(rows, width, generator=rng, device=DEV)
+
+    def grads(pre):
+        leaf = [t.clone().requires_grad_() for t in args[:5 + pre]]
+        out, _ = ops.norm_residual(*leaf)
+        return torch.autograd.grad(out, leaf, dout)
+
+    args[1][1, width // 2] = bad
+    alone, both = grads(0), grads(1)
+    for name, a, b in zip(("block", "residual", "gate", "post", "scale"), alone, both):
+        assert torch.equal(a, b), name
+    assert torch.equal(both[1], dout)
+    assert not both[5].any()
