@@ -1,9 +1,7 @@
-"""The sequence-model operators where a caller leaves their usual ground:
-states that autograd has saved, derivatives that there are none of,
-pools that share memory or are too large, views that negate,
-no channels, scratch that is aligned to
-a float and no more, values that are not finite just before an end,
-the long walks that large inputs take."""
+"""The sequence-model operators off the usual ground: states that autograd
+has saved, derivatives that do not exist, pools that share memory or are too
+large, views that negate, no channels, scratch aligned to a float only, values
+that are not finite beside masked ones, and the walks that only large inputs take."""
 
 import ctypes
 
