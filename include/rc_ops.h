@@ -1,7 +1,9 @@
 /*
  * rc_ops.h -- C ABI of the sequence-model operators of the MI355X library:
- * the short causal convolution, the selective state space scan, and the norms
- * before and after a block fused with its gate and residual scale.
+ * the short causal convolution, the selective state space scan, the norms
+ * before and after a block fused with its gate and residual scale, the gated
+ * delta rule, the norms of queries and keys with their rotation by position,
+ * and dropout.
  *
  * They are the nodes of a network whose recomputation rc.h plans: a segment
  * of a canonical strategy (Section 3 of Kusumoto et al.) is run forward,
@@ -195,6 +197,132 @@ typedef struct {
 int rc_norm_forward(const rc_norm_args* args, void* stream);
 int rc_norm_backward(const rc_norm_args* args, void* stream);
 int rc_norm_backward_workspace(const rc_norm_args* args, uint64_t* bytes_host);
+
+/* A (batch, time, head, channel) tensor: element (b, t, h, c) is
+ * data[b * batch + t * time + h * head + c].  data NULL: the tensor is absent. */
+typedef struct {
+  void* data;
+  int64_t batch, time, head;
+} rc_heads;
+
+/*
+ * Gated delta rule (linear attention whose state corrects what it returns for a key).
+ * Head h keeps a matrix S of key x value numbers; with k and q of key head
+ * h / (heads / key_heads),
+ *   S_t = exp(g) S_{t-1} + k (beta (v - exp(g) S_{t-1}^T k))^T,   o_t = scale S_t^T q.
+ * q, k: (batch, length, key_heads, key); v, o: (batch, length, heads, value), all of
+ * dtype.  g (absent: 0) and beta: (batch, length, heads), 32-bit floats; g is not
+ * positive (-infinity forgets everything).  States (batch, heads, key, value) are
+ * 32-bit floats, contiguous.  1 <= key, value <= 256; key_heads divides heads.
+ * kept: NULL, or what rc_delta_backward starts from (rc_delta_kept_bytes);
+ * it is written by rc_delta_forward and read by rc_delta_backward of the same
+ * sizes.  Both need scratch.
+ * Backward: do_ (required), dstate_out (may be NULL: 0) -> dq, dk, dv (dtype),
+ * dg (NULL exactly where g is absent) and dbeta (32-bit, contiguous
+ * (batch, length, heads)), dstate_in (may be NULL).
+ */
+typedef struct {
+  int32_t dtype;
+  int32_t batch, length, key_heads, heads, key, value;
+  float scale;
+  rc_heads q, k, v, o;
+  rc_view g, beta;
+  const float* state_in;            /* or NULL: 0 */
+  float* state_out;                 /* or NULL */
+  const int32_t* lengths;
+  float* kept;
+  rc_heads do_, dq, dk, dv;
+  float* dg;
+  float* dbeta;
+  const float* dstate_out;
+  float* dstate_in;
+  void* workspace;
+  uint64_t workspace_bytes;
+} rc_delta_args;
+
+int rc_delta_forward(const rc_delta_args* args, void* stream);
+int rc_delta_backward(const rc_delta_args* args, void* stream);
+int rc_delta_kept_bytes(const rc_delta_args* args, uint64_t* bytes_host);
+int rc_delta_forward_workspace(const rc_delta_args* args, uint64_t* bytes_host);
+int rc_delta_backward_workspace(const rc_delta_args* args, uint64_t* bytes_host);
+/* One token: q, k (batch, key_heads, key), v, o (batch, heads, value), g, beta
+ * (batch, heads) (time strides are not used); state (num_slots, heads, key,
+ * value), contiguous but for its slot stride, is updated in place; slots as
+ * rc_conv_step. */
+typedef struct {
+  int32_t dtype;
+  int32_t batch, key_heads, heads, key, value, num_slots;
+  float scale;
+  rc_heads q, k, v, o;
+  rc_view g, beta;
+  float* state;
+  int64_t state_slot;               /* slot stride of state */
+  const int32_t* slots;
+} rc_delta_step_args;
+int rc_delta_step(const rc_delta_step_args* args, void* stream);
+
+/*
+ * Norms of queries and keys, each head on its own, and their rotation by
+ * position.  For x of q (heads) and k (key_heads), each `channels` <= 256 wide:
+ *   y = x / sqrt(mean(x^2) + eps) * weight     (RC_QK_RMS)
+ *   y = x / sqrt(sum(x^2) + eps) * weight      (RC_QK_L2)
+ *   y = x weight                               (RC_QK_NONE),
+ * then pair i < rotated / 2 of y is turned by the angle position * inv_freq[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),
+ * channels (i, i + rotated / 2), or (2i, 2i + 1) where interleaved.  Channels
+ * from rotated on are not turned.  positions (batch, length), int32, element
+ * (b, t) at b * positions_batch + t * positions_time, NULL: t.  Angles are taken in
+ * 64 bits.  The weights (may be NULL: 1) are of param_dtype (RC_F32 or dtype),
+ * inv_freq [rotated / 2] 32-bit (NULL where rotated is 0).
+ * Backward: dq_out and dk_out, each may be absent (0) -> dq, dk, dq_weight,
+ * dk_weight (param_dtype; each may be NULL).
+ */
+enum rc_qk_norm { RC_QK_NONE = 0, RC_QK_RMS = 1, RC_QK_L2 = 2 };
+typedef struct {
+  int32_t dtype, param_dtype, norm, interleaved;
+  int32_t batch, length, heads, key_heads, channels, rotated;
+  float eps;
+  rc_heads q, k, q_out, k_out;
+  const void* q_weight;
+  const void* k_weight;
+  const float* inv_freq;
+  const int32_t* positions;
+  int64_t positions_batch, positions_time;
+  const int32_t* lengths;
+  rc_heads dq_out, dk_out, dq, dk;
+  void* dq_weight;
+  void* dk_weight;
+  void* workspace;
+  uint64_t workspace_bytes;
+} rc_qk_args;
+
+int rc_qk_forward(const rc_qk_args* args, void* stream);
+int rc_qk_backward(const rc_qk_args* args, void* stream);
+int rc_qk_backward_workspace(const rc_qk_args* args, uint64_t* bytes_host);
+
+/*
+ * Dropout whose mask is never stored: element i of x (in row-major order of
+ * rows x width) is kept where word i % 4 of Philox4x32-10 (Salmon, Moraes, Dror and
+ * Shaw, 2011) with key seed and counter (i / 4, tag) is not below p 2^32:
+ *   out = residual + (kept ? x / (1 - p) : 0).
+ * So forward, backward and a second run of either draw the same mask from the
+ * same seed and tag.  0 <= p <= 1 (1 drops everything).  The seed is
+ * *seed_device if that is not NULL (read when the kernel runs), else seed.
+ * x is of dtype; residual (may be absent) and out of out_dtype (RC_F32 or dtype;
+ * dtype without a residual).  Views use their batch strides as row strides.
+ * Backward: dx = kept ? dout / (1 - p) : 0.
+ */
+typedef struct {
+  int32_t dtype, out_dtype;
+  int64_t rows, width;
+  double p;
+  int64_t seed, tag;
+  const int64_t* seed_device;
+  rc_view x, residual, out;         /* backward: dout as out, dx as x */
+} rc_dropout_args;
+
+int rc_dropout_forward(const rc_dropout_args* args, void* stream);
+int rc_dropout_backward(const rc_dropout_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ using Opt = std::optional<Tensor>;
 
 namespace {
 
-constexpr int64_t kMaxTaps = 8, kMaxStates = 64, kMaxNormWidth = 16384;
+constexpr int64_t kMaxTaps = 8, kMaxStates = 64, kMaxNormWidth = 16384, kMaxHead = 256;
 
 // A library error as rcdp.RcError.
 [[noreturn]] void fail(int status, const char* where) {
@@ -40,13 +40,16 @@ int32_t code(at::ScalarType t) {
   return t == at::kFloat ? RC_F32 : t == at::kBFloat16 ? RC_BF16 : RC_F16;
 }
 
-// The tensor that gives sizes, type and device.
-void main_tensor(const char* name, const Tensor& t, int64_t dims) {
+void activations(const char* name, const Tensor& t) {
   TORCH_CHECK_VALUE(t.is_cuda(), name, " must be on a GPU: there is no CPU path");
-  TORCH_CHECK_VALUE(t.dim() == dims, name, " must have ", dims, " dimensions, not ", t.dim());
   TORCH_CHECK_VALUE(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16 ||
                         t.scalar_type() == at::kHalf,
                     name, " must be float32, bfloat16 or float16, not ", t.scalar_type());
+}
+// The tensor that gives sizes, type and device.
+void main_tensor(const char* name, const Tensor& t, int64_t dims) {
+  activations(name, t);
+  TORCH_CHECK_VALUE(t.dim() == dims, name, " must have ", dims, " dimensions, not ", t.dim());
   for (const int64_t n : t.sizes()) TORCH_CHECK_VALUE(n < (int64_t)1 << 31, name, " is too large");
 }
 
@@ -650,6 +653,359 @@ std::pair<Tensor, Opt> norm_residual(const Opt& block_, const Tensor& residual, 
   return {out[0], t.pre.defined() ? Opt(out[1]) : Opt()};
 }
 
+// ----------------------------------------------------------------- delta rule
+
+// A (batch, time, head, channel) or (batch, head, channel) tensor.
+rc_heads heads_view(const Tensor& t) {
+  if (!t.defined()) return {nullptr, 0, 0, 0};
+  if (t.dim() == 3) return {t.data_ptr(), t.stride(0), 0, t.stride(1)};
+  return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+
+struct DeltaIn {
+  Tensor q, k, v, g, beta, state, lengths;
+};
+
+rc_delta_args delta_args(const DeltaIn& t, double scale) {
+  rc_delta_args a = {};
+  a.dtype = code(t.v.scalar_type());
+  a.batch = (int32_t)t.v.size(0);
+  a.length = (int32_t)t.v.size(1);
+  a.heads = (int32_t)t.v.size(2);
+  a.value = (int32_t)t.v.size(3);
+  a.key_heads = (int32_t)t.q.size(2);
+  a.key = (int32_t)t.q.size(3);
+  a.scale = (float)scale;
+  a.q = heads_view(t.q);
+  a.k = heads_view(t.k);
+  a.v = heads_view(t.v);
+  a.g = view(t.g);
+  a.beta = view(t.beta);
+  a.state_in = ptr<float>(t.state);
+  a.lengths = ptr<int32_t>(t.lengths);
+  return a;
+}
+
+// o, and the final state if wanted; what the backward pass needs into *kept if that is not null.
+variable_list delta_forward(const DeltaIn& t, double scale, bool want_state, Tensor* kept) {
+  const c10::DeviceGuard guard(t.v.device());
+  rc_delta_args a = delta_args(t, scale);
+  variable_list out = {like(t.v)};
+  a.o = heads_view(out[0]);
+  const auto floats = t.v.options().dtype(at::kFloat);
+  if (want_state) {
+    out.push_back(at::empty({t.v.size(0), t.v.size(2), t.q.size(3), t.v.size(3)}, floats));
+    a.state_out = ptr<float>(out[1]);
+  }
+  if (kept) {
+    uint64_t n = 0;
+    check(rc_delta_kept_bytes(&a, &n), "rc_delta_kept_bytes");
+    *kept = at::empty({(int64_t)n / 4}, floats);
+    a.kept = ptr<float>(*kept);
+  }
+  const Tensor work = scratch(rc_delta_forward_workspace, a, t.v, "rc_delta_forward_workspace");
+  check(rc_delta_forward(&a, stream_of(t.v)), "rc_delta_forward");
+  return out;
+}
+
+struct Delta : torch::autograd::Function<Delta> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v,
+                               const Opt& decay, const Tensor& beta, const Opt& state_in,
+                               const Opt& ends, double scale, bool want_state) {
+    const Tensor g = given(decay), state = given(state_in), lengths = given(ends);
+    Tensor kept;
+    variable_list out = delta_forward({q, k, v, g, beta, state, lengths}, scale, want_state, &kept);
+    ctx->save_for_backward({q, k, v, g, beta, state, lengths, kept});
+    ctx->saved_data["scale"] = scale;
+    ctx->set_materialize_grads(false);
+    return out;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
+    const auto s = ctx->get_saved_variables();
+    const DeltaIn t = {s[0], s[1], s[2], s[3], s[4], s[5], s[6]};
+    const c10::DeviceGuard guard(t.v.device());
+    rc_delta_args a = delta_args(t, ctx->saved_data["scale"].toDouble());
+    const Tensor d_o = grads[0].defined() ? rows(grads[0]) : at::zeros_like(t.v);
+    const Tensor dout = grads.size() > 1 ? dense(grads[1]) : Tensor();
+    const Tensor dq = like(t.q), dk = like(t.k), dv = like(t.v), dg = like(t.g), dbeta = like(t.beta),
+                 ds = like(t.state, t.state.defined() && t.state.requires_grad());
+    a.kept = ptr<float>(s[7]);
+    a.do_ = heads_view(d_o);
+    a.dq = heads_view(dq);
+    a.dk = heads_view(dk);
+    a.dv = heads_view(dv);
+    a.dg = ptr<float>(dg);
+    a.dbeta = ptr<float>(dbeta);
+    a.dstate_out = ptr<float>(dout);
+    a.dstate_in = ptr<float>(ds);
+    const Tensor work = scratch(rc_delta_backward_workspace, a, t.v, "rc_delta_backward_workspace");
+    check(rc_delta_backward(&a, stream_of(t.v)), "rc_delta_backward");
+    return once({dq, dk, dv, dg, dbeta, ds, Tensor(), Tensor(), Tensor()});
+  }
+};
+
+// Checks of what the whole and the single-token form share; t.v is (tokens.., heads, value).
+void delta_expect(const DeltaIn& t) {
+  const int64_t dims = t.v.dim();
+  TORCH_CHECK_VALUE(t.q.dim() == dims, "q must have ", dims, " dimensions, not ", t.q.dim());
+  const int64_t h = t.v.size(-2), hk = t.q.size(-2), dk = t.q.size(-1), dv = t.v.size(-1);
+  TORCH_CHECK_VALUE(h == 0 || (hk > 0 && h % hk == 0), hk, " heads of q do not divide ", h, " heads of v");
+  TORCH_CHECK_VALUE(dk >= 1 && dk <= kMaxHead, "q must have 1 to ", kMaxHead, " channels, not ", dk);
+  TORCH_CHECK_VALUE(dv >= 1 && dv <= kMaxHead, "v must have 1 to ", kMaxHead, " channels, not ", dv);
+  std::vector<int64_t> shape(t.v.sizes().begin(), t.v.sizes().end() - 2);
+  shape.push_back(h);
+  expect("beta", t.beta, shape, at::kFloat, t.v);
+  if (t.g.defined()) expect("g", t.g, shape, at::kFloat, t.v);
+  shape.back() = hk;
+  shape.push_back(dk);
+  expect("q", t.q, shape, t.v.scalar_type(), t.v);
+  expect("k", t.k, shape, t.v.scalar_type(), t.v);
+}
+
+variable_list gated_delta(const Tensor& q, const Tensor& k, const Tensor& v, const Opt& g,
+                          const Tensor& beta, double scale, const Opt& state, const Opt& lengths,
+                          bool want_state) {
+  main_tensor("v", v, 4);
+  DeltaIn t = {q, k, v, given(g), beta, given(state), Tensor()};
+  delta_expect(t);
+  if (state) expect("state", *state, {v.size(0), v.size(2), q.size(3), v.size(3)}, at::kFloat, v);
+  t.lengths = lengths_of(lengths, v);
+  const bool grad = differentiated({&q, &k, &v, &t.g, &beta, &t.state});
+  t = {rows(q), rows(k), rows(v), rows(t.g), rows(beta), dense(t.state), t.lengths};
+  if (grad)
+    return Delta::apply(t.q, t.k, t.v, opt(t.g), t.beta, opt(t.state), opt(t.lengths), scale, want_state);
+  return delta_forward(t, scale, want_state, nullptr);
+}
+
+Tensor gated_delta_step(const Tensor& state, const Tensor& q, const Tensor& k, const Tensor& v,
+                        const Opt& g, const Tensor& beta, double scale, const Opt& slots_) {
+  main_tensor("v", v, 3);
+  DeltaIn t = {q, k, v, given(g), beta, Tensor(), Tensor()};
+  delta_expect(t);
+  const int64_t h = v.size(1), dk = q.size(2), dv = v.size(2);
+  TORCH_CHECK_VALUE(state.dim() == 4, "state must have 4 dimensions");
+  expect("state", state, {state.size(0), h, dk, dv}, at::kFloat, v);
+  TORCH_CHECK_VALUE((state.stride(3) == 1 || dv <= 1) && (state.stride(2) == dv || dk <= 1) &&
+                        (state.stride(1) == dk * dv || h <= 1),
+                    "each slot of state must be contiguous");
+  TORCH_CHECK_VALUE(!overlap(state.size(0), state.stride(0), 1, 0, h * dk * dv),
+                    "states must not share memory");
+  const Tensor slots = slots_of(slots_, v, state);
+  not_differentiated("gated_delta_step", {&state, &q, &k, &v, &t.g, &beta});
+  t = {rows(q), rows(k), rows(v), rows(t.g), rows(beta), Tensor(), Tensor()};
+  const c10::DeviceGuard guard(v.device());
+  const Tensor o = at::empty(v.sizes(), v.options());
+  rc_delta_step_args a = {};
+  a.dtype = code(v.scalar_type());
+  a.batch = (int32_t)v.size(0);
+  a.key_heads = (int32_t)q.size(1);
+  a.heads = (int32_t)h;
+  a.key = (int32_t)dk;
+  a.value = (int32_t)dv;
+  a.num_slots = (int32_t)state.size(0);
+  a.scale = (float)scale;
+  a.q = heads_view(t.q);
+  a.k = heads_view(t.k);
+  a.v = heads_view(t.v);
+  a.o = heads_view(o);
+  a.g = view(t.g);
+  a.beta = view(t.beta);
+  a.state = ptr<float>(state);
+  a.state_slot = state.stride(0);
+  a.slots = ptr<int32_t>(slots);
+  check(rc_delta_step(&a, stream_of(v)), "rc_delta_step");
+  written(state);
+  return o;
+}
+
+// ----------------------------------------------------------- queries and keys
+
+struct QkIn {
+  Tensor q, k, qw, kw, freq, positions, lengths;
+};
+
+rc_qk_args qk_args(const QkIn& t, int64_t norm, bool interleaved, int64_t param, double eps) {
+  rc_qk_args a = {};
+  a.dtype = code(t.q.scalar_type());
+  a.param_dtype = (int32_t)param;
+  a.norm = (int32_t)norm;
+  a.interleaved = interleaved;
+  a.batch = (int32_t)t.q.size(0);
+  a.length = (int32_t)t.q.size(1);
+  a.heads = (int32_t)t.q.size(2);
+  a.key_heads = (int32_t)t.k.size(2);
+  a.channels = (int32_t)t.q.size(3);
+  a.rotated = t.freq.defined() ? 2 * (int32_t)t.freq.size(0) : 0;
+  a.eps = (float)eps;
+  a.q = heads_view(t.q);
+  a.k = heads_view(t.k);
+  a.q_weight = ptr(t.qw);
+  a.k_weight = ptr(t.kw);
+  a.inv_freq = ptr<float>(t.freq);
+  if (t.positions.defined()) {
+    a.positions = ptr<int32_t>(t.positions);
+    a.positions_batch = t.positions.stride(0);
+    a.positions_time = t.positions.stride(1);
+  }
+  a.lengths = ptr<int32_t>(t.lengths);
+  return a;
+}
+
+variable_list qk_forward(const QkIn& t, int64_t norm, bool interleaved, int64_t param, double eps) {
+  const c10::DeviceGuard guard(t.q.device());
+  rc_qk_args a = qk_args(t, norm, interleaved, param, eps);
+  variable_list out = {like(t.q), like(t.k)};
+  a.q_out = heads_view(out[0]);
+  a.k_out = heads_view(out[1]);
+  check(rc_qk_forward(&a, stream_of(t.q)), "rc_qk_forward");
+  return out;
+}
+
+struct Qk : torch::autograd::Function<Qk> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Opt& qw,
+                               const Opt& kw, const Opt& freq, const Opt& positions, const Opt& ends,
+                               int64_t norm, bool interleaved, int64_t param, double eps) {
+    const QkIn t = {q, k, given(qw), given(kw), given(freq), given(positions), given(ends)};
+    ctx->save_for_backward({t.q, t.k, t.qw, t.kw, t.freq, t.positions, t.lengths});
+    ctx->saved_data["norm"] = norm;
+    ctx->saved_data["interleaved"] = interleaved;
+    ctx->saved_data["param"] = param;
+    ctx->saved_data["eps"] = eps;
+    ctx->set_materialize_grads(false);
+    return qk_forward(t, norm, interleaved, param, eps);
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
+    const auto s = ctx->get_saved_variables();
+    const QkIn t = {s[0], s[1], s[2], s[3], s[4], s[5], s[6]};
+    const c10::DeviceGuard guard(t.q.device());
+    rc_qk_args a = qk_args(t, ctx->saved_data["norm"].toInt(), ctx->saved_data["interleaved"].toBool(),
+                           ctx->saved_data["param"].toInt(), ctx->saved_data["eps"].toDouble());
+    const Tensor gq = rows(grads[0]), gk = rows(grads[1]), dq = like(t.q), dk = like(t.k),
+                 dqw = like(t.qw, t.qw.defined() && t.qw.requires_grad()),
+                 dkw = like(t.kw, t.kw.defined() && t.kw.requires_grad());
+    a.dq_out = heads_view(gq);
+    a.dk_out = heads_view(gk);
+    a.dq = heads_view(dq);
+    a.dk = heads_view(dk);
+    a.dq_weight = ptr(dqw);
+    a.dk_weight = ptr(dkw);
+    const Tensor work = scratch(rc_qk_backward_workspace, a, t.q, "rc_qk_backward_workspace");
+    check(rc_qk_backward(&a, stream_of(t.q)), "rc_qk_backward");
+    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()});
+  }
+};
+
+variable_list qk_norm(const Tensor& q, const Tensor& k, const Opt& qw, const Opt& kw, const Opt& freq,
+                      const Opt& positions, const Opt& lengths, int64_t norm, bool interleaved,
+                      double eps) {
+  main_tensor("q", q, 4);
+  QkIn t = {q, k, given(qw), given(kw), given(freq), given(positions), Tensor()};
+  const int64_t d = q.size(3);
+  TORCH_CHECK_VALUE(d >= 1 && d <= kMaxHead, "q must have 1 to ", kMaxHead, " channels, not ", d);
+  TORCH_CHECK_VALUE(k.dim() == 4, "k must have 4 dimensions, not ", k.dim());
+  expect("k", k, {q.size(0), q.size(1), k.size(2), d}, q.scalar_type(), q);
+  if (t.qw.defined()) expect("q_weight", t.qw, {d}, t.qw.scalar_type(), q);
+  if (t.kw.defined()) expect("k_weight", t.kw, {d}, t.kw.scalar_type(), q);
+  const int64_t param = param_type({{"q_weight", &t.qw}, {"k_weight", &t.kw}}, q);
+  if (t.freq.defined()) {
+    TORCH_CHECK_VALUE(t.freq.dim() == 1 && 2 * t.freq.size(0) <= d, "inv_freq must have at most ", d / 2,
+                      " numbers in one dimension, not ", t.freq.sizes());
+    expect("inv_freq", t.freq, t.freq.sizes(), at::kFloat, q);
+    if (t.freq.size(0) == 0) t.freq = Tensor();
+  }
+  TORCH_CHECK_VALUE(!differentiated({&t.freq}), "inv_freq has no gradient: detach it");
+  if (t.positions.defined()) expect("positions", t.positions, {q.size(0), q.size(1)}, at::kInt, q);
+  t.lengths = lengths_of(lengths, q);
+  const bool grad = differentiated({&q, &k, &t.qw, &t.kw});
+  t = {rows(q), rows(k), dense(t.qw), dense(t.kw), dense(t.freq), t.positions, t.lengths};
+  if (grad)
+    return Qk::apply(t.q, t.k, opt(t.qw), opt(t.kw), opt(t.freq), opt(t.positions), opt(t.lengths), norm,
+                     interleaved, param, eps);
+  return qk_forward(t, norm, interleaved, param, eps);
+}
+
+// -------------------------------------------------------------------- dropout
+
+rc_dropout_args dropout_args(const Tensor& seed, int64_t number, int64_t tag, double p) {
+  rc_dropout_args a = {};
+  a.p = p;
+  a.seed = number;
+  a.tag = tag;
+  a.seed_device = ptr<const int64_t>(seed);
+  return a;
+}
+// x and out (its gradient backward) as rows; both of the same shape.
+void dropout_rows(rc_dropout_args& a, const Tensor& x, const Tensor& out) {
+  a.dtype = code(x.scalar_type());
+  a.out_dtype = code(out.scalar_type());
+  a.rows = x.size(0);
+  a.width = x.size(1);
+  a.x = view(x);
+  a.out = view(out);
+}
+// Any shape as rows of the last dimension.
+Tensor as_rows(const Tensor& t) {
+  if (!t.defined()) return t;
+  const int64_t d = t.dim() ? t.size(-1) : 1;
+  return flat(t.dim() ? t : t.reshape({1, 1}), d ? t.numel() / d : 0);
+}
+
+Tensor dropout_forward(const Tensor& x, const Tensor& residual, const Tensor& seed, int64_t number,
+                       int64_t tag, double p) {
+  const c10::DeviceGuard guard(x.device());
+  const Tensor out = at::empty(x.sizes(), (residual.defined() ? residual : x).options());
+  const Tensor xs = as_rows(x), rs = as_rows(residual), ys = as_rows(out);
+  rc_dropout_args a = dropout_args(seed, number, tag, p);
+  dropout_rows(a, xs, ys);
+  a.residual = view(rs);
+  check(rc_dropout_forward(&a, stream_of(x)), "rc_dropout_forward");
+  return out;
+}
+
+struct Dropout : torch::autograd::Function<Dropout> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Opt& residual, const Opt& seed,
+                        int64_t number, int64_t tag, double p) {
+    ctx->save_for_backward({given(seed)});
+    ctx->saved_data["number"] = number;
+    ctx->saved_data["tag"] = tag;
+    ctx->saved_data["p"] = p;
+    ctx->saved_data["dtype"] = x.scalar_type();
+    ctx->saved_data["residual"] = residual.has_value();
+    return dropout_forward(x, given(residual), given(seed), number, tag, p);
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads) no_tangent(g);
+    const Tensor seed = ctx->get_saved_variables()[0], &g = grads[0];
+    const c10::DeviceGuard guard(g.device());
+    const Tensor dx = at::empty(g.sizes(), g.options().dtype(ctx->saved_data["dtype"].toScalarType()));
+    const Tensor gs = as_rows(g), xs = as_rows(dx);
+    rc_dropout_args a = dropout_args(seed, ctx->saved_data["number"].toInt(), ctx->saved_data["tag"].toInt(),
+                                     ctx->saved_data["p"].toDouble());
+    dropout_rows(a, xs, gs);
+    check(rc_dropout_backward(&a, stream_of(g)), "rc_dropout_backward");
+    const Tensor dr = ctx->saved_data["residual"].toBool() ? g : Tensor();
+    return once({dx, dr, Tensor(), Tensor(), Tensor(), Tensor()});
+  }
+};
+
+Tensor dropout(const Tensor& x, double p, const Opt& seed_, int64_t number, int64_t tag,
+               const Opt& residual_) {
+  activations("x", x);
+  const Tensor residual = given(residual_), seed = given(seed_);
+  TORCH_CHECK_VALUE(p >= 0 && p <= 1, "p must be from 0 to 1, not ", p);
+  if (residual.defined())
+    expect("residual", residual, x.sizes(),
+           residual.scalar_type() == at::kFloat ? at::kFloat : x.scalar_type(), x);
+  if (seed.defined()) {
+    TORCH_CHECK_VALUE(seed.numel() == 1, "seed must be one number, not ", seed.sizes());
+    expect("seed", seed, seed.sizes(), at::kLong, x);
+  }
+  if (differentiated({&x, &residual})) return Dropout::apply(x, opt(residual), opt(seed), number, tag, p);
+  return dropout_forward(x, residual, seed, number, tag, p);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_ops, m) {
@@ -658,4 +1014,8 @@ PYBIND11_MODULE(_ops, m) {
   m.def("selective_scan", &selective_scan);
   m.def("selective_scan_step", &selective_scan_step);
   m.def("norm_residual", &norm_residual);
+  m.def("gated_delta", &gated_delta);
+  m.def("gated_delta_step", &gated_delta_step);
+  m.def("qk_norm", &qk_norm);
+  m.def("dropout", &dropout);
 }

@@ -31,28 +31,6 @@ struct NormParams {
 // Threads of a workgroup with TPR threads a row.
 constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
-                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-// Sum over 32 or 64 lanes, in each of them (a mirror is as good as an
-// exchange once the lanes below are equal).
-template <int LANES>
-__device__ __forceinline__ float lane_sum(float x) {
-  x = dpp_add<0xB1>(x);                                // lanes 1 apart
-  x = dpp_add<0x4E>(x);                                // 2 apart
-  x = dpp_add<0x141>(x);                               // half rows mirrored
-  x = dpp_add<0x140>(x);                               // rows mirrored
-  const unsigned a = __builtin_bit_cast(unsigned, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
-  if (LANES == 32) return x;
-  const unsigned b = __builtin_bit_cast(unsigned, x);
-  const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
-}
-
 // Sums over the TPR threads of a row of M values.  lds has 16 M floats of its
 // own for each of two calls in a row: the barrier of one call is between the
 // reads of the one before and the writes of the one after.

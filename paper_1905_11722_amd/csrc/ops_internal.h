@@ -1,5 +1,5 @@
-// Shared by the sequence-model operators (conv.hip, scan.hip, norm.hip):
-// element types, wide loads and stores, activations, argument checks.
+// Shared by the sequence-model operators (conv.hip, scan.hip, norm.hip, delta.hip, qk.hip,
+// dropout.hip): element types, wide loads and stores, activations, argument checks.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -78,6 +78,39 @@ __device__ __forceinline__ float softplus(float x) {
   const float r = s - 1.f;
   const float l = r == 0.f ? w : kLn2 * __builtin_amdgcn_logf(s) * (w * fast_rcp(r));
   return __builtin_fmaxf(x, 0.f) + l;                  // a NaN comes through w
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// Sum over groups of 1, 2, 4 .. 64 lanes, in each of them (a mirror is as good as an
+// exchange once the lanes below are equal).
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float x) {
+  if (LANES == 1) return x;
+  x = dpp_add<0xB1>(x);                                // lanes 1 apart
+  if (LANES == 2) return x;
+  x = dpp_add<0x4E>(x);                                // 2 apart
+  if (LANES == 4) return x;
+  x = dpp_add<0x141>(x);                               // half rows mirrored
+  if (LANES == 8) return x;
+  x = dpp_add<0x140>(x);                               // rows mirrored
+  if (LANES == 16) return x;
+  const unsigned a = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+  if (LANES == 32) return x;
+  const unsigned b = __builtin_bit_cast(unsigned, x);
+  const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
+}
+
+// An element of a (batch, time, head, channel) tensor.
+template <class T>
+__device__ __forceinline__ T* at_head(const rc_heads& v, int64_t b, int64_t t, int64_t h) {
+  return static_cast<T*>(v.data) + b * v.batch + t * v.time + h * v.head;
 }
 
 __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -6,7 +6,12 @@ nodes of a network whose recomputation ``rcdp`` plans.
 * :func:`selective_scan` / :func:`selective_scan_step`: selective state space
   scan;
 * :func:`norm_residual`: the norms before and after a block, fused with the
-  block's gate and residual scale.
+  block's gate and residual scale;
+* :func:`gated_delta` / :func:`gated_delta_step`: gated delta rule, a linear
+  attention;
+* :func:`qk_norm`: the norms of its queries and keys for each head, with their
+  rotation by position;
+* :func:`dropout`: dropout whose mask is drawn again wherever it is needed.
 
 The whole-sequence forms are differentiable (once, in reverse mode); the ``*_step`` forms take
 one token of each sequence and update a pool of states in place, without
@@ -28,15 +33,18 @@ fallback.
 from __future__ import annotations
 
 import importlib
+import operator
 
 from . import rcdp
 
 __all__ = ["causal_conv", "causal_conv_step", "selective_scan", "selective_scan_step",
-           "norm_residual", "MAX_TAPS", "MAX_STATES", "MAX_NORM_WIDTH"]
+           "norm_residual", "gated_delta", "gated_delta_step", "qk_norm", "dropout",
+           "MAX_TAPS", "MAX_STATES", "MAX_NORM_WIDTH", "MAX_HEAD"]
 
-MAX_TAPS, MAX_STATES, MAX_NORM_WIDTH = 8, 64, 16384
+MAX_TAPS, MAX_STATES, MAX_NORM_WIDTH, MAX_HEAD = 8, 64, 16384, 256
 _CONV_ACTIVATIONS = {None: 0, "silu": 1}
 _GATE_ACTIVATIONS = {"silu": 1, "sigmoid": 2}
+_QK_NORMS = {None: 0, "rms": 1, "l2": 2}
 
 _native = None
 
@@ -154,3 +162,102 @@ def norm_residual(block, residual, gate=None, post_weight=None, scale=None, pre_
     return (_native or load()).norm_residual(
         block, residual, gate, post_weight, scale, pre_weight,
         _activation("gate_activation", gate_activation, _GATE_ACTIVATIONS), eps)
+
+
+def gated_delta(q, k, v, g, beta, *, scale=None, state=None, lengths=None, return_state=False):
+    """Gated delta rule over time: a linear attention whose state corrects what it holds for a key.
+
+    Each head keeps a matrix S of key x value numbers:
+
+    ``S = exp(g) S``, ``S = S + k (beta (v - S^T k))^T``, ``o = scale S^T q``
+
+    q, k: (batch, length, key_heads, key), v: (batch, length, heads, value),
+    key and value at most 256; key_heads divides heads, and head h takes q and k of
+    head h // (heads // key_heads).  g (None: 0; not positive, -inf forgets
+    everything before) and beta: (batch, length, heads), float32.  The state stays
+    bounded where beta k^T k is at most 2, as with keys of length one (:func:`qk_norm` with
+    ``norm="l2"``) and beta in (0, 1).  scale: default key ** -0.5.  state: float32
+    (batch, heads, key, value), the one before the first token (default:
+    zeros).  lengths: int32 (batch,), where each sequence ends; what lies past
+    it is not used, and is 0 in o.
+
+    Returns o, or with ``return_state`` (o, the float32 state after each
+    sequence).  For its gradients the forward pass keeps the state of every 32
+    tokens in 32 bits (key value / 8 bytes for each token and head) and what
+    each token wrote (4 value bytes).
+    """
+    out = (_native or load()).gated_delta(q, k, v, g, beta, _scale(scale, q), state, lengths, return_state)
+    return (out[0], out[1]) if return_state else out[0]
+
+
+def gated_delta_step(state, q, k, v, g, beta, *, scale=None, slots=None):
+    """:func:`gated_delta` for one token of each sequence.
+
+    q, k: (batch, key_heads, key), v: (batch, heads, value), g and beta: (batch,
+    heads).  state: float32 (slots, heads, key, value), a pool of running states
+    updated in place; slots as :func:`causal_conv_step`.  Returns o: (batch,
+    heads, value).
+    """
+    return (_native or load()).gated_delta_step(state, q, k, v, g, beta, _scale(scale, q), slots)
+
+
+def _scale(scale, q):
+    """The scale of a linear attention's outputs."""
+    if scale is not None:
+        return float(scale)
+    n = q.shape[-1] if getattr(q, "ndim", 0) else 0
+    return n ** -0.5 if n else 1.0
+
+
+def qk_norm(q, k, q_weight=None, k_weight=None, inv_freq=None, positions=None, *, norm="rms",
+            eps=1e-6, interleaved=False, lengths=None):
+    """Norms of queries and keys, each head on its own, with their rotation by position.
+
+    ``y = x / sqrt(mean(x^2) + eps) * weight`` ("rms"), or by the sum in place
+    of the mean ("l2": length one), or ``x * weight`` (None); then pair i of y
+    is turned by ``position * inv_freq[i]``: channels i and i + R / 2 (2i and 2i +
+    1 if ``interleaved``), R = 2 len(inv_freq).  Channels from R on are not turned.
+
+    q: (batch, length, heads, channels), k: (batch, length, key_heads,
+    channels), channels at most 256.  The weights: (channels,), float32 or q's
+    type.  inv_freq: float32 (R / 2,), without a gradient (None: no rotation).  positions:
+    int32 (batch, length), any (default: 0, 1, ..); angles are taken in 64 bits.
+    lengths: int32 (batch,), where each sequence ends; what lies past it is
+    not used, and is 0 in the results.  For single tokens length is 1 and positions
+    say where they are.
+
+    Returns (q, k).
+    """
+    out = (_native or load()).qk_norm(q, k, q_weight, k_weight, inv_freq, positions, lengths,
+                                      _activation("norm", norm, _QK_NORMS), bool(interleaved), eps)
+    return out[0], out[1]
+
+
+def dropout(x, p, seed, *, tag=0, residual=None):
+    """Dropout whose mask is never stored: ``residual + (kept ? x / (1 - p) : 0)``.
+
+    Element i of x (in the order of a contiguous x) is kept where word i % 4 of
+    Philox4x32-10 with key ``seed`` and counter (i // 4, ``tag``) is not below
+    p 2^32.  The same seed and tag draw the same mask again, in the backward
+    pass or where a node of a planned step is computed a second time; take
+    another tag for each use in a model and another seed for each step.
+
+    seed: an int, or an int64 tensor of one number on x's GPU, read when the
+    kernel runs, so that a captured graph draws another mask once the tensor
+    holds another number.  (The backward pass reads it again: between the two it must
+    not change.)  tag: an int.  p: from 0 to 1.  residual: of x's shape, float32
+    or x's type, which the result has then too.
+    """
+    number, where = (0, seed) if hasattr(seed, "data_ptr") else (_word("seed", seed), None)
+    return (_native or load()).dropout(x, p, where, number, _word("tag", tag), residual)
+
+
+def _word(name, value):
+    """An int as 64 bits (int64 or uint64)."""
+    try:
+        value = operator.index(value)
+    except TypeError:
+        raise ValueError(f"{name} must be an int, not {value!r}") from None
+    if not -(1 << 63) <= value < 1 << 64:
+        raise ValueError(f"{name} must fit 64 bits")
+    return value - (1 << 64) if value >= 1 << 63 else value
