@@ -206,7 +206,6 @@ template <class T, int KT, bool BACK>
 __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>;
-  __shared__ Tokens<KT, N> k, q;
   __shared__ double sums[kChunk];
   __shared__ float beta[kChunk];
   __shared__ float A[kChunk][kChunk + 4], inverse[kChunk][kChunk + 4];
@@ -215,8 +214,14 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   const int hk = h / (a.heads / a.key_heads), t0 = chunk * kChunk;
   const int live = min(length_of(a, b) - t0, kChunk);
   if (live <= 0) return;
-  k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, lane, 64);
-  q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, lane, 64);
+  // tokens 16m + lane % 16 over channels 32s + 8 (lane / 16) ..
+  const auto rows = [&](const rc_heads& x, int m, int s) {
+    const int t = 16 * m + lane % 16, c = 32 * s + lane / 16 * 8;
+    float v[8];
+    load_vec<8>(at_head<T>(x, b, t0 + (t < live ? t : 0), hk) + (c < a.key ? c : 0),
+                t < live ? a.key - c : 0, v);
+    return split<N>(v);
+  };
   Chunk& out = p.prepared[blockIdx.x];
   const double G = sum_of_g(a, b, h, t0, live);
   if (lane < kChunk) {
@@ -236,7 +241,8 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int n = 0; n < 2; n++) kk[m][n] = qk[m][n] = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int s = 0; s < KT; s++) {
-    const Pieces<N> ks[2] = {k.rows(0, s), k.rows(1, s)}, qs[2] = {q.rows(0, s), q.rows(1, s)};
+    const Pieces<N> ks[2] = {rows(a.k, 0, s), rows(a.k, 1, s)};
+    const Pieces<N> qs[2] = {rows(a.q, 0, s), rows(a.q, 1, s)};
 #pragma unroll
     for (int m = 0; m < 2; m++)
 #pragma unroll
@@ -292,11 +298,6 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   }
 }
 
-__device__ __forceinline__ Pieces<3> prepared(const bf16x8 (&from)[3][64]) {
-  const int lane = threadIdx.x % 64;
-  return {{from[0][lane], from[1][lane], from[2][lane]}};
-}
-
 // A head's state, 16 columns a wave: tile m of 16 rows, this lane's column and rows.
 template <int KT>
 __device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col,
@@ -323,14 +324,89 @@ __device__ __forceinline__ void store_state(float* to, const rc_delta_args& a, i
     }
 }
 
+// What a chunk's products need beside the state, loaded one chunk ahead: this thread's share of
+// the tokens' keys and queries, T and P, and for the lane's column and its eight tokens
+// (4 (lane / 16) + 0..3 and 16 more) the values or the outputs' gradients.  Loads
+// are unconditional with addresses inside the chunk; what is past its end is dropped when used.
+template <class T, int KT, int W, bool WIDE>
+struct Feed {
+  static constexpr int N = kPieces<T>, VECTORS = kChunk * KT * 4, EACH = (VECTORS + 64 * W - 1) / (64 * W);
+  typedef T TV __attribute__((ext_vector_type(8)));
+  TV k[EACH], q[EACH];
+  bf16x8 t[2][3], p[2][3];
+  T x[8];
+  float4 since[2], left[2], beta[2];
+  float whole;
+
+  __device__ static int row_of(int i) { return (threadIdx.x + i * 64 * W) / (KT * 4); }
+  __device__ static int channel_of(int i) { return (threadIdx.x + i * 64 * W) % (KT * 4) * 8; }
+
+  __device__ void fetch(const rc_delta_args& a, const Chunk& c, const rc_heads& values, int b, int h, int hk,
+                        int t0, int live, int col) {
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+      const int r = min(row_of(i), live - 1), ch = channel_of(i);
+      const T* from = at_head<T>(a.k, b, t0 + r, hk);
+      const T* fromq = at_head<T>(a.q, b, t0 + r, hk);
+      if (WIDE) {
+        const int at = ch < a.key ? ch : 0;
+        __builtin_memcpy(&k[i], from + at, sizeof(TV));
+        __builtin_memcpy(&q[i], fromq + at, sizeof(TV));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          k[i][e] = from[min(ch + e, a.key - 1)];
+          q[i][e] = fromq[min(ch + e, a.key - 1)];
+        }
+      }
+    }
+    const int lane = threadIdx.x % 64, row = lane / 16 * 4;
+#pragma unroll
+    for (int m = 0; m < 2; m++) {
+#pragma unroll
+      for (int i = 0; i < 3; i++) {
+        t[m][i] = c.t[m][i][lane];
+        p[m][i] = c.p[m][i][lane];
+      }
+      since[m] = *(const float4*)&c.since[16 * m + row];
+      left[m] = *(const float4*)&c.left[16 * m + row];
+      beta[m] = *(const float4*)&c.beta[16 * m + row];
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        x[4 * m + e] = at_head<T>(values, b, t0 + min(16 * m + row + e, live - 1), h)[min(col, a.value - 1)];
+    }
+    whole = c.since[kChunk - 1];
+  }
+  __device__ void put(Tokens<KT, N>& to_k, Tokens<KT, N>& to_q, int live, int key) const {
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+      const int r = row_of(i), ch = channel_of(i);
+      if (VECTORS % (64 * W) && r >= kChunk) break;
+      float v[8], w[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const bool on = r < live && ch + e < key;
+        v[e] = on ? (float)k[i][e] : 0.f;
+        w[e] = on ? (float)q[i][e] : 0.f;
+      }
+      to_k.put(r, ch, v);
+      to_q.put(r, ch, w);
+    }
+  }
+};
+__device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3]) { return {{x[0], x[1], x[2]}}; }
+__device__ __forceinline__ float element(const float4& v, int i) {
+  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+}
+
 // Forward: a wave holds 16 columns of the state in registers from the first chunk to the
 // last; columns do not depend on one another, and what a product leaves in a lane is what the
 // next one takes from it, so waves share nothing but the tokens in LDS.
-template <class T, int KT, int W>
+template <class T, int KT, int W, bool WIDE>
 __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  constexpr int N = kPieces<T>;
-  __shared__ Tokens<KT, N> k, q;
+  constexpr int N = kPieces<T>, BUFFERS = sizeof(Tokens<KT, N>) * 4 <= 128 * 1024 ? 2 : 1;
+  __shared__ Tokens<KT, N> tokens[BUFFERS][2];
   const int slices = (a.value + 16 * W - 1) / (16 * W);
   const int lane = threadIdx.x % 64, bh = blockIdx.x / slices, b = bh / a.heads, h = bh % a.heads;
   const int hk = h / (a.heads / a.key_heads), end = length_of(a, b);
@@ -338,18 +414,25 @@ __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
   const int col = wave * 16 + lane % 16, row = lane / 16 * 4;
   const bool on = col < a.value;
   const int64_t size = (int64_t)a.key * a.value;
+  const Chunk* prepared = p.prepared + (int64_t)bh * p.chunks;
   f32x4 S[2 * KT];
   load_state<KT>(a.state_in ? a.state_in + bh * size : nullptr, a, col, S);
-  const T* v = at_head<T>(a.v, b, 0, h) + (on ? col : 0);
   T* o = at_head<T>(a.o, b, 0, h) + col;
-  for (int chunk = 0; chunk * kChunk < end; chunk++) {
+  const int chunks = (end + kChunk - 1) / kChunk;
+  Feed<T, KT, W, WIDE> next;
+  if (chunks) next.fetch(a, prepared[0], a.v, b, h, hk, 0, min(end, kChunk), col);
+  for (int chunk = 0; chunk < chunks; chunk++) {
     const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    const Chunk& c = p.prepared[(int64_t)bh * p.chunks + chunk];
+    Tokens<KT, N>&k = tokens[chunk % BUFFERS][0], &q = tokens[chunk % BUFFERS][1];
+    if (BUFFERS == 1) __syncthreads();
+    next.put(k, q, live, a.key);
+    __syncthreads();
+    const Feed<T, KT, W, WIDE> c = next;
+    {
+      const int n = min(chunk + 1, chunks - 1);
+      next.fetch(a, prepared[n], a.v, b, h, hk, n * kChunk, min(end - n * kChunk, kChunk), col);
+    }
     if (p.states) store_state<KT>(p.states + ((int64_t)bh * p.chunks + chunk) * size, a, col, S);
-    __syncthreads();
-    k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, threadIdx.x, 64 * W);
-    q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, threadIdx.x, 64 * W);
-    __syncthreads();
     f32x4 r[2], out[2], w[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) r[m] = out[m] = w[m] = f32x4{0, 0, 0, 0};
@@ -367,31 +450,30 @@ __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const int t = 16 * m + row + e;
-        const float x = on && t < live ? (float)v[(t0 + (t < live ? t : 0)) * a.v.time] : 0.f;
-        r[m][e] = c.beta[t] * (x - c.since[t] * r[m][e]);
-        out[m][e] *= a.scale * c.since[t];
+        const float x = on && t < live ? (float)c.x[4 * m + e] : 0.f, since = element(c.since[m], e);
+        r[m][e] = element(c.beta[m], e) * (x - since * r[m][e]);
+        out[m][e] *= a.scale * since;
       }
     const Pieces<3> rs = operand<3>(r[0], r[1]);
 #pragma unroll
-    for (int m = 0; m < 2; m++) mul(w[m], prepared(c.t[m]), rs);
+    for (int m = 0; m < 2; m++) mul(w[m], pieces(c.t[m]), rs);
     const Pieces<3> ws = operand<3>(w[0], w[1]);
 #pragma unroll
     for (int m = 0; m < 2; m++) {
-      mul(out[m], prepared(c.p[m]), ws);
+      mul(out[m], pieces(c.p[m]), ws);
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const int t = 16 * m + row + e;
         if (on && t < live) o[(t0 + t) * a.o.time] = (T)out[m][e];
         if (p.written && on)
           p.written[(((int64_t)bh * p.chunks + chunk) * kChunk + t) * a.value + col] = w[m][e];
-        w[m][e] *= c.left[t];
+        w[m][e] *= element(c.left[m], e);
       }
     }
     const Pieces<3> us = operand<3>(w[0], w[1]);
-    const float whole = c.since[kChunk - 1];
 #pragma unroll
     for (int m = 0; m < 2 * KT; m++) {
-      S[m] *= whole;
+      S[m] *= c.whole;
       mul(S[m], k.columns(m), us);
     }
   }
@@ -401,11 +483,11 @@ __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
 }
 
 // Backward through the states, from the last chunk to the first.
-template <class T, int KT, int W>
+template <class T, int KT, int W, bool WIDE>
 __global__ __launch_bounds__(64 * W) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  constexpr int N = kPieces<T>;
-  __shared__ Tokens<KT, N> k, q;
+  constexpr int N = kPieces<T>, BUFFERS = sizeof(Tokens<KT, N>) * 4 <= 128 * 1024 ? 2 : 1;
+  __shared__ Tokens<KT, N> tokens[BUFFERS][2];
   const int slices = (a.value + 16 * W - 1) / (16 * W);
   const int lane = threadIdx.x % 64, bh = blockIdx.x / slices, b = bh / a.heads, h = bh % a.heads;
   const int hk = h / (a.heads / a.key_heads), end = length_of(a, b);
@@ -413,18 +495,28 @@ __global__ __launch_bounds__(64 * W) void k_delta_states_back(DeltaParams p) {
   const int col = wave * 16 + lane % 16, row = lane / 16 * 4;
   const bool on = col < a.value;
   const int64_t size = (int64_t)a.key * a.value;
+  const Chunk* prepared = p.prepared + (int64_t)bh * p.chunks;
   f32x4 E[2 * KT];
   load_state<KT>(a.dstate_out ? a.dstate_out + bh * size : nullptr, a, col, E);
-  const T* d_o = at_head<T>(a.do_, b, 0, h) + (on ? col : 0);
   T* dv = at_head<T>(a.dv, b, 0, h) + col;
-  for (int chunk = (end + kChunk - 1) / kChunk - 1; chunk >= 0; chunk--) {
+  const int chunks = (end + kChunk - 1) / kChunk;
+  Feed<T, KT, W, WIDE> next;
+  if (chunks) {
+    const int n = chunks - 1;
+    next.fetch(a, prepared[n], a.do_, b, h, hk, n * kChunk, end - n * kChunk, col);
+  }
+  for (int chunk = chunks - 1; chunk >= 0; chunk--) {
     const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    const Chunk& c = p.prepared[(int64_t)bh * p.chunks + chunk];
+    Tokens<KT, N>&k = tokens[chunk % BUFFERS][0], &q = tokens[chunk % BUFFERS][1];
+    if (BUFFERS == 1) __syncthreads();
+    next.put(k, q, live, a.key);
+    __syncthreads();
+    const Feed<T, KT, W, WIDE> c = next;
+    {
+      const int n = max(chunk - 1, 0);
+      next.fetch(a, prepared[n], a.do_, b, h, hk, n * kChunk, min(end - n * kChunk, kChunk), col);
+    }
     store_state<KT>(p.dstates + ((int64_t)bh * p.chunks + chunk) * size, a, col, E);
-    __syncthreads();
-    k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, threadIdx.x, 64 * W);
-    q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, threadIdx.x, 64 * W);
-    __syncthreads();
     f32x4 dw[2], dr[2], g[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) dw[m] = dr[m] = f32x4{0, 0, 0, 0};
@@ -438,32 +530,30 @@ __global__ __launch_bounds__(64 * W) void k_delta_states_back(DeltaParams p) {
     for (int m = 0; m < 2; m++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const int t = 16 * m + row + e;
-        g[m][e] = on && t < live ? (float)d_o[(t0 + (t < live ? t : 0)) * a.do_.time] : 0.f;
-        dw[m][e] *= c.left[t];
+        g[m][e] = on && 16 * m + row + e < live ? (float)c.x[4 * m + e] : 0.f;
+        dw[m][e] *= element(c.left[m], e);
       }
     const Pieces<N> gs = operand<N>(g[0], g[1]);
 #pragma unroll
-    for (int m = 0; m < 2; m++) mul(dw[m], prepared(c.p[m]), gs);
+    for (int m = 0; m < 2; m++) mul(dw[m], pieces(c.p[m]), gs);
     const Pieces<3> dws = operand<3>(dw[0], dw[1]);
 #pragma unroll
     for (int m = 0; m < 2; m++) {
-      mul(dr[m], prepared(c.t[m]), dws);
+      mul(dr[m], pieces(c.t[m]), dws);
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const int t = 16 * m + row + e;
         if (on) p.written[(((int64_t)bh * p.chunks + chunk) * kChunk + t) * a.value + col] = dr[m][e];
-        const float x = c.beta[t] * dr[m][e];
+        const float x = element(c.beta[m], e) * dr[m][e], since = element(c.since[m], e);
         if (on && t < live) dv[(t0 + t) * a.dv.time] = (T)x;
-        dr[m][e] = -c.since[t] * x;
-        g[m][e] *= a.scale * c.since[t];
+        dr[m][e] = -since * x;
+        g[m][e] *= a.scale * since;
       }
     }
     const Pieces<3> drs = operand<3>(dr[0], dr[1]), gos = operand<3>(g[0], g[1]);
-    const float whole = c.since[kChunk - 1];
 #pragma unroll
     for (int m = 0; m < 2 * KT; m++) {
-      E[m] *= whole;
+      E[m] *= c.whole;
       mul(E[m], k.columns(m), drs);
       mul(E[m], q.columns(m), gos);
     }
@@ -833,6 +923,11 @@ uint64_t workspace_of(const rc_delta_args& a, bool back) {
   return n;
 }
 
+// f(whether rows of the key are whole loads of eight).
+template <class F>
+int by_width(int32_t key, F&& f) {
+  return key % 8 ? f(std::false_type{}) : f(std::true_type{});
+}
 // f(integral_constant of the key's tiles of 32).
 template <class F>
 int by_key(int32_t key, F&& f) {
@@ -895,9 +990,11 @@ extern "C" int rc_delta_forward(const rc_delta_args* args, void* stream) {
         k_delta_prepare<T, KT, false><<<(unsigned)pairs_of(a), 64, 0, s>>>(p);
         if (int e = launched("k_delta_prepare")) return e;
       }
-      k_delta_forward<T, KT, kWaves>
-          <<<(unsigned)(bh * cdiv(a.value, 16 * kWaves)), 64 * kWaves, 0, s>>>(p);
-      return launched("k_delta_forward");
+      return by_width(a.key, [&](auto wide) {
+        k_delta_forward<T, KT, kWaves, decltype(wide)::value>
+            <<<(unsigned)(bh * cdiv(a.value, 16 * kWaves)), 64 * kWaves, 0, s>>>(p);
+        return launched("k_delta_forward");
+      });
     });
   });
 }
@@ -928,9 +1025,12 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
         k_delta_prepare<T, KT, true><<<(unsigned)pairs_of(a), 64, 0, s>>>(p);
         if (int e = launched("k_delta_prepare")) return e;
       }
-      k_delta_states_back<T, KT, kWaves>
-          <<<(unsigned)(bh * cdiv(a.value, 16 * kWaves)), 64 * kWaves, 0, s>>>(p);
-      if (int e = launched("k_delta_states_back")) return e;
+      const int e = by_width(a.key, [&](auto wide) {
+        k_delta_states_back<T, KT, kWaves, decltype(wide)::value>
+            <<<(unsigned)(bh * cdiv(a.value, 16 * kWaves)), 64 * kWaves, 0, s>>>(p);
+        return launched("k_delta_states_back");
+      });
+      if (e) return e;
       if (!p.chunks) return (int)RC_OK;
       k_delta_inputs_back<T, KT><<<(unsigned)pairs_of(a), 256, 0, s>>>(p);
       if (int e = launched("k_delta_inputs_back")) return e;
