@@ -1,0 +1,561 @@
+// Shared by the gated delta rule's kernels (delta.hip, delta_back.hip).  Each head keeps a matrix S (key x value); a token decays
+// it, reads what it holds for the key k, and writes back the difference to v:
+//   S_t = a_t S_{t-1} + k_t w_t^T,  w_t = beta_t (v_t - a_t S_{t-1}^T k_t),
+//   o_t = scale S_t^T q_t,  a = exp(g).
+//
+// The walk goes by chunks of 32 tokens.  With G the sum of g from the chunk's first token,
+// S the state before it, and D_ij = exp(G_i - G_j) for j <= i,
+//   W = T R,   R_i = beta_i (v_i - exp(G_i) S^T k_i),
+//   T = (I + A)^-1,   A_ij = beta_i D_ij k_i . k_j   for j < i,
+//   O_i = scale exp(G_i) S^T q_i + sum_j P_ij w_j,   P_ij = scale D_ij q_i . k_j,
+//   S' = exp(G_31) S + sum_j exp(G_31 - G_j) k_j w_j^T.
+// T and P need no state: k_delta_prepare computes them for all chunks at once, T by
+// forward substitution.  What is left of a chunk are five products of at most
+// 32 x key x value, k_delta_forward's, one chunk after the other.
+//
+// Backward, with dO and the gradient E of S':
+//   dW_j = sum_i P_ij do_i + exp(G_31 - G_j) E^T k_j,   dR = T^T dW,   dv = beta dR,
+//   dS = exp(G_31) E + sum_i exp(G_i) (scale q_i do_i^T - beta_i k_i dR_i^T)
+// again one chunk after the other, from the last (k_delta_states_back); w and dR do
+// not depend on how tokens are cut into chunks.  The other gradients then need no order
+// (k_delta_inputs_back).  With M_ij = D_ij scale do_i . w_j and N_ij = D_ij dR_i . w_j (j < i),
+//   dq_i = scale exp(G_i) S do_i + sum_j M_ij k_j
+//   x_i = exp(G_i) S dR_i + sum_j N_ij k_j,    dbeta_i = dR_i . v_i - k_i . x_i
+//   dk_i = -beta_i x_i (as read) + exp(G_31 - G_i) E w_i + sum_l (M_li q_l - beta_l N_li k_l) (as written)
+//   dG_i = q_i . dq_i + k_i . (dk_i as read - as written),  dG_31 += <E, S'>,
+//   dg_t = sum of dG_i over i >= t.
+//
+// Products run on the bf16 matrix instructions with operands taken apart into
+// bf16 numbers that add up to them: one for bf16, two for f16, three for 32 bits, and
+// the products of pieces down to 2^-16 of the largest: 32-bit results from instructions with 16
+// times the rate of the 32-bit ones.  D's exponents are differences
+// of sums in 64 bits, so a token that forgets everything costs the later ones nothing.
+#pragma once
+
+#include "ops_internal.h"
+
+namespace rcdelta {
+
+using namespace rcops;
+
+constexpr int kChunk = 32;
+constexpr int kMaxHead = 256;
+constexpr int kWaves = 4;                              // of a workgroup that walks
+
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// bf16 numbers that hold a T exactly.
+template <class T>
+constexpr int kPieces = sizeof(T) == 4 ? 3 : 2;
+template <>
+inline constexpr int kPieces<bf16> = 1;
+
+template <int N>
+struct Pieces {
+  bf16x8 p[N];
+};
+
+// Two at a time: one conversion, and what it left off for the next piece.
+template <int N>
+__device__ __forceinline__ Pieces<N> split(const float (&v)[8]) {
+  u32x4 w[N];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    f32x2 x = {v[2 * j], v[2 * j + 1]};
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+      w[i][j] = u;
+      x[0] -= __builtin_bit_cast(float, u << 16);
+      x[1] -= __builtin_bit_cast(float, u & 0xffff0000u);
+    }
+  }
+  Pieces<N> s;
+#pragma unroll
+  for (int i = 0; i < N; i++) s.p[i] = __builtin_bit_cast(bf16x8, w[i]);
+  return s;
+}
+
+// acc += A B for 16 x 32 by 32 x 16, the smallest products of pieces first.  A lane holds 8
+// numbers of row (column) lane % 16; which 8 of the 32 is free as long as both sides agree.
+// The result's lane holds rows 4 (lane / 16) + 0..3 of column lane % 16.
+template <int NA, int NB>
+__device__ __forceinline__ void mul(f32x4& acc, const Pieces<NA>& a, const Pieces<NB>& b) {
+#pragma unroll
+  for (int s = 2; s >= 0; s--)
+#pragma unroll
+    for (int i = 0; i <= s; i++)
+      if (i < NA && s - i < NB)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
+}
+
+// Two results of 16 rows each are 32 rows of an operand as they are: lane group g holds
+// rows 4g + 0..3 and 16 + 4g + 0..3.  All operands below take their 32 in that order.
+template <int N>
+__device__ __forceinline__ Pieces<N> operand(const f32x4& lo, const f32x4& hi) {
+  const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return split<N>(x);
+}
+
+// exp(x), x in 64 bits.
+__device__ __forceinline__ float exp_of(double x) {
+  const double e = x * 1.44269504088896340736;
+  const double n = __builtin_rint(e);
+  return __builtin_amdgcn_ldexpf(fast_exp2((float)(e - n)), (int)__builtin_fmax(n, -1000.0));
+}
+
+// 32 rows (tokens) of `32 KT` channels in LDS as pieces.  Within each 32 channels, groups of four
+// are ordered 0 4 1 5 2 6 3 7, so that a lane's operand (above) is 16 bytes.
+template <int KT, int N>
+struct Tokens {
+  static constexpr int STRIDE = KT * 32 + 8;
+  bf16 at[N][kChunk][STRIDE];
+
+  // From rows `row` elements apart; what is past `live` tokens or `n` channels is 0.
+  template <class T>
+  __device__ void load(const T* x, int64_t row, int live, int n, int thread, int threads) {
+    for (int i = thread; i < kChunk * KT * 4; i += threads) {
+      const int r = i / (KT * 4), c = i % (KT * 4) * 8;
+      float v[8];
+      load_vec<8>(x + (r < live ? r : 0) * row + (c < n ? c : 0), r < live ? n - c : 0, v);
+      put(r, c, v);
+    }
+  }
+  __device__ void put(int r, int c, const float (&v)[8]) {
+    const Pieces<N> s = split<N>(v);
+    bf16* to = &at[0][r][c / 32 * 32 + (c % 16 / 4) * 8 + c % 32 / 16 * 4];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      *(bf16x4*)(to + i * (kChunk * STRIDE)) = s.p[i].lo;
+      *(bf16x4*)(to + i * (kChunk * STRIDE) + 8) = s.p[i].hi;
+    }
+  }
+  // Row tile t (tokens 16t + ..) over channels 32s + 0..31.
+  __device__ Pieces<N> rows(int t, int s) const {
+    const int lane = threadIdx.x % 64;
+    Pieces<N> f;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+      f.p[i] = *(const bf16x8*)&at[i][16 * t + lane % 16][32 * s + lane / 16 * 8];
+    return f;
+  }
+  // Channels 16t + .. over the 32 tokens: reads that transpose four by four.
+  __device__ Pieces<N> columns(int t) const {
+    const int lane = threadIdx.x % 64;
+    Pieces<N> f;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const bf16* from =
+          &at[i][lane / 16 * 4 + lane % 16 / 4][t / 2 * 32 + lane % 4 * 8 + t % 2 * 4];
+      typedef s16x4 __attribute__((address_space(3))) * lds;
+      f.p[i].lo = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)from));
+      f.p[i].hi = __builtin_bit_cast(
+          bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(from + 16 * STRIDE)));
+    }
+    return f;
+  }
+  // Eight channels as they are where one piece is all.
+  __device__ void put(int r, int c, const bf16x8& v) {
+    bf16* to = &at[0][r][c / 32 * 32 + (c % 16 / 4) * 8 + c % 32 / 16 * 4];
+    *(bf16x4*)to = v.lo;
+    *(bf16x4*)(to + 8) = v.hi;
+  }
+  __device__ float value(int r, int c) const {
+    const int at_c = c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4;
+    float x = (float)at[N - 1][r][at_c];
+#pragma unroll
+    for (int i = N - 2; i >= 0; i--) x += (float)at[i][r][at_c];
+    return x;
+  }
+};
+
+// What k_delta_prepare leaves for one chunk of one head: T and P (backward: their
+// transposes) as operands of two row tiles, and numbers of each token.
+struct Chunk {
+  bf16x8 t[2][3][64], p[2][3][64];
+  float since[kChunk], left[kChunk], beta[kChunk];    // exp(G_i), exp(G_31 - G_i), beta_i
+};
+constexpr int kChunkVectors = sizeof(Chunk) / 16;
+static_assert(sizeof(Chunk) % 16 == 0, "copied in vectors");
+
+// States (and their gradients) of every chunk as a lane of the walks holds them, four rows of a
+// column together: [batch][heads][chunks][columns(value)][rows(key)] in 32 bits; w and dR likewise,
+// four tokens of a column together: [batch][heads][chunks][columns(value)][32].
+__host__ __device__ inline int rows_of(int key) {
+  return key <= 32 ? 32 : key <= 64 ? 64 : key <= 128 ? 128 : 256;
+}
+__host__ __device__ inline int columns_of(int value) { return (value + 31) / 32 * 32; }
+
+struct DeltaParams {
+  rc_delta_args a;
+  int32_t chunks;
+  Chunk* prepared;                                    // [batch][heads][chunks]
+  float* states;
+  float* written;                                     // w, or dR
+  const float* kept_written;
+  float* dstates;
+  float* partial;                                     // [2][batch][length][heads / each][key]
+  int32_t each;                                       // heads of a workgroup of k_delta_inputs_back
+};
+
+__device__ __forceinline__ int length_of(const rc_delta_args& a, int b) {
+  return a.lengths ? min(max(a.lengths[b], 0), a.length) : a.length;
+}
+__device__ __forceinline__ float at_token(const rc_view& v, int64_t b, int64_t t, int64_t h) {
+  return static_cast<const float*>(v.data)[b * v.batch + t * v.time + h];
+}
+
+// g of a token.  One below -1000 counts as -1000: exp of either is 0 in 32 bits, and
+// -infinity has no differences.
+__device__ __forceinline__ double log_decay(const rc_view& g, int64_t b, int64_t t, int64_t h) {
+  const float x = at_token(g, b, t, h);
+  return x < -1000.f ? -1000.0 : (double)x;
+}
+// G of a chunk's 32 tokens (in every lane's token lane % 32): sums from its first token.
+__device__ __forceinline__ double sum_of_g(const rc_delta_args& a, int b, int h, int t0, int live) {
+  const int i = threadIdx.x % 32;
+  double G = 0;
+  if (a.g.data && i < live) G = log_decay(a.g, b, t0 + i, h);
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const double before = __shfl_up(G, d, 32);
+    if (i >= d) G += before;
+  }
+  return G;
+}
+
+// One wave a chunk of a head.
+template <class T, int KT, bool BACK>
+__global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
+  const rc_delta_args& a = p.a;
+  constexpr int N = kPieces<T>;
+  __shared__ double sums[kChunk];
+  __shared__ float beta[kChunk];
+  __shared__ float A[kChunk][kChunk + 4], inverse[kChunk][kChunk + 4];
+  const int lane = threadIdx.x, bh = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+  const int b = bh / a.heads, h = bh % a.heads;
+  const int hk = h / (a.heads / a.key_heads), t0 = chunk * kChunk;
+  const int live = min(length_of(a, b) - t0, kChunk);
+  if (live <= 0) return;
+  // tokens 16m + lane % 16 over channels 32s + 8 (lane / 16) ..
+  const auto rows = [&](const rc_heads& x, int m, int s) {
+    const int t = 16 * m + lane % 16, c = 32 * s + lane / 16 * 8;
+    float v[8];
+    load_vec<8>(at_head<T>(x, b, t0 + (t < live ? t : 0), hk) + (c < a.key ? c : 0),
+                t < live ? a.key - c : 0, v);
+    return split<N>(v);
+  };
+  Chunk& out = p.prepared[blockIdx.x];
+  const double G = sum_of_g(a, b, h, t0, live);
+  if (lane < kChunk) {
+    const double last = __shfl(G, kChunk - 1);
+    sums[lane] = G;
+    beta[lane] = lane < live ? at_token(a.beta, b, t0 + lane, h) : 0.f;
+    out.since[lane] = exp_of(G);
+    out.left[lane] = exp_of(last - G);
+    out.beta[lane] = beta[lane];
+  }
+  __syncthreads();
+  // tiles of k_i . k_j and q_i . k_j with rows j (backward for P: rows i) and the other as columns
+  f32x4 kk[2][2], qk[2][2];
+#pragma unroll
+  for (int m = 0; m < 2; m++)
+#pragma unroll
+    for (int n = 0; n < 2; n++) kk[m][n] = qk[m][n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < KT; s++) {
+    const Pieces<N> ks[2] = {rows(a.k, 0, s), rows(a.k, 1, s)};
+    const Pieces<N> qs[2] = {rows(a.q, 0, s), rows(a.q, 1, s)};
+#pragma unroll
+    for (int m = 0; m < 2; m++)
+#pragma unroll
+      for (int n = 0; n < 2; n++) {
+        if (m <= n) mul(kk[m][n], ks[m], ks[n]);      // rows j of tile m, columns i of tile n
+        if (BACK ? m >= n : m <= n) mul(qk[m][n], BACK ? qs[m] : ks[m], BACK ? ks[n] : qs[n]);
+      }
+  }
+  const int col = lane % 16, row = lane / 16 * 4;
+#pragma unroll
+  for (int m = 0; m < 2; m++)
+#pragma unroll
+    for (int n = 0; n < 2; n++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        const int i = 16 * n + col, j = 16 * m + row + r;
+        A[i][j] = j < i ? beta[i] * exp_of(sums[i] - sums[j]) * kk[m][n][r] : 0.f;
+        const int pi = BACK ? j : i, pj = BACK ? i : j;
+        qk[m][n][r] = pj <= pi ? a.scale * exp_of(sums[pi] - sums[pj]) * qk[m][n][r] : 0.f;
+      }
+#pragma unroll
+  for (int n = 0; n < 2; n++) {
+    const Pieces<3> f = operand<3>(qk[0][n], qk[1][n]);
+#pragma unroll
+    for (int i = 0; i < 3; i++) out.p[n][i][lane] = f.p[i];
+  }
+  __syncthreads();
+  // T, a column a lane, by forward substitution
+  {
+    const int c = lane % 32;
+    float t[kChunk];
+#pragma unroll
+    for (int i = 0; i < kChunk; i++) {
+      float s = i == c ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < i; j++) s = fmaf(-A[i][j], t[j], s);
+      t[i] = s;
+      if (lane < 32) inverse[i][c] = s;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < 2; n++) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const int i = 16 * n + col, j = 16 * (e / 4) + row + e % 4;
+      x[e] = BACK ? inverse[j][i] : inverse[i][j];
+    }
+    const Pieces<3> f = split<3>(x);
+#pragma unroll
+    for (int i = 0; i < 3; i++) out.t[n][i][lane] = f.p[i];
+  }
+}
+
+// Column `col` of a head's state: tile m has this lane's rows 16m + 4 (lane / 16) + 0..3.
+template <int KT>
+__device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col,
+                                           f32x4 (&S)[2 * KT]) {
+  const int row = threadIdx.x % 64 / 16 * 4;
+#pragma unroll
+  for (int m = 0; m < 2 * KT; m++)
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int i = 16 * m + row + r;
+      S[m][r] = from && i < a.key && col < a.value ? from[(int64_t)i * a.value + col] : 0.f;
+    }
+}
+template <int KT>
+__device__ __forceinline__ void store_state(float* to, const rc_delta_args& a, int col,
+                                            const f32x4 (&S)[2 * KT]) {
+  const int row = threadIdx.x % 64 / 16 * 4;
+#pragma unroll
+  for (int m = 0; m < 2 * KT; m++)
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int i = 16 * m + row + r;
+      if (i < a.key && col < a.value) to[(int64_t)i * a.value + col] = S[m][r];
+    }
+}
+// The same into [column][row] (col < columns_of(value)).
+template <int KT>
+__device__ __forceinline__ void keep_state(float* to, int col, const f32x4 (&S)[2 * KT]) {
+  float* at = to + col * (32 * KT) + threadIdx.x % 64 / 16 * 4;
+#pragma unroll
+  for (int m = 0; m < 2 * KT; m++) *(f32x4*)(at + 16 * m) = S[m];
+}
+
+// What a chunk's products need beside the state, in LDS.
+template <int KT, int N>
+struct Stage {
+  Tokens<KT, N> k, q;
+  union {
+    Chunk c;
+    u32x4 raw[kChunkVectors];
+  };
+  __device__ Stage() {}
+};
+template <class T, int KT>
+constexpr int kStages = 2 * sizeof(Stage<KT, kPieces<T>>) <= 160 * 1024 ? 2 : 1;
+
+// The same one chunk ahead, this thread's share in registers, and for the lane's column and its
+// eight tokens (4 (lane / 16) + 0..3 and 16 more) the values or the outputs'
+// gradients.  Loads are unconditional with addresses inside the chunk; what is past its
+// end is dropped when used.  WIDE: the key is a multiple of eight.
+template <class T, int KT, int W, bool WIDE>
+struct Feed {
+  static constexpr int N = kPieces<T>, VECTORS = kChunk * KT * 4, THREADS = 64 * W;
+  static constexpr int EACH = (VECTORS + THREADS - 1) / THREADS;
+  static constexpr int RAW = (kChunkVectors + THREADS - 1) / THREADS;
+  typedef T TV __attribute__((ext_vector_type(8)));
+  TV k[EACH], q[EACH];
+  u32x4 raw[RAW];
+  T x[8];
+
+  __device__ static int row_of(int i) { return (threadIdx.x + i * THREADS) / (KT * 4); }
+  __device__ static int channel_of(int i) { return (threadIdx.x + i * THREADS) % (KT * 4) * 8; }
+
+  __device__ void fetch(const rc_delta_args& a, const Chunk& c, const rc_heads& values, int b, int h, int hk,
+                        int t0, int live, int col) {
+    const T* from_k = at_head<T>(a.k, b, t0, hk);
+    const T* from_q = at_head<T>(a.q, b, t0, hk);
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+      const int r = min(row_of(i), live - 1), ch = channel_of(i);
+      if (WIDE) {
+        const int at = ch < a.key ? ch : 0;
+        __builtin_memcpy(&k[i], from_k + r * a.k.time + at, sizeof(TV));
+        __builtin_memcpy(&q[i], from_q + r * a.q.time + at, sizeof(TV));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          k[i][e] = from_k[r * a.k.time + min(ch + e, a.key - 1)];
+          q[i][e] = from_q[r * a.q.time + min(ch + e, a.key - 1)];
+        }
+      }
+    }
+    const u32x4* from = reinterpret_cast<const u32x4*>(&c);
+#pragma unroll
+    for (int i = 0; i < RAW; i++) raw[i] = from[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)];
+    const T* from_x = at_head<T>(values, b, t0, h) + min(col, a.value - 1);
+    const int row = threadIdx.x % 64 / 16 * 4;
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = from_x[min(e / 4 * 16 + row + e % 4, live - 1) * values.time];
+  }
+  __device__ void put(Stage<KT, N>& to, int live, int key) const {
+    const bool all = live == kChunk && key == 32 * KT;
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+      const int r = row_of(i), ch = channel_of(i);
+      if (VECTORS % THREADS && r >= kChunk) break;
+      TV u = k[i], v = q[i];
+      if (!all) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const bool on = r < live && ch + e < key;
+          u[e] = on ? u[e] : (T)0.f;
+          v[e] = on ? v[e] : (T)0.f;
+        }
+      }
+      if constexpr (N == 1) {
+        to.k.put(r, ch, u);
+        to.q.put(r, ch, v);
+      } else {
+        float x[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          x[e] = (float)u[e];
+          y[e] = (float)v[e];
+        }
+        to.k.put(r, ch, x);
+        to.q.put(r, ch, y);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RAW; i++) to.raw[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)] = raw[i];
+  }
+};
+__device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {
+  const int lane = threadIdx.x % 64;
+  return {{x[0][lane], x[1][lane], x[2][lane]}};
+}
+
+// A walk's place: a workgroup takes 16 W columns of one head; those of one head are as many
+// workgroups apart as there are heads, for one of the eight caches as a rule.
+struct Walk {
+  int b, h, hk, bh, col, row, end, chunks;
+  bool on;
+  __device__ Walk(const rc_delta_args& a, int columns) {
+    const int heads = a.batch * a.heads, lane = threadIdx.x % 64;
+    bh = blockIdx.x % heads;
+    b = bh / a.heads;
+    h = bh % a.heads;
+    hk = h / (a.heads / a.key_heads);
+    col = blockIdx.x / heads * columns + threadIdx.x / 64 * 16 + lane % 16;
+    row = lane / 16 * 4;
+    on = col < a.value;
+    end = length_of(a, b);
+    chunks = (end + kChunk - 1) / kChunk;
+  }
+};
+
+// ------------------------------------------------------------------ host side
+
+inline int check(const rc_delta_args* a) {
+  if (!a || !dtype_ok(a->dtype) || a->batch < 0 || a->length < 0 || a->length > kMaxExtent ||
+      a->key < 1 || a->key > kMaxHead || a->value < 1 || a->value > kMaxHead)
+    return RC_E_ARG;
+  if (a->heads < 0 || a->key_heads < 0 || (a->heads && (!a->key_heads || a->heads % a->key_heads)))
+    return RC_E_ARG;
+  return RC_OK;
+}
+inline bool empty(const rc_delta_args& a) { return !a.batch || !a.heads; }
+
+inline int64_t chunks_of(const rc_delta_args& a) { return cdiv(a.length, kChunk); }
+// Chunks of all heads.  (batch x heads is checked first: it fits a launch.)
+inline int64_t pairs_of(const rc_delta_args& a) { return (int64_t)a.batch * a.heads * chunks_of(a); }
+inline uint64_t state_floats(const rc_delta_args& a) {
+  return (uint64_t)pairs_of(a) * columns_of(a.value) * rows_of(a.key);
+}
+inline uint64_t kept_bytes(const rc_delta_args& a) {
+  return (state_floats(a) + (uint64_t)pairs_of(a) * columns_of(a.value) * kChunk) * sizeof(float);
+}
+// Heads of a workgroup of k_delta_inputs_back: all that share a key head, or the largest part of
+// them that leaves two workgroups a compute unit.
+inline int heads_together(const rc_delta_args& a) {
+  const int per = a.heads / a.key_heads;
+  for (int each = per; each > 1; each--)
+    if (per % each == 0 && pairs_of(a) / each >= 512) return each;
+  return 1;
+}
+// Whether the sizes fit the launches.
+inline int fits(const rc_delta_args& a) {
+  const int64_t bh = (int64_t)a.batch * a.heads;
+  if (!launchable(bh, 256) || !launchable(bh * cdiv(a.value, 16 * kWaves), 64 * kWaves) ||
+      !launchable(pairs_of(a), 256))
+    return RC_E_OVERFLOW;
+  if (!launchable(cdiv(2 * (int64_t)a.batch * a.length * a.key_heads * a.key, 256), 256))
+    return RC_E_OVERFLOW;
+  return RC_OK;
+}
+inline uint64_t workspace_of(const rc_delta_args& a, bool back) {
+  if (empty(a)) return 0;
+  uint64_t n = (uint64_t)pairs_of(a) * sizeof(Chunk);
+  if (back) {
+    n += kept_bytes(a);
+    const int per = a.heads / a.key_heads, each = heads_together(a);
+    if (per != each) n += 2 * (uint64_t)a.batch * a.length * (a.heads / each) * a.key * sizeof(float);
+  }
+  return n;
+}
+
+// f(whether rows of the key are whole loads of eight).
+template <class F>
+inline int by_width(int32_t key, F&& f) {
+  return key % 8 ? f(std::false_type{}) : f(std::true_type{});
+}
+// f(integral_constant of the key's tiles of 32).
+template <class F>
+inline int by_key(int32_t key, F&& f) {
+  if (key <= 32) return f(std::integral_constant<int, 1>{});
+  if (key <= 64) return f(std::integral_constant<int, 2>{});
+  if (key <= 128) return f(std::integral_constant<int, 4>{});
+  return f(std::integral_constant<int, 8>{});
+}
+
+inline DeltaParams params(const rc_delta_args& a) {
+  DeltaParams p = {};
+  p.a = a;
+  p.chunks = (int32_t)chunks_of(a);
+  p.prepared = static_cast<Chunk*>(a.workspace);
+  p.states = a.kept;
+  return p;
+}
+
+template <class T, int KT, bool BACK>
+inline int prepare(const DeltaParams& p, hipStream_t s) {
+  if (!p.chunks) return RC_OK;
+  k_delta_prepare<T, KT, BACK><<<(unsigned)pairs_of(p.a), 64, 0, s>>>(p);
+  return launched("k_delta_prepare");
+}
+// Workgroups of a walk.
+inline unsigned walks_of(const rc_delta_args& a) {
+  return (unsigned)((int64_t)a.batch * a.heads * cdiv(a.value, 16 * kWaves));
+}
+
+}  // namespace rcdelta
