@@ -360,91 +360,107 @@ __device__ __forceinline__ void keep_state(float* to, int col, const f32x4 (&S)[
   for (int m = 0; m < 2 * KT; m++) *(f32x4*)(at + 16 * m) = S[m];
 }
 
-// What a chunk's products need beside the state, in LDS.
-template <int KT, int N>
+// What a chunk's products need beside the state, in LDS; x: the values, or the outputs'
+// gradients, of the workgroup's columns.
+template <class T, int KT, int W>
 struct Stage {
+  static constexpr int N = kPieces<T>, COLUMNS = 16 * W;
   Tokens<KT, N> k, q;
   union {
     Chunk c;
     u32x4 raw[kChunkVectors];
   };
+  T x[kChunk][COLUMNS + 8];
   __device__ Stage() {}
 };
-template <class T, int KT>
-constexpr int kStages = 2 * sizeof(Stage<KT, kPieces<T>>) <= 160 * 1024 ? 2 : 1;
+template <class T, int KT, int W>
+constexpr int kStages = 2 * sizeof(Stage<T, KT, W>) <= 160 * 1024 ? 2 : 1;
+// Workgroups a compute unit that a walk's registers are to leave room for: two (256 registers
+// a lane), where LDS has it.  With 512 the accumulators go where only matrix instructions reach
+// them, and 180 of 1170 instructions of a chunk were moves.
+template <class T, int KT, int W>
+constexpr int kTogether = KT <= 4 && kStages<T, KT, W> * sizeof(Stage<T, KT, W>) <= 80 * 1024 ? 2 : 1;
 
-// The same one chunk ahead, this thread's share in registers, and for the lane's column and its
-// eight tokens (4 (lane / 16) + 0..3 and 16 more) the values or the outputs'
-// gradients.  Loads are unconditional with addresses inside the chunk; what is past its
-// end is dropped when used.  WIDE: the key is a multiple of eight.
+// The same one chunk ahead, this thread's share in registers.  Loads are unconditional with
+// addresses inside the sequence; what is past its end is dropped on the way to LDS.
+// WIDE: key and value are multiples of eight.
 template <class T, int KT, int W, bool WIDE>
 struct Feed {
-  static constexpr int N = kPieces<T>, VECTORS = kChunk * KT * 4, THREADS = 64 * W;
+  static constexpr int THREADS = 64 * W, VECTORS = kChunk * KT * 4, COLUMNS = 16 * W;
   static constexpr int EACH = (VECTORS + THREADS - 1) / THREADS;
   static constexpr int RAW = (kChunkVectors + THREADS - 1) / THREADS;
+  static constexpr int PER_ROW = COLUMNS / 8, EACH_X = kChunk * PER_ROW / THREADS;
+  static_assert(EACH_X * THREADS == kChunk * PER_ROW, "whole vectors of values");
   typedef T TV __attribute__((ext_vector_type(8)));
-  TV k[EACH], q[EACH];
+  TV k[EACH], q[EACH], x[EACH_X];
   u32x4 raw[RAW];
-  T x[8];
 
   __device__ static int row_of(int i) { return (threadIdx.x + i * THREADS) / (KT * 4); }
   __device__ static int channel_of(int i) { return (threadIdx.x + i * THREADS) % (KT * 4) * 8; }
+  __device__ static int xrow_of(int i) { return (threadIdx.x + i * THREADS) / PER_ROW; }
+  __device__ static int xcol_of(int i) { return threadIdx.x % PER_ROW * 8; }
+
+  __device__ static void load(TV& to, const T* row, int c, int n) {
+    if (WIDE) {
+      __builtin_memcpy(&to, row + (c < n ? c : 0), sizeof(TV));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) to[e] = row[min(c + e, n - 1)];
+    }
+  }
+  __device__ static void mask(TV& v, int r, int live, int c, int n) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = r < live && c + e < n ? v[e] : (T)0.f;
+  }
 
   __device__ void fetch(const rc_delta_args& a, const Chunk& c, const rc_heads& values, int b, int h, int hk,
-                        int t0, int live, int col) {
+                        int t0, int live, int col0) {
     const T* from_k = at_head<T>(a.k, b, t0, hk);
     const T* from_q = at_head<T>(a.q, b, t0, hk);
+    const T* from_x = at_head<T>(values, b, t0, h);
 #pragma unroll
     for (int i = 0; i < EACH; i++) {
-      const int r = min(row_of(i), live - 1), ch = channel_of(i);
-      if (WIDE) {
-        const int at = ch < a.key ? ch : 0;
-        __builtin_memcpy(&k[i], from_k + r * a.k.time + at, sizeof(TV));
-        __builtin_memcpy(&q[i], from_q + r * a.q.time + at, sizeof(TV));
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          k[i][e] = from_k[r * a.k.time + min(ch + e, a.key - 1)];
-          q[i][e] = from_q[r * a.q.time + min(ch + e, a.key - 1)];
-        }
-      }
+      const int r = min(row_of(i), live - 1);
+      load(k[i], from_k + r * a.k.time, channel_of(i), a.key);
+      load(q[i], from_q + r * a.q.time, channel_of(i), a.key);
     }
+#pragma unroll
+    for (int i = 0; i < EACH_X; i++)
+      load(x[i], from_x + min(xrow_of(i), live - 1) * values.time, col0 + xcol_of(i), a.value);
     const u32x4* from = reinterpret_cast<const u32x4*>(&c);
 #pragma unroll
     for (int i = 0; i < RAW; i++) raw[i] = from[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)];
-    const T* from_x = at_head<T>(values, b, t0, h) + min(col, a.value - 1);
-    const int row = threadIdx.x % 64 / 16 * 4;
-#pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = from_x[min(e / 4 * 16 + row + e % 4, live - 1) * values.time];
   }
-  __device__ void put(Stage<KT, N>& to, int live, int key) const {
-    const bool all = live == kChunk && key == 32 * KT;
+  __device__ void put(Stage<T, KT, W>& to, int live, int key, int value, int col0) const {
+    const bool all = live == kChunk && key == 32 * KT && col0 + COLUMNS <= value;
 #pragma unroll
     for (int i = 0; i < EACH; i++) {
       const int r = row_of(i), ch = channel_of(i);
       if (VECTORS % THREADS && r >= kChunk) break;
       TV u = k[i], v = q[i];
       if (!all) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const bool on = r < live && ch + e < key;
-          u[e] = on ? u[e] : (T)0.f;
-          v[e] = on ? v[e] : (T)0.f;
-        }
+        mask(u, r, live, ch, key);
+        mask(v, r, live, ch, key);
       }
-      if constexpr (N == 1) {
+      if constexpr (kPieces<T> == 1) {
         to.k.put(r, ch, u);
         to.q.put(r, ch, v);
       } else {
-        float x[8], y[8];
+        float y[8], z[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          x[e] = (float)u[e];
-          y[e] = (float)v[e];
+          y[e] = (float)u[e];
+          z[e] = (float)v[e];
         }
-        to.k.put(r, ch, x);
-        to.q.put(r, ch, y);
+        to.k.put(r, ch, y);
+        to.q.put(r, ch, z);
       }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH_X; i++) {
+      TV v = x[i];
+      if (!all) mask(v, xrow_of(i), live, col0 + xcol_of(i), value);
+      *(TV*)&to.x[xrow_of(i)][xcol_of(i)] = v;
     }
 #pragma unroll
     for (int i = 0; i < RAW; i++) to.raw[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)] = raw[i];
@@ -456,9 +472,9 @@ __device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {
 }
 
 // A walk's place: a workgroup takes 16 W columns of one head; those of one head are as many
-// workgroups apart as there are heads, for one of the eight caches as a rule.
+// workgroups apart as there are heads, so that most share one of the eight caches.
 struct Walk {
-  int b, h, hk, bh, col, row, end, chunks;
+  int b, h, hk, bh, col0, col, row, end, chunks;
   bool on;
   __device__ Walk(const rc_delta_args& a, int columns) {
     const int heads = a.batch * a.heads, lane = threadIdx.x % 64;
@@ -466,7 +482,8 @@ struct Walk {
     b = bh / a.heads;
     h = bh % a.heads;
     hk = h / (a.heads / a.key_heads);
-    col = blockIdx.x / heads * columns + threadIdx.x / 64 * 16 + lane % 16;
+    col0 = blockIdx.x / heads * columns;
+    col = col0 + threadIdx.x / 64 * 16 + lane % 16;
     row = lane / 16 * 4;
     on = col < a.value;
     end = length_of(a, b);
@@ -524,10 +541,10 @@ inline uint64_t workspace_of(const rc_delta_args& a, bool back) {
   return n;
 }
 
-// f(whether rows of the key are whole loads of eight).
+// f(whether rows of key and value are whole loads of eight).
 template <class F>
-inline int by_width(int32_t key, F&& f) {
-  return key % 8 ? f(std::false_type{}) : f(std::true_type{});
+inline int by_width(const rc_delta_args& a, F&& f) {
+  return a.key % 8 || a.value % 8 ? f(std::false_type{}) : f(std::true_type{});
 }
 // f(integral_constant of the key's tiles of 32).
 template <class F>

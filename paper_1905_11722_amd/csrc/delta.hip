@@ -9,9 +9,9 @@ namespace {
 // last; columns do not depend on one another, and what a product leaves in a lane is what the
 // next one takes from it, so waves share nothing but the tokens in LDS.
 template <class T, int KT, int W, bool WIDE>
-__global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
+__global__ __launch_bounds__(64 * W, (kTogether<T, KT, W>)) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  __shared__ Stage<KT, kPieces<T>> stages[kStages<T, KT>];
+  __shared__ Stage<T, KT, W> stages[kStages<T, KT, W>];
   const Walk at(a, 16 * W);
   const int end = at.end, row = at.row;
   const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
@@ -20,21 +20,18 @@ __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
   load_state<KT>(a.state_in ? a.state_in + at.bh * size : nullptr, a, at.col, S);
   Feed<T, KT, W, WIDE> next;
   if (at.chunks)
-    next.fetch(a, p.prepared[first], a.v, at.b, at.h, at.hk, 0, min(end, kChunk), at.col);
+    next.fetch(a, p.prepared[first], a.v, at.b, at.h, at.hk, 0, min(end, kChunk), at.col0);
   for (int chunk = 0; chunk < at.chunks; chunk++) {
     const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    auto& stage = stages[chunk % kStages<T, KT>];
-    if (kStages<T, KT> == 1) __syncthreads();
-    next.put(stage, live, a.key);
+    auto& stage = stages[chunk % kStages<T, KT, W>];
+    if (kStages<T, KT, W> == 1) __syncthreads();
+    next.put(stage, live, a.key, a.value, at.col0);
     __syncthreads();
     const Chunk& c = stage.c;
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = at.on && e / 4 * 16 + row + e % 4 < live ? (float)next.x[e] : 0.f;
     {
       const int n = min(chunk + 1, at.chunks - 1);
       next.fetch(a, p.prepared[first + n], a.v, at.b, at.h, at.hk, n * kChunk,
-                 min(end - n * kChunk, kChunk), at.col);
+                 min(end - n * kChunk, kChunk), at.col0);
     }
     if (p.states && keeps)
       keep_state<KT>(p.states + (first + chunk) * (columns_of(a.value) * 32 * KT), at.col, S);
@@ -57,7 +54,7 @@ __global__ __launch_bounds__(64 * W) void k_delta_forward(DeltaParams p) {
       left[m] = *(const f32x4*)&c.left[16 * m + row];
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        r[m][e] = beta[e] * (x[4 * m + e] - since[e] * r[m][e]);
+        r[m][e] = beta[e] * ((float)stage.x[16 * m + row + e][at.col - at.col0] - since[e] * r[m][e]);
         out[m][e] *= a.scale * since[e];
       }
     }
@@ -226,7 +223,7 @@ extern "C" int rc_delta_forward(const rc_delta_args* args, void* stream) {
     return by_key(a.key, [&](auto kt) {
       constexpr int KT = decltype(kt)::value;
       if (int e = prepare<T, KT, false>(p, s)) return e;
-      return by_width(a.key, [&](auto wide) {
+      return by_width(a, [&](auto wide) {
         k_delta_forward<T, KT, kWaves, decltype(wide)::value><<<walks_of(a), 64 * kWaves, 0, s>>>(p);
         return launched("k_delta_forward");
       });

@@ -7,10 +7,10 @@ namespace {
 
 // Backward through the states, from the last chunk to the first, as k_delta_forward goes.
 template <class T, int KT, int W, bool WIDE>
-__global__ __launch_bounds__(64 * W) void k_delta_states_back(DeltaParams p) {
+__global__ __launch_bounds__(64 * W, (kTogether<T, KT, W>)) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>;
-  __shared__ Stage<KT, N> stages[kStages<T, KT>];
+  __shared__ Stage<T, KT, W> stages[kStages<T, KT, W>];
   const Walk at(a, 16 * W);
   const int end = at.end, row = at.row;
   const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
@@ -20,23 +20,23 @@ __global__ __launch_bounds__(64 * W) void k_delta_states_back(DeltaParams p) {
   Feed<T, KT, W, WIDE> next;
   if (at.chunks) {
     const int n = at.chunks - 1;
-    next.fetch(a, p.prepared[first + n], a.do_, at.b, at.h, at.hk, n * kChunk, end - n * kChunk, at.col);
+    next.fetch(a, p.prepared[first + n], a.do_, at.b, at.h, at.hk, n * kChunk, end - n * kChunk, at.col0);
   }
   for (int chunk = at.chunks - 1; chunk >= 0; chunk--) {
     const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    auto& stage = stages[chunk % kStages<T, KT>];
-    if (kStages<T, KT> == 1) __syncthreads();
-    next.put(stage, live, a.key);
+    auto& stage = stages[chunk % kStages<T, KT, W>];
+    if (kStages<T, KT, W> == 1) __syncthreads();
+    next.put(stage, live, a.key, a.value, at.col0);
     __syncthreads();
     const Chunk& c = stage.c;
     f32x4 g[2];
 #pragma unroll
     for (int e = 0; e < 8; e++)
-      g[e / 4][e % 4] = at.on && e / 4 * 16 + row + e % 4 < live ? (float)next.x[e] : 0.f;
+      g[e / 4][e % 4] = (float)stage.x[e / 4 * 16 + row + e % 4][at.col - at.col0];
     {
       const int n = max(chunk - 1, 0);
       next.fetch(a, p.prepared[first + n], a.do_, at.b, at.h, at.hk, n * kChunk,
-                 min(end - n * kChunk, kChunk), at.col);
+                 min(end - n * kChunk, kChunk), at.col0);
     }
     if (keeps) keep_state<KT>(p.dstates + (first + chunk) * (columns_of(a.value) * 32 * KT), at.col, E);
     f32x4 dw[2], dr[2];
@@ -389,7 +389,7 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
     return by_key(a.key, [&](auto kt) {
       constexpr int KT = decltype(kt)::value;
       if (int e = prepare<T, KT, true>(p, s)) return e;
-      const int e = by_width(a.key, [&](auto wide) {
+      const int e = by_width(a, [&](auto wide) {
         k_delta_states_back<T, KT, kWaves, decltype(wide)::value><<<walks_of(a), 64 * kWaves, 0, s>>>(p);
         return launched("k_delta_states_back");
       });
