@@ -40,7 +40,6 @@ using namespace rcops;
 
 constexpr int kChunk = 32;
 constexpr int kMaxHead = 256;
-constexpr int kWaves = 4;                              // of a workgroup that walks
 
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -327,78 +326,88 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   }
 }
 
-// Column `col` of a head's state: tile m has this lane's rows 16m + 4 (lane / 16) + 0..3.
-template <int KT>
-__device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col,
-                                           f32x4 (&S)[2 * KT]) {
-  const int row = threadIdx.x % 64 / 16 * 4;
+// Column `col` of a head's state from row `first` on: tile m has this lane's rows
+// 16m + 4 (lane / 16) + 0..3.
+template <int TILES>
+__device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col, int first,
+                                           f32x4 (&S)[TILES]) {
+  const int row = first + threadIdx.x % 64 / 16 * 4;
 #pragma unroll
-  for (int m = 0; m < 2 * KT; m++)
+  for (int m = 0; m < TILES; m++)
 #pragma unroll
     for (int r = 0; r < 4; r++) {
       const int i = 16 * m + row + r;
       S[m][r] = from && i < a.key && col < a.value ? from[(int64_t)i * a.value + col] : 0.f;
     }
 }
-template <int KT>
-__device__ __forceinline__ void store_state(float* to, const rc_delta_args& a, int col,
-                                            const f32x4 (&S)[2 * KT]) {
-  const int row = threadIdx.x % 64 / 16 * 4;
+template <int TILES>
+__device__ __forceinline__ void store_state(float* to, const rc_delta_args& a, int col, int first,
+                                            const f32x4 (&S)[TILES]) {
+  const int row = first + threadIdx.x % 64 / 16 * 4;
 #pragma unroll
-  for (int m = 0; m < 2 * KT; m++)
+  for (int m = 0; m < TILES; m++)
 #pragma unroll
     for (int r = 0; r < 4; r++) {
       const int i = 16 * m + row + r;
       if (i < a.key && col < a.value) to[(int64_t)i * a.value + col] = S[m][r];
     }
 }
-// The same into [column][row] (col < columns_of(value)).
-template <int KT>
-__device__ __forceinline__ void keep_state(float* to, int col, const f32x4 (&S)[2 * KT]) {
-  float* at = to + col * (32 * KT) + threadIdx.x % 64 / 16 * 4;
+// The same into [column][row], `rows` rows a column (col < columns_of(value)).
+template <int TILES>
+__device__ __forceinline__ void keep_state(float* to, int rows, int col, int first, const f32x4 (&S)[TILES]) {
+  float* at = to + col * rows + first + threadIdx.x % 64 / 16 * 4;
 #pragma unroll
-  for (int m = 0; m < 2 * KT; m++) *(f32x4*)(at + 16 * m) = S[m];
+  for (int m = 0; m < TILES; m++) *(f32x4*)(at + 16 * m) = S[m];
 }
+
+// A walk's workgroup: W waves side by side, 16 columns each, times R waves that have a part
+// each of the key's channels (rows of the state) in them, and L waves that load.
+template <int W_, int R_, int L_>
+struct Shape {
+  static constexpr int W = W_, R = R_, L = L_, COLUMNS = 16 * W;
+  static constexpr int WORKERS = 64 * W * R, LOADERS = 64 * L, THREADS = WORKERS + LOADERS;
+};
 
 // What a chunk's products need beside the state, in LDS; x: the values, or the outputs'
 // gradients, of the workgroup's columns.
-template <class T, int KT, int W>
+template <class T, int KT, class G>
 struct Stage {
-  static constexpr int N = kPieces<T>, COLUMNS = 16 * W;
-  Tokens<KT, N> k, q;
+  Tokens<KT, kPieces<T>> k, q;
   union {
     Chunk c;
     u32x4 raw[kChunkVectors];
   };
-  T x[kChunk][COLUMNS + 8];
+  T x[kChunk][G::COLUMNS + 8];
   __device__ Stage() {}
 };
-template <class T, int KT, int W>
-constexpr int kStages = 2 * sizeof(Stage<T, KT, W>) <= 160 * 1024 ? 2 : 1;
-// Workgroups a compute unit that a walk's registers are to leave room for: two (256 registers
-// a lane), where LDS has it.  With 512 the accumulators go where only matrix instructions reach
-// them, and 180 of 1170 instructions of a chunk were moves.
-template <class T, int KT, int W>
-constexpr int kTogether = KT <= 4 && kStages<T, KT, W> * sizeof(Stage<T, KT, W>) <= 80 * 1024 ? 2 : 1;
+template <class T, int KT, class G>
+constexpr int kStages = 2 * sizeof(Stage<T, KT, G>) <= 160 * 1024 ? 2 : 1;
+// Workgroups a compute unit that a walk's registers are to leave room for: two waves a SIMD
+// (256 registers a lane), where LDS has it.  With 512 the accumulators go where only matrix
+// instructions reach them, and 180 of 1170 instructions of a chunk were moves.
+template <class T, int KT, class G>
+constexpr int kTogether = G::THREADS > 256 || kStages<T, KT, G> * sizeof(Stage<T, KT, G>) > 76 * 1024
+                              ? 1 : 512 / G::THREADS;
 
-// The same one chunk ahead, this thread's share in registers.  Loads are unconditional with
-// addresses inside the sequence; what is past its end is dropped on the way to LDS.
+// A loading wave's part of the chunks: the next one's share in registers.  Loads are
+// unconditional with addresses inside the sequence; what is past its end is dropped on the way to LDS.
 // WIDE: key and value are multiples of eight.
-template <class T, int KT, int W, bool WIDE>
+template <class T, int KT, class G, bool WIDE>
 struct Feed {
-  static constexpr int THREADS = 64 * W, VECTORS = kChunk * KT * 4, COLUMNS = 16 * W;
+  static constexpr int THREADS = G::LOADERS, VECTORS = kChunk * KT * 4, COLUMNS = G::COLUMNS;
   static constexpr int EACH = (VECTORS + THREADS - 1) / THREADS;
   static constexpr int RAW = (kChunkVectors + THREADS - 1) / THREADS;
-  static constexpr int PER_ROW = COLUMNS / 8, EACH_X = kChunk * PER_ROW / THREADS;
-  static_assert(EACH_X * THREADS == kChunk * PER_ROW, "whole vectors of values");
+  static constexpr int PER_ROW = COLUMNS / 8, VECTORS_X = kChunk * PER_ROW;
+  static constexpr int EACH_X = (VECTORS_X + THREADS - 1) / THREADS;
   typedef T TV __attribute__((ext_vector_type(8)));
   TV k[EACH], q[EACH], x[EACH_X];
   u32x4 raw[RAW];
 
-  __device__ static int row_of(int i) { return (threadIdx.x + i * THREADS) / (KT * 4); }
-  __device__ static int channel_of(int i) { return (threadIdx.x + i * THREADS) % (KT * 4) * 8; }
-  __device__ static int xrow_of(int i) { return (threadIdx.x + i * THREADS) / PER_ROW; }
-  __device__ static int xcol_of(int i) { return threadIdx.x % PER_ROW * 8; }
+  __device__ static int index(int i) { return threadIdx.x - G::WORKERS + i * THREADS; }
+  __device__ static int row_of(int i) { return index(i) / (KT * 4); }
+  __device__ static int channel_of(int i) { return index(i) % (KT * 4) * 8; }
+  __device__ static int xrow_of(int i) { return index(i) / PER_ROW; }
+  __device__ static int xcol_of(int i) { return index(i) % PER_ROW * 8; }
 
   __device__ static void load(TV& to, const T* row, int c, int n) {
     if (WIDE) {
@@ -429,9 +438,9 @@ struct Feed {
       load(x[i], from_x + min(xrow_of(i), live - 1) * values.time, col0 + xcol_of(i), a.value);
     const u32x4* from = reinterpret_cast<const u32x4*>(&c);
 #pragma unroll
-    for (int i = 0; i < RAW; i++) raw[i] = from[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)];
+    for (int i = 0; i < RAW; i++) raw[i] = from[min(index(i), kChunkVectors - 1)];
   }
-  __device__ void put(Stage<T, KT, W>& to, int live, int key, int value, int col0) const {
+  __device__ void put(Stage<T, KT, G>& to, int live, int key, int value, int col0) const {
     const bool all = live == kChunk && key == 32 * KT && col0 + COLUMNS <= value;
 #pragma unroll
     for (int i = 0; i < EACH; i++) {
@@ -458,38 +467,94 @@ struct Feed {
     }
 #pragma unroll
     for (int i = 0; i < EACH_X; i++) {
+      if (VECTORS_X % THREADS && xrow_of(i) >= kChunk) break;
       TV v = x[i];
       if (!all) mask(v, xrow_of(i), live, col0 + xcol_of(i), value);
       *(TV*)&to.x[xrow_of(i)][xcol_of(i)] = v;
     }
 #pragma unroll
-    for (int i = 0; i < RAW; i++) to.raw[min((int)threadIdx.x + i * THREADS, kChunkVectors - 1)] = raw[i];
+    for (int i = 0; i < RAW; i++) to.raw[min(index(i), kChunkVectors - 1)] = raw[i];
   }
 };
+
 __device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {
   const int lane = threadIdx.x % 64;
   return {{x[0][lane], x[1][lane], x[2][lane]}};
 }
 
-// A walk's place: a workgroup takes 16 W columns of one head; those of one head are as many
-// workgroups apart as there are heads, so that most share one of the eight caches.
+// A walk's place.  Workgroups of one head are as many apart as there are heads, so
+// that most share one of the eight caches.
+template <class G>
 struct Walk {
-  int b, h, hk, bh, col0, col, row, end, chunks;
+  int b, h, hk, bh, col0, col, row, end, chunks, wave, part;
   bool on;
-  __device__ Walk(const rc_delta_args& a, int columns) {
+  __device__ Walk(const rc_delta_args& a) {
     const int heads = a.batch * a.heads, lane = threadIdx.x % 64;
     bh = blockIdx.x % heads;
     b = bh / a.heads;
     h = bh % a.heads;
     hk = h / (a.heads / a.key_heads);
-    col0 = blockIdx.x / heads * columns;
-    col = col0 + threadIdx.x / 64 * 16 + lane % 16;
+    wave = threadIdx.x / 64 % G::W;
+    part = threadIdx.x / 64 / G::W;
+    col0 = blockIdx.x / heads * G::COLUMNS;
+    col = col0 + wave * 16 + lane % 16;
     row = lane / 16 * 4;
     on = col < a.value;
     end = length_of(a, b);
     chunks = (end + kChunk - 1) / kChunk;
   }
 };
+
+// The loading waves' side of a walk over the chunks, forward or (BACK) from the last: chunk
+// by chunk as the working waves go, one chunk ahead of them in LDS where it holds two and
+// one more in registers.  A chunk has two barriers: at its start, and between the parts'
+// writes and reads of their sums over the key (Parts); with one stage a third at its end.
+template <class T, int KT, class G, bool WIDE, bool BACK>
+__device__ __forceinline__ void load_chunks(const DeltaParams& p, const Walk<G>& at, const rc_heads& values,
+                                            Stage<T, KT, G>* stages) {
+  constexpr int STAGES = kStages<T, KT, G>;
+  const rc_delta_args& a = p.a;
+  if (!at.chunks) return;
+  const Chunk* prepared = p.prepared + (int64_t)at.bh * p.chunks;
+  Feed<T, KT, G, WIDE> next;
+  const auto chunk_of = [&](int i) { return BACK ? at.chunks - 1 - i : i; };
+  const auto live_of = [&](int c) { return min(at.end - c * kChunk, kChunk); };
+  const auto fetch = [&](int i) {
+    const int c = chunk_of(min(i, at.chunks - 1));
+    next.fetch(a, prepared[c], values, at.b, at.h, at.hk, c * kChunk, live_of(c), at.col0);
+  };
+  const auto put = [&](int i) {
+    next.put(stages[i % STAGES], live_of(chunk_of(i)), a.key, a.value, at.col0);
+    fetch(i + 1);
+  };
+  fetch(0);
+  put(0);
+  for (int i = 0; i < at.chunks; i++) {
+    __syncthreads();
+    if (STAGES == 2 && i + 1 < at.chunks) put(i + 1);
+    if (G::R > 1) __syncthreads();
+    if (STAGES == 1) {
+      __syncthreads();
+      if (i + 1 < at.chunks) put(i + 1);
+    }
+  }
+}
+
+// Sums over the R waves that have parts of the key, in one order for all of them, so that
+// what they compute from them is the same; M results.
+template <class G, int M>
+struct Parts {
+  f32x4 at[M][G::R][G::W][64];
+  __device__ f32x4 sum(int m, int wave) const {
+    const int lane = threadIdx.x % 64;
+    f32x4 s = at[m][0][wave][lane];
+#pragma unroll
+    for (int i = 1; i < G::R; i++) s += at[m][i][wave][lane];
+    return s;
+  }
+};
+template <class G>
+struct Parts<G, 0> {};
 
 // ------------------------------------------------------------------ host side
 
@@ -523,7 +588,7 @@ inline int heads_together(const rc_delta_args& a) {
 // Whether the sizes fit the launches.
 inline int fits(const rc_delta_args& a) {
   const int64_t bh = (int64_t)a.batch * a.heads;
-  if (!launchable(bh, 256) || !launchable(bh * cdiv(a.value, 16 * kWaves), 64 * kWaves) ||
+  if (!launchable(bh, 256) || !launchable(bh * cdiv(a.value, 16), 512) ||
       !launchable(pairs_of(a), 256))
     return RC_E_OVERFLOW;
   if (!launchable(cdiv(2 * (int64_t)a.batch * a.length * a.key_heads * a.key, 256), 256))
@@ -571,8 +636,12 @@ inline int prepare(const DeltaParams& p, hipStream_t s) {
   return launched("k_delta_prepare");
 }
 // Workgroups of a walk.
+template <class G>
 inline unsigned walks_of(const rc_delta_args& a) {
-  return (unsigned)((int64_t)a.batch * a.heads * cdiv(a.value, 16 * kWaves));
+  return (unsigned)((int64_t)a.batch * a.heads * cdiv(a.value, G::COLUMNS));
 }
+// The shape of a walk's workgroups.
+template <int KT>
+using ShapeOf = Shape<KT >= 2 ? 2 : 4, KT >= 2 ? 2 : 1, 4>;
 
 }  // namespace rcdelta

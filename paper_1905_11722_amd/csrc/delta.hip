@@ -5,93 +5,107 @@ using namespace rcdelta;
 
 namespace {
 
-// Forward: a wave holds 16 columns of the state in registers from the first chunk to the
-// last; columns do not depend on one another, and what a product leaves in a lane is what the
-// next one takes from it, so waves share nothing but the tokens in LDS.
-template <class T, int KT, int W, bool WIDE>
-__global__ __launch_bounds__(64 * W, (kTogether<T, KT, W>)) void k_delta_forward(DeltaParams p) {
+// Forward: a wave holds 16 columns of the state, or R waves a part each of their rows,
+// in registers from the first chunk to the last.  Columns do not depend on one
+// another, and what a product leaves in a lane is what the next one takes from it, so waves share
+// the tokens in LDS, and the parts their sums over the key.
+template <class T, int KT, class G, bool WIDE>
+__global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  __shared__ Stage<T, KT, W> stages[kStages<T, KT, W>];
-  const Walk at(a, 16 * W);
-  const int end = at.end, row = at.row;
+  constexpr int STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
+  __shared__ Stage<T, KT, G> stages[STAGES];
+  __shared__ Parts<G, G::R == 1 ? 0 : 4> parts;
+  const Walk<G> at(a);
+  const int end = at.end, row = at.row, first_row = at.part * STEPS * 32, lane = threadIdx.x % 64;
   const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
   const bool keeps = at.col < columns_of(a.value);
-  f32x4 S[2 * KT];
-  load_state<KT>(a.state_in ? a.state_in + at.bh * size : nullptr, a, at.col, S);
-  Feed<T, KT, W, WIDE> next;
-  if (at.chunks)
-    next.fetch(a, p.prepared[first], a.v, at.b, at.h, at.hk, 0, min(end, kChunk), at.col0);
+  if (threadIdx.x >= G::WORKERS) {
+    load_chunks<T, KT, G, WIDE, false>(p, at, a.v, stages);
+    return;
+  }
+  f32x4 S[2 * STEPS];
+  load_state(a.state_in ? a.state_in + at.bh * size : nullptr, a, at.col, first_row, S);
   for (int chunk = 0; chunk < at.chunks; chunk++) {
     const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    auto& stage = stages[chunk % kStages<T, KT, W>];
-    if (kStages<T, KT, W> == 1) __syncthreads();
-    next.put(stage, live, a.key, a.value, at.col0);
+    const auto& stage = stages[chunk % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
-    {
-      const int n = min(chunk + 1, at.chunks - 1);
-      next.fetch(a, p.prepared[first + n], a.v, at.b, at.h, at.hk, n * kChunk,
-                 min(end - n * kChunk, kChunk), at.col0);
-    }
     if (p.states && keeps)
-      keep_state<KT>(p.states + (first + chunk) * (columns_of(a.value) * 32 * KT), at.col, S);
+      keep_state(p.states + (first + chunk) * (columns_of(a.value) * 32 * KT), 32 * KT, at.col, first_row, S);
     f32x4 r[2], out[2], w[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) r[m] = out[m] = w[m] = f32x4{0, 0, 0, 0};
+    Pieces<3> state[STEPS];
 #pragma unroll
-    for (int s = 0; s < KT; s++) {
-      const Pieces<3> state = operand<3>(S[2 * s], S[2 * s + 1]);
+    for (int s = 0; s < STEPS; s++) {
+      state[s] = operand<3>(S[2 * s], S[2 * s + 1]);
 #pragma unroll
-      for (int m = 0; m < 2; m++) {
-        mul(r[m], stage.k.rows(m, s), state);
-        mul(out[m], stage.q.rows(m, s), state);
-      }
+      for (int m = 0; m < 2; m++) mul(r[m], stage.k.rows(m, at.part * STEPS + s), state[s]);
     }
-    f32x4 left[2];
+    if constexpr (G::R > 1) {
+#pragma unroll
+      for (int m = 0; m < 2; m++) parts.at[m][at.part][at.wave][lane] = r[m];
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; s++)
+#pragma unroll
+      for (int m = 0; m < 2; m++) mul(out[m], stage.q.rows(m, at.part * STEPS + s), state[s]);
+    // read before the barrier, which nothing is moved over
+    f32x4 since[2], beta[2], left[2], x[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) {
-      const f32x4 since = *(const f32x4*)&c.since[16 * m + row], beta = *(const f32x4*)&c.beta[16 * m + row];
+      since[m] = *(const f32x4*)&c.since[16 * m + row];
+      beta[m] = *(const f32x4*)&c.beta[16 * m + row];
       left[m] = *(const f32x4*)&c.left[16 * m + row];
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        r[m][e] = beta[e] * ((float)stage.x[16 * m + row + e][at.col - at.col0] - since[e] * r[m][e]);
-        out[m][e] *= a.scale * since[e];
-      }
+      for (int e = 0; e < 4; e++) x[m][e] = (float)stage.x[16 * m + row + e][at.col - at.col0];
     }
+    const Pieces<3> t[2] = {pieces(c.t[0]), pieces(c.t[1])};
+    if constexpr (G::R > 1) {
+#pragma unroll
+      for (int m = 0; m < 2; m++) parts.at[2 + m][at.part][at.wave][lane] = out[m];
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < 2; m++) r[m] = parts.sum(m, at.wave);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; m++) r[m] = beta[m] * (x[m] - since[m] * r[m]);
     const Pieces<3> rs = operand<3>(r[0], r[1]);
 #pragma unroll
-    for (int m = 0; m < 2; m++) mul(w[m], pieces(c.t[m]), rs);
-    const Pieces<3> ws = operand<3>(w[0], w[1]);
-#pragma unroll
-    for (int m = 0; m < 2; m++) mul(out[m], pieces(c.p[m]), ws);
-    T* o = at_head<T>(a.o, at.b, t0, at.h) + row * a.o.time + at.col;
-    if (at.on) {
-      if (live == kChunk) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) o[(e / 4 * 16 + e % 4) * a.o.time] = (T)out[e / 4][e % 4];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-          if (e / 4 * 16 + row + e % 4 < live) o[(e / 4 * 16 + e % 4) * a.o.time] = (T)out[e / 4][e % 4];
-      }
-    }
-    if (p.written && keeps) {
-      float* to = p.written + ((first + chunk) * columns_of(a.value) + at.col) * kChunk + row;
-#pragma unroll
-      for (int m = 0; m < 2; m++) *(f32x4*)(to + 16 * m) = w[m];
-    }
-#pragma unroll
-    for (int m = 0; m < 2; m++) w[m] *= left[m];
-    const Pieces<3> us = operand<3>(w[0], w[1]);
+    for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
+    const Pieces<3> us = operand<3>(w[0] * left[0], w[1] * left[1]);
     const float whole = c.since[kChunk - 1];
 #pragma unroll
-    for (int m = 0; m < 2 * KT; m++) {
+    for (int m = 0; m < 2 * STEPS; m++) {
       S[m] *= whole;
-      mul(S[m], stage.k.columns(m), us);
+      mul(S[m], stage.k.columns(at.part * 2 * STEPS + m), us);
     }
+    // outputs: tile m by part m
+    const Pieces<3> ws = operand<3>(w[0], w[1]);
+#pragma unroll
+    for (int m = 0; m < 2; m++) {
+      if (G::R > 1 && at.part != m) continue;
+      if constexpr (G::R > 1) out[m] = parts.sum(2 + m, at.wave);
+      out[m] *= a.scale * since[m];
+      mul(out[m], pieces(c.p[m]), ws);
+      T* o = at_head<T>(a.o, at.b, t0 + 16 * m, at.h) + row * a.o.time + at.col;
+      if (at.on) {
+        if (live == kChunk) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[e * a.o.time] = (T)out[m][e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (16 * m + row + e < live) o[e * a.o.time] = (T)out[m][e];
+        }
+      }
+      if (p.written && keeps)
+        *(f32x4*)(p.written + ((first + chunk) * columns_of(a.value) + at.col) * kChunk + 16 * m + row) = w[m];
+    }
+    if (STAGES == 1) __syncthreads();
   }
-  if (a.state_out) store_state<KT>(a.state_out + at.bh * size, a, at.col, S);
-  if (at.on) {
+  if (a.state_out) store_state(a.state_out + at.bh * size, a, at.col, first_row, S);
+  if (at.on && at.part == 0) {
     T* o = at_head<T>(a.o, at.b, 0, at.h) + at.col;
     for (int t = end + row / 4; t < a.length; t += 4) o[t * a.o.time] = (T)0.f;
   }
@@ -224,7 +238,8 @@ extern "C" int rc_delta_forward(const rc_delta_args* args, void* stream) {
       constexpr int KT = decltype(kt)::value;
       if (int e = prepare<T, KT, false>(p, s)) return e;
       return by_width(a, [&](auto wide) {
-        k_delta_forward<T, KT, kWaves, decltype(wide)::value><<<walks_of(a), 64 * kWaves, 0, s>>>(p);
+        using G = ShapeOf<KT>;
+        k_delta_forward<T, KT, G, decltype(wide)::value><<<walks_of<G>(a), G::THREADS, 0, s>>>(p);
         return launched("k_delta_forward");
       });
     });

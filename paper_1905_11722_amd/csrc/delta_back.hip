@@ -6,92 +6,99 @@ using namespace rcdelta;
 namespace {
 
 // Backward through the states, from the last chunk to the first, as k_delta_forward goes.
-template <class T, int KT, int W, bool WIDE>
-__global__ __launch_bounds__(64 * W, (kTogether<T, KT, W>)) void k_delta_states_back(DeltaParams p) {
+template <class T, int KT, class G, bool WIDE>
+__global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  constexpr int N = kPieces<T>;
-  __shared__ Stage<T, KT, W> stages[kStages<T, KT, W>];
-  const Walk at(a, 16 * W);
-  const int end = at.end, row = at.row;
+  constexpr int N = kPieces<T>, STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
+  __shared__ Stage<T, KT, G> stages[STAGES];
+  __shared__ Parts<G, G::R == 1 ? 0 : 2> parts;
+  const Walk<G> at(a);
+  const int end = at.end, row = at.row, first_row = at.part * STEPS * 32, lane = threadIdx.x % 64;
   const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
   const bool keeps = at.col < columns_of(a.value);
-  f32x4 E[2 * KT];
-  load_state<KT>(a.dstate_out ? a.dstate_out + at.bh * size : nullptr, a, at.col, E);
-  Feed<T, KT, W, WIDE> next;
-  if (at.chunks) {
-    const int n = at.chunks - 1;
-    next.fetch(a, p.prepared[first + n], a.do_, at.b, at.h, at.hk, n * kChunk, end - n * kChunk, at.col0);
+  if (threadIdx.x >= G::WORKERS) {
+    load_chunks<T, KT, G, WIDE, true>(p, at, a.do_, stages);
+    return;
   }
-  for (int chunk = at.chunks - 1; chunk >= 0; chunk--) {
-    const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    auto& stage = stages[chunk % kStages<T, KT, W>];
-    if (kStages<T, KT, W> == 1) __syncthreads();
-    next.put(stage, live, a.key, a.value, at.col0);
+  f32x4 E[2 * STEPS];
+  load_state(a.dstate_out ? a.dstate_out + at.bh * size : nullptr, a, at.col, first_row, E);
+  for (int i = 0; i < at.chunks; i++) {
+    const int chunk = at.chunks - 1 - i, t0 = chunk * kChunk, live = min(end - t0, kChunk);
+    const auto& stage = stages[i % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
-    f32x4 g[2];
-#pragma unroll
-    for (int e = 0; e < 8; e++)
-      g[e / 4][e % 4] = (float)stage.x[e / 4 * 16 + row + e % 4][at.col - at.col0];
-    {
-      const int n = max(chunk - 1, 0);
-      next.fetch(a, p.prepared[first + n], a.do_, at.b, at.h, at.hk, n * kChunk,
-                 min(end - n * kChunk, kChunk), at.col0);
-    }
-    if (keeps) keep_state<KT>(p.dstates + (first + chunk) * (columns_of(a.value) * 32 * KT), at.col, E);
-    f32x4 dw[2], dr[2];
+    if (keeps)
+      keep_state(p.dstates + (first + chunk) * (columns_of(a.value) * 32 * KT), 32 * KT, at.col, first_row, E);
+    f32x4 dw[2], dr[2], g[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) dw[m] = dr[m] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int s = 0; s < KT; s++) {
+    for (int s = 0; s < STEPS; s++) {
       const Pieces<3> state = operand<3>(E[2 * s], E[2 * s + 1]);
 #pragma unroll
-      for (int m = 0; m < 2; m++) mul(dw[m], stage.k.rows(m, s), state);
+      for (int m = 0; m < 2; m++) mul(dw[m], stage.k.rows(m, at.part * STEPS + s), state);
+    }
+    if constexpr (G::R > 1) {
+#pragma unroll
+      for (int m = 0; m < 2; m++) parts.at[m][at.part][at.wave][lane] = dw[m];
+    }
+    // read, and computed, before the barrier, which nothing is moved over
+    f32x4 since[2], beta[2], from_o[2];
+#pragma unroll
+    for (int m = 0; m < 2; m++) {
+      since[m] = *(const f32x4*)&c.since[16 * m + row];
+      beta[m] = *(const f32x4*)&c.beta[16 * m + row];
+      from_o[m] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 4; e++) g[m][e] = (float)stage.x[16 * m + row + e][at.col - at.col0];
     }
     const Pieces<N> gs = operand<N>(g[0], g[1]);
+    const Pieces<3> t[2] = {pieces(c.t[0]), pieces(c.t[1])};
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
-      dw[m] *= *(const f32x4*)&c.left[16 * m + row];
-      mul(dw[m], pieces(c.p[m]), gs);
+    for (int m = 0; m < 2; m++) mul(from_o[m], pieces(c.p[m]), gs);
+    const Pieces<3> gos = operand<3>(g[0] * (a.scale * since[0]), g[1] * (a.scale * since[1]));
+    const float whole = c.since[kChunk - 1];
+    f32x4 left[2] = {*(const f32x4*)&c.left[row], *(const f32x4*)&c.left[16 + row]};
+#pragma unroll
+    for (int m = 0; m < 2 * STEPS; m++) {
+      E[m] *= whole;
+      mul(E[m], stage.q.columns(at.part * 2 * STEPS + m), gos);
     }
+    if constexpr (G::R > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < 2; m++) dw[m] = parts.sum(m, at.wave);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; m++) dw[m] = dw[m] * left[m] + from_o[m];
     const Pieces<3> dws = operand<3>(dw[0], dw[1]);
 #pragma unroll
-    for (int m = 0; m < 2; m++) mul(dr[m], pieces(c.t[m]), dws);
-    if (keeps) {
-      float* to = p.written + ((first + chunk) * columns_of(a.value) + at.col) * kChunk + row;
+    for (int m = 0; m < 2; m++) mul(dr[m], t[m], dws);
+    const Pieces<3> drs = operand<3>(-since[0] * beta[0] * dr[0], -since[1] * beta[1] * dr[1]);
 #pragma unroll
-      for (int m = 0; m < 2; m++) *(f32x4*)(to + 16 * m) = dr[m];
-    }
-#pragma unroll
-    for (int m = 0; m < 2; m++) dr[m] *= *(const f32x4*)&c.beta[16 * m + row];
-    T* dv = at_head<T>(a.dv, at.b, t0, at.h) + row * a.dv.time + at.col;
-    if (at.on) {
-      if (live == kChunk) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) dv[(e / 4 * 16 + e % 4) * a.dv.time] = (T)dr[e / 4][e % 4];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-          if (e / 4 * 16 + row + e % 4 < live) dv[(e / 4 * 16 + e % 4) * a.dv.time] = (T)dr[e / 4][e % 4];
-      }
-    }
+    for (int m = 0; m < 2 * STEPS; m++) mul(E[m], stage.k.columns(at.part * 2 * STEPS + m), drs);
 #pragma unroll
     for (int m = 0; m < 2; m++) {
-      const f32x4 since = *(const f32x4*)&c.since[16 * m + row];
-      dr[m] *= -since;
-      g[m] *= a.scale * since;
-    }
-    const Pieces<3> drs = operand<3>(dr[0], dr[1]), gos = operand<3>(g[0], g[1]);
-    const float whole = c.since[kChunk - 1];
+      if (G::R > 1 && at.part != m) continue;          // outputs: tile m by part m
+      if (keeps)
+        *(f32x4*)(p.written + ((first + chunk) * columns_of(a.value) + at.col) * kChunk + 16 * m + row) = dr[m];
+      dr[m] *= beta[m];
+      T* dv = at_head<T>(a.dv, at.b, t0 + 16 * m, at.h) + row * a.dv.time + at.col;
+      if (at.on) {
+        if (live == kChunk) {
 #pragma unroll
-    for (int m = 0; m < 2 * KT; m++) {
-      E[m] *= whole;
-      mul(E[m], stage.k.columns(m), drs);
-      mul(E[m], stage.q.columns(m), gos);
+          for (int e = 0; e < 4; e++) dv[e * a.dv.time] = (T)dr[m][e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (16 * m + row + e < live) dv[e * a.dv.time] = (T)dr[m][e];
+        }
+      }
     }
+    if (STAGES == 1) __syncthreads();
   }
-  if (a.dstate_in) store_state<KT>(a.dstate_in + at.bh * size, a, at.col, E);
-  if (at.on) {
+  if (a.dstate_in) store_state(a.dstate_in + at.bh * size, a, at.col, first_row, E);
+  if (at.on && at.part == 0) {
     T* dv = at_head<T>(a.dv, at.b, 0, at.h) + at.col;
     for (int t = end + row / 4; t < a.length; t += 4) dv[t * a.dv.time] = (T)0.f;
   }
@@ -390,7 +397,8 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
       constexpr int KT = decltype(kt)::value;
       if (int e = prepare<T, KT, true>(p, s)) return e;
       const int e = by_width(a, [&](auto wide) {
-        k_delta_states_back<T, KT, kWaves, decltype(wide)::value><<<walks_of(a), 64 * kWaves, 0, s>>>(p);
+        using G = ShapeOf<KT>;
+        k_delta_states_back<T, KT, G, decltype(wide)::value><<<walks_of<G>(a), G::THREADS, 0, s>>>(p);
         return launched("k_delta_states_back");
       });
       if (e) return e;
