@@ -109,17 +109,17 @@ __device__ __forceinline__ float exp_of(double x) {
   return __builtin_amdgcn_ldexpf(fast_exp2((float)(e - n)), (int)__builtin_fmax(n, -1000.0));
 }
 
-// 32 rows (tokens) of `32 KT` channels in LDS as pieces.  Within each 32 channels, groups of four
+// ROWS rows (tokens) of `32 KT` channels in LDS as pieces.  Within each 32 channels, groups of four
 // are ordered 0 4 1 5 2 6 3 7, so that a lane's operand (above) is 16 bytes.
-template <int KT, int N>
+template <int KT, int N, int ROWS = kChunk>
 struct Tokens {
   static constexpr int STRIDE = KT * 32 + 8;
-  bf16 at[N][kChunk][STRIDE];
+  bf16 at[N][ROWS][STRIDE];
 
   // From rows `row` elements apart; what is past `live` tokens or `n` channels is 0.
   template <class T>
   __device__ void load(const T* x, int64_t row, int live, int n, int thread, int threads) {
-    for (int i = thread; i < kChunk * KT * 4; i += threads) {
+    for (int i = thread; i < ROWS * KT * 4; i += threads) {
       const int r = i / (KT * 4), c = i % (KT * 4) * 8;
       float v[8];
       load_vec<8>(x + (r < live ? r : 0) * row + (c < n ? c : 0), r < live ? n - c : 0, v);
@@ -131,8 +131,8 @@ struct Tokens {
     bf16* to = &at[0][r][c / 32 * 32 + (c % 16 / 4) * 8 + c % 32 / 16 * 4];
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      *(bf16x4*)(to + i * (kChunk * STRIDE)) = s.p[i].lo;
-      *(bf16x4*)(to + i * (kChunk * STRIDE) + 8) = s.p[i].hi;
+      *(bf16x4*)(to + i * (ROWS * STRIDE)) = s.p[i].lo;
+      *(bf16x4*)(to + i * (ROWS * STRIDE) + 8) = s.p[i].hi;
     }
   }
   // Row tile t (tokens 16t + ..) over channels 32s + 0..31.
@@ -144,20 +144,28 @@ struct Tokens {
       f.p[i] = *(const bf16x8*)&at[i][16 * t + lane % 16][32 * s + lane / 16 * 8];
     return f;
   }
-  // Channels 16t + .. over the 32 tokens: reads that transpose four by four.
-  __device__ Pieces<N> columns(int t) const {
+  // Channels 16t + .. over rows 32s + 0..31: reads that transpose four by four.
+  __device__ Pieces<N> columns(int t, int s = 0) const {
     const int lane = threadIdx.x % 64;
     Pieces<N> f;
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const bf16* from =
-          &at[i][lane / 16 * 4 + lane % 16 / 4][t / 2 * 32 + lane % 4 * 8 + t % 2 * 4];
+          &at[i][32 * s + lane / 16 * 4 + lane % 16 / 4][t / 2 * 32 + lane % 4 * 8 + t % 2 * 4];
       typedef s16x4 __attribute__((address_space(3))) * lds;
       f.p[i].lo = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)from));
       f.p[i].hi = __builtin_bit_cast(
           bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(from + 16 * STRIDE)));
     }
     return f;
+  }
+  __device__ void put_one(int r, int c, float x) {
+    const int at_c = c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      at[i][r][at_c] = (bf16)x;
+      x -= (float)at[i][r][at_c];
+    }
   }
   // Eight channels as they are where one piece is all.
   __device__ void put(int r, int c, const bf16x8& v) {
@@ -183,9 +191,14 @@ struct Chunk {
 constexpr int kChunkVectors = sizeof(Chunk) / 16;
 static_assert(sizeof(Chunk) % 16 == 0, "copied in vectors");
 
-// States (and their gradients) of every chunk as a lane of the walks holds them, four rows of a
-// column together: [batch][heads][chunks][columns(value)][rows(key)] in 32 bits; w and dR likewise,
-// four tokens of a column together: [batch][heads][chunks][columns(value)][32].
+// States before, and gradients of states after, every block of tokens of k_delta_inputs_back as
+// a lane of the walks holds them, four rows of a column together: [batch][heads][blocks]
+// [columns(value)][rows(key)] in 32 bits; w and dR likewise, four tokens of a column
+// together: [batch][heads][chunks][columns(value)][32].  A block is two chunks where its keys,
+// queries and products of tokens fit LDS and registers: half of the states to write, keep and read.
+constexpr int block_of(int pieces, int rows) {
+  return rows <= 128 && 2 * pieces * 64 * (rows + 8) * 2 + 2 * 3 * 64 * 72 * 2 <= 152 * 1024 ? 64 : 32;
+}
 __host__ __device__ inline int rows_of(int key) {
   return key <= 32 ? 32 : key <= 64 ? 64 : key <= 128 ? 128 : 256;
 }
@@ -193,7 +206,7 @@ __host__ __device__ inline int columns_of(int value) { return (value + 31) / 32 
 
 struct DeltaParams {
   rc_delta_args a;
-  int32_t chunks;
+  int32_t chunks, blocks;
   Chunk* prepared;                                    // [batch][heads][chunks]
   float* states;
   float* written;                                     // w, or dR
@@ -571,8 +584,13 @@ inline bool empty(const rc_delta_args& a) { return !a.batch || !a.heads; }
 inline int64_t chunks_of(const rc_delta_args& a) { return cdiv(a.length, kChunk); }
 // Chunks of all heads.  (batch x heads is checked first: it fits a launch.)
 inline int64_t pairs_of(const rc_delta_args& a) { return (int64_t)a.batch * a.heads * chunks_of(a); }
+inline int block_of(const rc_delta_args& a) {
+  const int pieces = a.dtype == RC_BF16 ? 1 : a.dtype == RC_F16 ? 2 : 3;
+  return block_of(pieces, rows_of(a.key));
+}
+inline int64_t blocks_of(const rc_delta_args& a) { return cdiv(a.length, block_of(a)); }
 inline uint64_t state_floats(const rc_delta_args& a) {
-  return (uint64_t)pairs_of(a) * columns_of(a.value) * rows_of(a.key);
+  return (uint64_t)a.batch * a.heads * blocks_of(a) * columns_of(a.value) * rows_of(a.key);
 }
 inline uint64_t kept_bytes(const rc_delta_args& a) {
   return (state_floats(a) + (uint64_t)pairs_of(a) * columns_of(a.value) * kChunk) * sizeof(float);
@@ -582,7 +600,7 @@ inline uint64_t kept_bytes(const rc_delta_args& a) {
 inline int heads_together(const rc_delta_args& a) {
   const int per = a.heads / a.key_heads;
   for (int each = per; each > 1; each--)
-    if (per % each == 0 && pairs_of(a) / each >= 512) return each;
+    if (per % each == 0 && (int64_t)a.batch * a.heads * blocks_of(a) / each >= 512) return each;
   return 1;
 }
 // Whether the sizes fit the launches.
@@ -624,6 +642,7 @@ inline DeltaParams params(const rc_delta_args& a) {
   DeltaParams p = {};
   p.a = a;
   p.chunks = (int32_t)chunks_of(a);
+  p.blocks = (int32_t)blocks_of(a);
   p.prepared = static_cast<Chunk*>(a.workspace);
   p.states = a.kept;
   return p;

@@ -13,6 +13,7 @@ template <class T, int KT, class G, bool WIDE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
+  constexpr int EVERY = block_of(kPieces<T>, 32 * KT) / kChunk;
   __shared__ Stage<T, KT, G> stages[STAGES];
   __shared__ Parts<G, G::R == 1 ? 0 : 4> parts;
   const Walk<G> at(a);
@@ -30,8 +31,9 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     const auto& stage = stages[chunk % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
-    if (p.states && keeps)
-      keep_state(p.states + (first + chunk) * (columns_of(a.value) * 32 * KT), 32 * KT, at.col, first_row, S);
+    if (p.states && keeps && chunk % EVERY == 0)
+      keep_state(p.states + ((int64_t)at.bh * p.blocks + chunk / EVERY) * (columns_of(a.value) * 32 * KT),
+                 32 * KT, at.col, first_row, S);
     f32x4 r[2], out[2], w[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) r[m] = out[m] = w[m] = f32x4{0, 0, 0, 0};

@@ -10,6 +10,7 @@ template <class T, int KT, class G, bool WIDE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>, STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
+  constexpr int EVERY = block_of(N, 32 * KT) / kChunk;
   __shared__ Stage<T, KT, G> stages[STAGES];
   __shared__ Parts<G, G::R == 1 ? 0 : 2> parts;
   const Walk<G> at(a);
@@ -27,8 +28,9 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
     const auto& stage = stages[i % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
-    if (keeps)
-      keep_state(p.dstates + (first + chunk) * (columns_of(a.value) * 32 * KT), 32 * KT, at.col, first_row, E);
+    if (keeps && (i == 0 || chunk % EVERY == EVERY - 1))
+      keep_state(p.dstates + ((int64_t)at.bh * p.blocks + chunk / EVERY) * (columns_of(a.value) * 32 * KT),
+                 32 * KT, at.col, first_row, E);
     f32x4 dw[2], dr[2], g[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) dw[m] = dr[m] = f32x4{0, 0, 0, 0};
@@ -104,23 +106,53 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
   }
 }
 
-// The gradients of one chunk's inputs from the states before it and the gradients of those after
-// it, head by head of those that share a key head.  Four waves; each takes some of the
-// key's tiles of 16 channels, and reads its part of the states straight into operands.
+// Tile (i, j), j <= i, of a lower triangle's tiles row by row.
+struct Tile {
+  int i, j;
+  __device__ Tile(int n) {
+    i = (n >= 1) + (n >= 3) + (n >= 6);
+    j = n - i * (i + 1) / 2;
+  }
+};
+
+// The gradients of a block's inputs from the state before it and the gradient of the one after
+// it, head by head of those that share a key head.  A wave has 16 NT of the key's channels and reads
+// its part of both states straight into operands, 32 columns at a time and one time
+// ahead; do, v, w and dR of these columns pass through LDS.  What is between tokens (M, N and dR . v)
+// is tiles spread over the waves, then in LDS for all of them.
 template <class T, int KT>
-__global__ __launch_bounds__(256) void k_delta_inputs_back(DeltaParams p) {
+struct Inputs {
+  static constexpr int N = kPieces<T>, BLOCK = block_of(N, 32 * KT), TILES = BLOCK / 16, STEPS = BLOCK / 32;
+  static constexpr int WAVES = KT < 4 ? 2 * KT : 8, THREADS = 64 * WAVES, NT = 2 * KT / WAVES;
+  static constexpr int TRIANGLE = TILES * (TILES + 1) / 2, TASKS = 2 * TRIANGLE + TILES;
+  static constexpr int EACH = (TASKS + WAVES - 1) / WAVES;
+  struct Slice {
+    Tokens<1, N, BLOCK> od, vd;                        // rows: tokens
+    Tokens<BLOCK / 32, 3> rd, wr;                      // rows: columns of the state
+  };
+  struct Between {
+    Tokens<BLOCK / 32, 3, BLOCK> m, n;
+  };
+};
+
+template <class T, int KT>
+__global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
-  constexpr int N = kPieces<T>, NT = (2 * KT + 3) / 4;
-  __shared__ Tokens<KT, N> k, q;
-  __shared__ Tokens<1, N> od;                         // rows: tokens
-  __shared__ Tokens<1, 3> rd, wr;                     // rows: columns of the state
-  __shared__ float M[kChunk][kChunk + 4], Q[kChunk][kChunk + 4];   // M, N of the formulas
-  __shared__ double sums[kChunk];
-  __shared__ float dots[4][4][kChunk], inner[4], dot_v[kChunk], beta[kChunk];
+  using I = Inputs<T, KT>;
+  constexpr int N = I::N, BLOCK = I::BLOCK, TILES = I::TILES, STEPS = I::STEPS, NT = I::NT;
+  constexpr int THREADS = I::THREADS, WAVES = I::WAVES, ROWS = 32 * KT;
+  __shared__ Tokens<KT, N, BLOCK> k, q;
+  __shared__ union Shared {
+    typename I::Slice slice;
+    typename I::Between between;
+    __device__ Shared() {}
+  } lds;
+  __shared__ double sums[BLOCK];
+  __shared__ float since[BLOCK], left[BLOCK], beta[BLOCK], dot_v[BLOCK], dots[WAVES][4][BLOCK], inner[WAVES];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, row = lane / 16 * 4;
-  const int groups = a.heads / p.each, bg = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
+  const int groups = a.heads / p.each, bg = blockIdx.x / p.blocks, block = blockIdx.x % p.blocks;
   const int b = bg / groups, group = bg % groups, hk = group * p.each / (a.heads / a.key_heads);
-  const int t0 = chunk * kChunk, live = min(length_of(a, b) - t0, kChunk), here = min(a.length - t0, kChunk);
+  const int t0 = block * BLOCK, live = min(length_of(a, b) - t0, BLOCK), here = min(a.length - t0, BLOCK);
   const int cols = columns_of(a.value);
   // dq and dk of the key head, or their parts in 32 bits where other workgroups have more
   const auto store = [&](int which, int t, int c, float x) {
@@ -130,205 +162,237 @@ __global__ __launch_bounds__(256) void k_delta_inputs_back(DeltaParams p) {
       p.partial[((((int64_t)which * a.batch + b) * a.length + t0 + t) * groups + group) * a.key + c] = x;
   };
   if (live <= 0) {
-    for (int i = tid; i < here * a.key; i += 256) {
+    for (int i = tid; i < here * a.key; i += THREADS) {
       store(0, i / a.key, i % a.key, 0.f);
       store(1, i / a.key, i % a.key, 0.f);
     }
-    for (int i = tid; i < here * p.each; i += 256) {
+    for (int i = tid; i < here * p.each; i += THREADS) {
       const int64_t at = ((int64_t)b * a.length + t0 + i / p.each) * a.heads + group * p.each + i % p.each;
       if (a.dg) a.dg[at] = 0.f;
       a.dbeta[at] = 0.f;
     }
     return;
   }
-  k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, tid, 256);
-  q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, tid, 256);
-  f32x4 dq[2][NT], dk[2][NT];
+  k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, tid, THREADS);
+  q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, tid, THREADS);
+  f32x4 dq[NT][TILES], dk[NT][TILES];
 #pragma unroll
-  for (int m = 0; m < 2; m++)
+  for (int n = 0; n < NT; n++)
 #pragma unroll
-    for (int n = 0; n < NT; n++) dq[m][n] = dk[m][n] = f32x4{0, 0, 0, 0};
-  const int ti = wave > 0, tj = wave == 2;            // waves 0 to 2: tile (ti, tj) of M and N
+    for (int m = 0; m < TILES; m++) dq[n][m] = dk[n][m] = f32x4{0, 0, 0, 0};
   for (int h = group * p.each; h < (group + 1) * p.each; h++) {
-    const int64_t pair = ((int64_t)b * a.heads + h) * p.chunks + chunk;
-    const float* S = p.states + pair * cols * (32 * KT);
-    const float* E = p.dstates + pair * cols * (32 * KT);
-    const float* w_at = p.kept_written + pair * cols * kChunk;
-    const float* r_at = p.written + pair * cols * kChunk;
+    const int64_t bh = (int64_t)b * a.heads + h;
+    const float* S = p.states + (bh * p.blocks + block) * cols * ROWS;
+    const float* E = p.dstates + (bh * p.blocks + block) * cols * ROWS;
+    const int64_t chunk = bh * p.chunks + block * (BLOCK / kChunk);
+    const int last_chunk = (live - 1) / kChunk;
     __syncthreads();
     if (tid < 64) {
-      const double G = sum_of_g(a, b, h, t0, live);
-      if (tid < kChunk) {
-        sums[tid] = G;
-        beta[tid] = tid < live ? at_token(a.beta, b, t0 + tid, h) : 0.f;
+      // sums of g from the block's first token: its chunks' one after the other
+      double before = 0;
+#pragma unroll
+      for (int s = 0; s < STEPS; s++) {
+        const double G = before + sum_of_g(a, b, h, t0 + 32 * s, live - 32 * s);
+        if (tid < 32) sums[32 * s + tid] = G;
+        before = __shfl(G, 31, 32);
       }
     }
-    f32x4 xq[2][NT], xr[2][NT], xw[2][NT], m_tile = {0, 0, 0, 0}, n_tile = {0, 0, 0, 0};
+    __syncthreads();
+    if (tid < BLOCK) {
+      since[tid] = exp_of(sums[tid]);
+      left[tid] = exp_of(sums[BLOCK - 1] - sums[tid]);
+      beta[tid] = tid < live ? at_token(a.beta, b, t0 + tid, h) : 0.f;
+    }
+    f32x4 xq[NT][TILES], xr[NT][TILES], xw[NT][TILES], task[I::EACH];
 #pragma unroll
-    for (int m = 0; m < 2; m++)
+    for (int n = 0; n < NT; n++)
 #pragma unroll
-      for (int n = 0; n < NT; n++) xq[m][n] = xr[m][n] = xw[m][n] = f32x4{0, 0, 0, 0};
-    float es = 0.f;
-    for (int c0 = 0; c0 < cols; c0 += 32) {
-      __syncthreads();
-      if (tid < 128) {
-        const int t = tid / 4, c = c0 + tid % 4 * 8, n = a.value - c;
-        float x[8];
-        load_vec<8>(at_head<T>(a.do_, b, t0 + (t < live ? t : 0), h) + (n > 0 ? c : 0), t < live ? n : 0, x);
-        od.put(t, tid % 4 * 8, x);
-      } else {
-        const int c = (tid - 128) / 4, t = tid % 4 * 8;
-        float x[8];
-        load_vec<8>(w_at + (c0 + c) * kChunk + t, 8, x);
-        wr.put(c, t, x);
-        load_vec<8>(r_at + (c0 + c) * kChunk + t, 8, x);
-        rd.put(c, t, x);
-      }
-      float x[NT][8], y[NT][8];
+      for (int m = 0; m < TILES; m++) xq[n][m] = xr[n][m] = xw[n][m] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int n = 0; n < NT; n++) {
-        const int tile = min(wave * NT + n, 2 * KT - 1);
+    for (int i = 0; i < I::EACH; i++) task[i] = f32x4{0, 0, 0, 0};
+    float es = 0.f, x[NT][8], y[NT][8];
+    const auto fetch = [&](int c0) {
+#pragma unroll
+      for (int n = 0; n < NT; n++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          const int at = (c0 + e / 4 * 16 + row + e % 4) * (32 * KT) + 16 * tile + col;
+          const int at = (c0 + e / 4 * 16 + row + e % 4) * ROWS + 16 * (wave * NT + n) + col;
           x[n][e] = S[at];
           y[n][e] = E[at];
         }
-      }
+    };
+    fetch(0);
+    for (int c0 = 0; c0 < cols; c0 += 32) {
       __syncthreads();
-      const Pieces<N> os[2] = {od.rows(0, 0), od.rows(1, 0)};
-      const Pieces<3> rs[2] = {rd.columns(0), rd.columns(1)}, ws[2] = {wr.columns(0), wr.columns(1)};
+      for (int i = tid; i < BLOCK * 4; i += THREADS) {
+        {
+          const int t = i / 4, c = c0 + i % 4 * 8, n = t < live ? a.value - c : 0, at = c < a.value ? c : 0;
+          float v[8];
+          load_vec<8>(at_head<T>(a.do_, b, t0 + (t < live ? t : 0), h) + at, n, v);
+          lds.slice.od.put(t, i % 4 * 8, v);
+          load_vec<8>(at_head<T>(a.v, b, t0 + (t < live ? t : 0), h) + at, n, v);
+          lds.slice.vd.put(t, i % 4 * 8, v);
+        }
+        const int c = i / (BLOCK / 8), t = i % (BLOCK / 8) * 8;
+        const int64_t at = ((chunk + min(t / kChunk, last_chunk)) * cols + c0 + c) * kChunk + t % kChunk;
+        const int n = t < live ? 8 : 0;
+        float v[8];
+        load_vec<8>(p.kept_written + at, n, v);
+        lds.slice.wr.put(c, t, v);
+        load_vec<8>(p.written + at, n, v);
+        lds.slice.rd.put(c, t, v);
+      }
+      Pieces<3> ss[NT], ds[NT];
 #pragma unroll
       for (int n = 0; n < NT; n++) {
-        if (wave * NT + n < 2 * KT)
 #pragma unroll
-          for (int e = 0; e < 8; e++) es = fmaf(x[n][e], y[n][e], es);
-        const Pieces<3> ss = split<3>(x[n]), ds = split<3>(y[n]);
+        for (int e = 0; e < 8; e++) es = fmaf(x[n][e], y[n][e], es);
+        ss[n] = split<3>(x[n]);
+        ds[n] = split<3>(y[n]);
+      }
+      __syncthreads();
+      fetch(min(c0 + 32, cols - 32));
 #pragma unroll
-        for (int m = 0; m < 2; m++) {
-          mul(xq[m][n], os[m], ss);
-          mul(xr[m][n], rs[m], ss);
-          mul(xw[m][n], ws[m], ds);
+      for (int m = 0; m < TILES; m++) {
+        const Pieces<N> os = lds.slice.od.rows(m, 0);
+        const Pieces<3> rs = lds.slice.rd.columns(m), ws = lds.slice.wr.columns(m);
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+          mul(xq[n][m], os, ss[n]);
+          mul(xr[n][m], rs, ss[n]);
+          mul(xw[n][m], ws, ds[n]);
         }
       }
-      if (wave < 3) {
-        mul(m_tile, ti ? os[1] : os[0], tj ? ws[1] : ws[0]);
-        mul(n_tile, ti ? rs[1] : rs[0], tj ? ws[1] : ws[0]);
-      }
-    }
-    // dR . v, eight threads a token
-    {
-      const int t = tid / 8;
-      float s = 0.f;
-      if (t < live) {
-        const T* v = at_head<T>(a.v, b, t0 + t, h);
-        for (int c = tid % 8; c < a.value; c += 8) s = fmaf(r_at[c * kChunk + t], (float)v[c], s);
-      }
-      s = lane_sum<8>(s);
-      if (tid % 8 == 0) dot_v[t] = s;
-    }
-    if (wave < 3) {
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const int i = 16 * ti + row + e, j = 16 * tj + col;
-        const float d = exp_of(sums[i] - sums[j]);
-        M[i][j] = j <= i ? a.scale * d * m_tile[e] : 0.f;
-        Q[i][j] = j < i ? d * n_tile[e] : 0.f;
+      for (int i = 0; i < I::EACH; i++) {
+        const int n = wave + i * WAVES;
+        if (n < I::TRIANGLE) {
+          const Tile at(n);
+          mul(task[i], lds.slice.od.rows(at.i, 0), lds.slice.wr.columns(at.j));
+        } else if (n < 2 * I::TRIANGLE) {
+          const Tile at(n - I::TRIANGLE);
+          mul(task[i], lds.slice.rd.columns(at.i), lds.slice.wr.columns(at.j));
+        } else if (n < I::TASKS) {
+          mul(task[i], lds.slice.rd.columns(n - 2 * I::TRIANGLE), lds.slice.vd.rows(n - 2 * I::TRIANGLE, 0));
+        }
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; e++) M[row + e][16 + col] = Q[row + e][16 + col] = 0.f;
     }
     es = lane_sum<64>(es);
     if (lane == 0) inner[wave] = es;
     __syncthreads();
-    const double last = sums[kChunk - 1];
-    Pieces<3> m_rows[2], n_rows[2], m_cols[2], n_cols[2];
+    auto& between = lds.between;
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
-      float x[4][8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int i = 16 * m + col, j = e / 4 * 16 + row + e % 4;
-        x[0][e] = M[i][j];
-        x[1][e] = Q[i][j];
-        x[2][e] = M[j][i];
-        x[3][e] = -beta[j] * Q[j][i];
-      }
-      m_rows[m] = split<3>(x[0]);
-      n_rows[m] = split<3>(x[1]);
-      m_cols[m] = split<3>(x[2]);
-      n_cols[m] = split<3>(x[3]);
-    }
-    float dot[4][2][4];
-#pragma unroll
-    for (int d = 0; d < 4; d++)
-#pragma unroll
-      for (int m = 0; m < 2; m++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) dot[d][m][e] = 0.f;
-    float since[2][4], left[2][4];
-#pragma unroll
-    for (int m = 0; m < 2; m++)
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        since[m][e] = exp_of(sums[16 * m + row + e]);
-        left[m][e] = exp_of(last - sums[16 * m + row + e]);
-      }
-#pragma unroll
-    for (int n = 0; n < NT; n++) {
-      const int tile = wave * NT + n, c = 16 * tile + col;
-      if (tile >= 2 * KT) break;
-      const Pieces<N> kc = k.columns(tile), qc = q.columns(tile);
-#pragma unroll
-      for (int m = 0; m < 2; m++) {
+    for (int i = 0; i < I::EACH; i++) {
+      const int n = wave + i * WAVES;
+      if (n < 2 * I::TRIANGLE) {
+        const bool of_m = n < I::TRIANGLE;
+        const Tile at(of_m ? n : n - I::TRIANGLE);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          xq[m][n][e] *= a.scale * since[m][e];
-          xr[m][n][e] *= since[m][e];
-          xw[m][n][e] *= left[m][e];
-          dot[3][m][e] = fmaf(k.value(16 * m + row + e, c), xw[m][n][e], dot[3][m][e]);
+          const int ti = 16 * at.i + row + e, tj = 16 * at.j + col;
+          const float d = exp_of(sums[ti] - sums[tj]);
+          if (of_m)
+            between.m.put_one(ti, tj, tj <= ti ? a.scale * d * task[i][e] : 0.f);
+          else
+            between.n.put_one(ti, tj, tj < ti ? d * task[i][e] : 0.f);
         }
-        mul(xq[m][n], m_rows[m], kc);
-        mul(xr[m][n], n_rows[m], kc);
-        mul(xw[m][n], m_cols[m], qc);
-        mul(xw[m][n], n_cols[m], kc);
+      } else if (n < I::TASKS) {
+        const int m = n - 2 * I::TRIANGLE;
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const int t = 16 * m + row + e;
-          const float kv = k.value(t, c), qv = q.value(t, c);
-          const float read = -beta[t] * xr[m][n][e];
-          dot[0][m][e] = fmaf(qv, xq[m][n][e], fmaf(kv, read, dot[0][m][e]));
-          dot[1][m][e] = fmaf(kv, xw[m][n][e], dot[1][m][e]);
-          dot[2][m][e] = fmaf(kv, xr[m][n][e], dot[2][m][e]);
-          dq[m][n][e] += xq[m][n][e];
-          dk[m][n][e] += read + xw[m][n][e];
-        }
+        for (int e = 0; e < 4; e++)
+          if (row + e == col) dot_v[16 * m + col] = task[i][e];
       }
     }
-#pragma unroll
-    for (int d = 0; d < 4; d++)
-#pragma unroll
-      for (int m = 0; m < 2; m++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const float s = lane_sum<16>(dot[d][m][e]);
-          if (col == 0) dots[wave][d][16 * m + row + e] = s;
-        }
+    // the tiles above the diagonal that share an operand with one below
+    for (int i = tid; i < BLOCK * 8; i += THREADS) {
+      const int t = i / 8 / 16 * 32 + i / 8 % 16, c = t / 32 * 32 + 16 + i % 8 * 2;
+      if (t < BLOCK) {
+        between.m.put_one(t, c, 0.f);
+        between.m.put_one(t, c + 1, 0.f);
+        between.n.put_one(t, c, 0.f);
+        between.n.put_one(t, c + 1, 0.f);
+      }
+    }
     __syncthreads();
-    if (tid < kChunk) {
-      double s[4];
+#pragma unroll
+    for (int m = 0; m < TILES; m++) {
+      float dot[4][4];
 #pragma unroll
       for (int d = 0; d < 4; d++)
-        s[d] = (double)dots[0][d][tid] + dots[1][d][tid] + dots[2][d][tid] + dots[3][d][tid];
-      double dG = s[0] - s[1], total = s[3];
 #pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const double after = __shfl_down(dG, d, 32);
-        if (tid + d < 32) dG += after;
-        total += __shfl_xor(total, d, 32);
+        for (int e = 0; e < 4; e++) dot[d][e] = 0.f;
+      const f32x4 sm = *(const f32x4*)&since[16 * m + row], lm = *(const f32x4*)&left[16 * m + row],
+                  bm = *(const f32x4*)&beta[16 * m + row];
+#pragma unroll
+      for (int n = 0; n < NT; n++) {
+        const int tile = wave * NT + n, c = 16 * tile + col;
+        f32x4 kv, qv;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          kv[e] = k.value(16 * m + row + e, c);
+          qv[e] = q.value(16 * m + row + e, c);
+        }
+        f32x4 &u = xq[n][m], &r = xr[n][m], &w = xw[n][m];
+        u *= a.scale * sm;
+        r *= sm;
+        w *= lm;
+        const f32x4 from_states = kv * w;
+#pragma unroll
+        for (int s = 0; s <= m / 2; s++) {
+          const Pieces<N> kc = k.columns(tile, s);
+          mul(u, between.m.rows(m, s), kc);
+          mul(r, between.n.rows(m, s), kc);
+        }
+#pragma unroll
+        for (int s = m / 2; s < STEPS; s++) {
+          mul(w, between.m.columns(m, s), q.columns(tile, s));
+          const Pieces<N> kc = k.columns(tile, s);
+          float kb[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = N - 1; i >= 0; i--) v += (float)kc.p[i][e];
+            kb[e] = -beta[32 * s + e / 4 * 16 + row + e % 4] * v;
+          }
+          mul(w, between.n.columns(m, s), split<3>(kb));
+        }
+        const f32x4 read = -bm * r;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          dot[0][e] = fmaf(qv[e], u[e], fmaf(kv[e], read[e], dot[0][e]));
+          dot[1][e] = fmaf(kv[e], w[e], dot[1][e]);
+          dot[2][e] = fmaf(kv[e], r[e], dot[2][e]);
+          dot[3][e] += from_states[e];
+        }
+        dq[n][m] += u;
+        dk[n][m] += read + w;
       }
-      total += (double)exp_of(last) * ((double)inner[0] + inner[1] + inner[2] + inner[3]);
+#pragma unroll
+      for (int d = 0; d < 4; d++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float s = lane_sum<16>(dot[d][e]);
+          if (col == 0) dots[wave][d][16 * m + row + e] = s;
+        }
+    }
+    __syncthreads();
+    if (tid < BLOCK) {
+      double s[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < WAVES; w++)
+#pragma unroll
+        for (int d = 0; d < 4; d++) s[d] += (double)dots[w][d][tid];
+      double dG = s[0] - s[1], total = s[3], ends = 0;
+#pragma unroll
+      for (int d = 1; d < BLOCK; d *= 2) {
+        const double after = __shfl_down(dG, d, BLOCK);
+        if (tid + d < BLOCK) dG += after;
+        total += __shfl_xor(total, d, BLOCK);
+      }
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) ends += (double)inner[w];
+      total += (double)since[BLOCK - 1] * ends;
       const int64_t at = ((int64_t)b * a.length + t0 + tid) * a.heads + h;
       if (tid < here) {
         if (a.dg) a.dg[at] = tid < live ? (float)(dG + total) : 0.f;
@@ -338,16 +402,16 @@ __global__ __launch_bounds__(256) void k_delta_inputs_back(DeltaParams p) {
   }
 #pragma unroll
   for (int n = 0; n < NT; n++) {
-    const int tile = wave * NT + n, c = 16 * tile + col;
-    if (tile >= 2 * KT || c >= a.key) break;
+    const int c = 16 * (wave * NT + n) + col;
+    if (c >= a.key) break;
 #pragma unroll
-    for (int m = 0; m < 2; m++)
+    for (int m = 0; m < TILES; m++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const int t = 16 * m + row + e;
         if (t < here) {
-          store(0, t, c, dq[m][n][e]);
-          store(1, t, c, dk[m][n][e]);
+          store(0, t, c, dq[n][m][e]);
+          store(1, t, c, dk[n][m][e]);
         }
       }
   }
@@ -403,7 +467,8 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
       });
       if (e) return e;
       if (!p.chunks) return (int)RC_OK;
-      k_delta_inputs_back<T, KT><<<(unsigned)(pairs / p.each), 256, 0, s>>>(p);
+      k_delta_inputs_back<T, KT>
+          <<<(unsigned)((int64_t)a.batch * a.heads / p.each * p.blocks), Inputs<T, KT>::THREADS, 0, s>>>(p);
       if (int e = launched("k_delta_inputs_back")) return e;
       if (a.heads / p.each == a.key_heads) return (int)RC_OK;
       const int64_t n = (int64_t)a.batch * a.length * a.key_heads * a.key;
