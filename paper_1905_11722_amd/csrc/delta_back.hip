@@ -116,14 +116,15 @@ struct Tile {
 };
 
 // The gradients of a block's inputs from the state before it and the gradient of the one after
-// it, head by head of those that share a key head.  A wave has 16 NT of the key's channels and reads
-// its part of both states straight into operands, 32 columns at a time and one time
-// ahead; do, v, w and dR of these columns pass through LDS.  What is between tokens (M, N and dR . v)
+// it, head by head of those that share a key head.  A wave has 16 NT of the key's channels (for narrow
+// keys a part of the block's tokens too) and reads its part of both states straight into operands,
+// 32 columns at a time and one time ahead; do, v, w and dR of these columns pass through LDS.  What is between tokens (M, N and dR . v)
 // is tiles spread over the waves, then in LDS for all of them.
 template <class T, int KT>
 struct Inputs {
   static constexpr int N = kPieces<T>, BLOCK = block_of(N, 32 * KT), TILES = BLOCK / 16, STEPS = BLOCK / 32;
-  static constexpr int WAVES = KT < 4 ? 2 * KT : 8, THREADS = 64 * WAVES, NT = 2 * KT / WAVES;
+  static constexpr int WAVES = 8, THREADS = 64 * WAVES;
+  static constexpr int NT = KT > 4 ? KT / 4 : 1, PARTS = KT < 4 ? 4 / KT : 1, MT = TILES / PARTS;
   static constexpr int TRIANGLE = TILES * (TILES + 1) / 2, TASKS = 2 * TRIANGLE + TILES;
   static constexpr int EACH = (TASKS + WAVES - 1) / WAVES;
   struct Slice {
@@ -139,7 +140,7 @@ template <class T, int KT>
 __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
   using I = Inputs<T, KT>;
-  constexpr int N = I::N, BLOCK = I::BLOCK, TILES = I::TILES, STEPS = I::STEPS, NT = I::NT;
+  constexpr int N = I::N, BLOCK = I::BLOCK, MT = I::MT, STEPS = I::STEPS, NT = I::NT;
   constexpr int THREADS = I::THREADS, WAVES = I::WAVES, ROWS = 32 * KT;
   __shared__ Tokens<KT, N, BLOCK> k, q;
   __shared__ union Shared {
@@ -154,6 +155,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
   const int b = bg / groups, group = bg % groups, hk = group * p.each / (a.heads / a.key_heads);
   const int t0 = block * BLOCK, live = min(length_of(a, b) - t0, BLOCK), here = min(a.length - t0, BLOCK);
   const int cols = columns_of(a.value);
+  const bool wide = a.value % 8 == 0;
+  const int first_tile = wave / I::PARTS * NT, first_m = wave % I::PARTS * MT;
   // dq and dk of the key head, or their parts in 32 bits where other workgroups have more
   const auto store = [&](int which, int t, int c, float x) {
     if (groups == a.key_heads)
@@ -175,11 +178,11 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
   }
   k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, tid, THREADS);
   q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, tid, THREADS);
-  f32x4 dq[NT][TILES], dk[NT][TILES];
+  f32x4 dq[NT][MT], dk[NT][MT];
 #pragma unroll
   for (int n = 0; n < NT; n++)
 #pragma unroll
-    for (int m = 0; m < TILES; m++) dq[n][m] = dk[n][m] = f32x4{0, 0, 0, 0};
+    for (int m = 0; m < MT; m++) dq[n][m] = dk[n][m] = f32x4{0, 0, 0, 0};
   for (int h = group * p.each; h < (group + 1) * p.each; h++) {
     const int64_t bh = (int64_t)b * a.heads + h;
     const float* S = p.states + (bh * p.blocks + block) * cols * ROWS;
@@ -203,11 +206,11 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       left[tid] = exp_of(sums[BLOCK - 1] - sums[tid]);
       beta[tid] = tid < live ? at_token(a.beta, b, t0 + tid, h) : 0.f;
     }
-    f32x4 xq[NT][TILES], xr[NT][TILES], xw[NT][TILES], task[I::EACH];
+    f32x4 xq[NT][MT], xr[NT][MT], xw[NT][MT], task[I::EACH];
 #pragma unroll
     for (int n = 0; n < NT; n++)
 #pragma unroll
-      for (int m = 0; m < TILES; m++) xq[n][m] = xr[n][m] = xw[n][m] = f32x4{0, 0, 0, 0};
+      for (int m = 0; m < MT; m++) xq[n][m] = xr[n][m] = xw[n][m] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < I::EACH; i++) task[i] = f32x4{0, 0, 0, 0};
     float es = 0.f, x[NT][8], y[NT][8];
@@ -216,31 +219,65 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       for (int n = 0; n < NT; n++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          const int at = (c0 + e / 4 * 16 + row + e % 4) * ROWS + 16 * (wave * NT + n) + col;
+          const int at = (c0 + e / 4 * 16 + row + e % 4) * ROWS + 16 * (first_tile + n) + col;
           x[n][e] = S[at];
           y[n][e] = E[at];
         }
     };
+    // do and v by half of the threads, w and dR by the others: eight numbers of each of two, raw
+    constexpr int ITEMS = BLOCK * 4;
+    const int item = tid % ITEMS;
+    const bool walks = tid >= ITEMS, own = tid < 2 * ITEMS;
+    const int wt = item % (BLOCK / 8) * 8, xt = item / 4;
+    const bool on = (walks ? wt : xt) < live;
+    // an address that is always there, where one is not wide or not there
+    const auto slice_at = [&](int c0, int which) -> const char* {
+      if (walks)
+        return (const char*)((which ? p.written : p.kept_written) +
+                             ((chunk + min(wt / kChunk, last_chunk)) * cols + c0 + item / (BLOCK / 8)) * kChunk +
+                             wt % kChunk);
+      const int c = c0 + item % 4 * 8;
+      if (!wide || c >= a.value) return (const char*)S;
+      return (const char*)(at_head<T>(which ? a.v : a.do_, b, t0 + (on ? xt : 0), h) + c);
+    };
+    constexpr int FAR = sizeof(T) == 4 ? 16 : 0;       // the second half of eight 16-bit numbers: none
+    u32x4 pre[2][2];
+    const auto prefetch = [&](int c0) {
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const char* from = slice_at(c0, i);
+        __builtin_memcpy(&pre[i][0], from, 16);
+        __builtin_memcpy(&pre[i][1], from + (walks ? 16 : FAR), 16);
+      }
+    };
     fetch(0);
+    prefetch(0);
     for (int c0 = 0; c0 < cols; c0 += 32) {
       __syncthreads();
-      for (int i = tid; i < BLOCK * 4; i += THREADS) {
-        {
-          const int t = i / 4, c = c0 + i % 4 * 8, n = t < live ? a.value - c : 0, at = c < a.value ? c : 0;
+      if (walks && own) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
           float v[8];
-          load_vec<8>(at_head<T>(a.do_, b, t0 + (t < live ? t : 0), h) + at, n, v);
-          lds.slice.od.put(t, i % 4 * 8, v);
-          load_vec<8>(at_head<T>(a.v, b, t0 + (t < live ? t : 0), h) + at, n, v);
-          lds.slice.vd.put(t, i % 4 * 8, v);
+#pragma unroll
+          for (int e = 0; e < 8; e++) v[e] = on ? __builtin_bit_cast(float, (uint32_t)pre[i][e / 4][e % 4]) : 0.f;
+          (i ? lds.slice.rd : lds.slice.wr).put(item / (BLOCK / 8), wt, v);
         }
-        const int c = i / (BLOCK / 8), t = i % (BLOCK / 8) * 8;
-        const int64_t at = ((chunk + min(t / kChunk, last_chunk)) * cols + c0 + c) * kChunk + t % kChunk;
-        const int n = t < live ? 8 : 0;
-        float v[8];
-        load_vec<8>(p.kept_written + at, n, v);
-        lds.slice.wr.put(c, t, v);
-        load_vec<8>(p.written + at, n, v);
-        lds.slice.rd.put(c, t, v);
+      } else if (!walks) {
+        const int c = c0 + item % 4 * 8, n = on ? a.value - c : 0;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          float v[8];
+          if (wide) {
+            typedef T TV __attribute__((ext_vector_type(8)));
+            TV r;
+            __builtin_memcpy(&r, &pre[i], sizeof(r));
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = n > 0 ? (float)r[e] : 0.f;
+          } else {
+            load_vec<8>(at_head<T>(i ? a.v : a.do_, b, t0 + (on ? xt : 0), h) + (n > 0 ? c : 0), n, v);
+          }
+          (i ? lds.slice.vd : lds.slice.od).put(xt, item % 4 * 8, v);
+        }
       }
       Pieces<3> ss[NT], ds[NT];
 #pragma unroll
@@ -252,10 +289,11 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       }
       __syncthreads();
       fetch(min(c0 + 32, cols - 32));
+      prefetch(min(c0 + 32, cols - 32));
 #pragma unroll
-      for (int m = 0; m < TILES; m++) {
-        const Pieces<N> os = lds.slice.od.rows(m, 0);
-        const Pieces<3> rs = lds.slice.rd.columns(m), ws = lds.slice.wr.columns(m);
+      for (int m = 0; m < MT; m++) {
+        const Pieces<N> os = lds.slice.od.rows(first_m + m, 0);
+        const Pieces<3> rs = lds.slice.rd.columns(first_m + m), ws = lds.slice.wr.columns(first_m + m);
 #pragma unroll
         for (int n = 0; n < NT; n++) {
           mul(xq[n][m], os, ss[n]);
@@ -278,7 +316,7 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       }
     }
     es = lane_sum<64>(es);
-    if (lane == 0) inner[wave] = es;
+    if (lane == 0) inner[wave] = first_m ? 0.f : es;   // (parts of the tokens have the same states)
     __syncthreads();
     auto& between = lds.between;
 #pragma unroll
@@ -315,22 +353,23 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
     }
     __syncthreads();
 #pragma unroll
-    for (int m = 0; m < TILES; m++) {
+    for (int m = 0; m < MT; m++) {
+      const int mm = first_m + m;
       float dot[4][4];
 #pragma unroll
       for (int d = 0; d < 4; d++)
 #pragma unroll
         for (int e = 0; e < 4; e++) dot[d][e] = 0.f;
-      const f32x4 sm = *(const f32x4*)&since[16 * m + row], lm = *(const f32x4*)&left[16 * m + row],
-                  bm = *(const f32x4*)&beta[16 * m + row];
+      const f32x4 sm = *(const f32x4*)&since[16 * mm + row], lm = *(const f32x4*)&left[16 * mm + row],
+                  bm = *(const f32x4*)&beta[16 * mm + row];
 #pragma unroll
       for (int n = 0; n < NT; n++) {
-        const int tile = wave * NT + n, c = 16 * tile + col;
+        const int tile = first_tile + n, c = 16 * tile + col;
         f32x4 kv, qv;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          kv[e] = k.value(16 * m + row + e, c);
-          qv[e] = q.value(16 * m + row + e, c);
+          kv[e] = k.value(16 * mm + row + e, c);
+          qv[e] = q.value(16 * mm + row + e, c);
         }
         f32x4 &u = xq[n][m], &r = xr[n][m], &w = xw[n][m];
         u *= a.scale * sm;
@@ -338,14 +377,16 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         w *= lm;
         const f32x4 from_states = kv * w;
 #pragma unroll
-        for (int s = 0; s <= m / 2; s++) {
+        for (int s = 0; s < STEPS; s++) {
+          if (s > mm / 2) continue;
           const Pieces<N> kc = k.columns(tile, s);
-          mul(u, between.m.rows(m, s), kc);
-          mul(r, between.n.rows(m, s), kc);
+          mul(u, between.m.rows(mm, s), kc);
+          mul(r, between.n.rows(mm, s), kc);
         }
 #pragma unroll
-        for (int s = m / 2; s < STEPS; s++) {
-          mul(w, between.m.columns(m, s), q.columns(tile, s));
+        for (int s = 0; s < STEPS; s++) {
+          if (s < mm / 2) continue;
+          mul(w, between.m.columns(mm, s), q.columns(tile, s));
           const Pieces<N> kc = k.columns(tile, s);
           float kb[8];
 #pragma unroll
@@ -355,7 +396,7 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
             for (int i = N - 1; i >= 0; i--) v += (float)kc.p[i][e];
             kb[e] = -beta[32 * s + e / 4 * 16 + row + e % 4] * v;
           }
-          mul(w, between.n.columns(m, s), split<3>(kb));
+          mul(w, between.n.columns(mm, s), split<3>(kb));
         }
         const f32x4 read = -bm * r;
 #pragma unroll
@@ -373,16 +414,16 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const float s = lane_sum<16>(dot[d][e]);
-          if (col == 0) dots[wave][d][16 * m + row + e] = s;
+          if (col == 0) dots[wave][d][16 * mm + row + e] = s;
         }
     }
     __syncthreads();
     if (tid < BLOCK) {
       double s[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int w = 0; w < WAVES; w++)
+      for (int w = 0; w < WAVES; w += I::PARTS)
 #pragma unroll
-        for (int d = 0; d < 4; d++) s[d] += (double)dots[w][d][tid];
+        for (int d = 0; d < 4; d++) s[d] += (double)dots[w + tid / 16 / MT][d][tid];
       double dG = s[0] - s[1], total = s[3], ends = 0;
 #pragma unroll
       for (int d = 1; d < BLOCK; d *= 2) {
@@ -402,13 +443,13 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
   }
 #pragma unroll
   for (int n = 0; n < NT; n++) {
-    const int c = 16 * (wave * NT + n) + col;
+    const int c = 16 * (first_tile + n) + col;
     if (c >= a.key) break;
 #pragma unroll
-    for (int m = 0; m < TILES; m++)
+    for (int m = 0; m < MT; m++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const int t = 16 * m + row + e;
+        const int t = 16 * (first_m + m) + row + e;
         if (t < here) {
           store(0, t, c, dq[n][m][e]);
           store(1, t, c, dk[n][m][e]);
