@@ -109,6 +109,11 @@ __device__ __forceinline__ float exp_of(double x) {
   return __builtin_amdgcn_ldexpf(fast_exp2((float)(e - n)), (int)__builtin_fmax(n, -1000.0));
 }
 
+// The same for pairs of tokens, of which there are many: off by |x| 2^-24 of itself.
+__device__ __forceinline__ float decay_between(double x) {
+  return fast_exp2((float)(x * 1.44269504088896340736));
+}
+
 // ROWS rows (tokens) of `32 KT` channels in LDS as pieces.  Within each 32 channels, groups of four
 // are ordered 0 4 1 5 2 6 3 7, so that a lane's operand (above) is 16 bytes.
 template <int KT, int N, int ROWS = kChunk>
@@ -159,13 +164,13 @@ struct Tokens {
     }
     return f;
   }
-  __device__ void put_one(int r, int c, float x) {
-    const int at_c = c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4;
+  // Four channels of one row, c a multiple of four.
+  __device__ void put_four(int r, int c, const f32x4& x) {
+    const float v[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    const Pieces<N> s = split<N>(v);
+    bf16* to = &at[0][r][c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4];
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      at[i][r][at_c] = (bf16)x;
-      x -= (float)at[i][r][at_c];
-    }
+    for (int i = 0; i < N; i++) *(bf16x4*)(to + i * (ROWS * STRIDE)) = s.p[i].lo;
   }
   // Eight channels as they are where one piece is all.
   __device__ void put(int r, int c, const bf16x8& v) {
@@ -187,6 +192,7 @@ struct Tokens {
 struct Chunk {
   bf16x8 t[2][3][64], p[2][3][64];
   float since[kChunk], left[kChunk], beta[kChunk];    // exp(G_i), exp(G_31 - G_i), beta_i
+  double sum[kChunk];                                 // G_i
 };
 constexpr int kChunkVectors = sizeof(Chunk) / 16;
 static_assert(sizeof(Chunk) % 16 == 0, "copied in vectors");
@@ -196,8 +202,14 @@ static_assert(sizeof(Chunk) % 16 == 0, "copied in vectors");
 // [columns(value)][rows(key)] in 32 bits; w and dR likewise, four tokens of a column
 // together: [batch][heads][chunks][columns(value)][32].  A block is two chunks where its keys,
 // queries and products of tokens fit LDS and registers: half of the states to write, keep and read.
+// Bytes of LDS with the states' slices in it too, and without them.
+constexpr int block_bytes(int pieces, int rows, int block, bool held) {
+  return 2 * pieces * block * (rows + 8 + 40) * 2 + 2 * 3 * 32 * (block + 8) * 2 +
+         (held ? 2 * 3 * 32 * (rows + 8) * 2 : 0);
+}
+constexpr int kBlockBytes = 150 * 1024;
 constexpr int block_of(int pieces, int rows) {
-  return rows <= 128 && 2 * pieces * 64 * (rows + 8) * 2 + 2 * 3 * 64 * 72 * 2 <= 152 * 1024 ? 64 : 32;
+  return rows <= 128 && block_bytes(pieces, rows, 64, true) <= kBlockBytes ? 64 : 32;
 }
 __host__ __device__ inline int rows_of(int key) {
   return key <= 32 ? 32 : key <= 64 ? 64 : key <= 128 ? 128 : 256;
@@ -272,6 +284,7 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     out.since[lane] = exp_of(G);
     out.left[lane] = exp_of(last - G);
     out.beta[lane] = beta[lane];
+    out.sum[lane] = G;
   }
   __syncthreads();
   // tiles of k_i . k_j and q_i . k_j with rows j (backward for P: rows i) and the other as columns
@@ -300,9 +313,9 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
 #pragma unroll
       for (int r = 0; r < 4; r++) {
         const int i = 16 * n + col, j = 16 * m + row + r;
-        A[i][j] = j < i ? beta[i] * exp_of(sums[i] - sums[j]) * kk[m][n][r] : 0.f;
+        A[i][j] = j < i ? beta[i] * decay_between(sums[i] - sums[j]) * kk[m][n][r] : 0.f;
         const int pi = BACK ? j : i, pj = BACK ? i : j;
-        qk[m][n][r] = pj <= pi ? a.scale * exp_of(sums[pi] - sums[pj]) * qk[m][n][r] : 0.f;
+        qk[m][n][r] = pj <= pi ? a.scale * decay_between(sums[pi] - sums[pj]) * qk[m][n][r] : 0.f;
       }
 #pragma unroll
   for (int n = 0; n < 2; n++) {

@@ -117,8 +117,9 @@ struct Tile {
 
 // The gradients of a block's inputs from the state before it and the gradient of the one after
 // it, head by head of those that share a key head.  A wave has 16 NT of the key's channels (for narrow
-// keys a part of the block's tokens too) and reads its part of both states straight into operands,
-// 32 columns at a time and one time ahead; do, v, w and dR of these columns pass through LDS.  What is between tokens (M, N and dR . v)
+// keys a part of the block's tokens too).  Both states, do, v, w and dR pass through LDS, 32 columns at a
+// time and one time ahead in registers; where LDS has no room for the states a wave reads its part
+// of them straight into operands, a number a load (which is what bounds it then).  What is between tokens (M, N and dR . v)
 // is tiles spread over the waves, then in LDS for all of them.
 template <class T, int KT>
 struct Inputs {
@@ -127,9 +128,11 @@ struct Inputs {
   static constexpr int NT = KT > 4 ? KT / 4 : 1, PARTS = KT < 4 ? 4 / KT : 1, MT = TILES / PARTS;
   static constexpr int TRIANGLE = TILES * (TILES + 1) / 2, TASKS = 2 * TRIANGLE + TILES;
   static constexpr int EACH = (TASKS + WAVES - 1) / WAVES;
+  static constexpr bool HELD = block_bytes(N, 32 * KT, BLOCK, true) <= kBlockBytes;
   struct Slice {
     Tokens<1, N, BLOCK> od, vd;                        // rows: tokens
     Tokens<BLOCK / 32, 3> rd, wr;                      // rows: columns of the state
+    Tokens<HELD ? KT : 1, 3> s, e;                     // the same
   };
   struct Between {
     Tokens<BLOCK / 32, 3, BLOCK> m, n;
@@ -149,7 +152,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
     __device__ Shared() {}
   } lds;
   __shared__ double sums[BLOCK];
-  __shared__ float since[BLOCK], left[BLOCK], beta[BLOCK], dot_v[BLOCK], dots[WAVES][4][BLOCK], inner[WAVES];
+  __shared__ float since[BLOCK], left[BLOCK], beta[BLOCK], dot_v[BLOCK], dots[WAVES * NT][4][BLOCK],
+      inner[WAVES];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, row = lane / 16 * 4;
   const int groups = a.heads / p.each, bg = blockIdx.x / p.blocks, block = blockIdx.x % p.blocks;
   const int b = bg / groups, group = bg % groups, hk = group * p.each / (a.heads / a.key_heads);
@@ -176,6 +180,64 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
     }
     return;
   }
+  // do and v by half of the threads, w and dR by the others: eight numbers of each of two, raw
+  constexpr int ITEMS = BLOCK * 4;
+  constexpr int FAR = sizeof(T) == 4 ? 16 : 0;         // the second half of eight 16-bit numbers: none
+  const int item = tid % ITEMS, wt = item % (BLOCK / 8) * 8, xt = item / 4, xc = item % 4 * 8;
+  const int last_chunk = (live - 1) / kChunk;
+  const bool walks = tid >= ITEMS, own = tid < 2 * ITEMS, on = (walks ? wt : xt) < live;
+  const float *S, *E;
+  const char* from[2];
+  float x[NT][8], y[NT][8], next_beta;
+  double next_sum[3];
+  u32x4 pre[2][2];
+  const int held_row = min(tid / (KT * 4), 31), held_at = tid % (KT * 4) * 8;
+  const bool holds = tid < KT * 128;
+  const auto fetch = [&](int c0) {
+    if constexpr (I::HELD) {
+      __builtin_memcpy(&x[0], S + (c0 + held_row) * ROWS + held_at, 32);
+      __builtin_memcpy(&y[0], E + (c0 + held_row) * ROWS + held_at, 32);
+    }
+#pragma unroll
+    for (int n = 0; n < (I::HELD ? 0 : NT); n++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int at = (c0 + e / 4 * 16 + row + e % 4) * ROWS + 16 * (first_tile + n) + col;
+        x[n][e] = S[at];
+        y[n][e] = E[at];
+      }
+    // (an address that is always there, where one is not wide or not there)
+    const bool there = walks || (wide && c0 + xc < a.value);
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const char* at = there ? from[i] + c0 * (walks ? kChunk * 4 : (int)sizeof(T)) : (const char*)S;
+      __builtin_memcpy(&pre[i][0], at, 16);
+      __builtin_memcpy(&pre[i][1], at + (walks ? 16 : FAR), 16);
+    }
+  };
+  // The first loads of a head.
+  const auto enter = [&](int h) {
+    const int64_t bh = (int64_t)b * a.heads + h, chunk = bh * p.chunks + block * (BLOCK / kChunk);
+    S = p.states + (bh * p.blocks + block) * cols * ROWS;
+    E = p.dstates + (bh * p.blocks + block) * cols * ROWS;
+    if (walks) {
+      const int64_t at =
+          ((chunk + min(wt / kChunk, last_chunk)) * cols + item / (BLOCK / 8)) * kChunk + wt % kChunk;
+      from[0] = (const char*)(p.kept_written + at);
+      from[1] = (const char*)(p.written + at);
+    } else {
+      from[0] = (const char*)(at_head<T>(a.do_, b, t0 + (on ? xt : 0), h) + xc);
+      from[1] = (const char*)(at_head<T>(a.v, b, t0 + (on ? xt : 0), h) + xc);
+    }
+    const Chunk* c = p.prepared + chunk;
+    const int t = tid % BLOCK, mine = min(t / kChunk, last_chunk);
+    next_sum[0] = c[mine].sum[t % kChunk];
+    next_sum[1] = c[0].sum[kChunk - 1];
+    next_sum[2] = c[last_chunk].sum[kChunk - 1];
+    next_beta = c[mine].beta[t % kChunk];
+    fetch(0);
+  };
+  enter(group * p.each);
   k.load(at_head<T>(a.k, b, t0, hk), a.k.time, live, a.key, tid, THREADS);
   q.load(at_head<T>(a.q, b, t0, hk), a.q.time, live, a.key, tid, THREADS);
   f32x4 dq[NT][MT], dk[NT][MT];
@@ -184,27 +246,14 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
 #pragma unroll
     for (int m = 0; m < MT; m++) dq[n][m] = dk[n][m] = f32x4{0, 0, 0, 0};
   for (int h = group * p.each; h < (group + 1) * p.each; h++) {
-    const int64_t bh = (int64_t)b * a.heads + h;
-    const float* S = p.states + (bh * p.blocks + block) * cols * ROWS;
-    const float* E = p.dstates + (bh * p.blocks + block) * cols * ROWS;
-    const int64_t chunk = bh * p.chunks + block * (BLOCK / kChunk);
-    const int last_chunk = (live - 1) / kChunk;
-    __syncthreads();
-    if (tid < 64) {
-      // sums of g from the block's first token: its chunks' one after the other
-      double before = 0;
-#pragma unroll
-      for (int s = 0; s < STEPS; s++) {
-        const double G = before + sum_of_g(a, b, h, t0 + 32 * s, live - 32 * s);
-        if (tid < 32) sums[32 * s + tid] = G;
-        before = __shfl(G, 31, 32);
-      }
-    }
-    __syncthreads();
     if (tid < BLOCK) {
-      since[tid] = exp_of(sums[tid]);
-      left[tid] = exp_of(sums[BLOCK - 1] - sums[tid]);
-      beta[tid] = tid < live ? at_token(a.beta, b, t0 + tid, h) : 0.f;
+      // sums of g from the block's first token
+      const double end = last_chunk ? next_sum[1] + next_sum[2] : next_sum[1];
+      const double G = tid / kChunk > last_chunk ? end : tid < kChunk ? next_sum[0] : next_sum[1] + next_sum[0];
+      sums[tid] = G;
+      since[tid] = exp_of(G);
+      left[tid] = exp_of(end - G);
+      beta[tid] = tid < live ? next_beta : 0.f;
     }
     f32x4 xq[NT][MT], xr[NT][MT], xw[NT][MT], task[I::EACH];
 #pragma unroll
@@ -213,47 +262,9 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       for (int m = 0; m < MT; m++) xq[n][m] = xr[n][m] = xw[n][m] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < I::EACH; i++) task[i] = f32x4{0, 0, 0, 0};
-    float es = 0.f, x[NT][8], y[NT][8];
-    const auto fetch = [&](int c0) {
-#pragma unroll
-      for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const int at = (c0 + e / 4 * 16 + row + e % 4) * ROWS + 16 * (first_tile + n) + col;
-          x[n][e] = S[at];
-          y[n][e] = E[at];
-        }
-    };
-    // do and v by half of the threads, w and dR by the others: eight numbers of each of two, raw
-    constexpr int ITEMS = BLOCK * 4;
-    const int item = tid % ITEMS;
-    const bool walks = tid >= ITEMS, own = tid < 2 * ITEMS;
-    const int wt = item % (BLOCK / 8) * 8, xt = item / 4;
-    const bool on = (walks ? wt : xt) < live;
-    // an address that is always there, where one is not wide or not there
-    const auto slice_at = [&](int c0, int which) -> const char* {
-      if (walks)
-        return (const char*)((which ? p.written : p.kept_written) +
-                             ((chunk + min(wt / kChunk, last_chunk)) * cols + c0 + item / (BLOCK / 8)) * kChunk +
-                             wt % kChunk);
-      const int c = c0 + item % 4 * 8;
-      if (!wide || c >= a.value) return (const char*)S;
-      return (const char*)(at_head<T>(which ? a.v : a.do_, b, t0 + (on ? xt : 0), h) + c);
-    };
-    constexpr int FAR = sizeof(T) == 4 ? 16 : 0;       // the second half of eight 16-bit numbers: none
-    u32x4 pre[2][2];
-    const auto prefetch = [&](int c0) {
-#pragma unroll
-      for (int i = 0; i < 2; i++) {
-        const char* from = slice_at(c0, i);
-        __builtin_memcpy(&pre[i][0], from, 16);
-        __builtin_memcpy(&pre[i][1], from + (walks ? 16 : FAR), 16);
-      }
-    };
-    fetch(0);
-    prefetch(0);
+    float es = 0.f;
     for (int c0 = 0; c0 < cols; c0 += 32) {
-      __syncthreads();
+      if (c0) __syncthreads();
       if (walks && own) {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
@@ -263,7 +274,7 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
           (i ? lds.slice.rd : lds.slice.wr).put(item / (BLOCK / 8), wt, v);
         }
       } else if (!walks) {
-        const int c = c0 + item % 4 * 8, n = on ? a.value - c : 0;
+        const int n = on ? a.value - (c0 + xc) : 0;
 #pragma unroll
         for (int i = 0; i < 2; i++) {
           float v[8];
@@ -274,22 +285,37 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
 #pragma unroll
             for (int e = 0; e < 8; e++) v[e] = n > 0 ? (float)r[e] : 0.f;
           } else {
-            load_vec<8>(at_head<T>(i ? a.v : a.do_, b, t0 + (on ? xt : 0), h) + (n > 0 ? c : 0), n, v);
+            load_vec<8>((const T*)from[i] + (n > 0 ? c0 : 0), n, v);
           }
-          (i ? lds.slice.vd : lds.slice.od).put(xt, item % 4 * 8, v);
+          (i ? lds.slice.vd : lds.slice.od).put(xt, xc, v);
         }
       }
       Pieces<3> ss[NT], ds[NT];
+      if constexpr (I::HELD) {
+        if (holds) {
 #pragma unroll
-      for (int n = 0; n < NT; n++) {
+          for (int e = 0; e < 8; e++) es = fmaf(x[0][e], y[0][e], es);
+          lds.slice.s.put(held_row, held_at, x[0]);
+          lds.slice.e.put(held_row, held_at, y[0]);
+        }
+      } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) es = fmaf(x[n][e], y[n][e], es);
-        ss[n] = split<3>(x[n]);
-        ds[n] = split<3>(y[n]);
+        for (int n = 0; n < NT; n++) {
+#pragma unroll
+          for (int e = 0; e < 8; e++) es = fmaf(x[n][e], y[n][e], es);
+          ss[n] = split<3>(x[n]);
+          ds[n] = split<3>(y[n]);
+        }
       }
       __syncthreads();
+      if constexpr (I::HELD) {
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+          ss[n] = lds.slice.s.columns(first_tile + n);
+          ds[n] = lds.slice.e.columns(first_tile + n);
+        }
+      }
       fetch(min(c0 + 32, cols - 32));
-      prefetch(min(c0 + 32, cols - 32));
 #pragma unroll
       for (int m = 0; m < MT; m++) {
         const Pieces<N> os = lds.slice.od.rows(first_m + m, 0);
@@ -301,22 +327,23 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
           mul(xw[n][m], ws, ds[n]);
         }
       }
+      // tiles of M and N as their transposes: four of a lane's numbers lie side by side
 #pragma unroll
       for (int i = 0; i < I::EACH; i++) {
         const int n = wave + i * WAVES;
         if (n < I::TRIANGLE) {
           const Tile at(n);
-          mul(task[i], lds.slice.od.rows(at.i, 0), lds.slice.wr.columns(at.j));
+          mul(task[i], lds.slice.wr.columns(at.j), lds.slice.od.rows(at.i, 0));
         } else if (n < 2 * I::TRIANGLE) {
           const Tile at(n - I::TRIANGLE);
-          mul(task[i], lds.slice.rd.columns(at.i), lds.slice.wr.columns(at.j));
+          mul(task[i], lds.slice.wr.columns(at.j), lds.slice.rd.columns(at.i));
         } else if (n < I::TASKS) {
           mul(task[i], lds.slice.rd.columns(n - 2 * I::TRIANGLE), lds.slice.vd.rows(n - 2 * I::TRIANGLE, 0));
         }
       }
     }
     es = lane_sum<64>(es);
-    if (lane == 0) inner[wave] = first_m ? 0.f : es;   // (parts of the tokens have the same states)
+    if (lane == 0) inner[wave] = I::HELD || !first_m ? es : 0.f;   // (parts of the tokens have the same states)
     __syncthreads();
     auto& between = lds.between;
 #pragma unroll
@@ -325,15 +352,14 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       if (n < 2 * I::TRIANGLE) {
         const bool of_m = n < I::TRIANGLE;
         const Tile at(of_m ? n : n - I::TRIANGLE);
+        const int ti = 16 * at.i + col;
+        f32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          const int ti = 16 * at.i + row + e, tj = 16 * at.j + col;
-          const float d = exp_of(sums[ti] - sums[tj]);
-          if (of_m)
-            between.m.put_one(ti, tj, tj <= ti ? a.scale * d * task[i][e] : 0.f);
-          else
-            between.n.put_one(ti, tj, tj < ti ? d * task[i][e] : 0.f);
+          const int tj = 16 * at.j + row + e;
+          v[e] = (of_m ? tj <= ti : tj < ti) ? (of_m ? a.scale : 1.f) * decay_between(sums[ti] - sums[tj]) * task[i][e] : 0.f;
         }
+        (of_m ? between.m : between.n).put_four(ti, 16 * at.j + row, v);
       } else if (n < I::TASKS) {
         const int m = n - 2 * I::TRIANGLE;
 #pragma unroll
@@ -342,29 +368,35 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       }
     }
     // the tiles above the diagonal that share an operand with one below
-    for (int i = tid; i < BLOCK * 8; i += THREADS) {
-      const int t = i / 8 / 16 * 32 + i / 8 % 16, c = t / 32 * 32 + 16 + i % 8 * 2;
-      if (t < BLOCK) {
-        between.m.put_one(t, c, 0.f);
-        between.m.put_one(t, c + 1, 0.f);
-        between.n.put_one(t, c, 0.f);
-        between.n.put_one(t, c + 1, 0.f);
-      }
+    if (tid < BLOCK * 4) {
+      const int t = tid / 8 / 16 * 32 + tid / 8 % 16;  // tid / 8 of the upper halves' rows
+      const f32x4 zero = {0, 0, 0, 0};
+      (tid & 4 ? between.m : between.n).put_four(t, t / 32 * 32 + 16 + tid % 4 * 4, zero);
     }
     __syncthreads();
+    const float whole = since[BLOCK - 1];
 #pragma unroll
-    for (int m = 0; m < MT; m++) {
-      const int mm = first_m + m;
-      float dot[4][4];
+    for (int n = 0; n < NT; n++) {
+      const int tile = first_tile + n, c = 16 * tile + col;
+      Pieces<N> kc[STEPS], qc[STEPS];
+      Pieces<3> kb[STEPS];                             // -beta k
 #pragma unroll
-      for (int d = 0; d < 4; d++)
+      for (int s = 0; s < STEPS; s++) {
+        kc[s] = k.columns(tile, s);
+        qc[s] = q.columns(tile, s);
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 4; e++) dot[d][e] = 0.f;
-      const f32x4 sm = *(const f32x4*)&since[16 * mm + row], lm = *(const f32x4*)&left[16 * mm + row],
-                  bm = *(const f32x4*)&beta[16 * mm + row];
+        for (int e = 0; e < 8; e++) {
+          v[e] = 0.f;
 #pragma unroll
-      for (int n = 0; n < NT; n++) {
-        const int tile = first_tile + n, c = 16 * tile + col;
+          for (int i = N - 1; i >= 0; i--) v[e] += (float)kc[s].p[i][e];
+          v[e] *= -beta[32 * s + e / 4 * 16 + row + e % 4];
+        }
+        kb[s] = split<3>(v);
+      }
+#pragma unroll
+      for (int m = 0; m < MT; m++) {
+        const int mm = first_m + m;
         f32x4 kv, qv;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -372,72 +404,58 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
           qv[e] = q.value(16 * mm + row + e, c);
         }
         f32x4 &u = xq[n][m], &r = xr[n][m], &w = xw[n][m];
-        u *= a.scale * sm;
-        r *= sm;
-        w *= lm;
+        u *= a.scale * *(const f32x4*)&since[16 * mm + row];
+        r *= *(const f32x4*)&since[16 * mm + row];
+        w *= *(const f32x4*)&left[16 * mm + row];
         const f32x4 from_states = kv * w;
 #pragma unroll
         for (int s = 0; s < STEPS; s++) {
-          if (s > mm / 2) continue;
-          const Pieces<N> kc = k.columns(tile, s);
-          mul(u, between.m.rows(mm, s), kc);
-          mul(r, between.n.rows(mm, s), kc);
-        }
-#pragma unroll
-        for (int s = 0; s < STEPS; s++) {
-          if (s < mm / 2) continue;
-          mul(w, between.m.columns(mm, s), q.columns(tile, s));
-          const Pieces<N> kc = k.columns(tile, s);
-          float kb[8];
-#pragma unroll
-          for (int e = 0; e < 8; e++) {
-            float v = 0.f;
-#pragma unroll
-            for (int i = N - 1; i >= 0; i--) v += (float)kc.p[i][e];
-            kb[e] = -beta[32 * s + e / 4 * 16 + row + e % 4] * v;
+          if (s <= mm / 2) {
+            mul(u, between.m.rows(mm, s), kc[s]);
+            mul(r, between.n.rows(mm, s), kc[s]);
           }
-          mul(w, between.n.columns(mm, s), split<3>(kb));
+          if (s >= mm / 2) {
+            mul(w, between.m.columns(mm, s), qc[s]);
+            mul(w, between.n.columns(mm, s), kb[s]);
+          }
         }
-        const f32x4 read = -bm * r;
+        const f32x4 read = -*(const f32x4*)&beta[16 * mm + row] * r;
+        const f32x4 dot[4] = {qv * u + kv * read, kv * w, kv * r, from_states};
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-          dot[0][e] = fmaf(qv[e], u[e], fmaf(kv[e], read[e], dot[0][e]));
-          dot[1][e] = fmaf(kv[e], w[e], dot[1][e]);
-          dot[2][e] = fmaf(kv[e], r[e], dot[2][e]);
-          dot[3][e] += from_states[e];
-        }
+        for (int d = 0; d < 4; d++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float s = lane_sum<16>(dot[d][e]);
+            if (col == 0) dots[wave * NT + n][d][16 * mm + row + e] = s;
+          }
         dq[n][m] += u;
         dk[n][m] += read + w;
       }
-#pragma unroll
-      for (int d = 0; d < 4; d++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const float s = lane_sum<16>(dot[d][e]);
-          if (col == 0) dots[wave][d][16 * mm + row + e] = s;
-        }
     }
+    enter(min(h + 1, (group + 1) * p.each - 1));       // (unconditional, as every load that a loop hands on)
     __syncthreads();
-    if (tid < BLOCK) {
-      double s[4] = {0, 0, 0, 0};
+    // dg and dbeta by the last wave, while the others begin the next head
+    if (wave == WAVES - 1 && lane < BLOCK) {
+      float s[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int w = 0; w < WAVES; w += I::PARTS)
 #pragma unroll
-        for (int d = 0; d < 4; d++) s[d] += (double)dots[w + tid / 16 / MT][d][tid];
-      double dG = s[0] - s[1], total = s[3], ends = 0;
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int d = 0; d < 4; d++) s[d] += dots[(w + lane / 16 / MT) * NT + n][d][lane];
+      double dG = (double)s[0] - s[1], ends = 0;
 #pragma unroll
       for (int d = 1; d < BLOCK; d *= 2) {
         const double after = __shfl_down(dG, d, BLOCK);
-        if (tid + d < BLOCK) dG += after;
-        total += __shfl_xor(total, d, BLOCK);
+        if (lane + d < BLOCK) dG += after;
       }
 #pragma unroll
       for (int w = 0; w < WAVES; w++) ends += (double)inner[w];
-      total += (double)since[BLOCK - 1] * ends;
-      const int64_t at = ((int64_t)b * a.length + t0 + tid) * a.heads + h;
-      if (tid < here) {
-        if (a.dg) a.dg[at] = tid < live ? (float)(dG + total) : 0.f;
-        a.dbeta[at] = tid < live ? (float)(dot_v[tid] - s[2]) : 0.f;
+      const double total = (double)lane_sum<BLOCK>(s[3]) + whole * ends;
+      const int64_t at = ((int64_t)b * a.length + t0 + lane) * a.heads + h;
+      if (lane < here) {
+        if (a.dg) a.dg[at] = lane < live ? (float)(dG + total) : 0.f;
+        a.dbeta[at] = lane < live ? (float)(dot_v[lane] - s[2]) : 0.f;
       }
     }
   }
