@@ -32,6 +32,8 @@
 // of sums in 64 bits, so a token that forgets everything costs the later ones nothing.
 #pragma once
 
+#include <algorithm>
+
 #include "ops_internal.h"
 
 namespace rcdelta {
@@ -219,6 +221,10 @@ __host__ __device__ inline int columns_of(int value) { return (value + 31) / 32 
 struct DeltaParams {
   rc_delta_args a;
   int32_t chunks, blocks;
+  int32_t segments, segment;                          // of the length; chunks of one
+  float* between;                                     // [batch][heads][segments][rows(key)][rows(key)]
+  float* ends;                                        // [batch][heads][segments][columns(value)][rows(key)]
+  float* starts;
   Chunk* prepared;                                    // [batch][heads][chunks]
   float* states;
   float* written;                                     // w, or dR
@@ -354,6 +360,13 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
 
 // Column `col` of a head's state from row `first` on: tile m has this lane's rows
 // 16m + 4 (lane / 16) + 0..3.
+// Column `col` of a kept state (below).
+template <int TILES>
+__device__ __forceinline__ void load_kept(const float* from, int rows, int col, int first, f32x4 (&S)[TILES]) {
+  const float* at = from + col * rows + first + threadIdx.x % 64 / 16 * 4;
+#pragma unroll
+  for (int m = 0; m < TILES; m++) S[m] = *(const f32x4*)(at + 16 * m);
+}
 template <int TILES>
 __device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col, int first,
                                            f32x4 (&S)[TILES]) {
@@ -508,26 +521,41 @@ __device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {
   return {{x[0][lane], x[1][lane], x[2][lane]}};
 }
 
+// What a walk is for: everything, or (where the length is cut) what a segment makes of the state before
+// it: ENDS from no state, with the values' columns, and from a state of ones on the diagonal, without
+// values, so that S' = between S + ends.
+enum { kWhole = 0, kEnds = 1 };
+
 // A walk's place.  Workgroups of one head are as many apart as there are heads, so
 // that most share one of the eight caches.
-template <class G>
+template <class G, int MODE>
 struct Walk {
-  int b, h, hk, bh, col0, col, row, end, chunks, wave, part;
-  bool on;
-  __device__ Walk(const rc_delta_args& a) {
+  int b, h, hk, bh, col0, col, row, end, wave, part;
+  int segment, first, count;                           // chunks of this segment
+  bool on, diagonal, last;                             // last: the segment of the sequence's end
+  __device__ Walk(const DeltaParams& p, int rows) {
+    const rc_delta_args& a = p.a;
     const int heads = a.batch * a.heads, lane = threadIdx.x % 64;
+    const int values = (a.value + G::COLUMNS - 1) / G::COLUMNS;
+    const int slices = values + (MODE == kEnds ? (rows + G::COLUMNS - 1) / G::COLUMNS : 0);
     bh = blockIdx.x % heads;
+    const int slice = blockIdx.x / heads % slices;
+    segment = blockIdx.x / heads / slices;
     b = bh / a.heads;
     h = bh % a.heads;
     hk = h / (a.heads / a.key_heads);
     wave = threadIdx.x / 64 % G::W;
     part = threadIdx.x / 64 / G::W;
-    col0 = blockIdx.x / heads * G::COLUMNS;
+    diagonal = slice >= values;
+    col0 = (diagonal ? slice - values : slice) * G::COLUMNS;
     col = col0 + wave * 16 + lane % 16;
     row = lane / 16 * 4;
-    on = col < a.value;
+    on = col < (diagonal ? rows : a.value);
     end = length_of(a, b);
-    chunks = (end + kChunk - 1) / kChunk;
+    const int chunks = (end + kChunk - 1) / kChunk;
+    first = segment * p.segment;
+    count = min(max(chunks - first, 0), p.segment);
+    last = segment == (chunks ? (chunks - 1) / p.segment : 0);
   }
 };
 
@@ -535,33 +563,34 @@ struct Walk {
 // by chunk as the working waves go, one chunk ahead of them in LDS where it holds two and
 // one more in registers.  A chunk has two barriers: at its start, and between the parts'
 // writes and reads of their sums over the key (Parts); with one stage a third at its end.
-template <class T, int KT, class G, bool WIDE, bool BACK>
-__device__ __forceinline__ void load_chunks(const DeltaParams& p, const Walk<G>& at, const rc_heads& values,
+template <class T, int KT, class G, bool WIDE, bool BACK, int MODE>
+__device__ __forceinline__ void load_chunks(const DeltaParams& p, const Walk<G, MODE>& at, const rc_heads& values,
                                             Stage<T, KT, G>* stages) {
   constexpr int STAGES = kStages<T, KT, G>;
   const rc_delta_args& a = p.a;
-  if (!at.chunks) return;
+  if (!at.count) return;
   const Chunk* prepared = p.prepared + (int64_t)at.bh * p.chunks;
+  const int columns = at.diagonal ? 0 : a.value;       // of values: a walk from the diagonal has none
   Feed<T, KT, G, WIDE> next;
-  const auto chunk_of = [&](int i) { return BACK ? at.chunks - 1 - i : i; };
+  const auto chunk_of = [&](int i) { return at.first + (BACK ? at.count - 1 - i : i); };
   const auto live_of = [&](int c) { return min(at.end - c * kChunk, kChunk); };
   const auto fetch = [&](int i) {
-    const int c = chunk_of(min(i, at.chunks - 1));
+    const int c = chunk_of(min(i, at.count - 1));
     next.fetch(a, prepared[c], values, at.b, at.h, at.hk, c * kChunk, live_of(c), at.col0);
   };
   const auto put = [&](int i) {
-    next.put(stages[i % STAGES], live_of(chunk_of(i)), a.key, a.value, at.col0);
+    next.put(stages[i % STAGES], live_of(chunk_of(i)), a.key, columns, at.col0);
     fetch(i + 1);
   };
   fetch(0);
   put(0);
-  for (int i = 0; i < at.chunks; i++) {
+  for (int i = 0; i < at.count; i++) {
     __syncthreads();
-    if (STAGES == 2 && i + 1 < at.chunks) put(i + 1);
+    if (STAGES == 2 && i + 1 < at.count) put(i + 1);
     if (G::R > 1) __syncthreads();
     if (STAGES == 1) {
       __syncthreads();
-      if (i + 1 < at.chunks) put(i + 1);
+      if (i + 1 < at.count) put(i + 1);
     }
   }
 }
@@ -581,6 +610,88 @@ struct Parts {
 };
 template <class G>
 struct Parts<G, 0> {};
+
+// What a walk of a segment begins with.
+template <int KT, int MODE, class G, int TILES>
+__device__ __forceinline__ void begin(const DeltaParams& p, const Walk<G, MODE>& at, const float* given, int first,
+                                      f32x4 (&S)[TILES]) {
+  const rc_delta_args& a = p.a;
+  if (MODE == kEnds) {
+#pragma unroll
+    for (int m = 0; m < TILES; m++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) S[m][r] = at.diagonal && first + 16 * m + at.row + r == at.col ? 1.f : 0.f;
+  } else if (p.segments > 1) {
+    load_kept(p.starts + ((int64_t)at.bh * p.segments + at.segment) * columns_of(a.value) * (32 * KT), 32 * KT,
+              min(at.col, columns_of(a.value) - 1), first, S);
+  } else {
+    load_state(given ? given + (int64_t)at.bh * a.key * a.value : nullptr, a, at.col, first, S);
+  }
+}
+// What a walk of kEnds leaves: columns of `ends` or, row by row, of `between`.
+template <int KT, class G, int TILES>
+__device__ __forceinline__ void leave(const DeltaParams& p, const Walk<G, kEnds>& at, int first,
+                                      const f32x4 (&S)[TILES]) {
+  constexpr int ROWS = 32 * KT;
+  const int64_t segment = (int64_t)at.bh * p.segments + at.segment;
+  if (!at.diagonal) {
+    if (at.col < columns_of(p.a.value))
+      keep_state(p.ends + segment * columns_of(p.a.value) * ROWS, ROWS, at.col, first, S);
+  } else if (at.on) {
+    float* to = p.between + segment * ROWS * ROWS + at.col;
+#pragma unroll
+    for (int m = 0; m < TILES; m++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) to[(first + 16 * m + at.row + r) * ROWS] = S[m][r];
+  }
+}
+
+// The states between segments, one after the other: S' = between S + ends (BACK: from the last
+// to the first).  A workgroup has 16 columns of a head, each of its waves some of the
+// rows; the state is between them in LDS as an operand.
+template <int KT, bool BACK>
+__global__ __launch_bounds__(256) void k_delta_join(DeltaParams p) {
+  const rc_delta_args& a = p.a;
+  constexpr int ROWS = 32 * KT, TILES = (2 * KT + 3) / 4;
+  __shared__ bf16x8 state[2][KT][3][64];
+  const int heads = a.batch * a.heads, bh = blockIdx.x % heads, lane = threadIdx.x % 64;
+  const int cols = columns_of(a.value), col = blockIdx.x / heads * 16 + lane % 16, row = lane / 16 * 4;
+  const int tile = threadIdx.x / 64 * TILES;
+  const bool mine = tile < 2 * KT;
+  const int chunks = (length_of(a, bh / a.heads) + kChunk - 1) / kChunk;
+  const int last = chunks ? (chunks - 1) / p.segment : 0;
+  const float* given = BACK ? a.dstate_out : a.state_in;
+  f32x4 S[TILES];
+  load_state(given ? given + (int64_t)bh * a.key * a.value : nullptr, a, col, 16 * tile, S);
+  for (int i = 0; i <= last; i++) {
+    const int64_t at = (int64_t)bh * p.segments + (BACK ? last - i : i);
+    if (mine) keep_state(p.starts + at * cols * ROWS, ROWS, col, 16 * tile, S);
+    if (i == last) break;
+    if (mine) {
+#pragma unroll
+      for (int m = 0; m < TILES; m++) {
+        const Pieces<3> s = operand<3>(S[m], S[m]);
+#pragma unroll
+        for (int j = 0; j < 3; j++)
+          *((bf16x4*)&state[i % 2][(tile + m) / 2][j][lane] + (tile + m) % 2) = s.p[j].lo;
+      }
+    }
+    __syncthreads();
+    if (mine) {
+      load_kept(p.ends + at * cols * ROWS, ROWS, col, 16 * tile, S);
+#pragma unroll
+      for (int m = 0; m < TILES; m++)
+#pragma unroll
+        for (int s = 0; s < KT; s++) {
+          const float* from = p.between + (at * ROWS + 16 * (tile + m) + lane % 16) * ROWS + 32 * s + row;
+          const Pieces<3> b = operand<3>(*(const f32x4*)from, *(const f32x4*)(from + 16));
+          const Pieces<3> c = {
+              {state[i % 2][s][0][lane], state[i % 2][s][1][lane], state[i % 2][s][2][lane]}};
+          mul(S[m], b, c);
+        }
+    }
+  }
+}
 
 // ------------------------------------------------------------------ host side
 
@@ -626,9 +737,21 @@ inline int fits(const rc_delta_args& a) {
     return RC_E_OVERFLOW;
   return RC_OK;
 }
+// Segments of the length: more than one where the workgroups of a walk leave compute units idle and
+// there are enough chunks for each.  Cutting costs a second walk, over the segments' ends, of values
+// and key columns, and a step a segment that joins them.
+inline int segments_of(const rc_delta_args& a) {
+  const int64_t walks = (int64_t)a.batch * a.heads * cdiv(a.value, 32), chunks = chunks_of(a);
+  if (walks > 96) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({chunks / 8, 512 / walks, 16}));
+}
+inline uint64_t segment_floats(const rc_delta_args& a) {
+  const int n = segments_of(a), rows = rows_of(a.key);
+  return n == 1 ? 0 : (uint64_t)a.batch * a.heads * n * rows * (rows + 2 * columns_of(a.value));
+}
 inline uint64_t workspace_of(const rc_delta_args& a, bool back) {
   if (empty(a)) return 0;
-  uint64_t n = (uint64_t)pairs_of(a) * sizeof(Chunk);
+  uint64_t n = (uint64_t)pairs_of(a) * sizeof(Chunk) + segment_floats(a) * sizeof(float);
   if (back) {
     n += kept_bytes(a);
     const int per = a.heads / a.key_heads, each = heads_together(a);
@@ -658,6 +781,13 @@ inline DeltaParams params(const rc_delta_args& a) {
   p.blocks = (int32_t)blocks_of(a);
   p.prepared = static_cast<Chunk*>(a.workspace);
   p.states = a.kept;
+  p.segment = (int32_t)cdiv(p.chunks, segments_of(a));
+  p.segments = p.chunks ? (int32_t)cdiv(p.chunks, p.segment) : 1;
+  p.segment = std::max(p.segment, 1);
+  const int64_t n = (int64_t)a.batch * a.heads * p.segments * rows_of(a.key);
+  p.between = reinterpret_cast<float*>(p.prepared + pairs_of(a));
+  p.ends = p.between + n * rows_of(a.key);
+  p.starts = p.ends + n * columns_of(a.value);
   return p;
 }
 
@@ -668,9 +798,16 @@ inline int prepare(const DeltaParams& p, hipStream_t s) {
   return launched("k_delta_prepare");
 }
 // Workgroups of a walk.
-template <class G>
-inline unsigned walks_of(const rc_delta_args& a) {
-  return (unsigned)((int64_t)a.batch * a.heads * cdiv(a.value, G::COLUMNS));
+template <class G, int MODE>
+inline unsigned walks_of(const DeltaParams& p, int rows) {
+  const int64_t slices = cdiv(p.a.value, G::COLUMNS) + (MODE == kEnds ? cdiv(rows, G::COLUMNS) : 0);
+  return (unsigned)((int64_t)p.a.batch * p.a.heads * slices * p.segments);
+}
+template <int KT, bool BACK>
+inline int join(const DeltaParams& p, hipStream_t s) {
+  k_delta_join<KT, BACK>
+      <<<(unsigned)((int64_t)p.a.batch * p.a.heads * (columns_of(p.a.value) / 16)), 256, 0, s>>>(p);
+  return launched("k_delta_join");
 }
 // The shape of a walk's workgroups.
 template <int KT>

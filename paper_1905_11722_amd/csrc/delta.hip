@@ -9,26 +9,27 @@ namespace {
 // in registers from the first chunk to the last.  Columns do not depend on one
 // another, and what a product leaves in a lane is what the next one takes from it, so waves share
 // the tokens in LDS, and the parts their sums over the key.
-template <class T, int KT, class G, bool WIDE>
+template <class T, int KT, class G, bool WIDE, int MODE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
   constexpr int EVERY = block_of(kPieces<T>, 32 * KT) / kChunk;
   __shared__ Stage<T, KT, G> stages[STAGES];
   __shared__ Parts<G, G::R == 1 ? 0 : 4> parts;
-  const Walk<G> at(a);
+  const Walk<G, MODE> at(p, 32 * KT);
   const int end = at.end, row = at.row, first_row = at.part * STEPS * 32, lane = threadIdx.x % 64;
-  const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
-  const bool keeps = at.col < columns_of(a.value);
+  const int64_t first = (int64_t)at.bh * p.chunks;
+  const bool keeps = MODE == kWhole && at.col < columns_of(a.value);
+  if (MODE == kEnds && (!at.count || at.last)) return;             // no segment goes on from it
   if (threadIdx.x >= G::WORKERS) {
-    load_chunks<T, KT, G, WIDE, false>(p, at, a.v, stages);
+    load_chunks<T, KT, G, WIDE, false, MODE>(p, at, a.v, stages);
     return;
   }
   f32x4 S[2 * STEPS];
-  load_state(a.state_in ? a.state_in + at.bh * size : nullptr, a, at.col, first_row, S);
-  for (int chunk = 0; chunk < at.chunks; chunk++) {
-    const int t0 = chunk * kChunk, live = min(end - t0, kChunk);
-    const auto& stage = stages[chunk % STAGES];
+  begin<KT, MODE>(p, at, a.state_in, first_row, S);
+  for (int i = 0; i < at.count; i++) {
+    const int chunk = at.first + i, t0 = chunk * kChunk, live = min(end - t0, kChunk);
+    const auto& stage = stages[i % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
     if (p.states && keeps && chunk % EVERY == 0)
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
       for (int m = 0; m < 2; m++) parts.at[m][at.part][at.wave][lane] = r[m];
     }
 #pragma unroll
-    for (int s = 0; s < STEPS; s++)
+    for (int s = 0; s < (MODE == kWhole ? STEPS : 0); s++)
 #pragma unroll
       for (int m = 0; m < 2; m++) mul(out[m], stage.q.rows(m, at.part * STEPS + s), state[s]);
     // read before the barrier, which nothing is moved over
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     const Pieces<3> t[2] = {pieces(c.t[0]), pieces(c.t[1])};
     if constexpr (G::R > 1) {
 #pragma unroll
-      for (int m = 0; m < 2; m++) parts.at[2 + m][at.part][at.wave][lane] = out[m];
+      for (int m = 0; m < (MODE == kWhole ? 2 : 0); m++) parts.at[2 + m][at.part][at.wave][lane] = out[m];
       __syncthreads();
 #pragma unroll
       for (int m = 0; m < 2; m++) r[m] = parts.sum(m, at.wave);
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     // outputs: tile m by part m
     const Pieces<3> ws = operand<3>(w[0], w[1]);
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
+    for (int m = 0; m < (MODE == kWhole ? 2 : 0); m++) {
       if (G::R > 1 && at.part != m) continue;
       if constexpr (G::R > 1) out[m] = parts.sum(2 + m, at.wave);
       out[m] *= a.scale * since[m];
@@ -106,10 +107,15 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     }
     if (STAGES == 1) __syncthreads();
   }
-  if (a.state_out) store_state(a.state_out + at.bh * size, a, at.col, first_row, S);
-  if (at.on && at.part == 0) {
-    T* o = at_head<T>(a.o, at.b, 0, at.h) + at.col;
-    for (int t = end + row / 4; t < a.length; t += 4) o[t * a.o.time] = (T)0.f;
+  if constexpr (MODE == kEnds) {
+    leave<KT>(p, at, first_row, S);
+  } else if (at.last) {
+    if (a.state_out)
+      store_state(a.state_out + (int64_t)at.bh * a.key * a.value, a, at.col, first_row, S);
+    if (at.on && at.part == 0) {
+      T* o = at_head<T>(a.o, at.b, 0, at.h) + at.col;
+      for (int t = end + row / 4; t < a.length; t += 4) o[t * a.o.time] = (T)0.f;
+    }
   }
 }
 
@@ -241,7 +247,13 @@ extern "C" int rc_delta_forward(const rc_delta_args* args, void* stream) {
       if (int e = prepare<T, KT, false>(p, s)) return e;
       return by_width(a, [&](auto wide) {
         using G = ShapeOf<KT>;
-        k_delta_forward<T, KT, G, decltype(wide)::value><<<walks_of<G>(a), G::THREADS, 0, s>>>(p);
+        constexpr bool WIDE = decltype(wide)::value;
+        if (p.segments > 1) {
+          k_delta_forward<T, KT, G, WIDE, kEnds><<<walks_of<G, kEnds>(p, 32 * KT), G::THREADS, 0, s>>>(p);
+          if (int e = launched("k_delta_forward")) return e;
+          if (int e = join<KT, false>(p, s)) return e;
+        }
+        k_delta_forward<T, KT, G, WIDE, kWhole><<<walks_of<G, kWhole>(p, 0), G::THREADS, 0, s>>>(p);
         return launched("k_delta_forward");
       });
     });

@@ -6,29 +6,31 @@ using namespace rcdelta;
 namespace {
 
 // Backward through the states, from the last chunk to the first, as k_delta_forward goes.
-template <class T, int KT, class G, bool WIDE>
+template <class T, int KT, class G, bool WIDE, int MODE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>, STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
   constexpr int EVERY = block_of(N, 32 * KT) / kChunk;
   __shared__ Stage<T, KT, G> stages[STAGES];
   __shared__ Parts<G, G::R == 1 ? 0 : 2> parts;
-  const Walk<G> at(a);
+  const Walk<G, MODE> at(p, 32 * KT);
   const int end = at.end, row = at.row, first_row = at.part * STEPS * 32, lane = threadIdx.x % 64;
-  const int64_t size = (int64_t)a.key * a.value, first = (int64_t)at.bh * p.chunks;
-  const bool keeps = at.col < columns_of(a.value);
+  const int64_t first = (int64_t)at.bh * p.chunks;
+  const bool keeps = MODE == kWhole && at.col < columns_of(a.value);
+  const int last_chunk = (end + kChunk - 1) / kChunk - 1;
+  if (MODE == kEnds && (!at.count || at.segment == 0)) return;     // no segment goes on from it
   if (threadIdx.x >= G::WORKERS) {
-    load_chunks<T, KT, G, WIDE, true>(p, at, a.do_, stages);
+    load_chunks<T, KT, G, WIDE, true, MODE>(p, at, a.do_, stages);
     return;
   }
   f32x4 E[2 * STEPS];
-  load_state(a.dstate_out ? a.dstate_out + at.bh * size : nullptr, a, at.col, first_row, E);
-  for (int i = 0; i < at.chunks; i++) {
-    const int chunk = at.chunks - 1 - i, t0 = chunk * kChunk, live = min(end - t0, kChunk);
+  begin<KT, MODE>(p, at, a.dstate_out, first_row, E);
+  for (int i = 0; i < at.count; i++) {
+    const int chunk = at.first + at.count - 1 - i, t0 = chunk * kChunk, live = min(end - t0, kChunk);
     const auto& stage = stages[i % STAGES];
     __syncthreads();
     const Chunk& c = stage.c;
-    if (keeps && (i == 0 || chunk % EVERY == EVERY - 1))
+    if (keeps && (chunk == last_chunk || chunk % EVERY == EVERY - 1))
       keep_state(p.dstates + ((int64_t)at.bh * p.blocks + chunk / EVERY) * (columns_of(a.value) * 32 * KT),
                  32 * KT, at.col, first_row, E);
     f32x4 dw[2], dr[2], g[2];
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
 #pragma unroll
     for (int m = 0; m < 2 * STEPS; m++) mul(E[m], stage.k.columns(at.part * 2 * STEPS + m), drs);
 #pragma unroll
-    for (int m = 0; m < 2; m++) {
+    for (int m = 0; m < (MODE == kWhole ? 2 : 0); m++) {
       if (G::R > 1 && at.part != m) continue;          // outputs: tile m by part m
       if (keeps)
         *(f32x4*)(p.written + ((first + chunk) * columns_of(a.value) + at.col) * kChunk + 16 * m + row) = dr[m];
@@ -99,10 +101,15 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
     }
     if (STAGES == 1) __syncthreads();
   }
-  if (a.dstate_in) store_state(a.dstate_in + at.bh * size, a, at.col, first_row, E);
-  if (at.on && at.part == 0) {
-    T* dv = at_head<T>(a.dv, at.b, 0, at.h) + at.col;
-    for (int t = end + row / 4; t < a.length; t += 4) dv[t * a.dv.time] = (T)0.f;
+  if constexpr (MODE == kEnds) {
+    leave<KT>(p, at, first_row, E);
+  } else {
+    if (a.dstate_in && at.segment == 0)
+      store_state(a.dstate_in + (int64_t)at.bh * a.key * a.value, a, at.col, first_row, E);
+    if (at.on && at.part == 0 && at.last) {
+      T* dv = at_head<T>(a.dv, at.b, 0, at.h) + at.col;
+      for (int t = end + row / 4; t < a.length; t += 4) dv[t * a.dv.time] = (T)0.f;
+    }
   }
 }
 
@@ -511,7 +518,7 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
   const int64_t pairs = pairs_of(a);
   p.each = heads_together(a);
   p.kept_written = a.kept + state_floats(a);
-  p.dstates = reinterpret_cast<float*>(p.prepared + pairs);
+  p.dstates = p.between + segment_floats(a);
   p.written = p.dstates + state_floats(a);
   p.partial = p.written + pairs * columns_of(a.value) * kChunk;
   return by_dtype(a.dtype, [&](auto t) {
@@ -521,7 +528,13 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
       if (int e = prepare<T, KT, true>(p, s)) return e;
       const int e = by_width(a, [&](auto wide) {
         using G = ShapeOf<KT>;
-        k_delta_states_back<T, KT, G, decltype(wide)::value><<<walks_of<G>(a), G::THREADS, 0, s>>>(p);
+        constexpr bool WIDE = decltype(wide)::value;
+        if (p.segments > 1) {
+          k_delta_states_back<T, KT, G, WIDE, kEnds><<<walks_of<G, kEnds>(p, 32 * KT), G::THREADS, 0, s>>>(p);
+          if (int e = launched("k_delta_states_back")) return e;
+          if (int e = join<KT, true>(p, s)) return e;
+        }
+        k_delta_states_back<T, KT, G, WIDE, kWhole><<<walks_of<G, kWhole>(p, 0), G::THREADS, 0, s>>>(p);
         return launched("k_delta_states_back");
       });
       if (e) return e;

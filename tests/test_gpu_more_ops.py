@@ -44,6 +44,12 @@ DELTA = [  # dtype, batch, length, key_heads, heads, key, value, parts (g, s: st
     ("bf16", 2, 130, 1, 4, 128, 96, "gs", (130, 97)),
     ("f32", 1, 200, 1, 1, 64, 15, "gs", None),
     ("f32", 3, 66, 1, 2, 40, 65, "gs", (0, 0, 66)),
+    # few heads and many chunks: the length is cut into segments
+    ("f32", 1, 700, 1, 1, 16, 8, "gs", None),
+    ("bf16", 2, 1100, 1, 2, 128, 64, "gs", (1100, 530)),
+    ("f16", 3, 600, 1, 1, 64, 33, "gs", (599, 0, 1)),
+    ("bf16", 1, 1290, 1, 1, 200, 40, "g", (1285,)),
+    ("f32", 1, 530, 1, 2, 96, 100, "gs", None),
 ]
 
 
