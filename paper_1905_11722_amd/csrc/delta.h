@@ -676,6 +676,20 @@ __global__ __launch_bounds__(256) void k_delta_join(DeltaParams p) {
           *((bf16x4*)&state[i % 2][(tile + m) / 2][j][lane] + (tile + m) % 2) = s.p[j].lo;
       }
     }
+    // loads that do not wait for the state (of the widest keys there are too many to hold)
+    f32x4 between[TILES][KT][2];
+    const auto load = [&](int m, int s) {
+      const float* from =
+          p.between + (at * ROWS + 16 * min(tile + m, 2 * KT - 1) + lane % 16) * ROWS + 32 * s + row;
+      between[m][s][0] = *(const f32x4*)from;
+      between[m][s][1] = *(const f32x4*)(from + 16);
+    };
+    if (KT <= 4) {
+#pragma unroll
+      for (int m = 0; m < TILES; m++)
+#pragma unroll
+        for (int s = 0; s < KT; s++) load(m, s);
+    }
     __syncthreads();
     if (mine) {
       load_kept(p.ends + at * cols * ROWS, ROWS, col, 16 * tile, S);
@@ -683,11 +697,10 @@ __global__ __launch_bounds__(256) void k_delta_join(DeltaParams p) {
       for (int m = 0; m < TILES; m++)
 #pragma unroll
         for (int s = 0; s < KT; s++) {
-          const float* from = p.between + (at * ROWS + 16 * (tile + m) + lane % 16) * ROWS + 32 * s + row;
-          const Pieces<3> b = operand<3>(*(const f32x4*)from, *(const f32x4*)(from + 16));
+          if (KT > 4) load(m, s);
           const Pieces<3> c = {
               {state[i % 2][s][0][lane], state[i % 2][s][1][lane], state[i % 2][s][2][lane]}};
-          mul(S[m], b, c);
+          mul(S[m], operand<3>(between[m][s][0], between[m][s][1]), c);
         }
     }
   }
@@ -737,13 +750,19 @@ inline int fits(const rc_delta_args& a) {
     return RC_E_OVERFLOW;
   return RC_OK;
 }
-// Segments of the length: more than one where the workgroups of a walk leave compute units idle and
-// there are enough chunks for each.  Cutting costs a second walk, over the segments' ends, of values
-// and key columns, and a step a segment that joins them.
+// Segments of the length: more than one where the walks over the segments' ends (of values' and
+// key columns, one segment fewer) fit the compute units at once and each segment has eight chunks
+// (sixteen of the widest keys, whose joins take longer).  Cutting costs those walks, and a
+// step a segment that joins them: with fewer than three segments it never gained.
+// 8192 tokens of 128 x 128, 16, 8, 4 heads and one: 452, 430, 427, 423 us in one, in 3, 5, 8 and 16
+// segments 311, 203, 148, 125; 2048 tokens of 16 and 4 heads: 123, 119 us, in 3 and 8 segments
+// 104, 73; 2 x 16 heads 130, in 3 segments 177.
 inline int segments_of(const rc_delta_args& a) {
-  const int64_t walks = (int64_t)a.batch * a.heads * cdiv(a.value, 32), chunks = chunks_of(a);
-  if (walks > 96) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({chunks / 8, 512 / walks, 16}));
+  const int rows = rows_of(a.key);
+  const int64_t walks = (int64_t)a.batch * a.heads * (cdiv(a.value, 32) + rows / 32);
+  const int64_t fit = 1 + (rows <= 64 ? 512 : 256) / walks, most = chunks_of(a) / (rows > 128 ? 16 : 8);
+  const int64_t n = std::min<int64_t>({fit, most, 16});
+  return n < 3 ? 1 : (int)n;
 }
 inline uint64_t segment_floats(const rc_delta_args& a) {
   const int n = segments_of(a), rows = rows_of(a.key);
