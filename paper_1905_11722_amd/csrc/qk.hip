@@ -96,6 +96,23 @@ __device__ __forceinline__ void load_unit(const T* row, const Unit& u, bool on, 
 #pragma unroll
   for (int i = 0; i < 2; i++) load_vec<kPairs>(row + (u.n[i] ? u.c[i] : 0), on ? u.n[i] : 0, x[i]);
 }
+// The same as T, whole loads at addresses inside the row: what is past a unit's channels, or
+// not `on`, is dropped by `values`.  (A row shorter than a load is loaded one by one.)
+template <class T>
+struct Raw {
+  typedef T TV __attribute__((ext_vector_type(kPairs)));
+  TV v[2];
+  __device__ void load(const T* row, const Unit& u, int channels) {
+#pragma unroll
+    for (int i = 0; i < 2; i++) __builtin_memcpy(&v[i], row + min(u.c[i], channels - kPairs), sizeof(TV));
+  }
+  __device__ void values(const Unit& u, bool on, float (&x)[2][kPairs]) const {
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+      for (int e = 0; e < kPairs; e++) x[i][e] = on && e < u.n[i] ? (float)v[i][e] : 0.f;
+  }
+};
 template <class T>
 __device__ __forceinline__ void store_unit(T* row, const Unit& u, const float (&x)[2][kPairs]) {
 #pragma unroll
@@ -130,7 +147,8 @@ struct Place {
   }
 };
 
-template <class T, int L>
+// AHEAD: every unit is whole loads, and the next head's are in flight during this one's work.
+template <class T, int L, bool AHEAD>
 __global__ __launch_bounds__(kThreads) void k_qk_forward(QkParams p) {
   const rc_qk_args& a = p.a;
   const Place at(p);
@@ -144,11 +162,18 @@ __global__ __launch_bounds__(kThreads) void k_qk_forward(QkParams p) {
        i += (int64_t)p.blocks * (kThreads / L)) {
     const int b = (int)(i / a.length), t = (int)(i % a.length);
     const bool live = !a.lengths || t < a.lengths[b];
+    Raw<T> next;
+    if (AHEAD) next.load(at_head<T>(in, b, t, at.first), u, a.channels);
     float cos[kPairs], sin[kPairs];
     angles(a, u, b, t, cos, sin);
     for (int h = at.first; h < at.last; h++) {
       float x[2][kPairs], s = 0.f;
-      load_unit(at_head<T>(in, b, t, h), u, live, x);
+      if (AHEAD) {
+        next.values(u, live, x);
+        next.load(at_head<T>(in, b, t, min(h + 1, at.last - 1)), u, a.channels);
+      } else {
+        load_unit(at_head<T>(in, b, t, h), u, live, x);
+      }
 #pragma unroll
       for (int j = 0; j < 2 * kPairs; j++) s = fmaf(x[j / kPairs][j % kPairs], x[j / kPairs][j % kPairs], s);
       const float r = norm_of(a, lane_sum<L>(s));
@@ -165,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void k_qk_forward(QkParams p) {
   }
 }
 
-template <class T, int L>
+template <class T, int L, bool AHEAD>
 __global__ __launch_bounds__(kThreads) void k_qk_backward(QkParams p) {
   const rc_qk_args& a = p.a;
   __shared__ float sums[kThreads][2 * kPairs];
@@ -183,12 +208,25 @@ __global__ __launch_bounds__(kThreads) void k_qk_backward(QkParams p) {
        i += (int64_t)p.blocks * (kThreads / L)) {
     const int b = (int)(i / a.length), t = (int)(i % a.length);
     const bool live = !a.lengths || t < a.lengths[b];
+    const rc_heads& given = dout.data ? dout : in;
+    Raw<T> next_x, next_e;
+    if (AHEAD) {
+      next_x.load(at_head<T>(in, b, t, at.first), u, a.channels);
+      next_e.load(at_head<T>(given, b, t, at.first), u, a.channels);
+    }
     float cos[kPairs], sin[kPairs];
     angles(a, u, b, t, cos, sin);
     for (int h = at.first; h < at.last; h++) {
       float x[2][kPairs], e[2][kPairs], s = 0.f, d = 0.f;
-      load_unit(at_head<T>(in, b, t, h), u, live, x);
-      load_unit(at_head<T>(dout.data ? dout : in, b, t, h), u, live && dout.data, e);
+      if (AHEAD) {
+        next_x.values(u, live, x);
+        next_e.values(u, live && dout.data, e);
+        next_x.load(at_head<T>(in, b, t, min(h + 1, at.last - 1)), u, a.channels);
+        next_e.load(at_head<T>(given, b, t, min(h + 1, at.last - 1)), u, a.channels);
+      } else {
+        load_unit(at_head<T>(in, b, t, h), u, live, x);
+        load_unit(at_head<T>(given, b, t, h), u, live && dout.data, e);
+      }
       turn(a.interleaved, true, cos, sin, e);
 #pragma unroll
       for (int j = 0; j < 2 * kPairs; j++) {
@@ -286,6 +324,12 @@ uint64_t workspace_of(const QkParams& p) {
   return (uint64_t)p.blocks * (p.groups[0] + p.groups[1]) * p.a.channels * sizeof(float);
 }
 
+// Whether every unit that has channels has whole loads of them.
+bool whole_units(const rc_qk_args& a) {
+  return a.channels >= kPairs && a.channels % kPairs == 0 &&
+         a.rotated % (a.interleaved ? kPairs : 2 * kPairs) == 0;
+}
+
 template <class F>
 int by_lanes(int l, F&& f) {
   if (l <= 2) return f(std::integral_constant<int, 2>{});
@@ -307,8 +351,13 @@ extern "C" int rc_qk_forward(const rc_qk_args* args, void* stream) {
   if (int e = plan(a, false, &p)) return e;
   const unsigned grid = (unsigned)p.blocks * (p.groups[0] + p.groups[1]);
   return by_dtype(a.dtype, [&](auto t) {
+    using T = decltype(t);
     return by_lanes(lanes_of(a), [&](auto l) {
-      k_qk_forward<decltype(t), decltype(l)::value><<<grid, kThreads, 0, (hipStream_t)stream>>>(p);
+      constexpr int L = decltype(l)::value;
+      if (whole_units(a))
+        k_qk_forward<T, L, true><<<grid, kThreads, 0, (hipStream_t)stream>>>(p);
+      else
+        k_qk_forward<T, L, false><<<grid, kThreads, 0, (hipStream_t)stream>>>(p);
       return launched("k_qk_forward");
     });
   });
@@ -348,7 +397,11 @@ extern "C" int rc_qk_backward(const rc_qk_args* args, void* stream) {
     using T = decltype(t);
     if (grid) {
       const int e = by_lanes(lanes_of(a), [&](auto l) {
-        k_qk_backward<T, decltype(l)::value><<<grid, kThreads, 0, s>>>(p);
+        constexpr int L = decltype(l)::value;
+        if (whole_units(a))
+          k_qk_backward<T, L, true><<<grid, kThreads, 0, s>>>(p);
+        else
+          k_qk_backward<T, L, false><<<grid, kThreads, 0, s>>>(p);
         return launched("k_qk_backward");
       });
       if (e) return e;
