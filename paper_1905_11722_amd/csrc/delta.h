@@ -116,13 +116,27 @@ __device__ __forceinline__ float decay_between(double x) {
   return fast_exp2((float)(x * 1.44269504088896340736));
 }
 
-// ROWS rows (tokens) of `32 KT` channels in LDS as pieces.  Within each 32 channels, groups of four
-// are ordered 0 4 1 5 2 6 3 7, so that a lane's operand (above) is 16 bytes.
-template <int KT, int N, int ROWS = kChunk>
-struct Tokens {
-  static constexpr int STRIDE = KT * 32 + 8;
-  bf16 at[N][ROWS][STRIDE];
+// Elements between rows of `channels` (a multiple of 32) in LDS, 16-byte aligned.  In order: neither
+// reads of 16 rows (8 bytes each) nor transposing reads of four rows (32 bytes each) meet in one of 64
+// banks.  Paired: reads of eight rows (16 bytes each) do not, transposing ones hardly.  Three pieces
+// leave no room for that: only reads of rows do not meet.
+constexpr int stride_of(int channels, int pieces, bool paired) {
+  if (paired) return channels + (channels == 32 || pieces == 3 ? 8 : 40);
+  return channels + (channels == 64 || pieces == 3 ? 8 : 24);
+}
 
+// ROWS rows (tokens) of `32 KT` channels in LDS as pieces.  PAIRED: within each 32 channels groups
+// of four are ordered 0 4 1 5 2 6 3 7, so that a lane's operand of a row is one read; for the
+// walks, that mostly read rows (168 us for a prompt of 8192 tokens in order, 158 so).
+template <int KT, int N, int ROWS = kChunk, bool PAIRED = false>
+struct Tokens {
+  static constexpr int STRIDE = stride_of(KT * 32, N, PAIRED);
+  alignas(16) bf16 at[N][ROWS][STRIDE];
+
+  // Where channel c of a row is.
+  __device__ static int place(int c) {
+    return PAIRED ? c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4 : c;
+  }
   // From rows `row` elements apart; what is past `live` tokens or `n` channels is 0.
   template <class T>
   __device__ void load(const T* x, int64_t row, int live, int n, int thread, int threads) {
@@ -135,20 +149,39 @@ struct Tokens {
   }
   __device__ void put(int r, int c, const float (&v)[8]) {
     const Pieces<N> s = split<N>(v);
-    bf16* to = &at[0][r][c / 32 * 32 + (c % 16 / 4) * 8 + c % 32 / 16 * 4];
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      *(bf16x4*)(to + i * (ROWS * STRIDE)) = s.p[i].lo;
-      *(bf16x4*)(to + i * (ROWS * STRIDE) + 8) = s.p[i].hi;
+    for (int i = 0; i < N; i++) put(i, r, c, s.p[i]);
+  }
+  // Eight channels of one piece, c a multiple of eight.
+  __device__ void put(int i, int r, int c, const bf16x8& v) {
+    if constexpr (PAIRED) {
+      *(bf16x4*)&at[i][r][place(c)] = v.lo;
+      *(bf16x4*)&at[i][r][place(c) + 8] = v.hi;
+    } else {
+      *(bf16x8*)&at[i][r][c] = v;
     }
   }
-  // Row tile t (tokens 16t + ..) over channels 32s + 0..31.
+  // Four channels of one row, c a multiple of four.
+  __device__ void put_four(int r, int c, const f32x4& x) {
+    const float v[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    const Pieces<N> s = split<N>(v);
+#pragma unroll
+    for (int i = 0; i < N; i++) *(bf16x4*)&at[i][r][place(c)] = s.p[i].lo;
+  }
+  // Row tile t (rows 16t + ..) over channels 32s + 0..31.
   __device__ Pieces<N> rows(int t, int s) const {
     const int lane = threadIdx.x % 64;
     Pieces<N> f;
 #pragma unroll
-    for (int i = 0; i < N; i++)
-      f.p[i] = *(const bf16x8*)&at[i][16 * t + lane % 16][32 * s + lane / 16 * 8];
+    for (int i = 0; i < N; i++) {
+      const bf16* from = &at[i][16 * t + lane % 16][32 * s + lane / 16 * (PAIRED ? 8 : 4)];
+      if constexpr (PAIRED) {
+        f.p[i] = *(const bf16x8*)from;
+      } else {
+        f.p[i].lo = *(const bf16x4*)from;
+        f.p[i].hi = *(const bf16x4*)(from + 16);
+      }
+    }
     return f;
   }
   // Channels 16t + .. over rows 32s + 0..31: reads that transpose four by four.
@@ -157,8 +190,7 @@ struct Tokens {
     Pieces<N> f;
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      const bf16* from =
-          &at[i][32 * s + lane / 16 * 4 + lane % 16 / 4][t / 2 * 32 + lane % 4 * 8 + t % 2 * 4];
+      const bf16* from = &at[i][32 * s + lane / 16 * 4 + lane % 16 / 4][place(16 * t + lane % 4 * 4)];
       typedef s16x4 __attribute__((address_space(3))) * lds;
       f.p[i].lo = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)from));
       f.p[i].hi = __builtin_bit_cast(
@@ -166,25 +198,10 @@ struct Tokens {
     }
     return f;
   }
-  // Four channels of one row, c a multiple of four.
-  __device__ void put_four(int r, int c, const f32x4& x) {
-    const float v[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
-    const Pieces<N> s = split<N>(v);
-    bf16* to = &at[0][r][c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4];
-#pragma unroll
-    for (int i = 0; i < N; i++) *(bf16x4*)(to + i * (ROWS * STRIDE)) = s.p[i].lo;
-  }
-  // Eight channels as they are where one piece is all.
-  __device__ void put(int r, int c, const bf16x8& v) {
-    bf16* to = &at[0][r][c / 32 * 32 + (c % 16 / 4) * 8 + c % 32 / 16 * 4];
-    *(bf16x4*)to = v.lo;
-    *(bf16x4*)(to + 8) = v.hi;
-  }
   __device__ float value(int r, int c) const {
-    const int at_c = c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4;
-    float x = (float)at[N - 1][r][at_c];
+    float x = (float)at[N - 1][r][place(c)];
 #pragma unroll
-    for (int i = N - 2; i >= 0; i--) x += (float)at[i][r][at_c];
+    for (int i = N - 2; i >= 0; i--) x += (float)at[i][r][place(c)];
     return x;
   }
 };
@@ -206,8 +223,8 @@ static_assert(sizeof(Chunk) % 16 == 0, "copied in vectors");
 // queries and products of tokens fit LDS and registers: half of the states to write, keep and read.
 // Bytes of LDS with the states' slices in it too, and without them.
 constexpr int block_bytes(int pieces, int rows, int block, bool held) {
-  return 2 * pieces * block * (rows + 8 + 40) * 2 + 2 * 3 * 32 * (block + 8) * 2 +
-         (held ? 2 * 3 * 32 * (rows + 8) * 2 : 0);
+  return 2 * pieces * block * (stride_of(rows, pieces, false) + stride_of(32, pieces, false)) * 2 +
+         2 * 3 * 32 * stride_of(block, 3, false) * 2 + (held ? 2 * 3 * 32 * stride_of(rows, 3, false) * 2 : 0);
 }
 constexpr int kBlockBytes = 150 * 1024;
 constexpr int block_of(int pieces, int rows) {
@@ -411,7 +428,7 @@ struct Shape {
 // gradients, of the workgroup's columns.
 template <class T, int KT, class G>
 struct Stage {
-  Tokens<KT, kPieces<T>> k, q;
+  Tokens<KT, kPieces<T>, kChunk, true> k, q;
   union {
     Chunk c;
     u32x4 raw[kChunkVectors];
@@ -420,7 +437,7 @@ struct Stage {
   __device__ Stage() {}
 };
 template <class T, int KT, class G>
-constexpr int kStages = 2 * sizeof(Stage<T, KT, G>) <= 160 * 1024 ? 2 : 1;
+constexpr int kStages = 2 * sizeof(Stage<T, KT, G>) + 16 * 1024 <= 160 * 1024 ? 2 : 1;    // (and Parts)
 // Workgroups a compute unit that a walk's registers are to leave room for: two waves a SIMD
 // (256 registers a lane), where LDS has it.  With 512 the accumulators go where only matrix
 // instructions reach them, and 180 of 1170 instructions of a chunk were moves.
@@ -491,8 +508,8 @@ struct Feed {
         mask(v, r, live, ch, key);
       }
       if constexpr (kPieces<T> == 1) {
-        to.k.put(r, ch, u);
-        to.q.put(r, ch, v);
+        to.k.put(0, r, ch, u);
+        to.q.put(0, r, ch, v);
       } else {
         float y[8], z[8];
 #pragma unroll
