@@ -7,10 +7,10 @@
 // S the state before it, and D_ij = exp(G_i - G_j) for j <= i,
 //   W = T R,   R_i = beta_i (v_i - exp(G_i) S^T k_i),
 //   T = (I + A)^-1,   A_ij = beta_i D_ij k_i . k_j   for j < i,
-//   O_i = scale exp(G_i) S^T q_i + sum_j P_ij w_j,   P_ij = scale D_ij q_i . k_j,
+//   O_i = scale exp(G_i) S^T q_i + sum_j (P T)_ij R_j,   P_ij = scale D_ij q_i . k_j,
 //   S' = exp(G_31) S + sum_j exp(G_31 - G_j) k_j w_j^T.
-// T and P need no state: k_delta_prepare computes them for all chunks at once, T by
-// forward substitution.  What is left of a chunk are five products of at most
+// T and P T need no state: k_delta_prepare computes them for all chunks at once, T by
+// forward substitution (P W is P T R: W need not be an operand).  What is left of a chunk are five products of at most
 // 32 x key x value, k_delta_forward's, one chunk after the other.
 //
 // Backward, with dO and the gradient E of S':
@@ -206,8 +206,8 @@ struct Tokens {
   }
 };
 
-// What k_delta_prepare leaves for one chunk of one head: T and P (backward: their
-// transposes) as operands of two row tiles, and numbers of each token.
+// What k_delta_prepare leaves for one chunk of one head: T and P T (backward: the transposes of
+// T and P) as operands of two row tiles, and numbers of each token.
 struct Chunk {
   bf16x8 t[2][3][64], p[2][3][64];
   float since[kChunk], left[kChunk], beta[kChunk];    // exp(G_i), exp(G_31 - G_i), beta_i
@@ -340,38 +340,70 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
         const int pi = BACK ? j : i, pj = BACK ? i : j;
         qk[m][n][r] = pj <= pi ? a.scale * decay_between(sums[pi] - sums[pj]) * qk[m][n][r] : 0.f;
       }
-#pragma unroll
-  for (int n = 0; n < 2; n++) {
-    const Pieces<3> f = operand<3>(qk[0][n], qk[1][n]);
-#pragma unroll
-    for (int i = 0; i < 3; i++) out.p[n][i][lane] = f.p[i];
-  }
   __syncthreads();
-  // T, a column a lane, by forward substitution
+  // T of the two diagonal tiles, a column a lane, by forward substitution
   {
-    const int c = lane % 32;
-    float t[kChunk];
+    const int first = lane % 32 / 16 * 16;
+    float t[16];
 #pragma unroll
-    for (int i = 0; i < kChunk; i++) {
-      float s = i == c ? 1.f : 0.f;
+    for (int i = 0; i < 16; i++) {
+      float s = i == col ? 1.f : 0.f;
 #pragma unroll
-      for (int j = 0; j < i; j++) s = fmaf(-A[i][j], t[j], s);
+      for (int j = 0; j < i; j++) s = fmaf(-A[first + i][first + j], t[j], s);
       t[i] = s;
-      if (lane < 32) inverse[i][c] = s;
+      if (lane < 32) {
+        inverse[first + i][first + col] = s;
+        if (first) inverse[i][16 + col] = 0.f;
+      }
     }
   }
   __syncthreads();
+  // and of the one below, -T_11 A_10 T_00: four rows of a column a lane
+#pragma unroll
+  for (int step = 0; step < 2; step++) {
+    float s[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; j++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        s[e] = step ? fmaf(-inverse[16 + row + e][16 + j], A[16 + j][col], s[e])
+                    : fmaf(A[16 + row + e][j], inverse[j][col], s[e]);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; e++) (step ? inverse : A)[16 + row + e][col] = s[e];
+    __syncthreads();
+  }
+  Pieces<3> between[2];
+#pragma unroll
+  for (int n = 0; n < 2; n++) between[n] = operand<3>(qk[0][n], qk[1][n]);
+  f32x4 pt[2][2];
 #pragma unroll
   for (int n = 0; n < 2; n++) {
-    float x[8];
+    float x[8], y[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       const int i = 16 * n + col, j = 16 * (e / 4) + row + e % 4;
-      x[e] = BACK ? inverse[j][i] : inverse[i][j];
+      x[e] = inverse[i][j];
+      y[e] = inverse[j][i];
     }
-    const Pieces<3> f = split<3>(x);
+    const Pieces<3> f = split<3>(BACK ? y : x);
 #pragma unroll
     for (int i = 0; i < 3; i++) out.t[n][i][lane] = f.p[i];
+    if (!BACK) {
+      // columns n of P T, transposed: rows of it are what its operand has in a lane
+      const Pieces<3> columns = split<3>(y);
+#pragma unroll
+      for (int m = 0; m < 2; m++) {
+        pt[n][m] = f32x4{0, 0, 0, 0};
+        mul(pt[n][m], columns, between[m]);
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 2; n++) {
+    const Pieces<3> f = BACK ? between[n] : operand<3>(pt[0][n], pt[1][n]);
+#pragma unroll
+    for (int i = 0; i < 3; i++) out.p[n][i][lane] = f.p[i];
   }
 }
 

@@ -84,13 +84,12 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
       mul(S[m], stage.k.columns(at.part * 2 * STEPS + m), us);
     }
     // outputs: tile m by part m
-    const Pieces<3> ws = operand<3>(w[0], w[1]);
 #pragma unroll
     for (int m = 0; m < (MODE == kWhole ? 2 : 0); m++) {
       if (G::R > 1 && at.part != m) continue;
       if constexpr (G::R > 1) out[m] = parts.sum(2 + m, at.wave);
       out[m] *= a.scale * since[m];
-      mul(out[m], pieces(c.p[m]), ws);
+      mul(out[m], pieces(c.p[m]), rs);
       T* o = at_head<T>(a.o, at.b, t0 + 16 * m, at.h) + row * a.o.time + at.col;
       if (at.on) {
         if (live == kChunk) {
