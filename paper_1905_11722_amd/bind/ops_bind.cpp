@@ -750,7 +750,7 @@ void delta_expect(const DeltaIn& t) {
   const int64_t dims = t.v.dim();
   TORCH_CHECK_VALUE(t.q.dim() == dims, "q must have ", dims, " dimensions, not ", t.q.dim());
   const int64_t h = t.v.size(-2), hk = t.q.size(-2), dk = t.q.size(-1), dv = t.v.size(-1);
-  TORCH_CHECK_VALUE(h == 0 || (hk > 0 && h % hk == 0), hk, " heads of q do not divide ", h, " heads of v");
+  TORCH_CHECK_VALUE(h == 0 ? hk == 0 : hk > 0 && h % hk == 0, hk, " heads of q do not divide ", h, " heads of v");
   TORCH_CHECK_VALUE(dk >= 1 && dk <= kMaxHead, "q must have 1 to ", kMaxHead, " channels, not ", dk);
   TORCH_CHECK_VALUE(dv >= 1 && dv <= kMaxHead, "v must have 1 to ", kMaxHead, " channels, not ", dv);
   std::vector<int64_t> shape(t.v.sizes().begin(), t.v.sizes().end() - 2);

@@ -627,19 +627,19 @@ __device__ __forceinline__ void load_chunks(const DeltaParams& p, const Walk<G, 
     const int c = chunk_of(min(i, at.count - 1));
     next.fetch(a, prepared[c], values, at.b, at.h, at.hk, c * kChunk, live_of(c), at.col0);
   };
-  const auto put = [&](int i) {
-    next.put(stages[i % STAGES], live_of(chunk_of(i)), a.key, columns, at.col0);
-    fetch(i + 1);
-  };
+  const auto put = [&](int i) { next.put(stages[i % STAGES], live_of(chunk_of(i)), a.key, columns, at.col0); };
   fetch(0);
   put(0);
+  fetch(1);
   for (int i = 0; i < at.count; i++) {
     __syncthreads();
     if (STAGES == 2 && i + 1 < at.count) put(i + 1);
+    if (STAGES == 2) fetch(i + 2);                     // (not in a branch: the loop hands it on)
     if (G::R > 1) __syncthreads();
     if (STAGES == 1) {
       __syncthreads();
       if (i + 1 < at.count) put(i + 1);
+      fetch(i + 2);
     }
   }
 }
@@ -761,7 +761,8 @@ inline int check(const rc_delta_args* a) {
   if (!a || !dtype_ok(a->dtype) || a->batch < 0 || a->length < 0 || a->length > kMaxExtent ||
       a->key < 1 || a->key > kMaxHead || a->value < 1 || a->value > kMaxHead)
     return RC_E_ARG;
-  if (a->heads < 0 || a->key_heads < 0 || (a->heads && (!a->key_heads || a->heads % a->key_heads)))
+  if (a->heads < 0 || a->key_heads < 0 || !a->heads != !a->key_heads ||
+      (a->heads && a->heads % a->key_heads))
     return RC_E_ARG;
   return RC_OK;
 }

@@ -264,7 +264,8 @@ extern "C" int rc_delta_step(const rc_delta_step_args* args, void* stream) {
   const rc_delta_step_args& a = *args;
   if (!dtype_ok(a.dtype) || a.batch < 0 || a.num_slots < 0 || a.key < 1 || a.key > kMaxHead ||
       a.value < 1 || a.value > kMaxHead || a.heads < 0 || a.key_heads < 0 ||
-      (a.heads && (!a.key_heads || a.heads % a.key_heads)))
+      !a.heads != !a.key_heads ||
+      (a.heads && a.heads % a.key_heads))
     return RC_E_ARG;
   if (!a.batch || !a.heads) return RC_OK;
   if (!a.q.data || !a.k.data || !a.v.data || !a.o.data || !a.beta.data || !a.state ||

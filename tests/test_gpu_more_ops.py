@@ -95,6 +95,59 @@ def test_delta(case):
     compare_grads(x, outs, wants)
 
 
+@pytest.mark.parametrize("batch,length,key_heads,heads", [(64, 512, 1, 2), (16, 500, 2, 8)])
+def test_delta_heads_that_share_a_key_head(batch, length, key_heads, heads):
+    """So many blocks that one workgroup has all of a key head's heads, or some of them."""
+    x = delta_inputs("f32", batch, length, key_heads, heads, 8, 8, "g")
+    x.grads()
+    outs, wants = run_delta(x)
+    check(outs[0], wants[0], "o")
+    compare_grads(x, outs[:1], wants[:1])
+
+
+@pytest.mark.parametrize("key,value,length", [(16, 8, 90), (100, 33, 700)])
+def test_delta_scratch_aligned_to_a_float(key, value, length):
+    """Scratch and what is kept need no more than a float's alignment."""
+    from tests import more_ops_abi as abi
+    import ctypes
+    lib, n = abi.library(), ctypes.c_uint64()
+    x = delta_inputs("bf16", 1, length, 1, 1, key, value, "g")
+    g = {k: t.contiguous() for k, t in x.gpu.items()}
+    o, do = torch.empty_like(g["v"]), torch.randn_like(g["v"])
+    back = {k: torch.empty_like(t) for k, t in g.items()}
+
+    def heads(t):
+        return abi.Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+    def view(t):
+        return abi.abi.View(t.data_ptr(), t.stride(0), t.stride(1))
+
+    a = abi.DeltaArgs(dtype=1, batch=1, length=length, key_heads=1, heads=1, key=key, value=value, scale=0.2,
+                      q=heads(g["q"]), k=heads(g["k"]), v=heads(g["v"]), o=heads(o), g=view(g["g"]),
+                      beta=view(g["beta"]), do_=heads(do), dq=heads(back["q"]), dk=heads(back["k"]),
+                      dv=heads(back["v"]), dg=back["g"].data_ptr(), dbeta=back["beta"].data_ptr())
+    buffers = []
+
+    def floats(call):
+        assert getattr(lib, call)(a, n) == 0
+        buffers.append(torch.empty(n.value // 4 + 8, device=DEV))
+        return buffers[-1].data_ptr() + 4, n.value
+
+    got = []
+    for _ in range(2):
+        a.kept, _ = floats("rc_delta_kept_bytes")
+        a.workspace, a.workspace_bytes = floats("rc_delta_forward_workspace")
+        assert lib.rc_delta_forward(a, None) == 0
+        a.workspace, a.workspace_bytes = floats("rc_delta_backward_workspace")
+        assert lib.rc_delta_backward(a, None) == 0
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in (o, *back.values())])
+    leaves = [t.detach().requires_grad_() for t in g.values()]
+    want = ops.gated_delta(*leaves, scale=0.2)
+    for w, first, second in zip((want, *torch.autograd.grad(want, leaves, do)), *got):
+        assert torch.equal(w, first) and torch.equal(w, second)
+
+
 @pytest.mark.parametrize("of", ["o", "state"])
 def test_delta_gradient_of_one_output(of):
     x = delta_inputs("f32", 2, 50, 1, 2, 20, 30, "gs")
@@ -703,6 +756,7 @@ def test_refusals():
         lambda: ops.gated_delta(x, x[:, :, :1], x, g, g),
         lambda: ops.gated_delta(torch.cat([x, x[:, :, :1]], 2), torch.cat([x, x[:, :, :1]], 2), x, g, g),
         lambda: ops.gated_delta(x[..., :0], x[..., :0], x, g, g),
+        lambda: ops.gated_delta(x, x, x[:, :, :0], g[:, :, :0], g[:, :, :0]),
         lambda: ops.gated_delta(x, x, x[..., :0], g, g),
         lambda: ops.gated_delta(wide, wide, small, one, one),
         lambda: ops.gated_delta(small, small, wide, one, one),

@@ -86,7 +86,7 @@ def dropout(**kw):
 BAD = [("rc_delta_" + call, delta, change) for call in ("forward", "backward") for change in (
     dict(dtype=3), dict(dtype=-1), dict(batch=-1), dict(length=-1), dict(length=2 ** 30 + 1), dict(key=0),
     dict(key=257), dict(value=0), dict(value=257), dict(heads=-1), dict(key_heads=3), dict(key_heads=0),
-    dict(key_heads=-2), dict(q=NO_HEADS), dict(k=NO_HEADS), dict(v=NO_HEADS), dict(beta=NONE),
+    dict(key_heads=-2), dict(heads=0), dict(q=NO_HEADS), dict(k=NO_HEADS), dict(v=NO_HEADS), dict(beta=NONE),
     dict(kept=X + 2), dict(workspace=X + 1))] + [
     ("rc_delta_forward", delta, dict(o=NO_HEADS)),
     ("rc_delta_backward", delta, dict(do_=NO_HEADS)), ("rc_delta_backward", delta, dict(dq=NO_HEADS)),
@@ -95,7 +95,7 @@ BAD = [("rc_delta_" + call, delta, change) for call in ("forward", "backward") f
     ("rc_delta_backward", delta, dict(dbeta=None)), ("rc_delta_backward", delta, dict(kept=None))] + [
     ("rc_delta_step", step, change) for change in (
         dict(dtype=4), dict(batch=-1), dict(key=0), dict(key=257), dict(value=0), dict(value=300),
-        dict(key_heads=3), dict(num_slots=-1), dict(num_slots=2), dict(state=None), dict(state=X + 2),
+        dict(key_heads=3), dict(heads=0), dict(num_slots=-1), dict(num_slots=2), dict(state=None), dict(state=X + 2),
         dict(q=NO_HEADS), dict(beta=NONE), dict(o=NO_HEADS))] + [
     ("rc_qk_" + call, qk, change) for call in ("forward", "backward") for change in (
         dict(dtype=3), dict(param_dtype=2), dict(norm=3), dict(norm=-1), dict(batch=-1), dict(length=-1),
