@@ -3,8 +3,10 @@
 The model is a stack of residual blocks: projection, short causal
 convolution, projection to the scan's steps and its B and C, selective state space
 scan with a gate, projection back, and the norms after this block and before
-the next one.  Its operators come from ``paper_1905_11722_amd.ops``, its plain
-matrix products from PyTorch.
+the next one; or (``--mixer delta``) linear attention in the scan's place: norms and
+rotation of queries and keys, gated delta rule, and dropout onto the residual stream, whose
+mask is drawn again wherever a node is computed again.  Its operators come from
+``paper_1905_11722_amd.ops``, its plain matrix products from PyTorch.
 
 The training step is planned by ``paper_1905_11722_amd.rcdp``: every operation
 of the step is a node with its forward time (measured, in tenths of a microsecond) and
@@ -35,9 +37,6 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_1905_11722_amd import ops, rcdp, workloads  # noqa: E402
 
-NODES = ("project", "conv", "steps", "delta", "scan", "back", "join")      # of a block, in order
-
-
 class Model:
     """The stack's parameters and the function of each node.
 
@@ -45,6 +44,8 @@ class Model:
     channels with ``states`` states each, taps of the convolution, and
     steps of rank width / 16.
     """
+
+    kinds = ("project", "conv", "steps", "delta", "scan", "back", "join")     # of a block, in order
 
     def __init__(self, blocks, width, states=16, taps=4, dtype=torch.bfloat16, device="cuda", seed=0):
         rng = torch.Generator(device=device).manual_seed(seed)
@@ -76,14 +77,14 @@ class Model:
     @property
     def nodes(self):
         """Nodes of a step: the first norm, the blocks', the loss."""
-        return self.blocks * len(NODES) + 2
+        return self.blocks * len(self.kinds) + 2
 
     def place(self, node):
         """(block, kind) of a node; "start" and "loss" belong to no block."""
         if node in (0, self.nodes - 1):
             return None, "loss" if node else "start"
-        block, kind = divmod(node - 1, len(NODES))
-        return block, NODES[kind]
+        block, kind = divmod(node - 1, len(self.kinds))
+        return block, self.kinds[kind]
 
     def owned(self, node):
         """The parameters that a node takes."""
@@ -128,7 +129,7 @@ class Model:
         block, kind = self.place(node)
         if block is None:
             return [node - 1] if node else []
-        first = 1 + block * len(NODES)
+        first = 1 + block * len(self.kinds)
         return {"project": [first - 1], "conv": [first], "steps": [first + 1], "delta": [first + 2],
                 "scan": [first + 1, first + 2, first + 3, first], "back": [first + 4],
                 "join": [first + 5, first - 1]}[kind]
@@ -143,6 +144,17 @@ class Model:
             return (values[0][1] * dy).sum(dtype=torch.float32)
         return self.run(block, kind, values, None if state is None else state[block])
 
+    def prompt(self, b, values):
+        """(value, states after it) of block b over a prompt."""
+        p, n = self.p[b], self.states
+        both = self.run(b, "project", [values])
+        u, conv = ops.causal_conv(both[..., :self.inner], p["conv"], p["conv_bias"], return_state=True)
+        steps = self.run(b, "steps", [u])
+        B, C = steps[..., self.rank:self.rank + n], steps[..., self.rank + n:]
+        y, scan = ops.selective_scan(u, self.run(b, "delta", [steps]), p["A"], B, C, p["D"],
+                                     both[..., self.inner:], p["dt_bias"], softplus=True, return_state=True)
+        return self.run(b, "join", [self.run(b, "back", [y]), values]), (conv, scan)
+
     def graph(self, batch, length):
         """The step's nodes with their times and sizes (workloads.Graph)."""
         cost = measure(self, batch, length)
@@ -155,6 +167,90 @@ class Model:
         return workloads.Graph(self.nodes, [sorted(x) for x in succ], [cost[k][0] for k in kinds],
                                [cost[k][1] for k in kinds],
                                [k if b is None else f"{k}{b}" for b, k in places], kinds)
+
+
+class DeltaModel(Model):
+    """The stack with linear attention: heads of key = value = 64 channels, gates of each
+    head from the block's input, dropout of rate p onto the residual stream.  ``seed`` draws the
+    masks of a step, a block's by its tag: a training loop takes another for each step."""
+
+    kinds = ("project", "conv", "gates", "heads", "mix", "back", "join")
+
+    def __init__(self, blocks, width, taps=4, dtype=torch.bfloat16, device="cuda", seed=0, p=0.1):
+        rng = torch.Generator(device=device).manual_seed(seed)
+        self.blocks, self.width, self.taps, self.dtype, self.rate, self.seed = blocks, width, taps, dtype, p, 1
+        self.heads, self.channels = max(1, width // 64), 64
+        inner = self.heads * self.channels
+        self.inv_freq = 10000.0 ** (-torch.arange(32, device=device) / 32)
+
+        def matrix(rows, cols):
+            return (torch.randn(rows, cols, generator=rng, device=device) * rows ** -0.5).to(dtype)
+
+        self.p = [{"project": matrix(width, 3 * inner), "conv": matrix(taps, 3 * inner).t().float().contiguous(),
+                   "conv_bias": torch.zeros(3 * inner, device=device), "gates": matrix(width, 2 * self.heads),
+                   "decay": torch.full((self.heads,), -3.0, device=device), "back": matrix(inner, width),
+                   "pre": torch.ones(width, device=device)} for _ in range(blocks)]
+        for block in self.p:
+            for t in block.values():
+                t.requires_grad_()
+        self.first = torch.ones(width, device=device).requires_grad_()
+
+    def owned(self, node):
+        block, kind = self.place(node)
+        names = {"project": ["project"], "conv": ["conv", "conv_bias"], "gates": ["gates", "decay"],
+                 "back": ["back"], "join": ["pre"]}
+        return [self.first] if kind == "start" else [self.p[block][k] for k in names.get(kind, [])]
+
+    def split(self, u):
+        """Queries, keys and values, (..., heads, channels) each."""
+        return [t.unflatten(-1, (self.heads, -1)) for t in u.chunk(3, -1)]
+
+    def run(self, block, kind, values, state=None):
+        p = self.p[block]
+        if kind == "project":
+            return values[0][1] @ p["project"]
+        if kind == "conv":
+            if state is None:
+                return ops.causal_conv(values[0], p["conv"], p["conv_bias"])
+            return ops.causal_conv_step(state[0], values[0], p["conv"], p["conv_bias"])
+        if kind == "gates":
+            g, beta = (values[0][1] @ p["gates"]).float().chunk(2, -1)
+            return -torch.nn.functional.softplus(g + p["decay"]), torch.sigmoid(beta)
+        if kind == "heads":
+            q, k, _ = self.split(values[0])
+            if state is None:
+                return ops.qk_norm(q, k, inv_freq=self.inv_freq, norm="l2")
+            q, k = ops.qk_norm(q[:, None], k[:, None], None, None, self.inv_freq, state[2], norm="l2")
+            return q[:, 0], k[:, 0]
+        if kind == "mix":
+            (q, k), v, (g, beta) = values[0], self.split(values[1])[2], values[2]
+            if state is None:
+                return ops.gated_delta(q, k, v, g, beta).flatten(-2)
+            state[2].add_(1)                         # the next token's position
+            return ops.gated_delta_step(state[1], q, k, v, g, beta).flatten(-2)
+        if kind == "back":
+            return values[0] @ p["back"]
+        rate = 0.0 if state is not None else self.rate
+        out = ops.dropout(values[0], rate, self.seed, tag=block, residual=values[1][0])
+        return ops.norm_residual(None, out, pre_weight=p["pre"])
+
+    def predecessors(self, node):
+        block, kind = self.place(node)
+        if block is None:
+            return [node - 1] if node else []
+        first = 1 + block * len(self.kinds)
+        return {"project": [first - 1], "conv": [first], "gates": [first - 1], "heads": [first + 1],
+                "mix": [first + 3, first + 1, first + 2], "back": [first + 4], "join": [first + 5, first - 1]}[kind]
+
+    def prompt(self, b, values):
+        p = self.p[b]
+        u, conv = ops.causal_conv(self.run(b, "project", [values]), p["conv"], p["conv_bias"], return_state=True)
+        q, k = self.run(b, "heads", [u])
+        g, beta = self.run(b, "gates", [values])
+        o, S = ops.gated_delta(q, k, self.split(u)[2], g, beta, return_state=True)
+        at = torch.full((u.shape[0], 1), u.shape[1], dtype=torch.int32, device=u.device)
+        y = self.run(b, "back", [o.flatten(-2)])
+        return self.run(b, "join", [y, values], (conv, S, at)), (conv, S, at)
 
 
 def _tensors(value):
@@ -243,7 +339,7 @@ def measure(model, batch, length, repeats=5):
     its gradient and the scratch of its backward pass."""
     x = torch.randn(batch, length, model.width, device=model.first.device).to(model.dtype)
     step, last = Step(model, x, torch.randn_like(x)), model.nodes - 1
-    order = list(range(1 + len(NODES))) + [last]
+    order = list(range(1 + len(model.kinds))) + [last]
     cost = {}
 
     def pass_over():
@@ -251,11 +347,11 @@ def measure(model, batch, length, repeats=5):
             before = torch.cuda.memory_allocated()
             step.forward(v, True)
             cost[v] = torch.cuda.memory_allocated() - before
-            if v == len(NODES):                      # the last block's end, for the loss
+            if v == len(model.kinds):                      # the last block's end, for the loss
                 step.values[last - 1] = step.values[v]
         step.grads[last] = [torch.ones_like(step.values[last])]
         for v in reversed(order):
-            if v == len(NODES) and last - 1 != v:
+            if v == len(model.kinds) and last - 1 != v:
                 step.grads[v] = step.grads.pop(last - 1)
                 del step.values[last - 1]
             if v == 0:
@@ -282,7 +378,7 @@ def measure(model, batch, length, repeats=5):
             end.synchronize()
             spans.append(start.elapsed_time(end))
         times[v] = statistics.median(spans)
-        if v == len(NODES):
+        if v == len(model.kinds):
             step.values[last - 1] = step.values[v]
     return {model.place(v)[1]: (max(1, round(times[v] * 1e4)), max(1, -(-cost[v] // 1024))) for v in order}
 
@@ -323,17 +419,10 @@ def planned_step(model, x, dy, schedule, step=None):
 @torch.no_grad()
 def prompt(model, x):
     """(normed output, the states after the prompt) of a prompt."""
-    values, states, n = model.start(x), [], model.states
+    values, states = model.start(x), []
     for b in range(model.blocks):
-        p = model.p[b]
-        both = model.run(b, "project", [values])
-        u, conv = ops.causal_conv(both[..., :model.inner], p["conv"], p["conv_bias"], return_state=True)
-        steps = model.run(b, "steps", [u])
-        B, C = steps[..., model.rank:model.rank + n], steps[..., model.rank + n:]
-        y, scan = ops.selective_scan(u, model.run(b, "delta", [steps]), p["A"], B, C, p["D"],
-                                     both[..., model.inner:], p["dt_bias"], softplus=True, return_state=True)
-        states.append((conv, scan))
-        values = model.run(b, "join", [model.run(b, "back", [y]), values])
+        values, state = model.prompt(b, values)
+        states.append(state)
     return values[1], states
 
 
@@ -373,6 +462,7 @@ def measured(step):
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    ap.add_argument("--mixer", choices=("scan", "delta"), default="scan")
     ap.add_argument("--blocks", type=int, default=8)
     ap.add_argument("--width", type=int, default=1024)
     ap.add_argument("--batch", type=int, default=4)
@@ -383,7 +473,7 @@ def main():
     if not 1 <= a.tokens <= a.length:
         ap.error("--tokens must be at least 1 and at most the length")
     torch.manual_seed(1)
-    model = Model(a.blocks, a.width)
+    model = (DeltaModel if a.mixer == "delta" else Model)(a.blocks, a.width)
     x = torch.randn(a.batch, a.length, a.width, device="cuda").to(model.dtype)
     dy = torch.randn_like(x)
     graph, budget, schedule = plan(model, a.batch, a.length, a.fraction)
