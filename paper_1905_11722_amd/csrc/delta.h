@@ -277,8 +277,8 @@ __device__ __forceinline__ double sum_of_g(const rc_delta_args& a, int b, int h,
   return G;
 }
 
-// One wave a chunk of a head.
-template <class T, int KT, bool BACK>
+// One wave a chunk of a head; its loads first.
+template <class T, int KT, bool BACK, bool WIDE>
 __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>;
@@ -291,11 +291,29 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   const int live = min(length_of(a, b) - t0, kChunk);
   if (live <= 0) return;
   // tokens 16m + lane % 16 over channels 32s + 8 (lane / 16) ..
-  const auto rows = [&](const rc_heads& x, int m, int s) {
-    const int t = 16 * m + lane % 16, c = 32 * s + lane / 16 * 8;
+  typedef T TV __attribute__((ext_vector_type(8)));
+  TV raw[2][2][KT];
+#pragma unroll
+  for (int x = 0; x < 2; x++)
+#pragma unroll
+    for (int m = 0; m < 2; m++) {
+      const T* from = at_head<T>(x ? a.q : a.k, b, t0 + min(16 * m + lane % 16, live - 1), hk);
+#pragma unroll
+      for (int s = 0; s < KT; s++) {
+        const int c = 32 * s + lane / 16 * 8;
+        if (WIDE) {
+          __builtin_memcpy(&raw[x][m][s], from + (c < a.key ? c : 0), sizeof(TV));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; e++) raw[x][m][s][e] = from[min(c + e, a.key - 1)];
+        }
+      }
+    }
+  const auto rows = [&](int x, int m, int s) {
+    const int c = 32 * s + lane / 16 * 8, n = 16 * m + lane % 16 < live ? a.key - c : 0;
     float v[8];
-    load_vec<8>(at_head<T>(x, b, t0 + (t < live ? t : 0), hk) + (c < a.key ? c : 0),
-                t < live ? a.key - c : 0, v);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (WIDE ? 0 : e) < n ? (float)raw[x][m][s][e] : 0.f;
     return split<N>(v);
   };
   Chunk& out = p.prepared[blockIdx.x];
@@ -318,8 +336,8 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int n = 0; n < 2; n++) kk[m][n] = qk[m][n] = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int s = 0; s < KT; s++) {
-    const Pieces<N> ks[2] = {rows(a.k, 0, s), rows(a.k, 1, s)};
-    const Pieces<N> qs[2] = {rows(a.q, 0, s), rows(a.q, 1, s)};
+    const Pieces<N> ks[2] = {rows(0, 0, s), rows(0, 1, s)};
+    const Pieces<N> qs[2] = {rows(1, 0, s), rows(1, 1, s)};
 #pragma unroll
     for (int m = 0; m < 2; m++)
 #pragma unroll
@@ -336,9 +354,10 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
 #pragma unroll
       for (int r = 0; r < 4; r++) {
         const int i = 16 * n + col, j = 16 * m + row + r;
-        A[i][j] = j < i ? beta[i] * decay_between(sums[i] - sums[j]) * kk[m][n][r] : 0.f;
-        const int pi = BACK ? j : i, pj = BACK ? i : j;
-        qk[m][n][r] = pj <= pi ? a.scale * decay_between(sums[pi] - sums[pj]) * qk[m][n][r] : 0.f;
+        // (the decay of the later of the two, whichever of them that is)
+        const float d = m <= n || BACK ? decay_between(j <= i ? sums[i] - sums[j] : sums[j] - sums[i]) : 0.f;
+        if (m <= n) A[i][j] = j < i ? beta[i] * d * kk[m][n][r] : 0.f;
+        qk[m][n][r] = (BACK ? i <= j : j <= i) ? a.scale * d * qk[m][n][r] : 0.f;
       }
   __syncthreads();
   // T of the two diagonal tiles, a column a lane, by forward substitution
@@ -863,7 +882,10 @@ inline DeltaParams params(const rc_delta_args& a) {
 template <class T, int KT, bool BACK>
 inline int prepare(const DeltaParams& p, hipStream_t s) {
   if (!p.chunks) return RC_OK;
-  k_delta_prepare<T, KT, BACK><<<(unsigned)pairs_of(p.a), 64, 0, s>>>(p);
+  if (p.a.key % 8)
+    k_delta_prepare<T, KT, BACK, false><<<(unsigned)pairs_of(p.a), 64, 0, s>>>(p);
+  else
+    k_delta_prepare<T, KT, BACK, true><<<(unsigned)pairs_of(p.a), 64, 0, s>>>(p);
   return launched("k_delta_prepare");
 }
 // Workgroups of a walk.
