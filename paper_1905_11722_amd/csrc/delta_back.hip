@@ -169,16 +169,22 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
   const bool wide = a.value % 8 == 0;
   const int first_tile = wave / I::PARTS * NT, first_m = wave % I::PARTS * MT;
   // dq and dk of the key head, or their parts in 32 bits where other workgroups have more
-  const auto store = [&](int which, int t, int c, float x) {
-    if (groups == a.key_heads)
-      at_head<T>(which ? a.dk : a.dq, b, t0 + t, hk)[c] = (T)x;
-    else
-      p.partial[((((int64_t)which * a.batch + b) * a.length + t0 + t) * groups + group) * a.key + c] = x;
+  const bool whole_heads = groups == a.key_heads;
+  const auto row_of = [&](int which, int t) {
+    return at_head<T>(which ? a.dk : a.dq, b, t0 + t, hk);
+  };
+  const auto part_of = [&](int which, int t) {
+    return p.partial + ((((int64_t)which * a.batch + b) * a.length + t0 + t) * groups + group) * a.key;
   };
   if (live <= 0) {
-    for (int i = tid; i < here * a.key; i += THREADS) {
-      store(0, i / a.key, i % a.key, 0.f);
-      store(1, i / a.key, i % a.key, 0.f);
+    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int vectors = (a.key + 7) / 8;
+    for (int i = tid; i < 2 * here * vectors; i += THREADS) {
+      const int c = i % vectors * 8, t = i / vectors % here, which = i / vectors / here;
+      if (whole_heads)
+        store_vec<8>(row_of(which, t) + c, a.key - c, zero);
+      else
+        store_vec<8>(part_of(which, t) + c, a.key - c, zero);
     }
     for (int i = tid; i < here * p.each; i += THREADS) {
       const int64_t at = ((int64_t)b * a.length + t0 + i / p.each) * a.heads + group * p.each + i % p.each;
@@ -475,9 +481,13 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const int t = 16 * (first_m + m) + row + e;
-        if (t < here) {
-          store(0, t, c, dq[n][m][e]);
-          store(1, t, c, dk[n][m][e]);
+        if (t >= here) continue;
+        if (whole_heads) {
+          row_of(0, t)[c] = (T)dq[n][m][e];
+          row_of(1, t)[c] = (T)dk[n][m][e];
+        } else {
+          part_of(0, t)[c] = dq[n][m][e];
+          part_of(1, t)[c] = dk[n][m][e];
         }
       }
   }
