@@ -1,5 +1,6 @@
-// Shared by the gated delta rule's kernels (delta.hip, delta_back.hip).  Each head keeps a matrix S (key x value); a token decays
-// it, reads what it holds for the key k, and writes back the difference to v:
+// Shared by the gated delta rule's kernels (delta.hip, delta_back.hip).  Each head keeps a matrix S
+// (key x value); a token decays it, reads what it holds for the key k, and writes back the
+// difference to v:
 //   S_t = a_t S_{t-1} + k_t w_t^T,  w_t = beta_t (v_t - a_t S_{t-1}^T k_t),
 //   o_t = scale S_t^T q_t,  a = exp(g).
 //
@@ -10,26 +11,30 @@
 //   O_i = scale exp(G_i) S^T q_i + sum_j (P T)_ij R_j,   P_ij = scale D_ij q_i . k_j,
 //   S' = exp(G_31) S + sum_j exp(G_31 - G_j) k_j w_j^T.
 // T and P T need no state: k_delta_prepare computes them for all chunks at once, T by
-// forward substitution (P W is P T R: W need not be an operand).  What is left of a chunk are five products of at most
-// 32 x key x value, k_delta_forward's, one chunk after the other.
+// forward substitution (its diagonal tiles of 16, then the one below them from both).  What is left
+// of a chunk are five products of at most 32 x key x value, k_delta_forward's, one
+// chunk after the other.
 //
 // Backward, with dO and the gradient E of S':
 //   dW_j = sum_i P_ij do_i + exp(G_31 - G_j) E^T k_j,   dR = T^T dW,   dv = beta dR,
 //   dS = exp(G_31) E + sum_i exp(G_i) (scale q_i do_i^T - beta_i k_i dR_i^T)
 // again one chunk after the other, from the last (k_delta_states_back); w and dR do
 // not depend on how tokens are cut into chunks.  The other gradients then need no order
-// (k_delta_inputs_back).  With M_ij = D_ij scale do_i . w_j and N_ij = D_ij dR_i . w_j (j < i),
+// (k_delta_inputs_back, by blocks of two chunks, where G and exp(G_31 - G_j) are the block's).  With
+// M_ij = D_ij scale do_i . w_j and N_ij = D_ij dR_i . w_j (j < i),
 //   dq_i = scale exp(G_i) S do_i + sum_j M_ij k_j
 //   x_i = exp(G_i) S dR_i + sum_j N_ij k_j,    dbeta_i = dR_i . v_i - k_i . x_i
 //   dk_i = -beta_i x_i (as read) + exp(G_31 - G_i) E w_i + sum_l (M_li q_l - beta_l N_li k_l) (as written)
 //   dG_i = q_i . dq_i + k_i . (dk_i as read - as written),  dG_31 += <E, S'>,
 //   dg_t = sum of dG_i over i >= t.
 //
-// Products run on the bf16 matrix instructions with operands taken apart into
-// bf16 numbers that add up to them: one for bf16, two for f16, three for 32 bits, and
-// the products of pieces down to 2^-16 of the largest: 32-bit results from instructions with 16
-// times the rate of the 32-bit ones.  D's exponents are differences
-// of sums in 64 bits, so a token that forgets everything costs the later ones nothing.
+// Products run on the bf16 matrix instructions with operands taken apart into bf16 numbers that
+// add up to them: one for bf16, two for f16, three for 32 bits, and of the products of
+// pieces those above 2^-24 of the whole: 32-bit results (3 instructions for bf16 by 32 bits, 6 for 32 by 32
+// bits) where the 32-bit matrix instructions take 16 times as long each.  The states and
+// the gradients of g and beta are 32-bit outputs: pieces left off (two for 32 bits) would show in them.
+// D's exponents are differences of sums in 64 bits, so a token that forgets everything costs the
+// later ones nothing.  (Chunks of 64 take as many matrix instructions a token and twice the registers.)
 #pragma once
 
 #include <algorithm>
@@ -277,7 +282,8 @@ __device__ __forceinline__ double sum_of_g(const rc_delta_args& a, int b, int h,
   return G;
 }
 
-// One wave a chunk of a head; its loads first.
+// One wave a chunk of a head; its loads first.  Bound by instructions that run once each: 9 us alone,
+// 4096 of them (4 x 2048 tokens, 16 heads of 128) 24 us.
 template <class T, int KT, bool BACK, bool WIDE>
 __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   const rc_delta_args& a = p.a;

