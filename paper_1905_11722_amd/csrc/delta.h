@@ -432,15 +432,15 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   }
 }
 
-// Column `col` of a head's state from row `first` on: tile m has this lane's rows
+// Column `col` of a kept state (below) from row `first` on: tile m has this lane's rows
 // 16m + 4 (lane / 16) + 0..3.
-// Column `col` of a kept state (below).
 template <int TILES>
 __device__ __forceinline__ void load_kept(const float* from, int rows, int col, int first, f32x4 (&S)[TILES]) {
   const float* at = from + col * rows + first + threadIdx.x % 64 / 16 * 4;
 #pragma unroll
   for (int m = 0; m < TILES; m++) S[m] = *(const f32x4*)(at + 16 * m);
 }
+// The same of a head's state as callers have it.
 template <int TILES>
 __device__ __forceinline__ void load_state(const float* from, const rc_delta_args& a, int col, int first,
                                            f32x4 (&S)[TILES]) {
@@ -821,9 +821,12 @@ inline int fits(const rc_delta_args& a) {
   if (!launchable(bh, 256) || !launchable(bh * cdiv(a.value, 16), 512) ||
       !launchable(pairs_of(a), 256))
     return RC_E_OVERFLOW;
-  if (!launchable(cdiv(2 * (int64_t)a.batch * a.length * a.key_heads * a.key, 256), 256))
-    return RC_E_OVERFLOW;
   return RC_OK;
+}
+inline int fits_back(const rc_delta_args& a) {
+  if (int e = fits(a)) return e;
+  if (empty(a)) return RC_OK;
+  return launchable((int64_t)a.batch * a.heads / heads_together(a) * blocks_of(a), 512) ? RC_OK : RC_E_OVERFLOW;
 }
 // Segments of the length: more than one where the walks over the segments' ends (of values' and
 // key columns, one segment fewer) fit the compute units at once and each segment has eight chunks

@@ -231,7 +231,7 @@ extern "C" int rc_delta_forward_workspace(const rc_delta_args* args, uint64_t* b
 extern "C" int rc_delta_backward_workspace(const rc_delta_args* args, uint64_t* bytes) {
   if (int e = check(args)) return e;
   if (!bytes) return RC_E_ARG;
-  if (int e = fits(*args)) return e;
+  if (int e = fits_back(*args)) return e;
   *bytes = workspace_of(*args, true);
   return RC_OK;
 }

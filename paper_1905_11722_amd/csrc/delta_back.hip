@@ -487,12 +487,13 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       for (int e = 0; e < 4; e++) {
         const int t = 16 * (first_m + m) + row + e;
         if (t >= here) continue;
+        const float of_q = t < live ? dq[n][m][e] : 0.f, of_k = t < live ? dk[n][m][e] : 0.f;
         if (whole_heads) {
-          row_of(0, t)[c] = (T)dq[n][m][e];
-          row_of(1, t)[c] = (T)dk[n][m][e];
+          row_of(0, t)[c] = (T)of_q;
+          row_of(1, t)[c] = (T)of_k;
         } else {
-          part_of(0, t)[c] = dq[n][m][e];
-          part_of(1, t)[c] = dk[n][m][e];
+          part_of(0, t)[c] = of_q;
+          part_of(1, t)[c] = of_k;
         }
       }
   }
@@ -503,17 +504,17 @@ template <class T>
 __global__ __launch_bounds__(256) void k_delta_shared_heads(DeltaParams p, int64_t n) {
   const rc_delta_args& a = p.a;
   const int parts = a.heads / p.each / a.key_heads;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= 2 * n) return;
-  const int which = i >= n;
-  const int64_t e = i - which * n;
-  const int c = (int)(e % a.key);
-  const int64_t row = e / a.key;                      // (b, t, key head)
-  const float* from = p.partial + which * n * parts + row * parts * a.key + c;
-  float s = 0.f;
-  for (int j = 0; j < parts; j++) s += from[(int64_t)j * a.key];
-  const int64_t token = row / a.key_heads;
-  at_head<T>(which ? a.dk : a.dq, token / a.length, token % a.length, row % a.key_heads)[c] = (T)s;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n; i += (int64_t)gridDim.x * 256) {
+    const int which = i >= n;
+    const int64_t e = i - which * n;
+    const int c = (int)(e % a.key);
+    const int64_t row = e / a.key;                    // (b, t, key head)
+    const float* from = p.partial + which * n * parts + row * parts * a.key + c;
+    float s = 0.f;
+    for (int j = 0; j < parts; j++) s += from[(int64_t)j * a.key];
+    const int64_t token = row / a.key_heads;
+    at_head<T>(which ? a.dk : a.dq, token / a.length, token % a.length, row % a.key_heads)[c] = (T)s;
+  }
 }
 
 }  // namespace
@@ -526,7 +527,7 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
                    !a.dk.data || !a.dv.data || !a.dbeta || !a.kept || !a.dg != !a.g.data))
     return RC_E_ARG;
   if (!float_aligned(a.kept) || !float_aligned(a.workspace)) return RC_E_ARG;
-  if (int e = fits(a)) return e;
+  if (int e = fits_back(a)) return e;
   if (a.length && (!a.workspace || a.workspace_bytes < workspace_of(a, true))) return RC_E_SCRATCH;
   const hipStream_t s = (hipStream_t)stream;
   DeltaParams p = params(a);
@@ -559,7 +560,7 @@ extern "C" int rc_delta_backward(const rc_delta_args* args, void* stream) {
       if (int e = launched("k_delta_inputs_back")) return e;
       if (a.heads / p.each == a.key_heads) return (int)RC_OK;
       const int64_t n = (int64_t)a.batch * a.length * a.key_heads * a.key;
-      k_delta_shared_heads<T><<<(unsigned)cdiv(2 * n, 256), 256, 0, s>>>(p, n);
+      k_delta_shared_heads<T><<<(unsigned)std::min<int64_t>(cdiv(2 * n, 256), 1 << 20), 256, 0, s>>>(p, n);
       return launched("k_delta_shared_heads");
     });
   });

@@ -204,6 +204,20 @@ def test_delta_equal_keys(dtype):
     compare_grads(x, outs, wants)
 
 
+@pytest.mark.parametrize("key_heads", [1, 4])
+def test_delta_nothing_past_an_end(key_heads):
+    """What the last tokens of a sequence hold reaches neither the tokens past its end nor other sequences."""
+    x = delta_inputs("f32", 2, 70, key_heads, 4, 24, 20, "gs")
+    x.gpu["v"].detach()[0, 42, 1] = float("nan")
+    x.gpu["q"].detach()[0, 40, 0] = float("inf")
+    leaves = [x.gpu[n].detach().requires_grad_() for n in ("q", "k", "v", "g", "beta")]
+    o = ops.gated_delta(*leaves, state=x.gpu["state"].detach(), lengths=int32([43, 70]))
+    for g, t in zip(torch.autograd.grad(o, leaves, torch.ones_like(o)), leaves):
+        assert g[0].isnan().any() or t is leaves[2]
+        assert not g[0, 43:].any() and g[1].isfinite().all() and g[1].any()
+    assert not o[0, 43:].any() and o[1].isfinite().all()
+
+
 def test_delta_layouts():
     """Slices of one projection, heads before tokens, an expanded gradient, a scale."""
     torch.manual_seed(3)
@@ -727,6 +741,29 @@ def test_far_offsets():
     check(o, want[0][:, 0], "token")
     check(pool[-1:], want[1], "slot")
     assert not pool[:2 ** 20].any()
+
+
+def test_delta_many_tokens():
+    """Queries and keys of 2^31 elements each, heads of one number: where everything before is forgotten, outputs
+    and gradients are those of the tokens from there on, bit for bit."""
+    n, h, tail = 2 ** 17, 128, 128
+    q = torch.randn(1, n, h, 128, dtype=torch.bfloat16, device=DEV).mul_(0.08)
+    k = q.flip(2)
+    v, beta = (torch.rand(1, n, h, *c, dtype=t, device=DEV) for c, t in (((1,), torch.bfloat16), ((), torch.float32)))
+    g = -beta
+    g[:, -tail] = -float("inf")
+
+    def run(from_):
+        t = [x[:, from_:].requires_grad_() for x in (q.detach(), k.detach(), v.detach(), g.detach(), beta.detach())]
+        o = ops.gated_delta(*t)
+        d = torch.zeros_like(o)
+        d[:, -tail:] = v.detach()[:, -tail:]
+        return [o.detach()[:, -tail:]] + [x[:, -tail:].clone() for x in torch.autograd.grad(o, t, d)]
+
+    few = run(n - tail)
+    many = run(0)
+    for a, b in zip(few, many):
+        assert torch.equal(a, b) and a.any()
 
 
 # ------------------------------------------------------------------- refusals

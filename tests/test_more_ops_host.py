@@ -145,6 +145,7 @@ def test_scratch_that_is_too_small(call, size, make):
     ("rc_delta_forward", delta, dict(batch=2 ** 24, heads=4)),
     ("rc_delta_forward", delta, dict(batch=2 ** 16, length=2 ** 13)),
     ("rc_delta_backward", delta, dict(batch=2 ** 16, length=2 ** 13)),
+    ("rc_delta_backward", delta, dict(batch=2 ** 15, length=2 ** 13, heads=1, key_heads=1, key=129)),
     ("rc_delta_step", step, dict(batch=2 ** 24, num_slots=2 ** 24)),
     ("rc_delta_step", step, dict(batch=2 ** 28, heads=32, num_slots=2 ** 28)),
     ("rc_delta_forward", delta, dict(batch=2 ** 31 - 1, heads=2 ** 31 - 2, length=2 ** 30)),
