@@ -123,6 +123,28 @@ struct Tile {
   }
 };
 
+// Of sixteen numbers the sum of number i over a row's 16 lanes, in lane i: each exchange halves the
+// numbers that a lane still has.
+__device__ __forceinline__ float sixteen_sums(const f32x4 (&x)[4]) {
+  const int i = threadIdx.x % 16;
+  float v[16];
+#pragma unroll
+  for (int j = 0; j < 16; j++) v[j] = x[j / 4][j % 4];
+  const auto halve = [&](auto ctrl, auto n) {
+    constexpr int N = decltype(n)::value;
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const float keep = i & N ? v[N + j] : v[j], give = i & N ? v[j] : v[N + j];
+      v[j] = keep + dpp_of<decltype(ctrl)::value>(give);
+    }
+  };
+  halve(std::integral_constant<int, 0x140>{}, std::integral_constant<int, 8>{});  // rows mirrored
+  halve(std::integral_constant<int, 0x141>{}, std::integral_constant<int, 4>{});  // half rows mirrored
+  halve(std::integral_constant<int, 0x4E>{}, std::integral_constant<int, 2>{});   // 2 apart
+  halve(std::integral_constant<int, 0xB1>{}, std::integral_constant<int, 1>{});   // 1 apart
+  return v[0];
+}
+
 // The gradients of a block's inputs from the state before it and the gradient of the one after
 // it, head by head of those that share a key head.  A wave has 16 NT of the key's channels (for narrow
 // keys a part of the block's tokens too).  Both states, do, v, w and dR pass through LDS, 32 columns at a
@@ -131,7 +153,7 @@ struct Tile {
 // is tiles spread over the waves, then in LDS for all of them.
 // Bound by waiting for loads and LDS (47% of a wave's time), with one workgroup of eight waves a compute
 // unit, which is what LDS and 256 registers allow; the matrix instructions are busy 16% of it: 64 heads of
-// 128 x 128, 32 blocks each, 227 us.  Blocks of 32 tokens, that read twice the states, took 414 where these took
+// 128 x 128, 32 blocks each, 215 us.  Blocks of 32 tokens, that read twice the states, took 414 where these took
 // 298; states read straight into operands 284, through LDS with a head's first loads before the last one's sums end, 253.
 template <class T, int KT>
 struct Inputs {
@@ -418,8 +440,17 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         f32x4 kv, qv;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          kv[e] = k.value(16 * mm + row + e, c);
-          qv[e] = q.value(16 * mm + row + e, c);
+          if (I::PARTS == 1) {                         // as a lane has them already
+            kv[e] = qv[e] = 0.f;
+#pragma unroll
+            for (int i = N - 1; i >= 0; i--) {
+              kv[e] += (float)kc[m / 2].p[i][m % 2 * 4 + e];
+              qv[e] += (float)qc[m / 2].p[i][m % 2 * 4 + e];
+            }
+          } else {
+            kv[e] = k.value(16 * mm + row + e, c);
+            qv[e] = q.value(16 * mm + row + e, c);
+          }
         }
         f32x4 &u = xq[n][m], &r = xr[n][m], &w = xw[n][m];
         u *= a.scale * *(const f32x4*)&since[16 * mm + row];
@@ -439,13 +470,7 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         }
         const f32x4 read = -*(const f32x4*)&beta[16 * mm + row] * r;
         const f32x4 dot[4] = {qv * u + kv * read, kv * w, kv * r, from_states};
-#pragma unroll
-        for (int d = 0; d < 4; d++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float s = lane_sum<16>(dot[d][e]);
-            if (col == 0) dots[wave * NT + n][d][16 * mm + row + e] = s;
-          }
+        dots[wave * NT + n][col / 4][16 * mm + row + col % 4] = sixteen_sums(dot);
         dq[n][m] += u;
         dk[n][m] += read + w;
       }

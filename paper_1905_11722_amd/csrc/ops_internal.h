@@ -81,9 +81,13 @@ __device__ __forceinline__ float softplus(float x) {
 }
 
 template <int CTRL>
+__device__ __forceinline__ float dpp_of(float x) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
-  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
-                                           0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+  return x + dpp_of<CTRL>(x);
 }
 // Sum over groups of 1, 2, 4 .. 64 lanes, in each of them (a mirror is as good as an
 // exchange once the lanes below are equal).
