@@ -38,6 +38,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cstddef>
 
 #include "ops_internal.h"
 
@@ -504,89 +505,116 @@ constexpr int kTogether = G::THREADS > 256 || kStages<T, KT, G> * sizeof(Stage<T
 
 // A loading wave's part of the chunks: the next one's share in registers.  Loads are
 // unconditional with addresses inside the sequence; what is past its end is dropped on the way to LDS.
-// WIDE: key and value are multiples of eight.
-template <class T, int KT, class G, bool WIDE>
+// WIDE: key and value are multiples of eight.  READS: q and P (P T) are needed, and not only keys and T.
+template <class T, int KT, class G, bool WIDE, bool READS>
 struct Feed {
   static constexpr int THREADS = G::LOADERS, VECTORS = kChunk * KT * 4, COLUMNS = G::COLUMNS;
   static constexpr int EACH = (VECTORS + THREADS - 1) / THREADS;
-  static constexpr int RAW = (kChunkVectors + THREADS - 1) / THREADS;
+  // a chunk's vectors, without P's
+  static constexpr int SKIP = READS ? 0 : sizeof(Chunk::p) / 16, SKIP_FROM = offsetof(Chunk, p) / 16;
+  static constexpr int RAW_VECTORS = kChunkVectors - SKIP, RAW = (RAW_VECTORS + THREADS - 1) / THREADS;
   static constexpr int PER_ROW = COLUMNS / 8, VECTORS_X = kChunk * PER_ROW;
   static constexpr int EACH_X = (VECTORS_X + THREADS - 1) / THREADS;
+  // Vector i of a thread is STEP (XSTEP) rows below the one before, in the same channels.
+  static constexpr int STEP = THREADS / (KT * 4), XSTEP = THREADS / PER_ROW;
+  static_assert(THREADS % (KT * 4) == 0 && THREADS % PER_ROW == 0, "whole rows");
   typedef T TV __attribute__((ext_vector_type(8)));
   TV k[EACH], q[EACH], x[EACH_X];
   u32x4 raw[RAW];
+  int thread, row, c, xrow, xc;
+  int64_t at_k, at_q, at_x;                            // the first vector's row (WIDE: and channel)
 
-  __device__ static int index(int i) { return threadIdx.x - G::WORKERS + i * THREADS; }
-  __device__ static int row_of(int i) { return index(i) / (KT * 4); }
-  __device__ static int channel_of(int i) { return index(i) % (KT * 4) * 8; }
-  __device__ static int xrow_of(int i) { return index(i) / PER_ROW; }
-  __device__ static int xcol_of(int i) { return index(i) % PER_ROW * 8; }
-
-  __device__ static void load(TV& to, const T* row, int c, int n) {
+  __device__ Feed(const rc_delta_args& a, const rc_heads& values, int col0) {
+    thread = threadIdx.x - G::WORKERS;
+    row = thread / (KT * 4);
+    c = thread % (KT * 4) * 8;
+    xrow = thread / PER_ROW;
+    xc = thread % PER_ROW * 8;
+    at_k = row * a.k.time + first(c, a.key);
+    at_q = row * a.q.time + first(c, a.key);
+    at_x = xrow * values.time + first(col0 + xc, a.value);
+  }
+  // The channel that a wide load begins at.
+  __device__ static int first(int c, int n) { return WIDE && c < n ? c : 0; }
+  __device__ int raw_of(int i) const {
+    const int v = min(thread + i * THREADS, RAW_VECTORS - 1);
+    return v < SKIP_FROM ? v : v + SKIP;
+  }
+  // From row `at` + `down` rows, or from the first one (which is always there).
+  __device__ static void load(TV& to, const T* from, bool there, int64_t at, int64_t down, int c, int n) {
+    from += there ? at + down : first(c, n);
     if (WIDE) {
-      __builtin_memcpy(&to, row + (c < n ? c : 0), sizeof(TV));
+      __builtin_memcpy(&to, from, sizeof(TV));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; e++) to[e] = row[min(c + e, n - 1)];
+      for (int e = 0; e < 8; e++) to[e] = from[min(c + e, n - 1)];
     }
   }
-  __device__ static void mask(TV& v, int r, int live, int c, int n) {
+  __device__ static void mask(TV& v, bool there, int c, int n) {
+    if (WIDE) {
+      if (!there || c >= n) v = TV(0);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = r < live && c + e < n ? v[e] : (T)0.f;
+      for (int e = 0; e < 8; e++) v[e] = there && c + e < n ? v[e] : (T)0.f;
+    }
   }
 
-  __device__ void fetch(const rc_delta_args& a, const Chunk& c, const rc_heads& values, int b, int h, int hk,
+  __device__ void fetch(const rc_delta_args& a, const Chunk& chunk, const rc_heads& values, int b, int h, int hk,
                         int t0, int live, int col0) {
     const T* from_k = at_head<T>(a.k, b, t0, hk);
     const T* from_q = at_head<T>(a.q, b, t0, hk);
     const T* from_x = at_head<T>(values, b, t0, h);
 #pragma unroll
     for (int i = 0; i < EACH; i++) {
-      const int r = min(row_of(i), live - 1);
-      load(k[i], from_k + r * a.k.time, channel_of(i), a.key);
-      load(q[i], from_q + r * a.q.time, channel_of(i), a.key);
+      const bool there = row + i * STEP < live;
+      load(k[i], from_k, there, at_k, i * STEP * a.k.time, c, a.key);
+      if (READS) load(q[i], from_q, there, at_q, i * STEP * a.q.time, c, a.key);
     }
 #pragma unroll
     for (int i = 0; i < EACH_X; i++)
-      load(x[i], from_x + min(xrow_of(i), live - 1) * values.time, col0 + xcol_of(i), a.value);
-    const u32x4* from = reinterpret_cast<const u32x4*>(&c);
+      load(x[i], from_x, xrow + i * XSTEP < live, at_x, i * XSTEP * values.time, col0 + xc, a.value);
+    const u32x4* from = reinterpret_cast<const u32x4*>(&chunk);
 #pragma unroll
-    for (int i = 0; i < RAW; i++) raw[i] = from[min(index(i), kChunkVectors - 1)];
+    for (int i = 0; i < RAW; i++) raw[i] = from[raw_of(i)];
   }
-  __device__ void put(Stage<T, KT, G>& to, int live, int key, int value, int col0) const {
-    const bool all = live == kChunk && key == 32 * KT && col0 + COLUMNS <= value;
+  // ALL: no row and no channel is past an end.
+  template <bool ALL>
+  __device__ void put_tokens(Stage<T, KT, G>& to, int live, int key) const {
 #pragma unroll
     for (int i = 0; i < EACH; i++) {
-      const int r = row_of(i), ch = channel_of(i);
+      const int r = row + i * STEP;
       if (VECTORS % THREADS && r >= kChunk) break;
-      TV u = k[i], v = q[i];
-      if (!all) {
-        mask(u, r, live, ch, key);
-        mask(v, r, live, ch, key);
-      }
-      if constexpr (kPieces<T> == 1) {
-        to.k.put(0, r, ch, u);
-        to.q.put(0, r, ch, v);
-      } else {
-        float y[8], z[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          y[e] = (float)u[e];
-          z[e] = (float)v[e];
+      for (int which = 0; which < (READS ? 2 : 1); which++) {
+        TV u = which ? q[i] : k[i];
+        auto& tokens = which ? to.q : to.k;
+        if (!ALL) mask(u, r < live, c, key);
+        if constexpr (kPieces<T> == 1) {
+          tokens.put(0, r, c, u);
+        } else {
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) y[e] = (float)u[e];
+          tokens.put(r, c, y);
         }
-        to.k.put(r, ch, y);
-        to.q.put(r, ch, z);
       }
     }
+  }
+  __device__ void put(Stage<T, KT, G>& to, int live, int key, int value, int col0) const {
+    if (live == kChunk && key == 32 * KT)
+      put_tokens<true>(to, live, key);
+    else
+      put_tokens<false>(to, live, key);
 #pragma unroll
     for (int i = 0; i < EACH_X; i++) {
-      if (VECTORS_X % THREADS && xrow_of(i) >= kChunk) break;
+      const int r = xrow + i * XSTEP;
+      if (VECTORS_X % THREADS && r >= kChunk) break;
       TV v = x[i];
-      if (!all) mask(v, xrow_of(i), live, col0 + xcol_of(i), value);
-      *(TV*)&to.x[xrow_of(i)][xcol_of(i)] = v;
+      mask(v, r < live, col0 + xc, value);
+      *(TV*)&to.x[r][xc] = v;
     }
 #pragma unroll
-    for (int i = 0; i < RAW; i++) to.raw[min(index(i), kChunkVectors - 1)] = raw[i];
+    for (int i = 0; i < RAW; i++) to.raw[raw_of(i)] = raw[i];
   }
 };
 
@@ -645,7 +673,8 @@ __device__ __forceinline__ void load_chunks(const DeltaParams& p, const Walk<G, 
   if (!at.count) return;
   const Chunk* prepared = p.prepared + (int64_t)at.bh * p.chunks;
   const int columns = at.diagonal ? 0 : a.value;       // of values: a walk from the diagonal has none
-  Feed<T, KT, G, WIDE> next;
+  // (the gradient of the states takes both)
+  Feed<T, KT, G, WIDE, BACK || MODE == kWhole> next(a, values, at.col0);
   const auto chunk_of = [&](int i) { return at.first + (BACK ? at.count - 1 - i : i); };
   const auto live_of = [&](int c) { return min(at.end - c * kChunk, kChunk); };
   const auto fetch = [&](int i) {
