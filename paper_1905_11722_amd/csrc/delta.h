@@ -25,7 +25,9 @@
 //   dq_i = scale exp(G_i) S do_i + sum_j M_ij k_j
 //   x_i = exp(G_i) S dR_i + sum_j N_ij k_j,    dbeta_i = dR_i . v_i - k_i . x_i
 //   dk_i = -beta_i x_i (as read) + exp(G_31 - G_i) E w_i + sum_l (M_li q_l - beta_l N_li k_l) (as written)
-//   dG_i = q_i . dq_i + k_i . (dk_i as read - as written),  dG_31 += <E, S'>,
+//   dG_i = q_i . dq_i + k_i . (dk_i as read - as written)  (= the states' parts of it
+//          + sum_j Z_ij - sum_l Z_li, Z_ij = M_ij q_i . k_j - beta_i N_ij k_i . k_j, j < i),
+//   dG_31 += <E, S'>,
 //   dg_t = sum of dG_i over i >= t.
 //
 // Products run on the bf16 matrix instructions with operands taken apart into bf16 numbers that
@@ -858,17 +860,19 @@ inline int fits_back(const rc_delta_args& a) {
   return launchable((int64_t)a.batch * a.heads / heads_together(a) * blocks_of(a), 512) ? RC_OK : RC_E_OVERFLOW;
 }
 // Segments of the length: more than one where the walks over the segments' ends (of values' and
-// key columns, one segment fewer) fit the compute units at once and each segment has eight chunks
-// (sixteen of the widest keys, whose joins take longer).  Cutting costs those walks, and a
-// step a segment that joins them: with fewer than three segments it never gained.
-// 8192 tokens of 128 x 128, 16, 8, 4 heads and one: 452, 430, 427, 423 us in one, in 3, 5, 8 and 16
-// segments 311, 203, 148, 125; 2048 tokens of 16 and 4 heads: 123, 119 us, in 3 and 8 segments
-// 104, 73; 2 x 16 heads 130, in 3 segments 177.
+// key columns, one segment fewer) and those over the segments fit the compute units at once and each
+// segment has eight chunks (sixteen of the widest keys, whose joins take longer).  Cutting costs those
+// walks, and a step a segment that joins them: two segments gain from 128 chunks and keys of 65 to
+// 128 on, not for others.  Forward, all kernels, bf16 heads of 128 x 128, us in one segment and in as many as
+// this gives: 8192 tokens of 32, 24, 16 and 4 heads 444, 426, 425, 401 and in 2, 2, 3, 9 423, 395, 273, 132;
+// 2048 tokens of 16 heads 113, in 3 92 (32 heads in one: 119, in 2 122).
 inline int segments_of(const rc_delta_args& a) {
-  const int rows = rows_of(a.key);
-  const int64_t walks = (int64_t)a.batch * a.heads * (cdiv(a.value, 32) + rows / 32);
-  const int64_t fit = 1 + (rows <= 64 ? 512 : 256) / walks, most = chunks_of(a) / (rows > 128 ? 16 : 8);
-  const int64_t n = std::min<int64_t>({fit, most, 16});
+  const int rows = rows_of(a.key), room = rows <= 64 ? 512 : 256;
+  const int64_t values = (int64_t)a.batch * a.heads * cdiv(a.value, 32);
+  const int64_t ends = values + (int64_t)a.batch * a.heads * (rows / 32);
+  const int64_t most = chunks_of(a) / (rows > 128 ? 16 : 8);
+  const int64_t n = std::min<int64_t>({1 + room / ends, room / values, most, 16});
+  if (n == 2 && rows == 128 && chunks_of(a) >= 128) return 2;
   return n < 3 ? 1 : (int)n;
 }
 inline uint64_t segment_floats(const rc_delta_args& a) {

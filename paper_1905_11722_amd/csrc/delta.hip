@@ -14,7 +14,7 @@ namespace {
 // the other, with one or two waves a SIMD.  Waves of columns x parts of the key of 128, timed when the
 // same waves loaded and computed, us a chunk: 2 x 2 2.5, 2 x 4 2.7, 4 x 1 and 4 x 2 2.9, 4 x 4 3.6; with waves that only
 // load 1.75.  64 chunks of 64 heads of 128 x 128 with states kept (4 x 2048 tokens): 122 us; a prompt of
-// 8192 tokens, 16 heads, in three segments: 131 us for their ends, 9 to join them, 141 for the outputs.
+// 8192 tokens, 16 heads, in three segments: 104 us for their ends, 9 to join them, 141 for the outputs.
 template <class T, int KT, class G, bool WIDE, int MODE>
 __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;

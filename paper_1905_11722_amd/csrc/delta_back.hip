@@ -150,10 +150,13 @@ __device__ __forceinline__ float sixteen_sums(const f32x4 (&x)[4]) {
 // keys a part of the block's tokens too).  Both states, do, v, w and dR pass through LDS, 32 columns at a
 // time and one time ahead in registers; where LDS has no room for the states a wave reads its part
 // of them straight into operands, a number a load (which is what bounds it then).  What is between tokens (M, N and dR . v)
-// is tiles spread over the waves, then in LDS for all of them.
+// is tiles spread over the waves, then in LDS for all of them.  Pairs of tokens (i, j) reach dg through
+// Z_ij = M_ij q_i . k_j - beta_i N_ij k_i . k_j, whose sums by i and by j are added in 64 bits: what two tokens
+// past t have with each other leaves dg_t as the same number as it came, and not as two roundings of it.
 // Bound by waiting for loads and LDS (47% of a wave's time), with one workgroup of eight waves a compute
 // unit, which is what LDS and 256 registers allow; the matrix instructions are busy 16% of it: 64 heads of
-// 128 x 128, 32 blocks each, 215 us.  Blocks of 32 tokens, that read twice the states, took 414 where these took
+// 128 x 128, 32 blocks each, 246 us (215 with dg from dots of dq and dk, whose roundings
+// reached 2e-5 of dg over 64 tokens).  Blocks of 32 tokens, that read twice the states, took 414 where these took
 // 298; states read straight into operands 284, through LDS with a head's first loads before the last one's sums end, 253.
 template <class T, int KT>
 struct Inputs {
@@ -186,8 +189,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
     __device__ Shared() {}
   } lds;
   __shared__ double sums[BLOCK];
-  __shared__ float since[BLOCK], left[BLOCK], beta[BLOCK], dot_v[BLOCK], dots[WAVES * NT][4][BLOCK],
-      inner[WAVES];
+  __shared__ float since[BLOCK], left[BLOCK], beta[BLOCK], dot_v[BLOCK], dots[WAVES * NT][3][BLOCK],
+      inner[WAVES], of_rows[2 * I::TRIANGLE][16], of_columns[2 * I::TRIANGLE][16];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 16, row = lane / 16 * 4;
   const int groups = a.heads / p.each, bg = blockIdx.x / p.blocks, block = blockIdx.x % p.blocks;
   const int b = bg / groups, group = bg % groups, hk = group * p.each / (a.heads / a.key_heads);
@@ -393,13 +396,27 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         const bool of_m = n < I::TRIANGLE;
         const Tile at(of_m ? n : n - I::TRIANGLE);
         const int ti = 16 * at.i + col;
-        f32x4 v;
+        const auto& reads = of_m ? q : k;
+        f32x4 v, z = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < KT; s++) mul(z, k.rows(at.j, s), reads.rows(at.i, s));
+        const float by = of_m ? 1.f : -beta[ti];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const int tj = 16 * at.j + row + e;
           v[e] = (of_m ? tj <= ti : tj < ti) ? (of_m ? a.scale : 1.f) * decay_between(sums[ti] - sums[tj]) * task[i][e] : 0.f;
+          z[e] = tj < ti ? by * v[e] * z[e] : 0.f;
         }
         (of_m ? between.m : between.n).put_four(ti, 16 * at.j + row, v);
+        const float of_row = add_32_apart(add_16_apart((z[0] + z[1]) + (z[2] + z[3])));
+        float of_column = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float s = lane_sum<16>(z[e]);
+          if (col == e) of_column = s;
+        }
+        if (row == 0) of_rows[n][col] = of_row;
+        if (col < 4) of_columns[n][row + col] = of_column;
       } else if (n < I::TASKS) {
         const int m = n - 2 * I::TRIANGLE;
 #pragma unroll
@@ -456,7 +473,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         u *= a.scale * *(const f32x4*)&since[16 * mm + row];
         r *= *(const f32x4*)&since[16 * mm + row];
         w *= *(const f32x4*)&left[16 * mm + row];
-        const f32x4 from_states = kv * w;
+        const f32x4 minus_beta = -*(const f32x4*)&beta[16 * mm + row];
+        f32x4 dot[4] = {qv * u + kv * (minus_beta * r), kv * w, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
         for (int s = 0; s < STEPS; s++) {
           if (s <= mm / 2) {
@@ -468,25 +486,40 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
             mul(w, between.n.columns(mm, s), kb[s]);
           }
         }
-        const f32x4 read = -*(const f32x4*)&beta[16 * mm + row] * r;
-        const f32x4 dot[4] = {qv * u + kv * read, kv * w, kv * r, from_states};
-        dots[wave * NT + n][col / 4][16 * mm + row + col % 4] = sixteen_sums(dot);
+        dot[2] = kv * r;
+        const float s = sixteen_sums(dot);
+        if (col < 12) dots[wave * NT + n][col / 4][16 * mm + row + col % 4] = s;
         dq[n][m] += u;
-        dk[n][m] += read + w;
+        dk[n][m] += minus_beta * r + w;
       }
     }
     enter(min(h + 1, (group + 1) * p.each - 1));       // (unconditional, as every load that a loop hands on)
     __syncthreads();
     // dg and dbeta by the last wave, while the others begin the next head
     if (wave == WAVES - 1 && lane < BLOCK) {
-      float s[4] = {0, 0, 0, 0};
+      float s[3] = {0, 0, 0};
 #pragma unroll
       for (int w = 0; w < WAVES; w += I::PARTS)
 #pragma unroll
         for (int n = 0; n < NT; n++)
 #pragma unroll
-          for (int d = 0; d < 4; d++) s[d] += dots[(w + lane / 16 / MT) * NT + n][d][lane];
+          for (int d = 0; d < 3; d++) s[d] += dots[(w + lane / 16 / MT) * NT + n][d][lane];
       double dG = (double)s[0] - s[1], ends = 0;
+      const int own = lane / 16, t = lane % 16;
+      float pairs[I::TILES][4];
+#pragma unroll
+      for (int j = 0; j < I::TILES; j++) {
+        const int lo = min(j, own), hi = max(j, own), r = own * (own + 1) / 2 + lo, c = hi * (hi + 1) / 2 + own;
+        pairs[j][0] = of_rows[r][t];
+        pairs[j][1] = of_rows[I::TRIANGLE + r][t];
+        pairs[j][2] = of_columns[c][t];
+        pairs[j][3] = of_columns[I::TRIANGLE + c][t];
+      }
+#pragma unroll
+      for (int j = 0; j < I::TILES; j++) {
+        if (j <= own) dG += (double)pairs[j][0] + pairs[j][1];
+        if (j >= own) dG -= (double)pairs[j][2] + pairs[j][3];
+      }
 #pragma unroll
       for (int d = 1; d < BLOCK; d *= 2) {
         const double after = __shfl_down(dG, d, BLOCK);
@@ -494,7 +527,7 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       }
 #pragma unroll
       for (int w = 0; w < WAVES; w++) ends += (double)inner[w];
-      const double total = (double)lane_sum<BLOCK>(s[3]) + whole * ends;
+      const double total = (double)lane_sum<BLOCK>(s[1]) + whole * ends;
       const int64_t at = ((int64_t)b * a.length + t0 + lane) * a.heads + h;
       if (lane < here) {
         if (a.dg) a.dg[at] = lane < live ? (float)(dG + total) : 0.f;

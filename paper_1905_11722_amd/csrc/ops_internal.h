@@ -89,6 +89,17 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
   return x + dpp_of<CTRL>(x);
 }
+// Sum of each lane's with that of the lane 16 (32) away.
+__device__ __forceinline__ float add_16_apart(float x) {
+  const unsigned a = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ __forceinline__ float add_32_apart(float x) {
+  const unsigned a = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
 // Sum over groups of 1, 2, 4 .. 64 lanes, in each of them (a mirror is as good as an
 // exchange once the lanes below are equal).
 template <int LANES>
@@ -102,13 +113,8 @@ __device__ __forceinline__ float lane_sum(float x) {
   if (LANES == 8) return x;
   x = dpp_add<0x140>(x);                               // rows mirrored
   if (LANES == 16) return x;
-  const unsigned a = __builtin_bit_cast(unsigned, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
-  if (LANES == 32) return x;
-  const unsigned b = __builtin_bit_cast(unsigned, x);
-  const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
+  x = add_16_apart(x);
+  return LANES == 32 ? x : add_32_apart(x);
 }
 
 // An element of a (batch, time, head, channel) tensor.

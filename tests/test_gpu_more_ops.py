@@ -95,6 +95,24 @@ def test_delta(case):
     compare_grads(x, outs, wants)
 
 
+def test_delta_two_segments():
+    """The least length that is cut in two; the plain form's 4100 steps run on the GPU too, in 64 bits."""
+    x, ends = delta_inputs("bf16", 2, 4100, 8, 16, 66, 97, "gs"), (4100, 2000)
+    with torch.no_grad():
+        for n in ("q", "k", "v", "g", "beta"):
+            x.gpu[n][1, ends[1]:] = float("nan")
+            x.cpu[n][1, ends[1]:] = 0
+    x.grads()
+    names = ("q", "k", "v", "g", "beta")
+    outs = ops.gated_delta(*[x.gpu[n] for n in names], state=x.gpu["state"], lengths=int32(ends), return_state=True)
+    with torch.device(DEV):
+        wants = ref.gated_delta(*[x.cpu[n].to(DEV) for n in names], state=x.cpu["state"].to(DEV), lengths=ends)
+    wants = [w.cpu() for w in wants]
+    for n, o, w in zip(("o", "state"), outs, wants):
+        check(o, w, n)
+    compare_grads(x, outs, wants)
+
+
 @pytest.mark.parametrize("batch,length,key_heads,heads", [(64, 512, 1, 2), (16, 500, 2, 8)])
 def test_delta_heads_that_share_a_key_head(batch, length, key_heads, heads):
     """So many blocks that one workgroup has all of a key head's heads, or some of them."""
