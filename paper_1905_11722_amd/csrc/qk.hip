@@ -236,7 +236,8 @@ __global__ __launch_bounds__(kThreads) void k_qk_backward(QkParams p) {
         s = fmaf(v, v, s);
         d = fmaf(e[j / kPairs][j % kPairs] * w[j / kPairs][j % kPairs], v, d);
       }
-      const float r = norm_of(a, lane_sum<L>(s));
+      // (without eps a padded token's zeros would have no norm, and no share of the weights' sums)
+      const float size = lane_sum<L>(s), r = live ? norm_of(a, size) : 0.f;
       d = lane_sum<L>(d) * r;                          // e w . u
       if (a.norm == RC_QK_RMS) d /= (float)a.channels;
       if (a.norm == RC_QK_NONE) d = 0.f;
