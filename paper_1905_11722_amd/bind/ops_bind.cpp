@@ -919,6 +919,7 @@ variable_list qk_norm(const Tensor& q, const Tensor& k, const Opt& qw, const Opt
   if (t.positions.defined()) expect("positions", t.positions, {q.size(0), q.size(1)}, at::kInt, q);
   t.lengths = lengths_of(lengths, q);
   const bool grad = differentiated({&q, &k, &t.qw, &t.kw});
+  if (t.positions.defined()) t.positions = plain(t.positions);
   t = {rows(q), rows(k), dense(t.qw), dense(t.kw), dense(t.freq), t.positions, t.lengths};
   if (grad)
     return Qk::apply(t.q, t.k, opt(t.qw), opt(t.kw), opt(t.freq), opt(t.positions), opt(t.lengths), norm,
@@ -993,7 +994,8 @@ struct Dropout : torch::autograd::Function<Dropout> {
 Tensor dropout(const Tensor& x, double p, const Opt& seed_, int64_t number, int64_t tag,
                const Opt& residual_) {
   activations("x", x);
-  const Tensor residual = given(residual_), seed = given(seed_);
+  const Tensor residual = given(residual_);
+  Tensor seed = given(seed_);
   TORCH_CHECK_VALUE(p >= 0 && p <= 1, "p must be from 0 to 1, not ", p);
   if (residual.defined())
     expect("residual", residual, x.sizes(),
@@ -1001,6 +1003,7 @@ Tensor dropout(const Tensor& x, double p, const Opt& seed_, int64_t number, int6
   if (seed.defined()) {
     TORCH_CHECK_VALUE(seed.numel() == 1, "seed must be one number, not ", seed.sizes());
     expect("seed", seed, seed.sizes(), at::kLong, x);
+    seed = plain(seed);
   }
   if (differentiated({&x, &residual})) return Dropout::apply(x, opt(residual), opt(seed), number, tag, p);
   return dropout_forward(x, residual, seed, number, tag, p);

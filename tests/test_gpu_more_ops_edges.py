@@ -1,4 +1,5 @@
-"""The linear-attention operators off the usual ground: no eps under a root beside padded tokens."""
+"""The linear-attention operators off the usual ground: no eps under a root beside padded tokens, views that
+negate."""
 
 import pytest
 import torch
@@ -35,3 +36,20 @@ def test_qk_without_eps_beside_padded_tokens(dtype, channels, rotated, norm):
     for n, o, w in zip("qk", outs, wants):
         check(o, w, n)
     compare_grads(x, outs, wants)
+
+
+# ------------------------------------------------------------ views that negate
+
+
+def test_positions_and_seeds_that_negate():
+    """Lazily negated views of whole numbers are taken at their values too."""
+    x, freq = torch.randn(2, 5, 2, 8, device=DEV), torch.rand(4, device=DEV)
+    at = torch.randint(1, 99, (2, 5), dtype=torch.int32, device=DEV)
+    for a, b in zip(ops.qk_norm(x, x, None, None, freq, torch._neg_view(at)), ops.qk_norm(x, x, None, None, freq, -at)):
+        assert torch.equal(a, b)
+    seed = torch.tensor([5], device=DEV)
+    x.requires_grad_()
+    a, b = ops.dropout(x, 0.5, torch._neg_view(seed)), ops.dropout(x, 0.5, -5)
+    assert torch.equal(a, b)
+    for a, b in zip(*[torch.autograd.grad(y, x, torch.ones_like(y)) for y in (a, b)]):
+        assert torch.equal(a, b)
