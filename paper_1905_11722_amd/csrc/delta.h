@@ -37,6 +37,11 @@
 // the gradients of g and beta are 32-bit outputs: pieces left off (two for 32 bits) would show in them.
 // D's exponents are differences of sums in 64 bits, so a token that forgets everything costs the
 // later ones nothing.  (Chunks of 64 take as many matrix instructions a token and twice the registers.)
+//
+// A number that is not finite reaches what the formulas at the top let it reach, as NaN: its own token and
+// those after it.  A matrix product would hand it to the whole chunk, for 0 times NaN is NaN: where one is
+// found, which costs a compare and a branch a chunk (2 us of the 122 of 64 chunks), the product runs again
+// without it and the rows that it belongs to are set to NaN.
 #pragma once
 
 #include <algorithm>
@@ -90,6 +95,10 @@ __device__ __forceinline__ Pieces<N> split(const float (&v)[8]) {
   for (int i = 0; i < N; i++) s.p[i] = __builtin_bit_cast(bf16x8, w[i]);
   return s;
 }
+
+// Whether x is a number that pieces hold: not infinity, not NaN, nor so near the largest that its first
+// piece is rounded to infinity.
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) < 0x1.ffp127f; }
 
 // acc += A B for 16 x 32 by 32 x 16, the smallest products of pieces first.  A lane holds 8
 // numbers of row (column) lane % 16; which 8 of the 32 is free as long as both sides agree.
@@ -272,11 +281,9 @@ __device__ __forceinline__ double log_decay(const rc_view& g, int64_t b, int64_t
   const float x = at_token(g, b, t, h);
   return x < -1000.f ? -1000.0 : (double)x;
 }
-// G of a chunk's 32 tokens (in every lane's token lane % 32): sums from its first token.
-__device__ __forceinline__ double sum_of_g(const rc_delta_args& a, int b, int h, int t0, int live) {
+// G of a chunk's 32 tokens (in every lane's token lane % 32) from their g: sums from its first token.
+__device__ __forceinline__ double sum_of_g(double G) {
   const int i = threadIdx.x % 32;
-  double G = 0;
-  if (a.g.data && i < live) G = log_decay(a.g, b, t0 + i, h);
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
     const double before = __shfl_up(G, d, 32);
@@ -326,11 +333,15 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     return split<N>(v);
   };
   Chunk& out = p.prepared[blockIdx.x];
-  const double G = sum_of_g(a, b, h, t0, live);
+  // (a g that is no number leaves the sums as they are, for those of the tokens on either side of it, and has its
+  // token's beta say so)
+  const double g = a.g.data && lane % 32 < live ? log_decay(a.g, b, t0 + lane % 32, h) : 0.0;
+  const bool decays = g < __builtin_inf();
+  const double G = sum_of_g(decays ? g : 0.0);
   if (lane < kChunk) {
     const double last = __shfl(G, kChunk - 1);
     sums[lane] = G;
-    beta[lane] = lane < live ? at_token(a.beta, b, t0 + lane, h) : 0.f;
+    beta[lane] = lane >= live ? 0.f : decays ? at_token(a.beta, b, t0 + lane, h) : __builtin_nanf("");
     out.since[lane] = exp_of(G);
     out.left[lane] = exp_of(last - G);
     out.beta[lane] = beta[lane];
@@ -356,6 +367,7 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
       }
   }
   const int col = lane % 16, row = lane / 16 * 4;
+  bool odd = false;                                    // a number of A is not finite
 #pragma unroll
   for (int m = 0; m < 2; m++)
 #pragma unroll
@@ -365,10 +377,29 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
         const int i = 16 * n + col, j = 16 * m + row + r;
         // (the decay of the later of the two, whichever of them that is)
         const float d = m <= n || BACK ? decay_between(j <= i ? sums[i] - sums[j] : sums[j] - sums[i]) : 0.f;
-        if (m <= n) A[i][j] = j < i ? beta[i] * d * kk[m][n][r] : 0.f;
+        if (m <= n) {
+          const float x = j < i ? beta[i] * d * kk[m][n][r] : 0.f;
+          A[i][j] = x;
+          odd |= !is_finite(x);
+        }
         qk[m][n][r] = (BACK ? i <= j : j <= i) ? a.scale * d * qk[m][n][r] : 0.f;
       }
   __syncthreads();
+  // Such numbers count as 0 here, and T_ic is set to NaN below for c up to `upto`: where on the way from token c to
+  // token i there is one, whatever it is multiplied with.
+  odd = __any(odd);
+  int upto = -1;                                       // of row lane % 32
+  if (odd) {
+    for (int j = 0; j < lane % 32; j++)
+      if (!is_finite(A[lane % 32][j])) upto = j;
+    for (int j = 0; j <= upto; j++)
+      if (!is_finite(A[lane % 32][j])) A[lane % 32][j] = 0.f;
+    for (int d = 1; d < 32; d *= 2) {
+      const int before = __shfl_up(upto, d, 32);
+      if (lane % 32 >= d) upto = max(upto, before);
+    }
+    __syncthreads();
+  }
   // T of the two diagonal tiles, a column a lane, by forward substitution
   {
     const int first = lane % 32 / 16 * 16;
@@ -401,6 +432,10 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int e = 0; e < 4; e++) (step ? inverse : A)[16 + row + e][col] = s[e];
     __syncthreads();
   }
+  if (odd) {
+    for (int j = 0; lane < kChunk && j <= upto; j++) inverse[lane][j] = __builtin_nanf("");
+    __syncthreads();
+  }
   Pieces<3> between[2];
 #pragma unroll
   for (int n = 0; n < 2; n++) between[n] = operand<3>(qk[0][n], qk[1][n]);
@@ -419,10 +454,15 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int i = 0; i < 3; i++) out.t[n][i][lane] = f.p[i];
     if (!BACK) {
       // columns n of P T, transposed: rows of it are what its operand has in a lane
+      if (odd) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = is_finite(y[e]) ? y[e] : 0.f;
+      }
       const Pieces<3> columns = split<3>(y);
 #pragma unroll
       for (int m = 0; m < 2; m++) {
-        pt[n][m] = f32x4{0, 0, 0, 0};
+        const float from = odd && __shfl(upto, 16 * m + col) >= 0 ? __builtin_nanf("") : 0.f;
+        pt[n][m] = f32x4{from, from, from, from};
         mul(pt[n][m], columns, between[m]);
       }
     }
@@ -619,6 +659,17 @@ struct Feed {
     for (int i = 0; i < RAW; i++) to.raw[raw_of(i)] = raw[i];
   }
 };
+
+// The first row of a chunk with a number that is not finite in this lane's column (kChunk: none); a lane
+// has rows row + 0..3 and 16 + row + 0..3.
+__device__ __forceinline__ int first_odd(const f32x4 (&x)[2], int row) {
+  int at = kChunk;
+#pragma unroll
+  for (int i = 7; i >= 0; i--)
+    if (!is_finite(x[i / 4][i % 4])) at = i / 4 * 16 + row + i % 4;
+  at = min(at, __shfl_xor(at, 16));
+  return min(at, __shfl_xor(at, 32));
+}
 
 __device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {
   const int lane = threadIdx.x % 64;

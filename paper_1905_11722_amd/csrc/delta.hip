@@ -79,9 +79,23 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     }
 #pragma unroll
     for (int m = 0; m < 2; m++) r[m] = beta[m] * (x[m] - since[m] * r[m]);
-    const Pieces<3> rs = operand<3>(r[0], r[1]);
+    Pieces<3> rs = operand<3>(r[0], r[1]);
 #pragma unroll
     for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
+    // r of one token that is not finite has made all of its column's w NaN: those before it again
+    if (MODE == kWhole && __any(w[0][0] != w[0][0])) {
+      const int from = first_odd(r, row);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const bool there = i / 4 * 16 + row + i % 4 < from;
+        r[i / 4][i % 4] = there ? r[i / 4][i % 4] : 0.f;
+        w[i / 4][i % 4] = there ? 0.f : __builtin_nanf("");
+        since[i / 4][i % 4] = there ? since[i / 4][i % 4] : __builtin_nanf("");      // the outputs' factor
+      }
+      rs = operand<3>(r[0], r[1]);
+#pragma unroll
+      for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
+    }
     const Pieces<3> us = operand<3>(w[0] * left[0], w[1] * left[1]);
     const float whole = c.since[kChunk - 1];
 #pragma unroll

@@ -1,5 +1,5 @@
 """The linear-attention operators off the usual ground: no eps under a root beside padded tokens, views that
-negate."""
+negate, numbers that are not finite beside those that are."""
 
 import pytest
 import torch
@@ -53,3 +53,55 @@ def test_positions_and_seeds_that_negate():
     assert torch.equal(a, b)
     for a, b in zip(*[torch.autograd.grad(y, x, torch.ones_like(y)) for y in (a, b)]):
         assert torch.equal(a, b)
+
+
+# ------------------------------------------------------ numbers that are not finite
+
+WILD = [  # dtype, batch, length, key_heads, heads, key, value, the token
+    ("f32", 2, 100, 1, 2, 24, 20, 0), ("f32", 2, 100, 1, 2, 24, 20, 5), ("f32", 2, 100, 2, 2, 24, 20, 40),
+    ("f32", 2, 100, 1, 2, 24, 20, 99), ("bf16", 2, 100, 1, 2, 24, 20, 17), ("bf16", 2, 100, 1, 2, 128, 64, 31),
+    ("bf16", 1, 100, 1, 2, 128, 64, 63), ("f16", 1, 100, 1, 1, 64, 40, 64), ("f16", 2, 70, 1, 2, 128, 40, 20),
+    ("f32", 1, 70, 1, 2, 200, 33, 37), ("bf16", 1, 70, 1, 2, 256, 72, 50), ("bf16", 1, 800, 1, 2, 64, 64, 500),
+]
+
+
+def wild_inputs(case, of, value):
+    """(inputs, gradients of the outputs) with one number of `of` replaced."""
+    *sizes, at = case
+    x = usual.delta_inputs(*sizes, "gs")
+    rng = torch.Generator().manual_seed(7)
+    given = {"do": torch.randn(x.cpu["v"].shape, generator=rng).to(x.dtype),
+             "dstate": torch.randn(x.cpu["state"].shape, generator=rng)}
+    place = {"q": (0, at, 0, 3), "k": (0, at, 0, 3), "v": (0, at, 1 % sizes[4], 5), "g": (0, at, 0),
+             "beta": (0, at, 0), "state": (0, 0, 3, 5), "do": (0, at, 0, 5), "dstate": (0, 0, 3, 5)}[of]
+    for t in ([given[of]] if of in given else [x.gpu[of], x.cpu[of]]):
+        t[place] = value
+    return x, given
+
+
+def wild_values(of):
+    """(Infinity is not a decay, and its negative is one.)"""
+    return [float("nan")] + [float("inf"), -float("inf")] * (of != "g")
+
+
+def leaves_the_rest(got, want, own, what):
+    """Not finite where `want` is not, and within the usual bound of it elsewhere; token `own` of the first sequence (None: no
+    token) may be NaN."""
+    got, want = got.detach().cpu(), want.detach()
+    finite = want.isfinite()
+    assert not got[~finite].isfinite().any(), what
+    if own is not None:
+        finite[0, own] = False
+    check(got[finite], want[finite], what)
+
+
+@pytest.mark.parametrize("of", ["q", "k", "v", "g", "beta", "state"])
+@pytest.mark.parametrize("case", WILD, ids=lambda c: "-".join(map(str, c)))
+def test_delta_outputs_beside_a_number_that_is_not_finite(case, of):
+    """What depends on it by the definition, token by token in 64 bits, is not finite either, and all the rest is
+    what it is."""
+    for value in wild_values(of):
+        x, _ = wild_inputs(case, of, value)
+        (o, end), (want_o, want_end) = usual.run_delta(x)
+        leaves_the_rest(o, want_o, None if of == "state" else case[-1], f"o, {value}")
+        leaves_the_rest(end, want_end, None, f"state, {value}")
