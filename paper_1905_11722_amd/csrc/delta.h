@@ -39,9 +39,9 @@
 // later ones nothing.  (Chunks of 64 take as many matrix instructions a token and twice the registers.)
 //
 // A number that is not finite reaches what the formulas at the top let it reach, as NaN: its own token and
-// those after it.  A matrix product would hand it to the whole chunk, for 0 times NaN is NaN: where one is
-// found, which costs a compare and a branch a chunk (2 us of the 122 of 64 chunks), the product runs again
-// without it and the rows that it belongs to are set to NaN.
+// those after it, gradients of those before it where they go through its state.  A matrix product would hand it to the
+// whole chunk, for 0 times NaN is NaN: where one is found, which costs a compare and a branch a chunk (2 us of the
+// 122 of 64 chunks forward), the product runs again without it and the rows that it belongs to are set to NaN.
 #pragma once
 
 #include <algorithm>
@@ -154,13 +154,15 @@ struct Tokens {
   __device__ static int place(int c) {
     return PAIRED ? c / 32 * 32 + c % 16 / 4 * 8 + c % 32 / 16 * 4 + c % 4 : c;
   }
-  // From rows `row` elements apart; what is past `live` tokens or `n` channels is 0.
+  // From rows `row` elements apart; what is past `live` tokens or `n` channels, or not finite, is 0.
   template <class T>
   __device__ void load(const T* x, int64_t row, int live, int n, int thread, int threads) {
     for (int i = thread; i < ROWS * KT * 4; i += threads) {
       const int r = i / (KT * 4), c = i % (KT * 4) * 8;
       float v[8];
       load_vec<8>(x + (r < live ? r : 0) * row + (c < n ? c : 0), r < live ? n - c : 0, v);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = is_finite(v[e]) ? v[e] : 0.f;
       put(r, c, v);
     }
   }
@@ -669,6 +671,16 @@ __device__ __forceinline__ int first_odd(const f32x4 (&x)[2], int row) {
     if (!is_finite(x[i / 4][i % 4])) at = i / 4 * 16 + row + i % 4;
   at = min(at, __shfl_xor(at, 16));
   return min(at, __shfl_xor(at, 32));
+}
+
+// The last one (-1: none).
+__device__ __forceinline__ int last_odd(const f32x4 (&x)[2], int row) {
+  int at = -1;
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    if (!is_finite(x[i / 4][i % 4])) at = i / 4 * 16 + row + i % 4;
+  at = max(at, __shfl_xor(at, 16));
+  return max(at, __shfl_xor(at, 32));
 }
 
 __device__ __forceinline__ Pieces<3> pieces(const bf16x8 (&x)[3][64]) {

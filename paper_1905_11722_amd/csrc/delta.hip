@@ -84,6 +84,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
     for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
     // r of one token that is not finite has made all of its column's w NaN: those before it again
     if (MODE == kWhole && __any(w[0][0] != w[0][0])) {
+      asm volatile("" ::: "memory");                   // (T is read again, and not held for this)
       const int from = first_odd(r, row);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_for
       }
       rs = operand<3>(r[0], r[1]);
 #pragma unroll
-      for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
+      for (int m = 0; m < 2; m++) mul(w[m], pieces(c.t[m]), rs);
     }
     const Pieces<3> us = operand<3>(w[0] * left[0], w[1] * left[1]);
     const float whole = c.since[kChunk - 1];

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
     if (keeps && (chunk == last_chunk || chunk % EVERY == EVERY - 1))
       keep_state(p.dstates + ((int64_t)at.bh * p.blocks + chunk / EVERY) * (columns_of(a.value) * 32 * KT),
                  32 * KT, at.col, first_row, E);
-    f32x4 dw[2], dr[2], g[2];
+    f32x4 dw[2], dr[2], g[2], of_state[2];
 #pragma unroll
     for (int m = 0; m < 2; m++) dw[m] = dr[m] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -75,10 +75,40 @@ __global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_sta
       for (int m = 0; m < 2; m++) dw[m] = parts.sum(m, at.wave);
     }
 #pragma unroll
-    for (int m = 0; m < 2; m++) dw[m] = dw[m] * left[m] + from_o[m];
+    for (int m = 0; m < 2; m++) {
+      of_state[m] = dw[m] * left[m];
+      dw[m] = of_state[m] + from_o[m];
+    }
     const Pieces<3> dws = operand<3>(dw[0], dw[1]);
 #pragma unroll
     for (int m = 0; m < 2; m++) mul(dr[m], t[m], dws);
+    // do or dW of one token that is not finite has made all of its column's dR NaN: those after it again
+    if (MODE == kWhole && __any(dr[0][0] != dr[0][0])) {
+      asm volatile("" ::: "memory");                   // (what is in LDS is read again, and not held for this)
+#pragma unroll
+      for (int i = 0; i < 8; i++) g[i / 4][i % 4] = (float)stage.x[i / 4 * 16 + row + i % 4][at.col - at.col0];
+      int upto = last_odd(g, row);
+#pragma unroll
+      for (int i = 0; i < 8; i++) g[i / 4][i % 4] = is_finite(g[i / 4][i % 4]) ? g[i / 4][i % 4] : 0.f;
+      const Pieces<N> finite = operand<N>(g[0], g[1]);
+#pragma unroll
+      for (int m = 0; m < 2; m++) {
+        if constexpr (G::R > 1) of_state[m] = parts.sum(m, at.wave) * *(const f32x4*)&c.left[16 * m + row];
+        dw[m] = f32x4{0, 0, 0, 0};
+        mul(dw[m], pieces(c.p[m]), finite);
+        dw[m] += of_state[m];
+      }
+      upto = max(upto, last_odd(dw, row));
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const bool there = i / 4 * 16 + row + i % 4 > upto;
+        dw[i / 4][i % 4] = there ? dw[i / 4][i % 4] : 0.f;
+        dr[i / 4][i % 4] = there ? 0.f : __builtin_nanf("");
+      }
+      const Pieces<3> again = operand<3>(dw[0], dw[1]);
+#pragma unroll
+      for (int m = 0; m < 2; m++) mul(dr[m], pieces(c.t[m]), again);
+    }
     const Pieces<3> drs = operand<3>(-since[0] * beta[0] * dr[0], -since[1] * beta[1] * dr[1]);
 #pragma unroll
     for (int m = 0; m < 2 * STEPS; m++) mul(E[m], stage.k.columns(at.part * 2 * STEPS + m), drs);
@@ -405,7 +435,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         for (int e = 0; e < 4; e++) {
           const int tj = 16 * at.j + row + e;
           v[e] = (of_m ? tj <= ti : tj < ti) ? (of_m ? a.scale : 1.f) * decay_between(sums[ti] - sums[tj]) * task[i][e] : 0.f;
-          z[e] = tj < ti ? by * v[e] * z[e] : 0.f;
+          z[e] *= by * v[e];
+          z[e] = tj < ti && z[e] == z[e] ? z[e] : 0.f;
         }
         (of_m ? between.m : between.n).put_four(ti, 16 * at.j + row, v);
         const float of_row = add_32_apart(add_16_apart((z[0] + z[1]) + (z[2] + z[3])));
@@ -504,6 +535,11 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
         for (int n = 0; n < NT; n++)
 #pragma unroll
           for (int d = 0; d < 3; d++) s[d] += dots[(w + lane / 16 / MT) * NT + n][d][lane];
+      // Where w is NaN so are s[1] and the products of pairs, which count as 0: they would leave the dg of the tokens
+      // up to the first of them anyway, and those after it are NaN.  (dbeta from the first on: its g may be why.)
+      const unsigned long long lost = __ballot(s[1] != s[1]);
+      const int from = lost ? __builtin_ctzll(lost) : BLOCK;
+      if (s[1] != s[1]) s[1] = 0.f;
       double dG = (double)s[0] - s[1], ends = 0;
       const int own = lane / 16, t = lane % 16;
       float pairs[I::TILES][4];
@@ -530,8 +566,8 @@ __global__ __launch_bounds__((Inputs<T, KT>::THREADS)) void k_delta_inputs_back(
       const double total = (double)lane_sum<BLOCK>(s[1]) + whole * ends;
       const int64_t at = ((int64_t)b * a.length + t0 + lane) * a.heads + h;
       if (lane < here) {
-        if (a.dg) a.dg[at] = lane < live ? (float)(dG + total) : 0.f;
-        a.dbeta[at] = lane < live ? (float)(dot_v[lane] - s[2]) : 0.f;
+        if (a.dg) a.dg[at] = lane >= live ? 0.f : lane > from ? __builtin_nanf("") : (float)(dG + total);
+        a.dbeta[at] = lane >= live ? 0.f : lane >= from ? __builtin_nanf("") : (float)(dot_v[lane] - s[2]);
       }
     }
   }

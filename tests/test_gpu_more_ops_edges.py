@@ -105,3 +105,48 @@ def test_delta_outputs_beside_a_number_that_is_not_finite(case, of):
         (o, end), (want_o, want_end) = usual.run_delta(x)
         leaves_the_rest(o, want_o, None if of == "state" else case[-1], f"o, {value}")
         leaves_the_rest(end, want_end, None, f"state, {value}")
+
+
+@pytest.mark.parametrize("of", ["q", "k", "v", "g", "beta", "state", "do", "dstate"])
+@pytest.mark.parametrize("case", WILD, ids=lambda c: "-".join(map(str, c)))
+def test_delta_gradients_beside_a_number_that_is_not_finite(case, of):
+    """The same of the gradients."""
+    for value in wild_values(of):
+        x, given = wild_inputs(case, of, value)
+        x.grads()
+        outs, wants = usual.run_delta(x)
+        d = list(given.values())
+        got = torch.autograd.grad(outs, list(x.gpu.values()), [t.to(DEV) for t in d])
+        want = torch.autograd.grad(wants, list(x.cpu.values()), [t.double() for t in d])
+        for n, a, b in zip(x.gpu, got, want):
+            leaves_the_rest(a, b, None if "state" in (n, of) or of == "dstate" else case[-1], f"d{n}, {value}")
+
+
+def test_delta_many_numbers_that_are_not_finite():
+    """Of several tokens, columns and heads the first (backward: the last) counts; a sequence without one is as without
+    them, bit for bit."""
+    def run(wild):
+        x = usual.delta_inputs("bf16", 3, 90, 2, 4, 40, 48, "gs").gpu
+        do = torch.randn(3, 90, 4, 48, generator=torch.Generator().manual_seed(3)).to(DEV).bfloat16()
+        if wild:
+            x["v"][0, [7, 50, 33], [0, 0, 2], [1, 1, 30]] = float("inf")
+            x["k"][0, 60, 1] = float("nan")
+            do[1, [10, 70], [1, 3], [0, 47]] = float("nan")
+        leaves = [t.requires_grad_() for t in x.values()]
+        o = ops.gated_delta(*[x[n] for n in ("q", "k", "v", "g", "beta")], state=x["state"])
+        return [o.detach(), *torch.autograd.grad(o, leaves, do)]
+
+    wild, tame = run(True), run(False)
+    for a, b in zip(wild, tame):
+        assert torch.equal(a[2], b[2])
+    o, dq, dk, dv, dg, dbeta = wild[:6]
+    want = torch.ones(90, 4, 48, dtype=torch.bool, device=DEV)      # finite
+    want[7:, 0, 1] = want[33:, 2, 30] = False
+    want[60:, 2:] = False
+    assert torch.equal(o[0].isfinite(), want) and torch.equal(o[0][want], tame[0][0][want])
+    assert torch.equal(o[1], tame[0][1])
+    assert dv[1, :11, 1, 0].isnan().all() and dv[1, 11:, 1, 0].isfinite().all()
+    assert dv[1, :71, 3, 47].isnan().all() and dv[1, 71:, 3, 47].isfinite().all()
+    for t, head in ((dg, 1), (dbeta, 1)):
+        assert t[1, :11, head].isnan().all() and t[1, 11:, head].isfinite().all()
+    assert dk[1, 71:].isfinite().all() and dq[1, 71:].isfinite().all() and dq[1, :10].isfinite().all()
