@@ -1,5 +1,7 @@
 """The linear-attention operators off the usual ground: no eps under a root beside padded tokens, views that
-negate, numbers that are not finite beside those that are."""
+negate, numbers that are not finite beside those that are, lengths that are cut into segments."""
+
+import ctypes
 
 import pytest
 import torch
@@ -10,6 +12,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_1905_11722_amd import ops  # noqa: E402
+from tests import more_ops_abi as abi  # noqa: E402
 from tests import more_ops_reference as ref  # noqa: E402
 from tests import test_gpu_more_ops as usual  # noqa: E402
 from tests.test_gpu_ops import DEV, check, compare_grads  # noqa: E402
@@ -85,8 +88,8 @@ def wild_values(of):
 
 
 def leaves_the_rest(got, want, own, what):
-    """Not finite where `want` is not, and within the usual bound of it elsewhere; token `own` of the first sequence (None: no
-    token) may be NaN."""
+    """Not finite where `want` is not, and within the usual bound of it elsewhere; token `own` of the first sequence
+    (None: no token) may be NaN."""
     got, want = got.detach().cpu(), want.detach()
     finite = want.isfinite()
     assert not got[~finite].isfinite().any(), what
@@ -150,3 +153,65 @@ def test_delta_many_numbers_that_are_not_finite():
     for t, head in ((dg, 1), (dbeta, 1)):
         assert t[1, :11, head].isnan().all() and t[1, 11:, head].isfinite().all()
     assert dk[1, 71:].isfinite().all() and dq[1, 71:].isfinite().all() and dq[1, :10].isfinite().all()
+
+
+# -------------------------------------------------- lengths that are cut into segments
+
+CUT = [  # dtype, batch, length, key_heads, heads, key, value, parts, lengths, segments
+    ("f32", 1, 800, 1, 1, 16, 8, "gs", None, 3),
+    ("f16", 3, 800, 1, 1, 30, 33, "gs", (799, 0, 300), 3),
+    ("bf16", 2, 1030, 1, 2, 32, 96, "g", (1030, 31), 4),
+    ("f16", 3, 900, 1, 1, 64, 33, "gs", (899, 1, 257), 3),
+    ("f32", 1, 1100, 1, 2, 48, 64, "gs", (1095,), 4),
+    ("bf16", 1, 800, 2, 2, 64, 64, "s", None, 3),
+    ("f32", 1, 790, 1, 2, 96, 100, "gs", (790,), 3),
+    ("f16", 2, 1050, 1, 1, 128, 40, "gs", (1050, 520), 4),
+    ("bf16", 1, 1601, 1, 1, 200, 40, "g", (1597,), 3),
+    ("f32", 2, 1540, 1, 1, 256, 24, "gs", (1540, 600), 3),
+    ("f16", 1, 1540, 1, 2, 130, 70, "gs", None, 3),
+]
+
+
+def segments(dtype, batch, length, key_heads, heads, key, value):
+    """Into how many segments a length is cut, from the scratch that it takes beside the chunks'."""
+    lib, n = abi.library(), ctypes.c_uint64()
+
+    def scratch(tokens):
+        a = abi.DeltaArgs(dtype=("f32", "bf16", "f16").index(dtype), batch=batch, length=tokens, key_heads=key_heads,
+                          heads=heads, key=key, value=value)
+        assert lib.rc_delta_forward_workspace(a, n) == 0
+        return n.value
+
+    chunks = -(-length // 32) * scratch(32)                         # (one chunk is not cut)
+    rows, columns = 32 if key <= 32 else 64 if key <= 64 else 128 if key <= 128 else 256, -(-value // 32) * 32
+    each = 4 * batch * heads * rows * (rows + 2 * columns)
+    more = scratch(length) - chunks
+    assert more % each == 0
+    return max(1, more // each)
+
+
+@pytest.mark.parametrize("case", CUT, ids=lambda c: "-".join(map(str, c[:7])))
+def test_delta_cut_into_segments(case):
+    """Every width of keys and every type, ends in the first, in the last and in segments between; the bound is that
+    of the operator's other tests."""
+    *sizes, lengths, count = case
+    assert segments(*sizes[:7]) == count
+    x = usual.delta_inputs(*sizes)
+    if lengths is not None:
+        with torch.no_grad():
+            for i, e in enumerate(lengths):
+                for n in x.gpu:
+                    if n != "state":
+                        x.gpu[n][i, e:] = float("nan")
+                        x.cpu[n][i, e:] = 0
+    x.grads()
+    outs, wants = usual.run_delta(x, lengths)
+    for n, o, w in zip(("o", "state"), outs, wants):
+        check(o, w, n)
+    compare_grads(x, outs, wants)
+
+
+@pytest.mark.parametrize("key,value,length", [(16, 8, 800), (100, 33, 800), (200, 40, 1540)])
+def test_delta_cut_with_scratch_aligned_to_a_float(key, value, length):
+    assert segments("bf16", 1, length, 1, 1, key, value) == 3
+    usual.test_delta_scratch_aligned_to_a_float(key, value, length)
