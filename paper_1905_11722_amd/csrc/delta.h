@@ -540,13 +540,6 @@ struct Stage {
 };
 template <class T, int KT, class G>
 constexpr int kStages = 2 * sizeof(Stage<T, KT, G>) + 16 * 1024 <= 160 * 1024 ? 2 : 1;    // (and Parts)
-// Workgroups a compute unit that a walk's registers are to leave room for: two waves a SIMD
-// (256 registers a lane), where LDS has it.  With 512 the accumulators go where only matrix
-// instructions reach them, and 180 of 1170 instructions of a chunk were moves.
-template <class T, int KT, class G>
-constexpr int kTogether = G::THREADS > 256 || kStages<T, KT, G> * sizeof(Stage<T, KT, G>) > 76 * 1024
-                              ? 1 : 512 / G::THREADS;
-
 // A loading wave's part of the chunks: the next one's share in registers.  Loads are
 // unconditional with addresses inside the sequence; what is past its end is dropped on the way to LDS.
 // WIDE: key and value are multiples of eight.  READS: q and P (P T) are needed, and not only keys and T.

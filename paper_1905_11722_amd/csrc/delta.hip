@@ -16,7 +16,7 @@ namespace {
 // load 1.75.  64 chunks of 64 heads of 128 x 128 with states kept (4 x 2048 tokens): 122 us; a prompt of
 // 8192 tokens, 16 heads, in three segments: 104 us for their ends, 9 to join them, 141 for the outputs.
 template <class T, int KT, class G, bool WIDE, int MODE>
-__global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_forward(DeltaParams p) {
+__global__ __launch_bounds__(G::THREADS) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
   constexpr int EVERY = block_of(kPieces<T>, 32 * KT) / kChunk;

@@ -8,7 +8,7 @@ namespace {
 // Backward through the states, from the last chunk to the first, as k_delta_forward goes, and bound as
 // that is: 64 chunks of 64 heads of 128 x 128 129 us.
 template <class T, int KT, class G, bool WIDE, int MODE>
-__global__ __launch_bounds__(G::THREADS, (kTogether<T, KT, G>)) void k_delta_states_back(DeltaParams p) {
+__global__ __launch_bounds__(G::THREADS) void k_delta_states_back(DeltaParams p) {
   const rc_delta_args& a = p.a;
   constexpr int N = kPieces<T>, STEPS = KT / G::R, STAGES = kStages<T, KT, G>;
   constexpr int EVERY = block_of(N, 32 * KT) / kChunk;
