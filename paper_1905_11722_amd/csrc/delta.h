@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
   // token i there is one, whatever it is multiplied with.
   odd = __any(odd);
   int upto = -1;                                       // of row lane % 32
-  if (odd) {
+  if (__builtin_expect(odd, 0)) {
     for (int j = 0; j < lane % 32; j++)
       if (!is_finite(A[lane % 32][j])) upto = j;
     for (int j = 0; j <= upto; j++)
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int e = 0; e < 4; e++) (step ? inverse : A)[16 + row + e][col] = s[e];
     __syncthreads();
   }
-  if (odd) {
+  if (__builtin_expect(odd, 0)) {
     for (int j = 0; lane < kChunk && j <= upto; j++) inverse[lane][j] = __builtin_nanf("");
     __syncthreads();
   }
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64) void k_delta_prepare(DeltaParams p) {
     for (int i = 0; i < 3; i++) out.t[n][i][lane] = f.p[i];
     if (!BACK) {
       // columns n of P T, transposed: rows of it are what its operand has in a lane
-      if (odd) {
+      if (__builtin_expect(odd, 0)) {
 #pragma unroll
         for (int e = 0; e < 8; e++) y[e] = is_finite(y[e]) ? y[e] : 0.f;
       }

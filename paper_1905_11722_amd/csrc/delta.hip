@@ -83,7 +83,7 @@ __global__ __launch_bounds__(G::THREADS) void k_delta_forward(DeltaParams p) {
 #pragma unroll
     for (int m = 0; m < 2; m++) mul(w[m], t[m], rs);
     // r of one token that is not finite has made all of its column's w NaN: those before it again
-    if (MODE == kWhole && __any(w[0][0] != w[0][0])) {
+    if (MODE == kWhole && __builtin_expect(__any(w[0][0] != w[0][0]), 0)) {
       asm volatile("" ::: "memory");                   // (T is read again, and not held for this)
       const int from = first_odd(r, row);
 #pragma unroll

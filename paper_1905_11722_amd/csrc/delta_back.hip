@@ -83,7 +83,7 @@ __global__ __launch_bounds__(G::THREADS) void k_delta_states_back(DeltaParams p)
 #pragma unroll
     for (int m = 0; m < 2; m++) mul(dr[m], t[m], dws);
     // do or dW of one token that is not finite has made all of its column's dR NaN: those after it again
-    if (MODE == kWhole && __any(dr[0][0] != dr[0][0])) {
+    if (MODE == kWhole && __builtin_expect(__any(dr[0][0] != dr[0][0]), 0)) {
       asm volatile("" ::: "memory");                   // (what is in LDS is read again, and not held for this)
 #pragma unroll
       for (int i = 0; i < 8; i++) g[i / 4][i % 4] = (float)stage.x[i / 4 * 16 + row + i % 4][at.col - at.col0];
