@@ -214,6 +214,8 @@ typedef struct {
  * dtype.  g (absent: 0) and beta: (batch, length, heads), 32-bit floats; g is not
  * positive (-infinity forgets everything).  States (batch, heads, key, value) are
  * 32-bit floats, contiguous.  1 <= key, value <= 256; key_heads divides heads.
+ * A number that is not finite makes its own token's results NaN and those that depend
+ * on it (outputs after it; gradients where they go through the state), and no others.
  * kept: NULL, or what rc_delta_backward starts from (rc_delta_kept_bytes);
  * it is written by rc_delta_forward and read by rc_delta_backward of the same
  * sizes.  Both need scratch.
@@ -303,7 +305,8 @@ int rc_qk_backward_workspace(const rc_qk_args* args, uint64_t* bytes_host);
 /*
  * Dropout whose mask is never stored: element i of x (in row-major order of
  * rows x width) is kept where word i % 4 of Philox4x32-10 (Salmon, Moraes, Dror and
- * Shaw, 2011) with key seed and counter (i / 4, tag) is not below p 2^32:
+ * Shaw, 2011) with key seed and counter (i / 4, tag) is not below p 2^32 (rounded to a
+ * whole number):
  *   out = residual + (kept ? x / (1 - p) : 0).
  * So forward, backward and a second run of either draw the same mask from the
  * same seed and tag.  0 <= p <= 1 (1 drops everything).  The seed is

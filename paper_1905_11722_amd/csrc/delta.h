@@ -40,8 +40,9 @@
 //
 // A number that is not finite reaches what the formulas at the top let it reach, as NaN: its own token and
 // those after it, gradients of those before it where they go through its state.  A matrix product would hand it to the
-// whole chunk, for 0 times NaN is NaN: where one is found, which costs a compare and a branch a chunk (2 us of the
-// 122 of 64 chunks forward), the product runs again without it and the rows that it belongs to are set to NaN.
+// whole chunk, for 0 times NaN is NaN: where one is found, which costs a compare and a branch a chunk (forward
+// 122 to 124 us for 64 chunks, 140 to 146 for 86 of a prompt, whose states nobody writes), the product runs again
+// without it and the rows that it belongs to are set to NaN.
 #pragma once
 
 #include <algorithm>
@@ -916,12 +917,15 @@ inline int fits_back(const rc_delta_args& a) {
   return launchable((int64_t)a.batch * a.heads / heads_together(a) * blocks_of(a), 512) ? RC_OK : RC_E_OVERFLOW;
 }
 // Segments of the length: more than one where the walks over the segments' ends (of values' and
-// key columns, one segment fewer) and those over the segments fit the compute units at once and each
-// segment has eight chunks (sixteen of the widest keys, whose joins take longer).  Cutting costs those
+// key columns, one segment fewer) and those over the segments fit the compute units at once, counted as
+// slices of 32 columns, two a compute unit for keys up to 64 and one for others, and each
+// segment has eight chunks (sixteen of the widest keys, whose joins take longer).  (For keys of 33 to 64 in float16 and
+// float32 LDS holds one, so that as many as this gives may take two rounds: 8192 tokens of 64 x 64 in float32
+// with room for 512 and for 256, 8 heads 112 and 125 us, 16 heads 215 and 199.)  Cutting costs those
 // walks, and a step a segment that joins them: two segments gain from 128 chunks and keys of 65 to
 // 128 on, not for others.  Forward, all kernels, bf16 heads of 128 x 128, us in one segment and in as many as
-// this gives: 8192 tokens of 32, 24, 16 and 4 heads 444, 426, 425, 401 and in 2, 2, 3, 9 423, 395, 273, 132;
-// 2048 tokens of 16 heads 113, in 3 92 (32 heads in one: 119, in 2 122).
+// this gives: 8192 tokens of 32, 24, 16 and 4 heads 478, 452, 441, 421 and in 2, 2, 3, 9 455, 397, 274, 127;
+// 2048 tokens of 16 heads 120, in 3 90 (32 heads in one: 126, in 2 125).
 inline int segments_of(const rc_delta_args& a) {
   const int rows = rows_of(a.key), room = rows <= 64 ? 512 : 256;
   const int64_t values = (int64_t)a.batch * a.heads * cdiv(a.value, 32);

@@ -13,8 +13,8 @@ namespace {
 // Bound by the way through a chunk: sums over the key, their exchange, T, and the state, each after
 // the other, with one or two waves a SIMD.  Waves of columns x parts of the key of 128, timed when the
 // same waves loaded and computed, us a chunk: 2 x 2 2.5, 2 x 4 2.7, 4 x 1 and 4 x 2 2.9, 4 x 4 3.6; with waves that only
-// load 1.75.  64 chunks of 64 heads of 128 x 128 with states kept (4 x 2048 tokens): 122 us; a prompt of
-// 8192 tokens, 16 heads, in three segments: 104 us for their ends, 9 to join them, 141 for the outputs.
+// load 1.75.  64 chunks of 64 heads of 128 x 128 with states kept (4 x 2048 tokens): 124 us; a prompt of
+// 8192 tokens, 16 heads, in three segments: 103 us for their ends, 9 to join them, 147 for the outputs.
 template <class T, int KT, class G, bool WIDE, int MODE>
 __global__ __launch_bounds__(G::THREADS) void k_delta_forward(DeltaParams p) {
   const rc_delta_args& a = p.a;

@@ -181,12 +181,14 @@ __device__ __forceinline__ float sixteen_sums(const f32x4 (&x)[4]) {
 // time and one time ahead in registers; where LDS has no room for the states a wave reads its part
 // of them straight into operands, a number a load (which is what bounds it then).  What is between tokens (M, N and dR . v)
 // is tiles spread over the waves, then in LDS for all of them.  Pairs of tokens (i, j) reach dg through
-// Z_ij = M_ij q_i . k_j - beta_i N_ij k_i . k_j, whose sums by i and by j are added in 64 bits: what two tokens
-// past t have with each other leaves dg_t as the same number as it came, and not as two roundings of it.
+// Z_ij = M_ij q_i . k_j - beta_i N_ij k_i . k_j, in 32-bit sums over rows and over columns of a tile that are added to
+// one another in 64 bits: what two tokens past t have with each other leaves dg_t but for those sums' roundings,
+// of 16 numbers each, where dots of dq and dk left the roundings of sums over all that a token has.
 // Bound by waiting for loads and LDS (47% of a wave's time), with one workgroup of eight waves a compute
 // unit, which is what LDS and 256 registers allow; the matrix instructions are busy 16% of it: 64 heads of
 // 128 x 128, 32 blocks each, 246 us (215 with dg from dots of dq and dk, whose roundings
-// reached 2e-5 of dg over 64 tokens).  Blocks of 32 tokens, that read twice the states, took 414 where these took
+// reached 2e-5 of dg over 64 tokens).  Registers spill: 100 bytes a lane for these heads, 348 for bf16 keys above 128,
+// 36 and 184 for f16 of 33 to 64 and above 128, 148 and 192 for f32.  Blocks of 32 tokens, that read twice the states, took 414 where these took
 // 298; states read straight into operands 284, through LDS with a head's first loads before the last one's sums end, 253.
 template <class T, int KT>
 struct Inputs {

@@ -183,9 +183,13 @@ def gated_delta(q, k, v, g, beta, *, scale=None, state=None, lengths=None, retur
 
     Returns o, or with ``return_state`` (o, the float32 state after each
     sequence).  For its gradients the forward pass keeps the state of every 64
-    tokens in 32 bits (key value / 16 bytes for each token and head; of every 32, and twice
-    that, for keys above 128 and for more than 64 in float16 or float32) and what each token
-    wrote (4 value bytes).
+    tokens in 32 bits (of every 32 for keys above 128 and for more than 64 in float16 or float32)
+    and what each token wrote, with key taken up to 32, 64, 128 or 256, value to a multiple of 32 and the
+    length to one of those tokens: 4 key value bytes for each such block and 4 value bytes for each token, of each head.
+
+    A number that is not finite (or a float32 above 3.39e38) makes its own token's results NaN and those that
+    depend on it: outputs after it, and gradients on whichever side they go through the state.  All others are
+    what they are without it.
     """
     out = (_native or load()).gated_delta(q, k, v, g, beta, _scale(scale, q), state, lengths, return_state)
     return (out[0], out[1]) if return_state else out[0]
@@ -239,7 +243,7 @@ def dropout(x, p, seed, *, tag=0, residual=None):
 
     Element i of x (in the order of a contiguous x) is kept where word i % 4 of
     Philox4x32-10 with key ``seed`` and counter (i // 4, ``tag``) is not below
-    p 2^32.  The same seed and tag draw the same mask again, in the backward
+    p 2^32 (rounded to a whole number).  The same seed and tag draw the same mask again, in the backward
     pass or where a node of a planned step is computed a second time; take
     another tag for each use in a model and another seed for each step.
 
